@@ -55,7 +55,8 @@
 extern "C" {
 #endif
 
-typedef enum { PQ_FMT_NVFP4 = 0, PQ_FMT_INT4 = 1, PQ_FMT_INT3 = 2 } pq_format;
+/* PQ_FMT_BF16 (the values as they are) is a format of the key-value cache only. */
+typedef enum { PQ_FMT_NVFP4 = 0, PQ_FMT_INT4 = 1, PQ_FMT_INT3 = 2, PQ_FMT_BF16 = 3 } pq_format;
 
 typedef enum {
   PQ_OP_CALIB_MOMENTS = 0,
@@ -513,6 +514,80 @@ int pq_hadamard_quantize_act_packed(const int32_t* perm, pq_format fmt, int grou
                                     int64_t M, int64_t K, int64_t ld, const float* tensor_scale,
                                     void* operand, size_t operand_size, void* y_bf16, int64_t ldy,
                                     void* stream);
+
+/*
+ * Key-value cache of a transformer's attention in the per-group formats, and the attention of one new token a sequence over it.
+ *
+ * The cache holds keys and values of `pages` pages of `page` tokens, kv_heads heads of head_dim channels each, in a buffer of
+ * pq_kv_cache_bytes bytes whose layout is private to the library.  A token's place is its slot, page index * page + place in the
+ * page; which pages belong to which sequence, in which order, is the caller's.  Every (token, head) row of keys and of values is
+ * quantized by itself, in groups along head_dim, with the arithmetic of the header comment: what the cache holds of a row is what
+ * pq_quantize_act makes of it.
+ *
+ *   fmt, group   PQ_FMT_NVFP4 with 16; PQ_FMT_INT4 with 32, 64, 128 or 256, at most head_dim; PQ_FMT_BF16 with 0 (unquantized)
+ *   head_dim     64, 128 or 256
+ *   page         32, 64, 128, 256, 512 or 1024
+ *   data         device memory, 16-byte aligned; need not be initialised
+ *   k_tensor_scale, v_tensor_scale   float [1] device each, NVFP4 only (T of the header comment, one for all keys, one for all
+ *                values; magnitudes above 2688 T saturate); ignored by the other formats
+ * Bytes of a token and head, keys and values: NVFP4 2 (head_dim / 2 + head_dim / 16), INT4 2 (head_dim / 2 + 2 head_dim / group),
+ * BF16 4 head_dim.
+ */
+typedef struct {
+  pq_format fmt;
+  int group;
+  int kv_heads;
+  int head_dim;
+  int page;
+  int64_t pages;
+  void* data;
+  const float* k_tensor_scale;
+  const float* v_tensor_scale;
+} pq_kv_cache;
+
+/* Bytes of `data`; 0 for arguments that no cache has. */
+size_t pq_kv_cache_bytes(pq_format fmt, int group, int kv_heads, int head_dim, int page, int64_t pages);
+
+/*
+ * Quantizes the keys and values of n tokens into the cache: k, v bf16, element (token, head, channel) at
+ * token * ld + head * head_ld + channel (slices of the rows of a fused projection are read where they are); strides multiples of 8,
+ * pointers 16-byte aligned.  slots: int64 [n] device, distinct; a slot outside 0 .. pages * page - 1 (-1 for a row of padding)
+ * keeps nothing.  n may be 0.  Other slots of a page keep what they held: pages fill token by token.
+ */
+int pq_kv_write(const pq_kv_cache* cache, const void* k_bf16, int64_t k_ld, int64_t k_head_ld, const void* v_bf16, int64_t v_ld,
+                int64_t v_head_ld, const int64_t* slots, int64_t n, void* stream);
+
+/*
+ * Reads n slots back as bf16 (the stored value, code * scale (* T) in binary32, rounded to nearest even): what attention over a
+ * cached prefix starts with.  Arguments as for pq_kv_write, which slots need not be distinct here; a slot outside the cache reads
+ * as zeros.  The outputs may not overlap each other or the cache.
+ */
+int pq_kv_read(const pq_kv_cache* cache, const int64_t* slots, int64_t n, void* k_bf16, int64_t k_ld, int64_t k_head_ld, void* v_bf16,
+               int64_t v_ld, int64_t v_head_ld, void* stream);
+
+/*
+ * Attention of one new token a sequence over what the cache holds of that sequence:
+ *   out[b, h] = sum_t p_t v[t, h'],  p = softmax over t of scale * (q[b, h] . k[t, h']),  h' = h / (q_heads / kv_heads)
+ * over the sequence's tokens t = 0 .. lengths[b] - 1, with a window > 0 over the last `window` of them.  Token t lies in page
+ * table[b, t / page].  A sequence of length 0 (or below) gives zeros and lse = -inf.
+ *
+ * q: bf16, (seq, head, channel) at seq * q_ld + head * q_head_ld + channel; out: bf16, likewise; strides multiples of 8, pointers
+ * 16-byte aligned.  table: int32 device, (seq, i) at seq * table_ld + i; entries past a sequence's last page are not read.
+ * lengths: int32 [seqs] device.  max_len: no length is longer (host; a longer one is cut to it); max_len <= page * table_ld.
+ * A page outside 0 .. pages - 1 is not read: its tokens are left out.  What lies in a page behind a sequence's last token or in
+ * front of its window does not matter, NaN included.  q_heads: a multiple of kv_heads.
+ * lse: float [seqs, q_heads] or NULL: ln of the sum of exp(scale * q . k), with which outputs over parts of a context are joined.
+ * Scores, the softmax's sums and the outputs' are held in fp32; out is rounded once to bf16.
+ * workspace: pq_attn_decode_workspace_bytes(cache, seqs, q_heads, max_len, window) bytes, 16-byte aligned; its first
+ * PQ_ATTN_DECODE_ZERO_BYTES must be zero before the first call, and every call leaves them zero.  Calls that may overlap need
+ * workspaces of their own.  seqs may be 0.  May be captured into a HIP graph; results are the same bits from run to run.
+ */
+#define PQ_ATTN_DECODE_ZERO_BYTES ((size_t)4096)
+size_t pq_attn_decode_workspace_bytes(const pq_kv_cache* cache, int64_t seqs, int q_heads, int64_t max_len, int64_t window);
+int pq_attn_decode(const pq_kv_cache* cache, const void* q_bf16, int64_t q_ld, int64_t q_head_ld, const int32_t* table,
+                   int64_t table_ld, const int32_t* lengths, int64_t seqs, int q_heads, int64_t max_len, int64_t window, float scale,
+                   void* out_bf16, int64_t out_ld, int64_t out_head_ld, float* lse, void* workspace, size_t workspace_bytes,
+                   void* stream);
 
 /*
  * Measurement aids (no part of the method and not covered by the version contract of the calls above:

@@ -668,6 +668,133 @@ int pq_qgemm_check_int_scales(pq_format fmt, int group, const void* scales, int6
   return run_check_int_scales(fmt, group, scales, rows, K, bad_count, workspace, as_stream(stream));
 }
 
+static const char* kv_cache_error(pq_format fmt, int group, int kv_heads, int head_dim, int page, int64_t pages, int* code) {
+  *code = PQ_ERR_FORMAT;
+  if (fmt == PQ_FMT_NVFP4) {
+    if (group != 16) return "NVFP4 uses groups of 16";
+  } else if (fmt == PQ_FMT_BF16) {
+    if (group != 0) return "the unquantized cache has no groups (group 0)";
+  } else if (fmt == PQ_FMT_INT4) {
+    if (group != 32 && group != 64 && group != 128 && group != 256) return "INT4 offers group 32, 64, 128 or 256";
+  } else {
+    return "a cache holds NVFP4, INT4 or BF16";
+  }
+  *code = PQ_ERR_SHAPE;
+  if (head_dim != 64 && head_dim != 128 && head_dim != 256) return "head_dim must be 64, 128 or 256";
+  if (group > head_dim) return "a group may not be longer than a head";
+  if (kv_heads <= 0 || kv_heads > 4096) return "kv_heads must be 1 .. 4096";
+  if (page != 32 && page != 64 && page != 128 && page != 256 && page != 512 && page != 1024)
+    return "page must be 32, 64, 128, 256, 512 or 1024 tokens";
+  if (pages <= 0 || pages > INT32_MAX) return "pages must be 1 .. 2^31 - 1";
+  *code = PQ_OK;
+  return nullptr;
+}
+
+static int check_kv_cache(const char* who, const pq_kv_cache* c) {
+  if (!c) return fail(PQ_ERR_NULL, "%s: cache is NULL", who);
+  int code;
+  const char* what = kv_cache_error(c->fmt, c->group, c->kv_heads, c->head_dim, c->page, c->pages, &code);
+  if (what)
+    return fail(code, "%s: %s (fmt=%d group=%d kv_heads=%d head_dim=%d page=%d pages=%lld)", who, what, (int)c->fmt, c->group,
+                c->kv_heads, c->head_dim, c->page, (long long)c->pages);
+  if (!c->data) return fail(PQ_ERR_NULL, "%s: the cache's data is NULL", who);
+  if (c->fmt == PQ_FMT_NVFP4 && (!c->k_tensor_scale || !c->v_tensor_scale))
+    return fail(PQ_ERR_NULL, "%s: NVFP4 needs the tensor scales of keys and values", who);
+  if (!aligned16(c->data)) return fail(PQ_ERR_SHAPE, "%s: the cache's data must be 16-byte aligned", who);
+  return PQ_OK;
+}
+
+// rows of heads: the heads of a token, and tokens, do not overlap when written (`out`); 16-byte pieces are aligned
+static int check_head_rows(const char* who, const char* name, const void* p, int64_t ld, int64_t head_ld, int64_t rows, int heads, int dim,
+                           bool out) {
+  if (!aligned16(p) || ld % 8 || head_ld % 8)
+    return fail(PQ_ERR_SHAPE, "%s: %s must be 16-byte aligned and its strides (%lld, %lld) multiples of 8", who, name, (long long)ld,
+                (long long)head_ld);
+  if (ld < 0 || head_ld < 0 || (heads > 1 && head_ld < dim && out) ||
+      (rows > 1 && out && ld < (heads - 1) * head_ld + dim && head_ld < (rows - 1) * ld + dim))
+    return fail(PQ_ERR_SHAPE, "%s: the rows of %s overlap (strides %lld, %lld)", who, name, (long long)ld, (long long)head_ld);
+  return PQ_OK;
+}
+
+size_t pq_kv_cache_bytes(pq_format fmt, int group, int kv_heads, int head_dim, int page, int64_t pages) {
+  int code;
+  if (const char* what = kv_cache_error(fmt, group, kv_heads, head_dim, page, pages, &code)) {
+    (void)fail(code, "pq_kv_cache_bytes: %s", what);
+    return 0;
+  }
+  return kv_cache_bytes(fmt, group, kv_heads, head_dim, page, pages);
+}
+
+static int check_kv_rows(const char* who, const pq_kv_cache* cache, const void* k, int64_t k_ld, int64_t k_head, const void* v,
+                         int64_t v_ld, int64_t v_head, const int64_t* slots, int64_t n, bool out) {
+  int rc = check_kv_cache(who, cache);
+  if (rc) return rc;
+  if (n < 0 || n > INT32_MAX) return fail(PQ_ERR_SHAPE, "%s: n=%lld outside 0 .. 2^31 - 1", who, (long long)n);
+  if (n == 0) return PQ_OK;
+  if (!k || !v || !slots) return fail(PQ_ERR_NULL, "%s: a required pointer is NULL", who);
+  rc = check_head_rows(who, "k", k, k_ld, k_head, n, cache->kv_heads, cache->head_dim, out);
+  return rc ? rc : check_head_rows(who, "v", v, v_ld, v_head, n, cache->kv_heads, cache->head_dim, out);
+}
+
+int pq_kv_write(const pq_kv_cache* cache, const void* k, int64_t k_ld, int64_t k_head_ld, const void* v, int64_t v_ld,
+                int64_t v_head_ld, const int64_t* slots, int64_t n, void* stream) {
+  const int rc = check_kv_rows("pq_kv_write", cache, k, k_ld, k_head_ld, v, v_ld, v_head_ld, slots, n, false);
+  if (rc || n == 0) return rc;
+  return run_kv_write(*cache, k, k_ld, k_head_ld, v, v_ld, v_head_ld, slots, n, as_stream(stream));
+}
+
+int pq_kv_read(const pq_kv_cache* cache, const int64_t* slots, int64_t n, void* k, int64_t k_ld, int64_t k_head_ld, void* v,
+               int64_t v_ld, int64_t v_head_ld, void* stream) {
+  const int rc = check_kv_rows("pq_kv_read", cache, k, k_ld, k_head_ld, v, v_ld, v_head_ld, slots, n, true);
+  if (rc || n == 0) return rc;
+  return run_kv_read(*cache, slots, n, k, k_ld, k_head_ld, v, v_ld, v_head_ld, as_stream(stream));
+}
+
+// what the call and the size of its workspace depend on
+static int check_attn_shape(const char* who, const pq_kv_cache* c, int64_t seqs, int q_heads, int64_t max_len, int64_t window) {
+  int code;
+  const char* what = kv_cache_error(c->fmt, c->group, c->kv_heads, c->head_dim, c->page, c->pages, &code);
+  if (what) return fail(code, "%s: %s", who, what);
+  if (seqs < 0 || seqs > 65535) return fail(PQ_ERR_SHAPE, "%s: seqs=%lld outside 0 .. 65535", who, (long long)seqs);
+  if (q_heads <= 0 || q_heads > 65535 || q_heads % c->kv_heads)
+    return fail(PQ_ERR_SHAPE, "%s: q_heads=%d must be a positive multiple of kv_heads=%d", who, q_heads, c->kv_heads);
+  if (max_len < 0 || max_len > (1 << 30)) return fail(PQ_ERR_SHAPE, "%s: max_len=%lld outside 0 .. 2^30", who, (long long)max_len);
+  if (window < 0) return fail(PQ_ERR_SHAPE, "%s: window=%lld is negative", who, (long long)window);
+  return PQ_OK;
+}
+
+size_t pq_attn_decode_workspace_bytes(const pq_kv_cache* cache, int64_t seqs, int q_heads, int64_t max_len, int64_t window) {
+  if (!cache || check_attn_shape("pq_attn_decode_workspace_bytes", cache, seqs, q_heads, max_len, window)) return 0;
+  return attn_decode_workspace_bytes(*cache, seqs, q_heads, max_len, window);
+}
+
+int pq_attn_decode(const pq_kv_cache* cache, const void* q, int64_t q_ld, int64_t q_head_ld, const int32_t* table, int64_t table_ld,
+                   const int32_t* lengths, int64_t seqs, int q_heads, int64_t max_len, int64_t window, float scale, void* out,
+                   int64_t out_ld, int64_t out_head_ld, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "pq_attn_decode";
+  int rc = check_kv_cache(who, cache);
+  if (rc) return rc;
+  rc = check_attn_shape(who, cache, seqs, q_heads, max_len, window);
+  if (rc || seqs == 0) return rc;
+  if (!q || !table || !lengths || !out) return fail(PQ_ERR_NULL, "%s: a required pointer is NULL", who);
+  if (!(scale - scale == 0.0f)) return fail(PQ_ERR_SHAPE, "%s: scale=%g is not finite", who, (double)scale);
+  if (table_ld < 0 || table_ld * cache->page < max_len)
+    return fail(PQ_ERR_SHAPE, "%s: max_len=%lld tokens need more than table_ld=%lld pages of %d", who, (long long)max_len,
+                (long long)table_ld, cache->page);
+  rc = check_head_rows(who, "q", q, q_ld, q_head_ld, seqs, q_heads, cache->head_dim, false);
+  if (!rc) rc = check_head_rows(who, "out", out, out_ld, out_head_ld, seqs, q_heads, cache->head_dim, true);
+  if (rc) return rc;
+  if (((uintptr_t)table | (uintptr_t)lengths | (uintptr_t)lse) & 3)
+    return fail(PQ_ERR_SHAPE, "%s: table, lengths and lse must be 4-byte aligned", who);
+  const size_t need = attn_decode_workspace_bytes(*cache, seqs, q_heads, max_len, window);
+  if (!workspace || workspace_bytes < need)
+    return fail(PQ_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", who, need, workspace ? workspace_bytes : (size_t)0);
+  if (!aligned16(workspace)) return fail(PQ_ERR_SHAPE, "%s: workspace must be 16-byte aligned", who);
+  const AttnCall a{(const uint16_t*)q, q_ld, q_head_ld, table, table_ld, lengths, (int)seqs, q_heads, (int)max_len,
+                   window >= max_len ? 0 : (int)window, scale, (uint16_t*)out, out_ld, out_head_ld, lse, workspace};
+  return run_attn_decode(*cache, a, as_stream(stream));
+}
+
 int pq_probe_stream(const void* src, size_t read_bytes, void* dst, size_t write_bytes, void* stream) {
   if ((read_bytes && !src) || (write_bytes && !dst))
     return fail(PQ_ERR_NULL, "pq_probe_stream: NULL buffer with a non-zero size");

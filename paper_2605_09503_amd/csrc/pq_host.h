@@ -163,6 +163,28 @@ int run_qgemm_packed(pq_format fmt, int group, const void* a_operand, const floa
                      const void* w_operand, const float* w_ts, int64_t M, int64_t N, int64_t K,
                      const void* bias, void* y, int64_t ldy, bool out_f32, hipStream_t st);
 
+// key-value cache (pq_kv.hip) and the attention over it (pq_attn.hip); arguments checked by pq_api.hip
+size_t kv_cache_bytes(pq_format fmt, int group, int kv_heads, int head_dim, int page, int64_t pages);
+int run_kv_write(const pq_kv_cache& c, const void* k, int64_t k_ld, int64_t k_head, const void* v, int64_t v_ld, int64_t v_head,
+                 const int64_t* slots, int64_t n, hipStream_t st);
+int run_kv_read(const pq_kv_cache& c, const int64_t* slots, int64_t n, void* k, int64_t k_ld, int64_t k_head, void* v, int64_t v_ld,
+                int64_t v_head, hipStream_t st);
+struct AttnCall {
+  const uint16_t* q;
+  int64_t q_ld, q_head;
+  const int32_t* table;
+  int64_t table_ld;
+  const int32_t* lengths;
+  int seqs, q_heads, max_len, window;      // window 0: none
+  float scale;
+  uint16_t* out;
+  int64_t out_ld, out_head;
+  float* lse;                              // or null
+  void* ws;
+};
+size_t attn_decode_workspace_bytes(const pq_kv_cache& c, int64_t seqs, int q_heads, int64_t max_len, int64_t window);
+int run_attn_decode(const pq_kv_cache& c, const AttnCall& a, hipStream_t st);
+
 int run_check_int_scales(pq_format fmt, int group, const void* scales, int64_t rows, int64_t K, int64_t* bad_count,
                          void* ws, hipStream_t st);
 int launch_probe_stream(const void* src, size_t read_bytes, void* dst, size_t write_bytes, hipStream_t st);

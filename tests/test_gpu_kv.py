@@ -1,0 +1,342 @@
+"""The key-value cache and the attention over it against the oracle in 64 bits.
+
+Tolerances.  Reading back is bit-exact.  Attention: scores are sums of D exact products in fp32, so a score is off by at most
+(D + 16) 2^-24 of the largest sum of |scale q k|, and a weight by e to that power; weights are rounded once to fp16 (2^-11), the
+output once to bf16 (2^-8).  The sums over tokens add 2^-24 a token of what they add up.  An fp16 weight (with its value's scale) is
+at least 2^6 where the largest is, and below 2^-14 of steps of 2^-24: it may be off by 2^-31 of the largest weight times scale, which
+is what is left of an element whose tokens of any weight hold zeros."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import formats as OF
+from oracle import kv as OK
+from paper_2605_09503_amd import pq
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+NV, I4, BF = pq.FMT_NVFP4, pq.FMT_INT4, pq.FMT_BF16
+FORMATS = [(NV, 16, 64), (NV, 16, 128), (NV, 16, 256), (I4, 32, 64), (I4, 64, 64), (I4, 32, 128), (I4, 64, 128), (I4, 128, 128),
+           (I4, 32, 256), (I4, 64, 256), (I4, 128, 256), (I4, 256, 256), (BF, 0, 64), (BF, 0, 128), (BF, 0, 256)]
+
+
+def bits(t):
+    return t.contiguous().view(torch.int16).cpu().numpy().view(np.uint16)
+
+
+def f64(t):
+    return OF.bf16_bits_to_f64(bits(t))
+
+
+def rows(rng, n, heads, dim, gap=8):
+    """bf16 [n, heads, dim], a slice of wider rows; channel sizes differ, some groups are far smaller than others."""
+    x = rng.standard_normal((n, heads * dim)) * np.exp(rng.standard_normal(heads * dim))
+    x *= np.where(rng.random((n, heads * dim)) < 0.02, 20.0, 1.0)
+    wide = np.full((n, heads * dim + 2 * gap), 7.0)
+    wide[:, gap:-gap] = x
+    t = pq.bf16_from_bits(OF.f64_to_bf16_bits_rne(wide), DEV)
+    return t[:, gap:-gap].unflatten(1, (heads, dim))
+
+
+def make_cache(fmt, group, heads, dim, page, pages, k, v, garbage=True):
+    ts = [torch.full((1,), np.float32(np.abs(f64(t)).max(initial=1.0) / 2688).item(), device=DEV) for t in (k, v)]
+    cache = pq.alloc_kv_cache(fmt, group, heads, dim, page, pages, *(ts if fmt == NV else ()))
+    cache.data.fill_(0xFF if garbage else 0)            # scales and bf16 values of all ones are NaN
+    return cache, [t.item() for t in ts]
+
+
+def same_bits(got, want):
+    """equal as values: a zero's sign does not count"""
+    a, b = (np.where(x == 0x8000, 0, x) for x in (bits(got), want))
+    assert np.array_equal(a, b)
+
+
+@pytest.mark.parametrize("fmt,group,dim", FORMATS)
+@pytest.mark.parametrize("n,heads,page", [(1, 1, 32), (37, 3, 64), (130, 2, 256)])
+def test_write_then_read(fmt, group, dim, n, heads, page):
+    rng = np.random.default_rng(100 + n)
+    pages = (n + 40) // page + 2
+    k, v = rows(rng, n, heads, dim), rows(rng, n, heads, dim)
+    cache, (kt, vt) = make_cache(fmt, group, heads, dim, page, pages, k, v)
+    want = [OK.read_back(fmt, group, f64(t), s) for t, s in ((k, kt), (v, vt))]
+    slots = torch.from_numpy(rng.permutation(pages * page)[:n]).to(DEV)
+    first = n // 2                                       # in two calls: the second leaves the first's tokens alone
+    pq.pq_kv_write(cache, k[:first], v[:first], slots[:first])
+    pq.pq_kv_write(cache, k[first:], v[first:], slots[first:])
+    for got, w in zip(pq.pq_kv_read(cache, slots), want):
+        same_bits(got, w)
+    order = torch.from_numpy(rng.permutation(n)).to(DEV)
+    out = torch.full((n, heads, 2 * dim), 3.0, dtype=torch.bfloat16, device=DEV)      # k and v side by side, repeated slots
+    again = torch.cat([order[:n // 2], order[:n - n // 2]])
+    got = pq.pq_kv_read(cache, slots[again], out[:, :, :dim], out[:, :, dim:])
+    for g, w in zip(got, want):
+        same_bits(g, w[again.cpu().numpy()])
+
+
+@pytest.mark.parametrize("fmt,group,dim", FORMATS)
+def test_runs_of_slots(fmt, group, dim):
+    # whole blocks and their edges, in order, as a prompt writes and reads them
+    rng = np.random.default_rng(3)
+    n, heads, page = 150, 2, 64
+    k, v = rows(rng, n, heads, dim), rows(rng, n, heads, dim)
+    cache, (kt, vt) = make_cache(fmt, group, heads, dim, page, 4, k, v)
+    want = [OK.read_back(fmt, group, f64(t), s) for t, s in ((k, kt), (v, vt))]
+    for start in (0, 32, 5):
+        slots = torch.arange(start, start + n, device=DEV)
+        pq.pq_kv_write(cache, k, v, slots)
+        for got, w in zip(pq.pq_kv_read(cache, slots), want):
+            same_bits(got, w)
+
+
+@pytest.mark.parametrize("fmt,group,dim", [(NV, 16, 128), (I4, 32, 64), (BF, 0, 256)])
+def test_slots_outside(fmt, group, dim):
+    rng = np.random.default_rng(4)
+    k, v = rows(rng, 40, 2, dim), rows(rng, 40, 2, dim)
+    cache, (kt, vt) = make_cache(fmt, group, 2, dim, 32, 2, k, v, garbage=False)
+    slots = torch.arange(40, device=DEV)
+    slots[3], slots[20], slots[33] = -1, 64, 1 << 40
+    pq.pq_kv_write(cache, k, v, slots)
+    got = pq.pq_kv_read(cache, slots)
+    inside = np.ones(40, bool)
+    inside[[3, 20, 33]] = False
+    for g, t, s in zip(got, (k, v), (kt, vt)):
+        want = OK.read_back(fmt, group, f64(t), s)
+        want[~inside] = 0
+        same_bits(g, want)
+
+
+def test_values_at_the_quantizer_s_edges():
+    # groups of zeros, of one magnitude, of ties, of bf16's smallest and largest; beyond the tensor scale
+    for fmt, group in ((NV, 16), (I4, 32), (I4, 128)):
+        x = np.zeros((8, 1, 128))
+        x[1] = 3.0
+        x[2, 0, :64] = np.arange(64) / 8 - 4
+        x[3, 0, ::3] = 2.0 ** -133
+        x[4, 0, ::5] = 2.0 ** -126
+        x[5, 0, ::7] = 1e30
+        x[6, 0, :] = np.where(np.arange(128) % 2, 3.5, -7.0)
+        x[7, 0, 5] = -1.0
+        t = pq.bf16_from_bits(OF.f64_to_bf16_bits_rne(x), DEV)
+        ts = torch.full((1,), 0.01, device=DEV)
+        cache = pq.alloc_kv_cache(fmt, group, 1, 128, 32, 1, *((ts, ts) if fmt == NV else ()))
+        slots = torch.arange(8, device=DEV)
+        pq.pq_kv_write(cache, t, t, slots)
+        want = OK.read_back(fmt, group, f64(t), ts.item())
+        for got in pq.pq_kv_read(cache, slots):
+            same_bits(got, want)
+
+
+def test_nothing_to_write():
+    cache = pq.alloc_kv_cache(I4, 64, 2, 64, 32, 1)
+    none = torch.empty((0, 2, 64), dtype=torch.bfloat16, device=DEV)
+    slots = torch.empty(0, dtype=torch.int64, device=DEV)
+    pq.pq_kv_write(cache, none, none, slots)
+    k, v = pq.pq_kv_read(cache, slots)
+    assert k.shape == v.shape == (0, 2, 64)
+
+
+# ------------------------------------------------------------------------ attention
+
+def run_case(fmt, group, dim, lengths, heads=2, per=4, page=32, window=0, scale=None, seed=0, lse=True, noise=True, big=None,
+             q_scale=1.0, max_len=None):
+    """One call checked against the oracle; the cache is full of NaN behind every sequence, and in front of its window."""
+    rng = np.random.default_rng(seed)
+    seqs, Hq = len(lengths), heads * per
+    scale = dim ** -0.5 if scale is None else scale
+    n = [max(0, m) for m in lengths]
+    top = max(n + [1]) if max_len is None else max_len
+    per_seq = (top + page - 1) // page
+    pages = seqs * per_seq + 3
+    table = np.full((seqs, per_seq + 1), -1, dtype=np.int32)
+    order = rng.permutation(pages)[:seqs * per_seq].reshape(seqs, per_seq)
+    for b, m in enumerate(n):
+        table[b, :(m + page - 1) // page] = order[b, :(m + page - 1) // page]
+    k, v = rows(rng, sum(n), heads, dim), rows(rng, sum(n), heads, dim)
+    if big is not None:
+        v = v * big
+    cache, (kt, vt) = make_cache(fmt, group, heads, dim, page, pages, k, v)
+    pos = [np.arange(m) for m in n]
+    slots = np.concatenate([table[b][p // page].astype(np.int64) * page + p % page for b, p in enumerate(pos)] or [np.zeros(0, np.int64)])
+    keep = np.concatenate([p >= OK.attended(m, window).start for p, m in zip(pos, n)] or [np.zeros(0, bool)])
+    if not noise:
+        keep[:] = True
+    sl = np.where(keep, slots, -1)                       # what the window leaves out stays NaN
+    pq.pq_kv_write(cache, k, v, torch.from_numpy(sl).to(DEV))
+    wide = torch.randn(seqs, Hq + 1, dim, generator=torch.Generator().manual_seed(seed)) * q_scale
+    q = wide.to(torch.bfloat16).to(DEV)[:, 1:]
+    lse_t = torch.full((seqs, Hq), 5.0, device=DEV) if lse else None
+    wide_table = torch.from_numpy(np.concatenate([table, table], 1)).to(DEV)[:, :per_seq + 1]
+    lens = torch.tensor(lengths, dtype=torch.int32, device=DEV)
+    ws = pq.pq_attn_decode_workspace(cache, seqs, Hq, top, window)
+    out = pq.pq_attn_decode(cache, q, wide_table, lens, top, scale, lse=lse_t, window=window, workspace=ws)
+    out2 = torch.full((seqs, 2, Hq, dim), 9.0, dtype=torch.bfloat16, device=DEV)
+    assert pq.pq_attn_decode(cache, q, wide_table, lens, top, scale, out=out2[:, 1], window=window, workspace=ws).data_ptr() \
+        == out2[:, 1].data_ptr()
+    torch.cuda.synchronize()
+    assert torch.equal(out.view(torch.int16), out2[:, 1].contiguous().view(torch.int16)), "not the same bits from call to call"
+    assert bool((out2[:, 0] == 9.0).all())
+    assert int(ws[:pq.ATTN_DECODE_ZERO_BYTES].max()) == 0
+    ks, vs = OK.stored(fmt, group, f64(k), kt), OK.stored(fmt, group, f64(v), vt)
+    got, q64, at = f64(out), f64(q), 0
+    for b, m in enumerate(n):
+        r = OK.attended(m, window)
+        sel = slice(at + r.start, at + m)
+        at += m
+        want, wlse, mag, big_s = OK.attention(q64[b], ks[sel], vs[sel], scale)
+        ds = (dim + 16) * 2.0 ** -24 * big_s
+        sums = len(r) * 2.0 ** -24
+        tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -11 + 2 * ds[:, None] + 2 * sums) * mag * (1 + 2.0 ** -7) + 1e-38
+        if len(r):
+            tol = tol + len(r) * 2.0 ** -31 * np.abs(vs[sel]).max()
+        worst = np.abs(got[b] - want) - tol
+        assert np.all(worst <= 0), "seq %d (%d tokens): off by %g over the tolerance" % (b, m, worst.max())
+        if lse:
+            got_l = lse_t[b].cpu().numpy().astype(np.float64)
+            if len(r) == 0:
+                assert np.all(got_l == -np.inf)
+            else:
+                assert np.all(np.abs(got_l - wlse) <= ds + sums + 2.0 ** -22 * (1 + np.abs(wlse))), np.abs(got_l - wlse).max()
+    return out
+
+
+@pytest.mark.parametrize("fmt,group,dim", FORMATS)
+def test_lengths(fmt, group, dim):
+    run_case(fmt, group, dim, [0, 1, 2, 31, 32, 33, 63, 64, 65, 96, 97, 250, -4, 129])
+
+
+@pytest.mark.parametrize("fmt,group,dim", FORMATS)
+def test_long_sequences(fmt, group, dim):
+    run_case(fmt, group, dim, [2500, 1, 777], page=64, seed=1)
+
+
+@pytest.mark.parametrize("per", [1, 2, 3, 5, 7, 8, 12, 15, 16, 17, 20, 31, 32, 33, 48, 70])
+@pytest.mark.parametrize("fmt,group,dim", [(I4, 64, 128), (NV, 16, 64), (BF, 0, 256), (I4, 32, 256)])
+def test_queries_a_head(fmt, group, dim, per):
+    run_case(fmt, group, dim, [70, 5, 300], heads=2 if per < 20 else 1, per=per, seed=per)
+
+
+@pytest.mark.parametrize("fmt,group,dim", [(I4, 32, 64), (I4, 128, 128), (NV, 16, 256), (NV, 16, 128), (BF, 0, 128)])
+@pytest.mark.parametrize("window", [1, 15, 32, 33, 100, 400, 5000])
+def test_windows(fmt, group, dim, window):
+    run_case(fmt, group, dim, [0, 1, 33, 64, 100, 401, 1030], window=window, page=64, seed=window)
+
+
+@pytest.mark.parametrize("page", [32, 64, 128, 256, 512, 1024])
+def test_pages(page):
+    run_case(I4, 64, 128, [40, 1500, 3], page=page, seed=page)
+    run_case(NV, 16, 64, [40, 1500, 3], page=page, seed=page, heads=3, per=1)
+
+
+@pytest.mark.parametrize("fmt,group,dim", [(I4, 64, 128), (NV, 16, 128), (BF, 0, 64)])
+def test_many_sequences(fmt, group, dim):
+    rng = np.random.default_rng(9)
+    run_case(fmt, group, dim, [int(m) for m in rng.integers(0, 200, 150)], heads=1, per=2)
+    run_case(fmt, group, dim, [int(m) for m in rng.integers(0, 20, 700)], heads=1, per=1, lse=False)
+
+
+@pytest.mark.parametrize("fmt,group,dim", [(I4, 64, 128), (NV, 16, 128), (BF, 0, 128)])
+def test_one_long_sequence(fmt, group, dim):
+    run_case(fmt, group, dim, [30011], heads=1, per=4, page=256)
+
+
+@pytest.mark.parametrize("fmt,group,dim", [(I4, 64, 128), (NV, 16, 128), (BF, 0, 128)])
+def test_sharp_and_flat_scores(fmt, group, dim):
+    run_case(fmt, group, dim, [500, 33], scale=1.0, q_scale=4.0)            # one token takes nearly all
+    run_case(fmt, group, dim, [500, 33], scale=0.0)                         # the mean
+    run_case(fmt, group, dim, [500, 33], scale=-0.05)
+    run_case(fmt, group, dim, [500, 33], q_scale=1e-30, scale=1e28)
+    run_case(fmt, group, dim, [500, 33], q_scale=1e18, scale=1e-20)
+
+
+@pytest.mark.parametrize("fmt,group,dim", [(I4, 64, 128), (I4, 32, 64), (BF, 0, 128)])
+@pytest.mark.parametrize("big", [1e30, 1e-25, 3e5])
+def test_sizes_of_values(fmt, group, dim, big):
+    # fp16 weights carry the groups' scales: neither overflow nor underflow may come of it
+    run_case(fmt, group, dim, [500, 33, 1], big=big)
+
+
+@pytest.mark.parametrize("fmt,group,dim", [(I4, 64, 128), (NV, 16, 128), (BF, 0, 128)])
+def test_pages_outside_are_left_out(fmt, group, dim):
+    rng = np.random.default_rng(12)
+    n, page = 200, 32
+    k, v = rows(rng, n, 1, dim), rows(rng, n, 1, dim)
+    cache, (kt, vt) = make_cache(fmt, group, 1, dim, page, 8, k, v)
+    slots = np.arange(n)
+    pq.pq_kv_write(cache, k, v, torch.from_numpy(slots).to(DEV))
+    table = np.arange(8, dtype=np.int32)[None].repeat(2, 0)
+    table[0, 2], table[0, 5], table[1, :7] = -1, 8, 1 << 30
+    q = torch.randn(2, 4, dim, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).to(DEV)
+    lse = torch.empty(2, 4, device=DEV)
+    out = pq.pq_attn_decode(cache, q, torch.from_numpy(table).to(DEV), torch.tensor([n, n], dtype=torch.int32, device=DEV), n, 0.1, lse=lse)
+    inside = np.ones(n, bool)
+    inside[64:96] = inside[160:192] = False
+    want, wlse, mag, _ = OK.attention(f64(q)[0], OK.stored(fmt, group, f64(k), kt)[inside], OK.stored(fmt, group, f64(v), vt)[inside], 0.1)
+    assert np.all(np.abs(f64(out)[0] - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * mag)
+    assert np.abs(lse[0].cpu().numpy() - wlse).max() < 1e-4
+    assert np.all(f64(out)[1] == 0) and bool((lse[1] == -np.inf).all())
+
+
+def test_lengths_beyond_max_len_are_cut():
+    rng = np.random.default_rng(13)
+    k, v = rows(rng, 96, 1, 64), rows(rng, 96, 1, 64)
+    cache, _ = make_cache(I4, 32, 1, 64, 32, 3, k, v)
+    pq.pq_kv_write(cache, k, v, torch.arange(96, device=DEV))
+    table = torch.arange(3, dtype=torch.int32, device=DEV)[None]
+    q = torch.randn(1, 2, 64, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16).to(DEV)
+    call = lambda n, top: pq.pq_attn_decode(cache, q, table, torch.tensor([n], dtype=torch.int32, device=DEV), top, 0.1)
+    assert torch.equal(call(50, 96), call(1 << 30, 50))
+
+
+def test_no_sequences():
+    cache = pq.alloc_kv_cache(I4, 64, 2, 64, 32, 1)
+    q = torch.empty((0, 4, 64), dtype=torch.bfloat16, device=DEV)
+    out = pq.pq_attn_decode(cache, q, torch.empty((0, 1), dtype=torch.int32, device=DEV), torch.empty(0, dtype=torch.int32, device=DEV), 32, 0.1)
+    assert out.shape == (0, 4, 64)
+
+
+@pytest.mark.parametrize("fmt,group", [(I4, 64), (NV, 16), (BF, 0)])
+def test_graph_replays_and_other_streams(fmt, group):
+    """A decode step (write, attention) captured once: replays follow the lengths and slots in device memory, and a second stream
+    with a workspace of its own gives the same."""
+    rng = np.random.default_rng(14)
+    dim, heads, page, n = 128, 2, 32, 120
+    k, v = rows(rng, n, heads, dim), rows(rng, n, heads, dim)
+    cache, (kt, vt) = make_cache(fmt, group, heads, dim, page, 4, k, v)
+    pq.pq_kv_write(cache, k, v, torch.arange(n, device=DEV))
+    q = torch.randn(1, 8, dim, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).to(DEV)
+    table = torch.arange(4, dtype=torch.int32, device=DEV)[None]
+    lengths, slot = torch.tensor([n - 4], dtype=torch.int32, device=DEV), torch.tensor([n - 5], device=DEV)
+    kn, vn = k[:1].clone(), v[:1].clone()
+    ws = pq.pq_attn_decode_workspace(cache, 1, 8, 128)
+    out = torch.empty_like(q)
+    other = torch.cuda.Stream()
+
+    def step(o, w):
+        pq.pq_kv_write(cache, kn, vn, slot)
+        pq.pq_attn_decode(cache, q, table, lengths, 128, 0.1, out=o, workspace=w)
+
+    step(out, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(out, ws)
+    ws2 = pq.pq_attn_decode_workspace(cache, 1, 8, 128)
+    for i in range(4):
+        kn.copy_(k[10 + i:11 + i])
+        vn.copy_(v[20 + i:21 + i])
+        slot.fill_(n - 5 + i)
+        lengths.fill_(n - 4 + i)
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = out.clone()
+        eager = torch.empty_like(q)
+        other.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(other):
+            step(eager, ws2)
+        torch.cuda.current_stream().wait_stream(other)
+        torch.cuda.synchronize()
+        assert torch.equal(got.view(torch.int16), eager.view(torch.int16))
+        rk, rv = pq.pq_kv_read(cache, slot)
+        same_bits(rk, OK.read_back(fmt, group, f64(kn), kt))
+        same_bits(rv, OK.read_back(fmt, group, f64(vn), vt))
