@@ -575,7 +575,7 @@ int pq_kv_read(const pq_kv_cache* cache, const int64_t* slots, int64_t n, void* 
  * 16-byte aligned.  table: int32 device, (seq, i) at seq * table_ld + i; entries past a sequence's last page are not read.
  * lengths: int32 [seqs] device.  max_len: no length is longer (host; a longer one is cut to it); max_len <= page * table_ld.
  * A page outside 0 .. pages - 1 is not read: its tokens are left out.  What lies in a page behind a sequence's last token or in
- * front of its window does not matter, NaN included.  q_heads: a multiple of kv_heads.
+ * front of its window does not matter, NaN included.  q_heads: a multiple of kv_heads; seqs * q_heads * (max_len / 32 + 32) <= 2^30.
  * lse: float [seqs, q_heads] or NULL: ln of the sum of exp(scale * q . k), with which outputs over parts of a context are joined.
  * Scores, the softmax's sums and the outputs' are held in fp32; out is rounded once to bf16.
  * workspace: pq_attn_decode_workspace_bytes(cache, seqs, q_heads, max_len, window) bytes, 16-byte aligned; its first

@@ -760,6 +760,9 @@ static int check_attn_shape(const char* who, const pq_kv_cache* c, int64_t seqs,
     return fail(PQ_ERR_SHAPE, "%s: q_heads=%d must be a positive multiple of kv_heads=%d", who, q_heads, c->kv_heads);
   if (max_len < 0 || max_len > (1 << 30)) return fail(PQ_ERR_SHAPE, "%s: max_len=%lld outside 0 .. 2^30", who, (long long)max_len);
   if (window < 0) return fail(PQ_ERR_SHAPE, "%s: window=%lld is negative", who, (long long)window);
+  if (seqs * q_heads * (max_len / 32 + 32) > (int64_t)1 << 30)
+    return fail(PQ_ERR_SHAPE, "%s: seqs=%lld sequences of max_len=%lld and q_heads=%d are too many for one call", who, (long long)seqs,
+                (long long)max_len, q_heads);
   return PQ_OK;
 }
 

@@ -1,5 +1,12 @@
-// Attention of one new token a sequence over the paged cache (layout: pq_kv.h), the plain way: a workgroup takes a query head of
-// a sequence, its waves the tokens in turn, a lane D / 64 channels; running maximum and sum of the softmax in fp32.
+// Attention of one new token a sequence over the paged cache (layout: pq_kv.h).
+//
+//   out = sum_t p_t v_t / sum_t p_t,   p_t = 2^(c s_t - M),   s_t = q . k_t,   c = scale log2 e,   M any reference
+//
+// The queries that share a key head are the columns of both products, so the cache is read once for all of them:
+//   scores   S[token, head]  = K Q      v_mfma_f32_16x16x32, 16 tokens x 32 channels of keys, codes straight from memory
+//   outputs  O[channel, head] += V' P   the same instruction, 16 channels x 32 tokens; the scores' result layout (lane 16 q + h
+//                                       holds tokens 4 q .. 4 q + 3 of head h) is the operand layout of the weights
+// Nothing goes through LDS or between lanes in the loop.
 #include "pq_kv.h"
 #include "pq_qgemm_common.h"
 
@@ -9,92 +16,721 @@ KvView kv_view(const pq_kv_cache& c);
 
 namespace {
 
-// the stored key / value of a channel without the tensor scale
-template <class L>
-__device__ __forceinline__ float kv_key(const uint8_t* block, int t, int ch) {
-  const uint8_t* at = block + L::k_chunk(t, ch / 8);
-  if constexpr (L::FMT == kBf16) return bf16_to_f32(reinterpret_cast<const uint16_t*>(at)[ch % 8]);
-  else {
-    const uint32_t code = *reinterpret_cast<const uint32_t*>(at) >> (ch % 8 * 4);
-    if constexpr (L::FMT == kNvfp4)
-      return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code & 15u, 1.0f, 0)[0] * e4m3_decode(block[L::k_byte_at(t, ch / 16)]);
-    else
-      return (float)((int)(code & 15u) - 8) *
-             div_const(bf16_to_f32(*reinterpret_cast<const uint16_t*>(block + L::int_scale_at(t, ch / L::G))), 7.0f, 1.0f / 7.0f);
-  }
+typedef float float4_t __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+typedef uint16_t ushort2_t __attribute__((ext_vector_type(2)));
+typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
+
+constexpr int kAttnWaves = 4;            // of a workgroup; they take a segment's blocks in turn
+constexpr int kWorkers = 512;            // workgroups that share all blocks evenly: two a compute unit
+constexpr int kMaxSplits = 1024;         // workgroups that may hold a part of a pair: counters in the workspace
+constexpr int kLeastBlocks = 4;          // of a workgroup
+
+constexpr float kNoReference = -1e38f;   // M before the first token
+// A weight with its value's scale stays below 2^15 (fp16); M follows when it would not, to 2^7 and less: seldom, so that neither the
+// maximum over the lanes nor the rescaling is part of an ordinary block.
+constexpr float kHeadroom = 15.0f, kStart = 7.0f;
+
+__device__ __forceinline__ float4_t mfma(const uint4_t& a, const uint4_t& b, const float4_t& c, IntC<0>) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8_t, a), __builtin_bit_cast(half8_t, b), c, 0, 0, 0);
 }
+__device__ __forceinline__ float4_t mfma(const uint4_t& a, const uint4_t& b, const float4_t& c, IntC<1>) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
+
+// two fp32 to fp16, nearest even, packed
+__device__ __forceinline__ uint32_t cvt_pk_f16(float lo, float hi) {
+  typedef float f32x2_t __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){lo, hi}, half2_t));
+}
+
+// over the four lanes of a column (16 apart)
+__device__ __forceinline__ float column_max(float v) {
+  v = fmaxf(v, __shfl_xor(v, 16));
+  return fmaxf(v, __shfl_xor(v, 32));
+}
+__device__ __forceinline__ float column_sum(float v) {
+  v += __shfl_xor(v, 16);
+  return v + __shfl_xor(v, 32);
+}
+
+// what a lane holds of a block: codes (or bf16 values) and scales, loaded one block ahead
 template <class L>
-__device__ __forceinline__ float kv_value(const uint8_t* block, int t, int ch) {
-  const int n = ch % L::GV / L::PER, j = ch / L::GV * L::PER + ch % L::PER;
-  if constexpr (L::FMT == kBf16) return bf16_to_f32(reinterpret_cast<const uint16_t*>(block + L::v_pair(t, n, j / 2))[j % 2]);
-  else {
-    const uint32_t code = *reinterpret_cast<const uint16_t*>(block + L::v_quad(t, n, j / 4)) >> (j % 4 * 4);
-    if constexpr (L::FMT == kNvfp4)
-      return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code & 15u, 1.0f, 0)[0] * e4m3_decode(block[L::v_byte_at(t, ch / 16)]);
-    else
-      return (float)((int)(code & 15u) - 8) *
-             div_const(bf16_to_f32(*reinterpret_cast<const uint16_t*>(block + L::v_at + L::int_scale_at(t, ch / L::G))), 7.0f, 1.0f / 7.0f);
+struct Block {
+  static constexpr int NP = L::code_bytes / 1024;            // 16-byte pieces of the keys, and of the values
+  static constexpr int NS = L::FMT == kInt4 ? L::NG : 1;
+  uint4_t k[NP], v[NP];
+  uint4_t ks[NS], vs[NS];                                    // NVFP4: x, y of ks[0] the tiles' bytes for NK <= 4, all four for 8
+
+  __device__ __forceinline__ void load(const uint8_t* __restrict__ p, int lane) {
+    const int q = lane >> 4, n = lane & 15;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) k[i] = *reinterpret_cast<const uint4_t*>(p + i * 1024 + lane * 16);
+#pragma unroll
+    for (int i = 0; i < NP; ++i) v[i] = *reinterpret_cast<const uint4_t*>(p + L::v_at + i * 1024 + lane * 16);
+    if constexpr (L::FMT == kInt4) {
+#pragma unroll
+      for (int i = 0; i < NS; ++i) {
+        ks[i] = *reinterpret_cast<const uint4_t*>(p + L::code_bytes + q * 16 * NS + i * 16);
+        vs[i] = *reinterpret_cast<const uint4_t*>(p + L::v_at + L::code_bytes + q * 16 * NS + i * 16);
+      }
+    } else if constexpr (L::FMT == kNvfp4) {
+      constexpr int NK = L::NK;
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const uint8_t* at = p + L::code_bytes + ((s * 2 + (q >> 1)) * 16 + n) * NK;
+        if constexpr (NK == 2) ks[0][s] = *reinterpret_cast<const uint16_t*>(at);
+        else if constexpr (NK == 4) ks[0][s] = *reinterpret_cast<const uint32_t*>(at);
+        else {
+          const uint2 two = *reinterpret_cast<const uint2*>(at);
+          ks[0][2 * s] = two.x;
+          ks[0][2 * s + 1] = two.y;
+        }
+      }
+      const uint2 two = *reinterpret_cast<const uint2*>(p + L::v_byte_at(0, 0) + ((n / (256 / L::D)) * 4 + q) * 8);
+      vs[0][0] = two.x;
+      vs[0][1] = two.y;
+    }
+  }
+
+  // values of tokens outside [lo, hi) of the block become zeros: their weights are, and what lies there may be NaN
+  __device__ __forceinline__ void clear_values(int lane, int lo, int hi) {
+    const int q = lane >> 4;
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int t = s * 16 + q * 4 + r;
+        const bool keep = t >= lo && t < hi;
+        if constexpr (L::FMT == kBf16) {
+#pragma unroll
+          for (int w = 0; w < L::D / 32; ++w) {
+            const int f = (s * 4 + r) * (L::D / 32) + w;
+            v[f >> 2][f & 3] = keep ? v[f >> 2][f & 3] : 0u;
+          }
+        } else if constexpr (L::FMT == kNvfp4) {
+          vs[0][s] &= keep ? ~0u : ~(0xFFu << (8 * ((r & 1) * 2 + (r >> 1))));
+        } else {
+#pragma unroll
+          for (int g = 0; g < L::NG; ++g) {
+            const int x = (s * 4 + r) * L::NG + g;
+            vs[x >> 3][(x >> 1) & 3] &= keep ? ~0u : ~(0xFFFFu << (16 * (x & 1)));
+          }
+        }
+      }
+  }
+};
+
+// INT4: the scale of group g of token (s, r) of the lane
+template <class L>
+__device__ __forceinline__ float int_h(const uint4_t (&sc)[Block<L>::NS], int s, int r, int g) {
+  const int x = (s * 4 + r) * L::NG + g;
+  const uint32_t two = sc[x >> 3][(x >> 1) & 3];
+  return x & 1 ? bf16_hi(two) : bf16_lo(two);
+}
+
+// eight codes, two quads (of two tokens' values, or a key's chunk): the codes a of both as a pair of fp16 subnormals, the odd ones
+// 16 times as large
+struct IntCodes {
+  uint32_t d, swapped;
+  __device__ __forceinline__ explicit IntCodes(uint32_t x) : d(x), swapped(__builtin_amdgcn_perm(0u, x, 0x02030001u)) {}
+  __device__ __forceinline__ uint32_t pair(int a) const {
+    const uint32_t x = a & 2 ? swapped : d;
+    return a & 1 ? (x << 1) & 0x80708070u : x & 0x80078007u;
+  }
+};
+
+// The queries as the second operand, and what else the loop keeps of a pair.
+template <class L, int NT>
+struct Query {
+  uint4_t q[NT][L::NK];
+  float c[NT];                         // scores to powers of two
+
+  // queries first .. first + count - 1 of the sequence's; columns past them are zeros
+  __device__ __forceinline__ void load(const AttnCall& a, const uint16_t* __restrict__ src, int count, int lane, float key_unit) {
+    const int kq = lane >> 4, n = lane & 15;
+    const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;           // c is positive: the sign goes to the query
+    const float scale = fabsf(a.scale) * 1.4426950408889634f * key_unit;
+#pragma unroll
+    for (int ct = 0; ct < NT; ++ct) {
+      const bool ok = ct * 16 + n < count;
+      uint4_t x[L::NK];
+      float top = 0.0f;
+#pragma unroll
+      for (int kk = 0; kk < L::NK; ++kk) {
+        x[kk] = (uint4_t){0u, 0u, 0u, 0u};
+        if (ok) x[kk] = *reinterpret_cast<const uint4_t*>(src + (ct * 16 + n) * a.q_head + kk * 32 + kq * 8);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) x[kk][w] ^= flip;
+      }
+      if constexpr (L::FMT == kBf16) {
+        c[ct] = scale;
+#pragma unroll
+        for (int kk = 0; kk < L::NK; ++kk) q[ct][kk] = x[kk];
+      } else {
+        // fp16, the head's largest in [2^13, 2^14): bf16's eight bits stay exact down to 2^-27 of it
+#pragma unroll
+        for (int kk = 0; kk < L::NK; ++kk)
+#pragma unroll
+          for (int w = 0; w < 4; ++w) top = fmaxf(top, fmaxf(fabsf(bf16_lo(x[kk][w])), fabsf(bf16_hi(x[kk][w]))));
+        const int e = max((int)(as_u32(column_max(top)) >> 23) - 127, -100);
+        const float down = as_f32((uint32_t)(127 + 13 - e) << 23);
+        c[ct] = ldexpf(scale, e - 13);
+#pragma unroll
+        for (int kk = 0; kk < L::NK; ++kk) {
+          float f[8];
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            f[2 * w] = bf16_lo(x[kk][w]) * down;
+            f[2 * w + 1] = bf16_hi(x[kk][w]) * down;
+          }
+          if constexpr (L::FMT == kNvfp4) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) q[ct][kk][w] = cvt_pk_f16(f[2 * w], f[2 * w + 1]);
+          } else {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {                              // the order of IntCodes, and its factor
+              const float m = w & 1 ? 0.0625f : 1.0f;
+              q[ct][kk][w] = cvt_pk_f16(f[w] * m, f[w + 4] * m);
+            }
+          }
+        }
+      }
+    }
+  }
+};
+
+// The running result of a wave: O[channel n = 4 q + r of instruction j, head] and the sums of the weights, both times 2^M.
+template <class L, int NT>
+struct Result {
+  float4_t acc[NT][L::NJ];
+  float m[NT], l[NT];
+
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int ct = 0; ct < NT; ++ct) {
+      m[ct] = kNoReference;
+      l[ct] = 0.0f;
+#pragma unroll
+      for (int j = 0; j < L::NJ; ++j) acc[ct][j] = (float4_t){0.0f, 0.0f, 0.0f, 0.0f};
+    }
+  }
+};
+
+template <class L, int NT>
+__device__ __forceinline__ void attend_block(Block<L>& x, const Query<L, NT>& query, Result<L, NT>& out, int lane, int lo, int hi) {
+  constexpr IntC<L::FMT == kBf16> kType{};
+  const bool part = lo > 0 || hi < kKvBlock;                           // wave-uniform
+  if (__builtin_expect(part, 0)) x.clear_values(lane, lo, hi);
+  const int kq = lane >> 4;
+
+  // scores
+  float4_t s_[NT][2];
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    float4_t sum[NT][L::NG];
+#pragma unroll
+    for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+      for (int g = 0; g < (L::FMT == kInt4 ? L::NG : 1); ++g) sum[ct][g] = (float4_t){0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int kk = 0; kk < L::NK; ++kk) {
+      const int e = s * L::NK + kk;
+      uint4_t a;
+      if constexpr (L::FMT == kBf16) {
+        a = x.k[e];
+      } else {
+        const uint32_t d = x.k[e >> 2][e & 3];
+        if constexpr (L::FMT == kInt4) {
+#pragma unroll
+          for (int w = 0; w < 4; ++w) a[w] = IntCodes(d).pair(w);
+        } else {
+          // the bytes of chunks kk and kk ^ 1 convert together
+          const uint32_t bytes = L::NK == 8 ? x.ks[0][2 * s + (kk >> 2)] : x.ks[0][s];
+          const half2_t two = kk & 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)bytes, 1.0f, 1)
+                                     : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)bytes, 1.0f, 0);
+          const half2_t sc = kk & 1 ? (half2_t){two.y, two.y} : (half2_t){two.x, two.x};
+          a[0] = h2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, 1.0f, 0) * sc);
+          a[1] = h2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, 1.0f, 1) * sc);
+          a[2] = h2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, 1.0f, 2) * sc);
+          a[3] = h2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, 1.0f, 3) * sc);
+        }
+      }
+      const int g = L::FMT == kInt4 ? kk * 32 / (L::G ? L::G : 1) : 0;
+#pragma unroll
+      for (int ct = 0; ct < NT; ++ct) sum[ct][g] = mfma(a, query.q[ct][kk], sum[ct][g], kType);
+    }
+#pragma unroll
+    for (int ct = 0; ct < NT; ++ct) {
+      if constexpr (L::FMT == kInt4) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          float v = int_h<L>(x.ks, s, r, 0) * sum[ct][0][r];
+#pragma unroll
+          for (int g = 1; g < L::NG; ++g) v = __builtin_fmaf(int_h<L>(x.ks, s, r, g), sum[ct][g][r], v);
+          s_[ct][s][r] = v;
+        }
+      } else {
+        s_[ct][s] = sum[ct][0];
+      }
+    }
+  }
+  // INT4: 2^eb bounds the lane's scales; kept from going where the sum of the weights would overflow
+  float eb = 0.0f;
+  if constexpr (L::FMT == kInt4) {
+    ushort2_t top = {0, 0};
+#pragma unroll
+    for (int w = 0; w < 4 * L::NG; ++w) {
+      const uint32_t two = x.vs[w >> 2][w & 3];        // by value: a bit cast of a vector's element takes its first
+      top = __builtin_elementwise_max(top, __builtin_bit_cast(ushort2_t, two));
+    }
+    eb = (float)(max((int)max(top.x, top.y) >> 7, 127 - 80) - 126);
+  }
+  // weights
+  float p[NT][2][4];
+#pragma unroll
+  for (int ct = 0; ct < NT; ++ct) {
+    if (__builtin_expect(part, 0)) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int t = (i >> 2) * 16 + kq * 4 + (i & 3);
+        if (t < lo || t >= hi) s_[ct][i >> 2][i & 3] = -1e38f;
+      }
+    }
+    float top = fmaxf(s_[ct][0][0], s_[ct][0][1]);
+#pragma unroll
+    for (int i = 2; i < 8; ++i) top = fmaxf(top, s_[ct][i >> 2][i & 3]);
+    const float bound = top * query.c[ct] + eb;
+    if (__builtin_expect(__any(bound > out.m[ct] + kHeadroom), 0)) {
+      const float b = column_max(bound);
+      const float m = b > out.m[ct] + kHeadroom ? b - kStart : out.m[ct];
+      const float f = __builtin_amdgcn_exp2f(out.m[ct] - m);
+      out.m[ct] = m;
+      out.l[ct] *= f;
+#pragma unroll
+      for (int j = 0; j < L::NJ; ++j) out.acc[ct][j] *= f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s_[ct][i >> 2][i & 3], query.c[ct], -out.m[ct]));
+      if (__builtin_expect(part, 0)) {
+        const int t = (i >> 2) * 16 + kq * 4 + (i & 3);
+        w = t < lo || t >= hi ? 0.0f : w;
+      }
+      p[ct][i >> 2][i & 3] = w;
+      out.l[ct] += w;
+    }
+  }
+  // outputs
+  if constexpr (L::FMT == kInt4) {
+    uint4_t w[NT][L::NG];
+#pragma unroll
+    for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+      for (int g = 0; g < L::NG; ++g)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int s = i >> 1, r = (i & 1) * 2;
+          w[ct][g][i] = cvt_pk_f16(p[ct][s][r] * int_h<L>(x.vs, s, r, g), p[ct][s][r + 1] * int_h<L>(x.vs, s, r + 1, g));
+        }
+#pragma unroll
+    for (int j = 0; j < L::NJ; ++j) {
+      uint4_t a;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int f = i * L::NQ + j / 4;
+        a[i] = IntCodes(x.v[f >> 2][f & 3]).pair(j & 3);
+      }
+#pragma unroll
+      for (int ct = 0; ct < NT; ++ct) out.acc[ct][j] = mfma(a, w[ct][j / L::PER], out.acc[ct][j], kType);
+    }
+  } else if constexpr (L::FMT == kNvfp4) {
+    uint4_t w[NT];
+#pragma unroll
+    for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[ct][i] = cvt_pk_f16(p[ct][i >> 1][i & 1], p[ct][i >> 1][(i & 1) + 2]);
+    half2_t sc[4];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      sc[2 * s] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x.vs[0][s], 1.0f, 0);
+      sc[2 * s + 1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x.vs[0][s], 1.0f, 1);
+    }
+#pragma unroll
+    for (int jq = 0; jq < L::NQ; ++jq) {
+      uint32_t even[2], odd[2];                    // bytes: channels 0 and 2 (1 and 3) of tokens 0 | 2, then of tokens 1 | 3
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const int f0 = (s * 2) * L::NQ + jq, f1 = (s * 2 + 1) * L::NQ + jq;
+        const uint32_t x0 = x.v[f0 >> 2][f0 & 3], x1 = x.v[f1 >> 2][f1 & 3];
+        even[s] = (x0 & 0x0F0F0F0Fu) | ((x1 << 4) & 0xF0F0F0F0u);
+        odd[s] = ((x0 >> 4) & 0x0F0F0F0Fu) | (x1 & 0xF0F0F0F0u);
+      }
+      auto channel = [&](const uint32_t (&d)[2], auto byte, int j) {
+        constexpr int B = decltype(byte)::value;
+        uint4_t a;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          a[2 * s] = h2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d[s], 1.0f, B) * sc[2 * s]);
+          a[2 * s + 1] = h2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d[s], 1.0f, B + 2) * sc[2 * s + 1]);
+        }
+#pragma unroll
+        for (int ct = 0; ct < NT; ++ct) out.acc[ct][j] = mfma(a, w[ct], out.acc[ct][j], kType);
+      };
+      channel(even, IntC<0>{}, jq * 4);
+      channel(odd, IntC<0>{}, jq * 4 + 1);
+      channel(even, IntC<1>{}, jq * 4 + 2);
+      channel(odd, IntC<1>{}, jq * 4 + 3);
+    }
+  } else {
+    // the weights as two bf16 each, 16 bits: one would add as much error as the output's own rounding
+    uint4_t w[NT][2];
+#pragma unroll
+    for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float p0 = p[ct][i >> 1][(i & 1) * 2], p1 = p[ct][i >> 1][(i & 1) * 2 + 1];
+        const uint32_t two = cvt_pk_bf16(p0, p1);
+        w[ct][0][i] = two;
+        w[ct][1][i] = cvt_pk_bf16(p0 - bf16_lo(two), p1 - bf16_hi(two));
+      }
+#pragma unroll
+    for (int j = 0; j < L::NJ; ++j) {
+      uint4_t a;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int f0 = (i * 2) * (L::D / 32) + j / 2, f1 = f0 + L::D / 32;
+        a[i] = __builtin_amdgcn_perm(x.v[f1 >> 2][f1 & 3], x.v[f0 >> 2][f0 & 3], j & 1 ? 0x07060302u : 0x05040100u);
+      }
+#pragma unroll
+      for (int ct = 0; ct < NT; ++ct) {
+        out.acc[ct][j] = mfma(a, w[ct][0], out.acc[ct][j], kType);
+        out.acc[ct][j] = mfma(a, w[ct][1], out.acc[ct][j], kType);
+      }
+    }
   }
 }
 
-constexpr float kNoScore = -1e38f;       // a running maximum before the first score
+// ------------------------------------------------------------------------ which blocks are whose
+// All blocks of all pairs (sequence, key head, sixteen or thirty-two of its queries) are numbered sequence by sequence, pair by pair.
+// A worker takes `per` of them in a row: the work is even whatever the lengths.  Where `per` is small, or the pairs are many, each
+// pair's blocks are padded to a multiple of it instead: no worker then holds two pairs.
+struct Plan {
+  int per;                 // blocks a worker
+  bool padded;
+};
+struct Lengths {           // of sequence b: first block, blocks (at least one), first token and end
+  int first_token, end, first, n;
+};
+__device__ __forceinline__ Lengths lengths_of(const AttnCall& a, int b) {
+  Lengths r;
+  r.end = min(max(a.lengths[b], 0), a.max_len);
+  r.first_token = a.window ? max(0, r.end - a.window) : 0;
+  r.first = r.first_token / kKvBlock;
+  r.n = max(1, (r.end + kKvBlock - 1) / kKvBlock - r.first);
+  return r;
+}
+__device__ __forceinline__ int wave_sum_i32(int v) {
+#pragma unroll
+  for (int off = 32; off; off >>= 1) v += __shfl_xor(v, off);
+  return v;
+}
+__device__ __forceinline__ int wave_max_i32(int v) {
+#pragma unroll
+  for (int off = 32; off; off >>= 1) v = max(v, __shfl_xor(v, off));
+  return v;
+}
+__device__ __forceinline__ int wave_scan_i32(int v, int lane) {        // inclusive
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int o = __shfl_up(v, off);
+    if (lane >= off) v += o;
+  }
+  return v;
+}
 
-template <class L>
-__global__ __launch_bounds__(256) void attn_decode_kernel(KvView cache, AttnCall a) {
-  constexpr int D = L::D, C = D / 64;
-  __shared__ float part[4][D + 2];
-  const int h = blockIdx.x, b = blockIdx.y, head = h / (a.q_heads / cache.heads);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int len = min(a.lengths[b], a.max_len), first = a.window ? max(0, len - a.window) : 0;
-  float c = a.scale;
-  if constexpr (L::FMT == kNvfp4) c *= *cache.k_ts;
-  float q[C], acc[C] = {}, m = kNoScore, l = 0.0f;
-#pragma unroll
-  for (int j = 0; j < C; ++j) q[j] = bf16_to_f32(a.q[b * a.q_ld + h * a.q_head + lane * C + j]);
-  for (int t = first + wave; t < len; t += 4) {
-    const int64_t page = a.table[b * a.table_ld + (t >> cache.page_log2)];
-    if (page < 0 || page >= cache.pages) continue;
-    const uint8_t* block = kv_block<L>(cache, (page << cache.page_log2) + (t & ((1 << cache.page_log2) - 1)), head);
-    float s = 0.0f;
-#pragma unroll
-    for (int j = 0; j < C; ++j) s = __builtin_fmaf(q[j], kv_key<L>(block, t & 31, lane * C + j), s);
-#pragma unroll
-    for (int off = 32; off; off >>= 1) s += __shfl_xor(s, off);
-    s *= c;
-    const float m2 = fmaxf(m, s), f = __expf(m - m2), p = __expf(s - m2);
-    m = m2;
-    l = l * f + p;
-#pragma unroll
-    for (int j = 0; j < C; ++j) acc[j] = acc[j] * f + p * kv_value<L>(block, t & 31, lane * C + j);
+template <class L, int NT>
+constexpr int part_floats() { return NT * (L::NJ * 256 + 32); }        // a part's outputs, then (M, l) of its heads
+
+// the part of a pair that worker w holds, first the one that began it
+__device__ __forceinline__ int part_slot(int w, int w_first) { return w == w_first ? 2 * w + 1 : 2 * w; }
+
+template <class L, int NT>
+__global__ __launch_bounds__(64 * kAttnWaves, (L::D == 256 && NT == 2) ? 1 : 2) void attn_decode_kernel(KvView cache, AttnCall a,
+                                                                                                       int chunks) {
+  constexpr int NJ = L::NJ;
+  __shared__ float4_t shared_acc[2][NT * NJ][64];
+  __shared__ float shared_ml[2][NT][2][64];
+  __shared__ int last_one;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kq = lane >> 4, col = lane & 15;
+  const int per_head = a.q_heads / cache.heads, pairs = cache.heads * chunks;      // pairs of a sequence
+  int* counters = static_cast<int*>(a.ws);
+  float* parts = reinterpret_cast<float*>(static_cast<uint8_t*>(a.ws) + PQ_ATTN_DECODE_ZERO_BYTES);
+
+  // the plan: the same in every wave
+  int blocks = 0, longest = 0;
+  for (int b0 = 0; b0 < a.seqs; b0 += 64) {
+    const int n = b0 + lane < a.seqs ? lengths_of(a, b0 + lane).n : 0;
+    blocks += wave_sum_i32(n);
+    longest = max(longest, wave_max_i32(n));
   }
+  Plan plan;
+  plan.per = max((int)(((int64_t)blocks * pairs + kWorkers - 1) / kWorkers), kLeastBlocks);
+  plan.padded = plan.per < 16;
+  if (plan.padded) {
+    int items = 0;
+    for (int b0 = 0; b0 < a.seqs; b0 += 64) {
+      const int n = b0 + lane < a.seqs ? lengths_of(a, b0 + lane).n : 0;
+      items += wave_sum_i32((n + plan.per - 1) / plan.per);
+    }
+    if (items * pairs > (int)gridDim.x || items * pairs > kMaxSplits) plan.padded = false;
+  }
+  if (!plan.padded && a.seqs * pairs >= 4 * kWorkers) {                // pairs enough: one a worker
+    plan.per = longest;
+    plan.padded = true;
+  }
+  auto padded = [&](int n) { return plan.padded ? (n + plan.per - 1) / plan.per * plan.per : n; };
+
+  const int64_t u_begin = (int64_t)blockIdx.x * plan.per;
+  int64_t u = u_begin, base = 0;
+  int b = 0;                                                           // the sequence that holds block u, its first block `base`
+  for (int b0 = 0;; b0 += 64) {
+    if (b0 >= a.seqs) return;                                          // workgroups past the last block
+    const int n = b0 + lane < a.seqs ? padded(lengths_of(a, b0 + lane).n) * pairs : 0;
+    const int incl = wave_scan_i32(n, lane);
+    const uint64_t past = __ballot(base + incl > u);
+    if (past) {
+      const int at = __ffsll((unsigned long long)past) - 1;
+      base += __shfl(incl - n, at);
+      b = b0 + at;
+      break;
+    }
+    base += __shfl(incl, 63);
+  }
+  b = __builtin_amdgcn_readfirstlane(b);
+
+  int64_t u_end = u_begin + plan.per;
+  while (u < u_end && b < a.seqs) {
+    const Lengths len = lengths_of(a, b);
+    const int np = padded(len.n), off = (int)(u - base);
+    const int pair = off / np, t_at = off % np;
+    const int64_t pair_base = base + (int64_t)pair * np;
+    int t0, t1, w_first, w_last;
+    if (plan.padded) {                                                 // even parts
+      const int k = t_at / plan.per, of = np / plan.per;
+      t0 = (int)((int64_t)len.n * k / of);
+      t1 = (int)((int64_t)len.n * (k + 1) / of);
+      w_first = (int)(pair_base / plan.per);
+      w_last = w_first + of - 1;
+      u = u_end;
+    } else {
+      t0 = t_at;
+      t1 = min(np, t_at + (int)(u_end - u));
+      w_first = (int)(pair_base / plan.per);
+      w_last = (int)((pair_base + np - 1) / plan.per);
+      u = pair_base + np;
+      if (pair + 1 == pairs) base = u;
+    }
+    const int seq = b;
+    if (!plan.padded && pair + 1 == pairs) ++b;
+
+    const int head = pair / chunks, h0 = pair % chunks * 16 * NT;
+    const int count = min(per_head - h0, 16 * NT);
+    Query<L, NT> query;
+    const float key_unit = L::FMT == kNvfp4 ? *cache.k_ts : L::FMT == kInt4 ? 16777216.0f / 7.0f : 1.0f;
+    query.load(a, a.q + seq * a.q_ld + (int64_t)(head * per_head + h0) * a.q_head, count, lane, key_unit);
+    Result<L, NT> res;
+    res.clear();
+
+    const int32_t* table = a.table + seq * a.table_ld;
+    const int n_mine = (t1 - t0 - wave + kAttnWaves - 1) / kAttnWaves;
+    if (n_mine > 0) {
+      int pages = 0;                                                   // of this wave's next 64 blocks, a lane each
+      auto fetch_pages = [&](int i) {
+        const int mine = i + lane;
+        pages = 0;
+        if (mine < n_mine) {
+          const int token = (len.first + t0 + wave + mine * kAttnWaves) * kKvBlock;
+          pages = token < len.end ? table[token >> cache.page_log2] : -1;
+          if (pages < 0 || pages >= cache.pages) pages = -1;
+        }
+      };
+      auto address = [&](int i, bool& ok) {
+        const int page = __builtin_amdgcn_readlane(pages, i & 63);
+        ok = page >= 0;
+        const int block = len.first + t0 + wave + i * kAttnWaves, in_page = block & ((1 << (cache.page_log2 - 5)) - 1);
+        return cache.data + ((((int64_t)(ok ? page : 0) * cache.heads + head) << (cache.page_log2 - 5)) + in_page) * L::bytes;
+      };
+      fetch_pages(0);
+      Block<L> cur, next;
+      bool ok, ok_next = false;
+      cur.load(address(0, ok), lane);
+      for (int i = 0; i < n_mine; ++i) {
+        if (i + 1 < n_mine) {
+          if (((i + 1) & 63) == 0) fetch_pages(i + 1);
+          next.load(address(i + 1, ok_next), lane);
+        }
+        const int token = (len.first + t0 + wave + i * kAttnWaves) * kKvBlock;
+        const int lo = ok ? max(0, len.first_token - token) : kKvBlock, hi = min(kKvBlock, len.end - token);
+        attend_block<L, NT>(cur, query, res, lane, lo, hi);
+        cur = next;
+        ok = ok_next;
+      }
+    }
+    if constexpr (L::FMT == kInt4)                                     // the odd codes came 16 times as large
 #pragma unroll
-  for (int j = 0; j < C; ++j) part[wave][lane * C + j] = acc[j];
-  if (lane == 0) {
-    part[wave][D] = m;
-    part[wave][D + 1] = l;
+      for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+        for (int j = 1; j < NJ; j += 2) res.acc[ct][j] *= 0.0625f;
+#pragma unroll
+    for (int ct = 0; ct < NT; ++ct) res.l[ct] = column_sum(res.l[ct]);
+
+    // join the waves: 2, 3 into 0, 1, then 1 into 0
+    auto put = [&](int at) {
+#pragma unroll
+      for (int ct = 0; ct < NT; ++ct) {
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) shared_acc[at][ct * NJ + j][lane] = res.acc[ct][j];
+        shared_ml[at][ct][0][lane] = res.m[ct];
+        shared_ml[at][ct][1][lane] = res.l[ct];
+      }
+    };
+    auto take = [&](int at) {
+#pragma unroll
+      for (int ct = 0; ct < NT; ++ct) {
+        const float om = shared_ml[at][ct][0][lane], ol = shared_ml[at][ct][1][lane];
+        const float m = fmaxf(res.m[ct], om);
+        const float f = __builtin_amdgcn_exp2f(res.m[ct] - m), g = __builtin_amdgcn_exp2f(om - m);
+        res.m[ct] = m;
+        res.l[ct] = res.l[ct] * f + ol * g;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) res.acc[ct][j] = res.acc[ct][j] * f + shared_acc[at][ct * NJ + j][lane] * g;
+      }
+    };
+    __syncthreads();                                                   // the last segment's reads are over
+    if (wave >= 2) put(wave - 2);
+    __syncthreads();
+    if (wave < 2) take(wave);
+    if (wave == 1) put(1);
+    __syncthreads();
+    if (wave == 0) take(1);
+
+    bool write = wave == 0;
+    if (w_first != w_last) {                                           // a part of a pair: the last worker to finish joins them
+      constexpr int kFloats = part_floats<L, NT>();
+      if (wave == 0) {
+        float* part = parts + (size_t)part_slot(blockIdx.x, w_first) * kFloats;
+#pragma unroll
+        for (int ct = 0; ct < NT; ++ct) {
+          const int heads = min(16, count - ct * 16);
+          if (col < heads) {
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+              *reinterpret_cast<float4_t*>(part + ct * NJ * 256 + ((j * 4 + kq) * heads + col) * 4) = res.acc[ct][j];
+            if (kq == 0) *reinterpret_cast<float2*>(part + NT * NJ * 256 + ct * 32 + col * 2) = make_float2(res.m[ct], res.l[ct]);
+          }
+        }
+        __threadfence();
+        if (lane == 0) last_one = atomicAdd(counters + w_first, 1) == w_last - w_first;
+      }
+      __syncthreads();
+      if (!last_one) continue;
+      __threadfence();
+      // the common reference and the sum of the weights, then the outputs; the waves take the parts in turn
+#pragma unroll
+      for (int ct = 0; ct < NT; ++ct) {
+        const int heads = min(16, count - ct * 16);
+        float m = kNoReference;
+        for (int w = w_first + kq; w <= w_last; w += 4)
+          if (col < heads) m = fmaxf(m, parts[(size_t)part_slot(w, w_first) * kFloats + NT * NJ * 256 + ct * 32 + col * 2]);
+        m = column_max(m);
+        float l = 0.0f;
+        float4_t acc[NJ];
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[j] = (float4_t){0.0f, 0.0f, 0.0f, 0.0f};
+        if (col < heads) {
+#pragma unroll 2
+          for (int w = w_first + wave; w <= w_last; w += kAttnWaves) {
+            const float* part = parts + (size_t)part_slot(w, w_first) * kFloats;
+            const float2 ml = *reinterpret_cast<const float2*>(part + NT * NJ * 256 + ct * 32 + col * 2);
+            const float f = __builtin_amdgcn_exp2f(ml.x - m);
+            l += ml.y * f;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j)
+              acc[j] += *reinterpret_cast<const float4_t*>(part + ct * NJ * 256 + ((j * 4 + kq) * heads + col) * 4) * f;
+          }
+        }
+        res.m[ct] = m;
+        res.l[ct] = l;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) res.acc[ct][j] = acc[j];
+      }
+      __syncthreads();
+      if (wave >= 2) put(wave - 2);
+      __syncthreads();
+      if (wave < 2) take(wave);
+      if (wave == 1) put(1);
+      __syncthreads();
+      if (wave == 0) take(1);
+      if (threadIdx.x == 0) counters[w_first] = 0;                     // for the next call
+    }
+    if (write) {
+      const float unit = L::FMT == kNvfp4 ? *cache.v_ts : L::FMT == kInt4 ? 16777216.0f / 7.0f : 1.0f;
+#pragma unroll
+      for (int ct = 0; ct < NT; ++ct) {
+        const int h = ct * 16 + col;
+        if (h >= count) continue;
+        const int64_t q_head = head * per_head + h0 + h;
+        const float inv = res.l[ct] > 0.0f ? 1.0f / res.l[ct] : 0.0f;
+        uint16_t* o = a.out + seq * a.out_ld + q_head * a.out_head;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int g = 0; g < NJ / L::PER; ++g) {
+            uint32_t two[L::PER / 2];
+#pragma unroll
+            for (int j = 0; j < L::PER / 2; ++j)
+              two[j] = cvt_pk_bf16(res.acc[ct][g * L::PER + 2 * j][r] * inv * unit, res.acc[ct][g * L::PER + 2 * j + 1][r] * inv * unit);
+            __builtin_memcpy(__builtin_assume_aligned(o + g * L::GV + (kq * 4 + r) * L::PER, L::PER >= 8 ? 16 : L::PER * 2), two, L::PER * 2);
+          }
+        if (a.lse && kq == 0)
+          a.lse[(int64_t)seq * a.q_heads + q_head] = res.l[ct] > 0.0f ? (res.m[ct] + log2f(res.l[ct])) * 0.6931471805599453f : -INFINITY;
+      }
+    }
   }
-  __syncthreads();
-  if (threadIdx.x >= D) return;
-  float top = kNoScore, total = 0.0f, sum = 0.0f;
-  for (int w = 0; w < 4; ++w) top = fmaxf(top, part[w][D]);
-  for (int w = 0; w < 4; ++w) {
-    const float f = __expf(part[w][D] - top);
-    total += part[w][D + 1] * f;
-    sum += part[w][threadIdx.x] * f;
-  }
-  float o = total > 0.0f ? sum / total : 0.0f;
-  if constexpr (L::FMT == kNvfp4) o *= *cache.v_ts;
-  a.out[b * a.out_ld + h * a.out_head + threadIdx.x] = (uint16_t)cvt_pk_bf16(o, 0.0f);
-  if (a.lse && threadIdx.x == 0) a.lse[(int64_t)b * a.q_heads + h] = total > 0.0f ? top + logf(total) : -INFINITY;
+}
+
+// queries of a key head that share a pass: two tiles of columns where one does not hold them
+int tiles_of(const pq_kv_cache& c, int q_heads) { return q_heads / c.kv_heads > 16 ? 2 : 1; }
+int chunks_of(const pq_kv_cache& c, int q_heads) {
+  const int width = 16 * tiles_of(c, q_heads);
+  return (q_heads / c.kv_heads + width - 1) / width;
+}
+int64_t grid_of(const pq_kv_cache& c, int64_t seqs, int q_heads, int64_t max_len, int64_t window) {
+  const int64_t pairs = seqs * c.kv_heads * chunks_of(c, q_heads);
+  int64_t n = (max_len + kKvBlock - 1) / kKvBlock;                     // blocks of the longest sequence
+  if (window) n = n < window / kKvBlock + 2 ? n : window / kKvBlock + 2;
+  if (n < 1) n = 1;
+  const int64_t parts = pairs * ((n + kLeastBlocks - 1) / kLeastBlocks), most = pairs > kMaxSplits ? pairs : kMaxSplits;
+  return parts < most ? parts : most;
 }
 
 }  // namespace
 
-size_t attn_decode_workspace_bytes(const pq_kv_cache&, int64_t, int, int64_t, int64_t) { return PQ_ATTN_DECODE_ZERO_BYTES; }
+size_t attn_decode_workspace_bytes(const pq_kv_cache& c, int64_t seqs, int q_heads, int64_t max_len, int64_t window) {
+  int64_t workers = grid_of(c, seqs, q_heads, max_len, window);
+  if (workers > kMaxSplits) workers = kMaxSplits;
+  const int tiles = tiles_of(c, q_heads);
+  const size_t floats = tiles * (size_t)(c.head_dim / 16 * 256 + 32);
+  return PQ_ATTN_DECODE_ZERO_BYTES + (size_t)workers * 2 * floats * sizeof(float);
+}
 
 int run_attn_decode(const pq_kv_cache& c, const AttnCall& a, hipStream_t st) {
+  const int grid = (int)grid_of(c, a.seqs, a.q_heads, a.max_len, a.window), chunks = chunks_of(c, a.q_heads);
   return kv_dispatch(c.fmt, c.group, c.head_dim, [&](auto l) {
-    attn_decode_kernel<decltype(l)><<<dim3(a.q_heads, a.seqs), 256, 0, st>>>(kv_view(c), a);
+    if (tiles_of(c, a.q_heads) == 1) attn_decode_kernel<decltype(l), 1><<<grid, 64 * kAttnWaves, 0, st>>>(kv_view(c), a, chunks);
+    else attn_decode_kernel<decltype(l), 2><<<grid, 64 * kAttnWaves, 0, st>>>(kv_view(c), a, chunks);
     return check_hip(hipGetLastError(), "pq_attn_decode");
   });
 }

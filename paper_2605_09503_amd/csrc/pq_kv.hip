@@ -59,7 +59,10 @@ __global__ __launch_bounds__(256) void kv_write_kernel(KvView cache, KvRows k, K
           codes = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(codes, f[6] * sc.inv, f[7] * sc.inv, 1.0f, 3);
           if (ok && c % LPG == 0) block[L::k_byte_at(t, c / LPG)] = (uint8_t)sc.byte;
         } else {
-          codes = int_codes8(f, int_scale<kInt4>(a).inv) ^ 0x88888888u;      // z + 8
+          const float inv = int_scale<kInt4>(a).inv;
+          codes = 0;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) codes |= int_encode(f[j], inv, j & 3) << (j & 4) * 4;
           if (ok && c % LPG == 0) *reinterpret_cast<uint16_t*>(block + L::int_scale_at(t, c / LPG)) = (uint16_t)(as_u32(a) >> 16);
         }
         if (ok) *reinterpret_cast<uint32_t*>(block + L::k_chunk(t, c)) = codes;
@@ -106,10 +109,8 @@ __global__ __launch_bounds__(256) void kv_write_kernel(KvView cache, KvRows k, K
           for (int j = 0; j < PAIRS; ++j) {
             const int at = g * PER + 2 * j;                    // nibble of the first of two
             const float lo = bf16_lo(x[g * PAIRS + j]), hi = bf16_hi(x[g * PAIRS + j]);
-            uint32_t two;
-            if constexpr (L::FMT == kNvfp4) two = nv4_code_pair(lo, hi, inv);
-            else two = (int_code(lo, inv, 7.0f) | int_code(hi, inv, 7.0f) << 4) ^ 0x88u;
-            codes[at / 8] |= two << (at % 8 * 4);
+            if constexpr (L::FMT == kNvfp4) codes[at / 8] |= nv4_code_pair(lo, hi, inv) << (at % 8 * 4);
+            else codes[at / 8] |= (int_encode(lo, inv, at & 3) | int_encode(hi, inv, (at + 1) & 3)) << (at & 4) * 4;
           }
         }
         if (ok)
@@ -121,9 +122,7 @@ __global__ __launch_bounds__(256) void kv_write_kernel(KvView cache, KvRows k, K
   }
 }
 
-// a code's value: INT4 z * s, NVFP4 value * s_b * T, every step one binary32 operation
-__device__ __forceinline__ float int_value(uint32_t nibble, float s) { return (float)((int)(nibble & 15u) - 8) * s; }
-
+// values: INT4 z * s, NVFP4 value * s_b * T, every step one binary32 operation
 template <class L>
 __global__ __launch_bounds__(256) void kv_read_kernel(KvView cache, const int64_t* __restrict__ slots, int64_t n, KvRows k, KvRows v) {
   constexpr int D = L::D;
@@ -162,7 +161,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvView cache, const int64_
             const float a = as_f32((uint32_t)*reinterpret_cast<const uint16_t*>(block + L::int_scale_at(t, c / (L::G / 8))) << 16);
             const float s = div_const(a, 7.0f, 1.0f / 7.0f);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) f[j] = int_value(codes >> (4 * j), s);
+            for (int j = 0; j < 8; ++j) f[j] = int_decode(codes >> (j & 4) * 4, j & 3) * s;
           }
           y = make_uint4(cvt_pk_bf16(f[0], f[1]), cvt_pk_bf16(f[2], f[3]), cvt_pk_bf16(f[4], f[5]), cvt_pk_bf16(f[6], f[7]));
         }
@@ -196,12 +195,11 @@ __global__ __launch_bounds__(256) void kv_read_kernel(KvView cache, const int64_
 #pragma unroll
             for (int j = 0; j < PAIRS; ++j) {
               const int at = g * PER + 2 * j;
-              const uint32_t two = quad[at / 4] >> (at % 4 * 4);
               if constexpr (L::FMT == kNvfp4) {
-                const auto f = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(two, 1.0f, 0);
+                const auto f = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(quad[at / 4] >> (at % 4 * 4), 1.0f, 0);
                 y[g * PAIRS + j] = cvt_pk_bf16(f[0] * s * T, f[1] * s * T);
               } else {
-                y[g * PAIRS + j] = cvt_pk_bf16(int_value(two, s), int_value(two >> 4, s));
+                y[g * PAIRS + j] = cvt_pk_bf16(int_decode(quad[at / 4], at & 3) * s, int_decode(quad[at / 4], (at + 1) & 3) * s);
               }
             }
           }

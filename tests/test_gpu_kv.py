@@ -137,6 +137,24 @@ def test_nothing_to_write():
 
 # ------------------------------------------------------------------------ attention
 
+def check(got, got_lse, q64, ks, vs, scale, label=""):
+    """one sequence's outputs and lse (or None) against the oracle over the attended tokens, within the tolerance above"""
+    want, wlse, mag, top = OK.attention(q64, ks, vs, scale)
+    n, dim = ks.shape[0], q64.shape[1]
+    ds, sums = (dim + 16) * 2.0 ** -24 * top, n * 2.0 ** -24
+    tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -11 + 2 * ds[:, None] + 2 * sums) * mag * (1 + 2.0 ** -7) + 1e-38
+    if n:
+        tol = tol + n * 2.0 ** -31 * np.abs(vs).max()
+    worst = (np.abs(got - want) - tol).max()
+    assert worst <= 0, "%s: off by %g over the tolerance" % (label, worst)
+    if got_lse is not None:
+        if n == 0:
+            assert np.all(got_lse == -np.inf), label
+        else:
+            off = (np.abs(got_lse - wlse) - (ds + sums + 2.0 ** -22 * (1 + np.abs(wlse)))).max()
+            assert off <= 0, "%s: lse off by %g over the tolerance" % (label, off)
+
+
 def run_case(fmt, group, dim, lengths, heads=2, per=4, page=32, window=0, scale=None, seed=0, lse=True, noise=True, big=None,
              q_scale=1.0, max_len=None):
     """One call checked against the oracle; the cache is full of NaN behind every sequence, and in front of its window."""
@@ -182,20 +200,8 @@ def run_case(fmt, group, dim, lengths, heads=2, per=4, page=32, window=0, scale=
         r = OK.attended(m, window)
         sel = slice(at + r.start, at + m)
         at += m
-        want, wlse, mag, big_s = OK.attention(q64[b], ks[sel], vs[sel], scale)
-        ds = (dim + 16) * 2.0 ** -24 * big_s
-        sums = len(r) * 2.0 ** -24
-        tol = 2.0 ** -8 * np.abs(want) + (2.0 ** -11 + 2 * ds[:, None] + 2 * sums) * mag * (1 + 2.0 ** -7) + 1e-38
-        if len(r):
-            tol = tol + len(r) * 2.0 ** -31 * np.abs(vs[sel]).max()
-        worst = np.abs(got[b] - want) - tol
-        assert np.all(worst <= 0), "seq %d (%d tokens): off by %g over the tolerance" % (b, m, worst.max())
-        if lse:
-            got_l = lse_t[b].cpu().numpy().astype(np.float64)
-            if len(r) == 0:
-                assert np.all(got_l == -np.inf)
-            else:
-                assert np.all(np.abs(got_l - wlse) <= ds + sums + 2.0 ** -22 * (1 + np.abs(wlse))), np.abs(got_l - wlse).max()
+        check(got[b], lse_t[b].cpu().numpy().astype(np.float64) if lse else None, q64[b], ks[sel], vs[sel], scale,
+              "sequence %d, %d tokens" % (b, m))
     return out
 
 
@@ -270,9 +276,8 @@ def test_pages_outside_are_left_out(fmt, group, dim):
     out = pq.pq_attn_decode(cache, q, torch.from_numpy(table).to(DEV), torch.tensor([n, n], dtype=torch.int32, device=DEV), n, 0.1, lse=lse)
     inside = np.ones(n, bool)
     inside[64:96] = inside[160:192] = False
-    want, wlse, mag, _ = OK.attention(f64(q)[0], OK.stored(fmt, group, f64(k), kt)[inside], OK.stored(fmt, group, f64(v), vt)[inside], 0.1)
-    assert np.all(np.abs(f64(out)[0] - want) <= 2.0 ** -8 * np.abs(want) + 2.0 ** -10 * mag)
-    assert np.abs(lse[0].cpu().numpy() - wlse).max() < 1e-4
+    check(f64(out)[0], lse[0].cpu().numpy().astype(np.float64), f64(q)[0], OK.stored(fmt, group, f64(k), kt)[inside],
+          OK.stored(fmt, group, f64(v), vt)[inside], 0.1)
     assert np.all(f64(out)[1] == 0) and bool((lse[1] == -np.inf).all())
 
 
