@@ -54,47 +54,67 @@ __device__ __forceinline__ float column_sum(float v) {
   return v + __shfl_xor(v, 32);
 }
 
-// what a lane holds of a block: codes (or bf16 values) and scales, loaded one block ahead
+// What a lane holds of a block, codes (or bf16 values) and scales.
 template <class L>
-struct Block {
-  static constexpr int NP = L::code_bytes / 1024;            // 16-byte pieces of the keys, and of the values
+struct Part {
+  static constexpr int NP = L::code_bytes / 1024;            // 16-byte pieces of the codes
   static constexpr int NS = L::FMT == kInt4 ? L::NG : 1;
-  uint4_t k[NP], v[NP];
-  uint4_t ks[NS], vs[NS];                                    // NVFP4: x, y of ks[0] the tiles' bytes for NK <= 4, all four for 8
+  static constexpr int registers = 4 * NP + (L::FMT == kInt4 ? 4 * NS : L::FMT == kNvfp4 ? 2 : 0);
+  uint4_t c[NP], sc[NS];
 
-  __device__ __forceinline__ void load(const uint8_t* __restrict__ p, int lane) {
-    const int q = lane >> 4, n = lane & 15;
+  __device__ __forceinline__ void load_codes(const uint8_t* __restrict__ p, uint32_t lane) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) k[i] = *reinterpret_cast<const uint4_t*>(p + i * 1024 + lane * 16);
+    for (int i = 0; i < NP; ++i) c[i] = *reinterpret_cast<const uint4_t*>(p + (lane * 16 + i * 1024));
+  }
+  // INT4: 16-byte pieces of the four tokens 4 q .. of both tiles
+  __device__ __forceinline__ void load_int_scales(const uint8_t* __restrict__ p, uint32_t lane) {
 #pragma unroll
-    for (int i = 0; i < NP; ++i) v[i] = *reinterpret_cast<const uint4_t*>(p + L::v_at + i * 1024 + lane * 16);
-    if constexpr (L::FMT == kInt4) {
-#pragma unroll
-      for (int i = 0; i < NS; ++i) {
-        ks[i] = *reinterpret_cast<const uint4_t*>(p + L::code_bytes + q * 16 * NS + i * 16);
-        vs[i] = *reinterpret_cast<const uint4_t*>(p + L::v_at + L::code_bytes + q * 16 * NS + i * 16);
-      }
-    } else if constexpr (L::FMT == kNvfp4) {
+    for (int i = 0; i < NS; ++i) sc[i] = *reinterpret_cast<const uint4_t*>(p + ((lane >> 4) * (16 * NS) + L::code_bytes + i * 16));
+  }
+  // INT4: the scale of group g of token (s, r) of the lane
+  __device__ __forceinline__ float h(int s, int r, int g) const {
+    const int x = (s * 4 + r) * L::NG + g;
+    const uint32_t two = sc[x >> 3][(x >> 1) & 3];
+    return x & 1 ? bf16_hi(two) : bf16_lo(two);
+  }
+};
+
+template <class L>
+struct Keys : Part<L> {
+  __device__ __forceinline__ void load(const uint8_t* __restrict__ p, uint32_t lane) {
+    this->load_codes(p, lane);
+    if constexpr (L::FMT == kInt4) this->load_int_scales(p, lane);
+    if constexpr (L::FMT == kNvfp4) {                        // the bytes of tile s in sc[s] (16 channels' tiles: two words each)
       constexpr int NK = L::NK;
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
-        const uint8_t* at = p + L::code_bytes + ((s * 2 + (q >> 1)) * 16 + n) * NK;
-        if constexpr (NK == 2) ks[0][s] = *reinterpret_cast<const uint16_t*>(at);
-        else if constexpr (NK == 4) ks[0][s] = *reinterpret_cast<const uint32_t*>(at);
+        const uint8_t* at = p + (((lane >> 5) * 16 + (lane & 15)) * NK + (L::code_bytes + s * 32 * NK));
+        if constexpr (NK == 2) this->sc[0][s] = *reinterpret_cast<const uint16_t*>(at);
+        else if constexpr (NK == 4) this->sc[0][s] = *reinterpret_cast<const uint32_t*>(at);
         else {
           const uint2 two = *reinterpret_cast<const uint2*>(at);
-          ks[0][2 * s] = two.x;
-          ks[0][2 * s + 1] = two.y;
+          this->sc[0][2 * s] = two.x;
+          this->sc[0][2 * s + 1] = two.y;
         }
       }
-      const uint2 two = *reinterpret_cast<const uint2*>(p + L::v_byte_at(0, 0) + ((n / (256 / L::D)) * 4 + q) * 8);
-      vs[0][0] = two.x;
-      vs[0][1] = two.y;
     }
   }
+};
 
-  // values of tokens outside [lo, hi) of the block become zeros: their weights are, and what lies there may be NaN
-  __device__ __forceinline__ void clear_values(int lane, int lo, int hi) {
+template <class L>
+struct Values : Part<L> {
+  __device__ __forceinline__ void load(const uint8_t* __restrict__ block, uint32_t lane) {
+    const uint8_t* p = block + L::v_at;
+    this->load_codes(p, lane);
+    if constexpr (L::FMT == kInt4) this->load_int_scales(p, lane);
+    if constexpr (L::FMT == kNvfp4) {
+      const uint2 two = *reinterpret_cast<const uint2*>(p + (((lane & 15) / (256 / L::D) * 4 + (lane >> 4)) * 8 + L::code_bytes));
+      this->sc[0][0] = two.x;
+      this->sc[0][1] = two.y;
+    }
+  }
+  // tokens outside [lo, hi) of the block become zeros: their weights are, and what lies there may be NaN
+  __device__ __forceinline__ void clear(int lane, int lo, int hi) {
     const int q = lane >> 4;
 #pragma unroll
     for (int s = 0; s < 2; ++s)
@@ -106,28 +126,20 @@ struct Block {
 #pragma unroll
           for (int w = 0; w < L::D / 32; ++w) {
             const int f = (s * 4 + r) * (L::D / 32) + w;
-            v[f >> 2][f & 3] = keep ? v[f >> 2][f & 3] : 0u;
+            this->c[f >> 2][f & 3] = keep ? this->c[f >> 2][f & 3] : 0u;
           }
         } else if constexpr (L::FMT == kNvfp4) {
-          vs[0][s] &= keep ? ~0u : ~(0xFFu << (8 * ((r & 1) * 2 + (r >> 1))));
+          this->sc[0][s] &= keep ? ~0u : ~(0xFFu << (8 * ((r & 1) * 2 + (r >> 1))));
         } else {
 #pragma unroll
           for (int g = 0; g < L::NG; ++g) {
             const int x = (s * 4 + r) * L::NG + g;
-            vs[x >> 3][(x >> 1) & 3] &= keep ? ~0u : ~(0xFFFFu << (16 * (x & 1)));
+            this->sc[x >> 3][(x >> 1) & 3] &= keep ? ~0u : ~(0xFFFFu << (16 * (x & 1)));
           }
         }
       }
   }
 };
-
-// INT4: the scale of group g of token (s, r) of the lane
-template <class L>
-__device__ __forceinline__ float int_h(const uint4_t (&sc)[Block<L>::NS], int s, int r, int g) {
-  const int x = (s * 4 + r) * L::NG + g;
-  const uint32_t two = sc[x >> 3][(x >> 1) & 3];
-  return x & 1 ? bf16_hi(two) : bf16_lo(two);
-}
 
 // eight codes, two quads (of two tokens' values, or a key's chunk): the codes a of both as a pair of fp16 subnormals, the odd ones
 // 16 times as large
@@ -146,23 +158,26 @@ struct Query {
   uint4_t q[NT][L::NK];
   float c[NT];                         // scores to powers of two
 
-  // queries first .. first + count - 1 of the sequence's; columns past them are zeros
-  __device__ __forceinline__ void load(const AttnCall& a, const uint16_t* __restrict__ src, int count, int lane, float key_unit) {
+  // count queries of the key head; columns past them are zeros
+  __device__ __forceinline__ void fetch(const AttnCall& a, const uint16_t* __restrict__ src, int count, int lane) {
     const int kq = lane >> 4, n = lane & 15;
+#pragma unroll
+    for (int ct = 0; ct < NT; ++ct)
+#pragma unroll
+      for (int kk = 0; kk < L::NK; ++kk) {
+        q[ct][kk] = (uint4_t){0u, 0u, 0u, 0u};
+        if (ct * 16 + n < count) q[ct][kk] = *reinterpret_cast<const uint4_t*>(src + (ct * 16 + n) * a.q_head + kk * 32 + kq * 8);
+      }
+  }
+  __device__ __forceinline__ void convert(const AttnCall& a, float key_unit) {
     const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;           // c is positive: the sign goes to the query
     const float scale = fabsf(a.scale) * 1.4426950408889634f * key_unit;
 #pragma unroll
     for (int ct = 0; ct < NT; ++ct) {
-      const bool ok = ct * 16 + n < count;
       uint4_t x[L::NK];
       float top = 0.0f;
 #pragma unroll
-      for (int kk = 0; kk < L::NK; ++kk) {
-        x[kk] = (uint4_t){0u, 0u, 0u, 0u};
-        if (ok) x[kk] = *reinterpret_cast<const uint4_t*>(src + (ct * 16 + n) * a.q_head + kk * 32 + kq * 8);
-#pragma unroll
-        for (int w = 0; w < 4; ++w) x[kk][w] ^= flip;
-      }
+      for (int kk = 0; kk < L::NK; ++kk) x[kk] = q[ct][kk] ^ flip;
       if constexpr (L::FMT == kBf16) {
         c[ct] = scale;
 #pragma unroll
@@ -217,15 +232,10 @@ struct Result {
   }
 };
 
+// scores of a block's tokens, 16 s + 4 q + r in s_[.][s][r]
 template <class L, int NT>
-__device__ __forceinline__ void attend_block(Block<L>& x, const Query<L, NT>& query, Result<L, NT>& out, int lane, int lo, int hi) {
+__device__ __forceinline__ void block_scores(const Keys<L>& x, const Query<L, NT>& query, float4_t (&s_)[NT][2]) {
   constexpr IntC<L::FMT == kBf16> kType{};
-  const bool part = lo > 0 || hi < kKvBlock;                           // wave-uniform
-  if (__builtin_expect(part, 0)) x.clear_values(lane, lo, hi);
-  const int kq = lane >> 4;
-
-  // scores
-  float4_t s_[NT][2];
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     float4_t sum[NT][L::NG];
@@ -238,15 +248,15 @@ __device__ __forceinline__ void attend_block(Block<L>& x, const Query<L, NT>& qu
       const int e = s * L::NK + kk;
       uint4_t a;
       if constexpr (L::FMT == kBf16) {
-        a = x.k[e];
+        a = x.c[e];
       } else {
-        const uint32_t d = x.k[e >> 2][e & 3];
+        const uint32_t d = x.c[e >> 2][e & 3];
         if constexpr (L::FMT == kInt4) {
 #pragma unroll
           for (int w = 0; w < 4; ++w) a[w] = IntCodes(d).pair(w);
         } else {
           // the bytes of chunks kk and kk ^ 1 convert together
-          const uint32_t bytes = L::NK == 8 ? x.ks[0][2 * s + (kk >> 2)] : x.ks[0][s];
+          const uint32_t bytes = L::NK == 8 ? x.sc[0][2 * s + (kk >> 2)] : x.sc[0][s];
           const half2_t two = kk & 2 ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)bytes, 1.0f, 1)
                                      : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)bytes, 1.0f, 0);
           const half2_t sc = kk & 1 ? (half2_t){two.y, two.y} : (half2_t){two.x, two.x};
@@ -265,9 +275,9 @@ __device__ __forceinline__ void attend_block(Block<L>& x, const Query<L, NT>& qu
       if constexpr (L::FMT == kInt4) {
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
-          float v = int_h<L>(x.ks, s, r, 0) * sum[ct][0][r];
+          float v = x.h(s, r, 0) * sum[ct][0][r];
 #pragma unroll
-          for (int g = 1; g < L::NG; ++g) v = __builtin_fmaf(int_h<L>(x.ks, s, r, g), sum[ct][g][r], v);
+          for (int g = 1; g < L::NG; ++g) v = __builtin_fmaf(x.h(s, r, g), sum[ct][g][r], v);
           s_[ct][s][r] = v;
         }
       } else {
@@ -275,13 +285,23 @@ __device__ __forceinline__ void attend_block(Block<L>& x, const Query<L, NT>& qu
       }
     }
   }
+}
+
+// their weights, and the values' sums; tokens outside [lo, hi) are left out
+template <class L, int NT>
+__device__ __forceinline__ void block_outputs(Values<L>& x, float4_t (&s_)[NT][2], const Query<L, NT>& query, Result<L, NT>& out, int lane,
+                                              int lo, int hi) {
+  constexpr IntC<L::FMT == kBf16> kType{};
+  const int kq = lane >> 4;
+  const bool part = lo > 0 || hi < kKvBlock;                           // wave-uniform
+  if (__builtin_expect(part, 0)) x.clear(lane, lo, hi);
   // INT4: 2^eb bounds the lane's scales; kept from going where the sum of the weights would overflow
   float eb = 0.0f;
   if constexpr (L::FMT == kInt4) {
     ushort2_t top = {0, 0};
 #pragma unroll
     for (int w = 0; w < 4 * L::NG; ++w) {
-      const uint32_t two = x.vs[w >> 2][w & 3];        // by value: a bit cast of a vector's element takes its first
+      const uint32_t two = x.sc[w >> 2][w & 3];        // by value: a bit cast of a vector's element takes its first
       top = __builtin_elementwise_max(top, __builtin_bit_cast(ushort2_t, two));
     }
     eb = (float)(max((int)max(top.x, top.y) >> 7, 127 - 80) - 126);
@@ -331,7 +351,7 @@ __device__ __forceinline__ void attend_block(Block<L>& x, const Query<L, NT>& qu
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int s = i >> 1, r = (i & 1) * 2;
-          w[ct][g][i] = cvt_pk_f16(p[ct][s][r] * int_h<L>(x.vs, s, r, g), p[ct][s][r + 1] * int_h<L>(x.vs, s, r + 1, g));
+          w[ct][g][i] = cvt_pk_f16(p[ct][s][r] * x.h(s, r, g), p[ct][s][r + 1] * x.h(s, r + 1, g));
         }
 #pragma unroll
     for (int j = 0; j < L::NJ; ++j) {
@@ -339,7 +359,7 @@ __device__ __forceinline__ void attend_block(Block<L>& x, const Query<L, NT>& qu
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int f = i * L::NQ + j / 4;
-        a[i] = IntCodes(x.v[f >> 2][f & 3]).pair(j & 3);
+        a[i] = IntCodes(x.c[f >> 2][f & 3]).pair(j & 3);
       }
 #pragma unroll
       for (int ct = 0; ct < NT; ++ct) out.acc[ct][j] = mfma(a, w[ct][j / L::PER], out.acc[ct][j], kType);
@@ -353,8 +373,8 @@ __device__ __forceinline__ void attend_block(Block<L>& x, const Query<L, NT>& qu
     half2_t sc[4];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      sc[2 * s] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x.vs[0][s], 1.0f, 0);
-      sc[2 * s + 1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x.vs[0][s], 1.0f, 1);
+      sc[2 * s] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x.sc[0][s], 1.0f, 0);
+      sc[2 * s + 1] = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8((int)x.sc[0][s], 1.0f, 1);
     }
 #pragma unroll
     for (int jq = 0; jq < L::NQ; ++jq) {
@@ -362,7 +382,7 @@ __device__ __forceinline__ void attend_block(Block<L>& x, const Query<L, NT>& qu
 #pragma unroll
       for (int s = 0; s < 2; ++s) {
         const int f0 = (s * 2) * L::NQ + jq, f1 = (s * 2 + 1) * L::NQ + jq;
-        const uint32_t x0 = x.v[f0 >> 2][f0 & 3], x1 = x.v[f1 >> 2][f1 & 3];
+        const uint32_t x0 = x.c[f0 >> 2][f0 & 3], x1 = x.c[f1 >> 2][f1 & 3];
         even[s] = (x0 & 0x0F0F0F0Fu) | ((x1 << 4) & 0xF0F0F0F0u);
         odd[s] = ((x0 >> 4) & 0x0F0F0F0Fu) | (x1 & 0xF0F0F0F0u);
       }
@@ -400,7 +420,7 @@ __device__ __forceinline__ void attend_block(Block<L>& x, const Query<L, NT>& qu
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int f0 = (i * 2) * (L::D / 32) + j / 2, f1 = f0 + L::D / 32;
-        a[i] = __builtin_amdgcn_perm(x.v[f1 >> 2][f1 & 3], x.v[f0 >> 2][f0 & 3], j & 1 ? 0x07060302u : 0x05040100u);
+        a[i] = __builtin_amdgcn_perm(x.c[f1 >> 2][f1 & 3], x.c[f0 >> 2][f0 & 3], j & 1 ? 0x07060302u : 0x05040100u);
       }
 #pragma unroll
       for (int ct = 0; ct < NT; ++ct) {
@@ -415,16 +435,12 @@ __device__ __forceinline__ void attend_block(Block<L>& x, const Query<L, NT>& qu
 // All blocks of all pairs (sequence, key head, sixteen or thirty-two of its queries) are numbered sequence by sequence, pair by pair.
 // A worker takes `per` of them in a row: the work is even whatever the lengths.  Where `per` is small, or the pairs are many, each
 // pair's blocks are padded to a multiple of it instead: no worker then holds two pairs.
-struct Plan {
-  int per;                 // blocks a worker
-  bool padded;
-};
-struct Lengths {           // of sequence b: first block, blocks (at least one), first token and end
+struct Lengths {           // of a sequence: first attended token and end, first block, blocks (at least one)
   int first_token, end, first, n;
 };
-__device__ __forceinline__ Lengths lengths_of(const AttnCall& a, int b) {
+__device__ __forceinline__ Lengths lengths_of(const AttnCall& a, int length) {
   Lengths r;
-  r.end = min(max(a.lengths[b], 0), a.max_len);
+  r.end = min(max(length, 0), a.max_len);
   r.first_token = a.window ? max(0, r.end - a.window) : 0;
   r.first = r.first_token / kKvBlock;
   r.n = max(1, (r.end + kKvBlock - 1) / kKvBlock - r.first);
@@ -449,16 +465,33 @@ __device__ __forceinline__ int wave_scan_i32(int v, int lane) {        // inclus
   return v;
 }
 
+// a part's outputs, then (M, l) of its heads
 template <class L, int NT>
-constexpr int part_floats() { return NT * (L::NJ * 256 + 32); }        // a part's outputs, then (M, l) of its heads
+constexpr uint32_t part_bytes_of() { return NT * (L::NJ * 1024 + 256); }
 
 // the part of a pair that worker w holds, first the one that began it
 __device__ __forceinline__ int part_slot(int w, int w_first) { return w == w_first ? 2 * w + 1 : 2 * w; }
 
+// blocks that a wave has loads in flight for
+template <class L>
+constexpr int depth_of() {
+  constexpr int r = 2 * Part<L>::registers;
+  return r <= 24 ? 4 : r <= 32 ? 3 : r <= 48 ? 2 : 1;
+}
+
+// the part buffer is written and read by workgroups of different chiplets in one launch: past the caches that they do not share
+constexpr int kAgent = 16;               // sc1 of a buffer instruction
+__device__ __forceinline__ void put_part(__amdgpu_buffer_rsrc_t buf, uint32_t at, const float4_t& v) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4_t, v), buf, at, 0, kAgent);
+}
+__device__ __forceinline__ float4_t get_part(__amdgpu_buffer_rsrc_t buf, uint32_t at) {
+  return __builtin_bit_cast(float4_t, __builtin_amdgcn_raw_buffer_load_b128(buf, at, 0, kAgent));
+}
+
 template <class L, int NT>
 __global__ __launch_bounds__(64 * kAttnWaves, (L::D == 256 && NT == 2) ? 1 : 2) void attn_decode_kernel(KvView cache, AttnCall a,
-                                                                                                       int chunks) {
-  constexpr int NJ = L::NJ;
+                                                                                                       int chunks, uint32_t part_bytes) {
+  constexpr int NJ = L::NJ, PD = depth_of<L>();
   __shared__ float4_t shared_acc[2][NT * NJ][64];
   __shared__ float shared_ml[2][NT][2][64];
   __shared__ int last_one;
@@ -466,116 +499,121 @@ __global__ __launch_bounds__(64 * kAttnWaves, (L::D == 256 && NT == 2) ? 1 : 2) 
   const int kq = lane >> 4, col = lane & 15;
   const int per_head = a.q_heads / cache.heads, pairs = cache.heads * chunks;      // pairs of a sequence
   int* counters = static_cast<int*>(a.ws);
-  float* parts = reinterpret_cast<float*>(static_cast<uint8_t*>(a.ws) + PQ_ATTN_DECODE_ZERO_BYTES);
+  const auto parts = __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t*>(a.ws) + PQ_ATTN_DECODE_ZERO_BYTES, 0, part_bytes, 0x00027000);
+  const float key_unit = L::FMT == kNvfp4 ? *cache.k_ts : L::FMT == kInt4 ? 16777216.0f / 7.0f : 1.0f;
+  const float value_unit = L::FMT == kNvfp4 ? *cache.v_ts : L::FMT == kInt4 ? 16777216.0f / 7.0f : 1.0f;
 
   // the plan: the same in every wave
+  const int length0 = lane < a.seqs ? a.lengths[lane] : 0;             // of the first 64 sequences: often of all
+  auto length_at = [&](int b0) { return b0 == 0 ? length0 : b0 + lane < a.seqs ? a.lengths[b0 + lane] : 0; };
   int blocks = 0, longest = 0;
   for (int b0 = 0; b0 < a.seqs; b0 += 64) {
-    const int n = b0 + lane < a.seqs ? lengths_of(a, b0 + lane).n : 0;
+    const int n = b0 + lane < a.seqs ? lengths_of(a, length_at(b0)).n : 0;
     blocks += wave_sum_i32(n);
     longest = max(longest, wave_max_i32(n));
   }
-  Plan plan;
-  plan.per = max((int)(((int64_t)blocks * pairs + kWorkers - 1) / kWorkers), kLeastBlocks);
-  plan.padded = plan.per < 16;
-  if (plan.padded) {
+  blocks = __builtin_amdgcn_readfirstlane(blocks);
+  longest = __builtin_amdgcn_readfirstlane(longest);
+  int per = max((blocks * pairs + kWorkers - 1) / kWorkers, kLeastBlocks);         // blocks a worker
+  bool padded = per < 16;
+  if (padded) {
     int items = 0;
-    for (int b0 = 0; b0 < a.seqs; b0 += 64) {
-      const int n = b0 + lane < a.seqs ? lengths_of(a, b0 + lane).n : 0;
-      items += wave_sum_i32((n + plan.per - 1) / plan.per);
-    }
-    if (items * pairs > (int)gridDim.x || items * pairs > kMaxSplits) plan.padded = false;
+    for (int b0 = 0; b0 < a.seqs; b0 += 64)
+      items += wave_sum_i32(b0 + lane < a.seqs ? (lengths_of(a, length_at(b0)).n + per - 1) / per : 0);
+    items = __builtin_amdgcn_readfirstlane(items) * pairs;
+    if (items > (int)gridDim.x || items > kMaxSplits) padded = false;
   }
-  if (!plan.padded && a.seqs * pairs >= 4 * kWorkers) {                // pairs enough: one a worker
-    plan.per = longest;
-    plan.padded = true;
+  if (!padded && a.seqs * pairs >= 4 * kWorkers) {                     // pairs enough: one a worker
+    per = longest;
+    padded = true;
   }
-  auto padded = [&](int n) { return plan.padded ? (n + plan.per - 1) / plan.per * plan.per : n; };
+  auto counted = [&](int n) { return padded ? (n + per - 1) / per * per : n; };
 
-  const int64_t u_begin = (int64_t)blockIdx.x * plan.per;
-  int64_t u = u_begin, base = 0;
-  int b = 0;                                                           // the sequence that holds block u, its first block `base`
+  const int u_begin = blockIdx.x * per, u_end = u_begin + per;         // seqs * pairs * blocks fit 31 bits
+  int u = u_begin, base = 0, b = 0;                                    // the sequence that holds block u, its first block `base`
   for (int b0 = 0;; b0 += 64) {
     if (b0 >= a.seqs) return;                                          // workgroups past the last block
-    const int n = b0 + lane < a.seqs ? padded(lengths_of(a, b0 + lane).n) * pairs : 0;
+    const int n = b0 + lane < a.seqs ? counted(lengths_of(a, length_at(b0)).n) * pairs : 0;
     const int incl = wave_scan_i32(n, lane);
     const uint64_t past = __ballot(base + incl > u);
     if (past) {
       const int at = __ffsll((unsigned long long)past) - 1;
-      base += __shfl(incl - n, at);
+      base += __builtin_amdgcn_readlane(incl - n, at);
       b = b0 + at;
       break;
     }
-    base += __shfl(incl, 63);
+    base += __builtin_amdgcn_readlane(incl, 63);
   }
-  b = __builtin_amdgcn_readfirstlane(b);
 
-  int64_t u_end = u_begin + plan.per;
   while (u < u_end && b < a.seqs) {
-    const Lengths len = lengths_of(a, b);
-    const int np = padded(len.n), off = (int)(u - base);
-    const int pair = off / np, t_at = off % np;
-    const int64_t pair_base = base + (int64_t)pair * np;
-    int t0, t1, w_first, w_last;
-    if (plan.padded) {                                                 // even parts
-      const int k = t_at / plan.per, of = np / plan.per;
-      t0 = (int)((int64_t)len.n * k / of);
-      t1 = (int)((int64_t)len.n * (k + 1) / of);
-      w_first = (int)(pair_base / plan.per);
-      w_last = w_first + of - 1;
-      u = u_end;
-    } else {
-      t0 = t_at;
-      t1 = min(np, t_at + (int)(u_end - u));
-      w_first = (int)(pair_base / plan.per);
-      w_last = (int)((pair_base + np - 1) / plan.per);
-      u = pair_base + np;
-      if (pair + 1 == pairs) base = u;
+    const Lengths len = lengths_of(a, b < 64 ? __builtin_amdgcn_readlane(length0, b) : __builtin_amdgcn_readfirstlane(a.lengths[b]));
+    const int seq = b, np = __builtin_amdgcn_readfirstlane(counted(len.n));
+    const int pair = __builtin_amdgcn_readfirstlane((u - base) / np), pair_base = base + pair * np, t_at = u - pair_base;
+    int t0 = t_at, t1 = min(np, t_at + u_end - u);
+    int w_first = __builtin_amdgcn_readfirstlane(pair_base / per), w_last = __builtin_amdgcn_readfirstlane((pair_base + np - 1) / per);
+    if (padded) {                                                      // even parts
+      const int k = blockIdx.x - w_first, of = w_last - w_first + 1, each = __builtin_amdgcn_readfirstlane(len.n / of), more = len.n - each * of;
+      t0 = k * each + min(k, more);
+      t1 = t0 + each + (k < more);
     }
-    const int seq = b;
-    if (!plan.padded && pair + 1 == pairs) ++b;
+    u = padded ? u_end : pair_base + np;
+    if (pair + 1 == pairs) {
+      base += np * pairs;
+      ++b;
+    }
 
-    const int head = pair / chunks, h0 = pair % chunks * 16 * NT;
+    const int head = __builtin_amdgcn_readfirstlane(pair / chunks), h0 = (pair - head * chunks) * 16 * NT;
     const int count = min(per_head - h0, 16 * NT);
+    const int32_t* table = a.table + seq * a.table_ld;
+    const int n_mine = (t1 - t0 - wave + kAttnWaves - 1) / kAttnWaves, block0 = len.first + t0 + wave;
+    // pages of this wave's blocks, a lane each, 64 blocks in a register: of even and odd runs of 64
+    int pages[2];
+    auto fetch_pages = [&](int run) {
+      const int token = (block0 + (run * 64 + lane) * kAttnWaves) * kKvBlock;
+      int p = -1;
+      if (run * 64 + lane < n_mine && token < len.end) p = table[token >> cache.page_log2];
+      return p < cache.pages ? p : -1;
+    };
+    auto page_of = [&](int i) {
+      const int even = __builtin_amdgcn_readlane(pages[0], i & 63), odd = __builtin_amdgcn_readlane(pages[1], i & 63);
+      return i & 64 ? odd : even;
+    };
+    auto address = [&](int i) {
+      const int page = max(page_of(i), 0), in_page = (block0 + i * kAttnWaves) & ((1 << (cache.page_log2 - 5)) - 1);
+      return cache.data + ((((int64_t)page * cache.heads + head) << (cache.page_log2 - 5)) + in_page) * L::bytes;
+    };
     Query<L, NT> query;
-    const float key_unit = L::FMT == kNvfp4 ? *cache.k_ts : L::FMT == kInt4 ? 16777216.0f / 7.0f : 1.0f;
-    query.load(a, a.q + seq * a.q_ld + (int64_t)(head * per_head + h0) * a.q_head, count, lane, key_unit);
+    query.fetch(a, a.q + seq * a.q_ld + (int64_t)(head * per_head + h0) * a.q_head, count, lane);
+    Keys<L> keys[PD];
+    Values<L> values[PD];
+    if (n_mine > 0) {
+      pages[0] = fetch_pages(0);
+      pages[1] = fetch_pages(1);
+#pragma unroll
+      for (int d = 0; d < PD; ++d) {
+        const uint8_t* p = address(min(d, n_mine - 1));
+        keys[d].load(p, lane);
+        values[d].load(p, lane);
+      }
+    }
+    query.convert(a, key_unit);
     Result<L, NT> res;
     res.clear();
-
-    const int32_t* table = a.table + seq * a.table_ld;
-    const int n_mine = (t1 - t0 - wave + kAttnWaves - 1) / kAttnWaves;
-    if (n_mine > 0) {
-      int pages = 0;                                                   // of this wave's next 64 blocks, a lane each
-      auto fetch_pages = [&](int i) {
-        const int mine = i + lane;
-        pages = 0;
-        if (mine < n_mine) {
-          const int token = (len.first + t0 + wave + mine * kAttnWaves) * kKvBlock;
-          pages = token < len.end ? table[token >> cache.page_log2] : -1;
-          if (pages < 0 || pages >= cache.pages) pages = -1;
-        }
-      };
-      auto address = [&](int i, bool& ok) {
-        const int page = __builtin_amdgcn_readlane(pages, i & 63);
-        ok = page >= 0;
-        const int block = len.first + t0 + wave + i * kAttnWaves, in_page = block & ((1 << (cache.page_log2 - 5)) - 1);
-        return cache.data + ((((int64_t)(ok ? page : 0) * cache.heads + head) << (cache.page_log2 - 5)) + in_page) * L::bytes;
-      };
-      fetch_pages(0);
-      Block<L> cur, next;
-      bool ok, ok_next = false;
-      cur.load(address(0, ok), lane);
-      for (int i = 0; i < n_mine; ++i) {
-        if (i + 1 < n_mine) {
-          if (((i + 1) & 63) == 0) fetch_pages(i + 1);
-          next.load(address(i + 1, ok_next), lane);
-        }
-        const int token = (len.first + t0 + wave + i * kAttnWaves) * kKvBlock;
-        const int lo = ok ? max(0, len.first_token - token) : kKvBlock, hi = min(kKvBlock, len.end - token);
-        attend_block<L, NT>(cur, query, res, lane, lo, hi);
-        cur = next;
-        ok = ok_next;
+    for (int i0 = 0; i0 < n_mine; i0 += PD) {
+#pragma unroll
+      for (int d = 0; d < PD; ++d) {
+        const int i = i0 + d;
+        if (i >= n_mine) break;
+        if (i && (i & 63) == 0) pages[(i >> 6) + 1 & 1] = fetch_pages((i >> 6) + 1);
+        // the block after next ones replaces this one; past the end the last once more, so that the loads in flight are always as many
+        const uint8_t* next = address(min(i + PD, n_mine - 1));
+        float4_t s[NT][2];
+        block_scores<L, NT>(keys[d], query, s);
+        keys[d].load(next, lane);
+        const int token = (block0 + i * kAttnWaves) * kKvBlock;
+        const int lo = page_of(i) >= 0 ? max(0, len.first_token - token) : kKvBlock, hi = min(kKvBlock, len.end - token);
+        block_outputs<L, NT>(values[d], s, query, res, lane, lo, hi);
+        values[d].load(next, lane);
       }
     }
     if constexpr (L::FMT == kInt4)                                     // the odd codes came 16 times as large
@@ -618,47 +656,49 @@ __global__ __launch_bounds__(64 * kAttnWaves, (L::D == 256 && NT == 2) ? 1 : 2) 
 
     bool write = wave == 0;
     if (w_first != w_last) {                                           // a part of a pair: the last worker to finish joins them
-      constexpr int kFloats = part_floats<L, NT>();
+      constexpr uint32_t kPart = part_bytes_of<L, NT>();
       if (wave == 0) {
-        float* part = parts + (size_t)part_slot(blockIdx.x, w_first) * kFloats;
+        const uint32_t part = part_slot(blockIdx.x, w_first) * kPart;
 #pragma unroll
         for (int ct = 0; ct < NT; ++ct) {
           const int heads = min(16, count - ct * 16);
           if (col < heads) {
+            const uint32_t at = part + ct * (NJ * 1024 + 256);
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
-              *reinterpret_cast<float4_t*>(part + ct * NJ * 256 + ((j * 4 + kq) * heads + col) * 4) = res.acc[ct][j];
-            if (kq == 0) *reinterpret_cast<float2*>(part + NT * NJ * 256 + ct * 32 + col * 2) = make_float2(res.m[ct], res.l[ct]);
+            for (int j = 0; j < NJ; ++j) put_part(parts, at + ((j * 4 + kq) * heads + col) * 16, res.acc[ct][j]);
+            if (kq == 0) put_part(parts, at + NJ * 1024 + col * 16, (float4_t){res.m[ct], res.l[ct], 0.0f, 0.0f});
           }
         }
-        __threadfence();
-        if (lane == 0) last_one = atomicAdd(counters + w_first, 1) == w_last - w_first;
+        // the stores have reached memory before the counter says so
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        if (lane == 0)
+          last_one = __hip_atomic_fetch_add(counters + w_first, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == w_last - w_first;
       }
       __syncthreads();
-      if (!last_one) continue;
-      __threadfence();
+      if (!__builtin_amdgcn_readfirstlane(last_one)) continue;
       // the common reference and the sum of the weights, then the outputs; the waves take the parts in turn
 #pragma unroll
       for (int ct = 0; ct < NT; ++ct) {
         const int heads = min(16, count - ct * 16);
-        float m = kNoReference;
-        for (int w = w_first + kq; w <= w_last; w += 4)
-          if (col < heads) m = fmaxf(m, parts[(size_t)part_slot(w, w_first) * kFloats + NT * NJ * 256 + ct * 32 + col * 2]);
-        m = column_max(m);
-        float l = 0.0f;
+        float m = kNoReference, l = 0.0f;
         float4_t acc[NJ];
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[j] = (float4_t){0.0f, 0.0f, 0.0f, 0.0f};
         if (col < heads) {
+          for (int w = w_first + kq; w <= w_last; w += 4)
+            m = fmaxf(m, get_part(parts, part_slot(w, w_first) * kPart + ct * (NJ * 1024 + 256) + NJ * 1024 + col * 16)[0]);
+        }
+        m = column_max(m);
+        if (col < heads) {
 #pragma unroll 2
           for (int w = w_first + wave; w <= w_last; w += kAttnWaves) {
-            const float* part = parts + (size_t)part_slot(w, w_first) * kFloats;
-            const float2 ml = *reinterpret_cast<const float2*>(part + NT * NJ * 256 + ct * 32 + col * 2);
-            const float f = __builtin_amdgcn_exp2f(ml.x - m);
-            l += ml.y * f;
+            const uint32_t at = part_slot(w, w_first) * kPart + ct * (NJ * 1024 + 256);
+            const float4_t ml = get_part(parts, at + NJ * 1024 + col * 16);
+            const float f = __builtin_amdgcn_exp2f(ml[0] - m);
+            l += ml[1] * f;
 #pragma unroll
-            for (int j = 0; j < NJ; ++j)
-              acc[j] += *reinterpret_cast<const float4_t*>(part + ct * NJ * 256 + ((j * 4 + kq) * heads + col) * 4) * f;
+            for (int j = 0; j < NJ; ++j) acc[j] += get_part(parts, at + ((j * 4 + kq) * heads + col) * 16) * f;
           }
         }
         res.m[ct] = m;
@@ -676,7 +716,6 @@ __global__ __launch_bounds__(64 * kAttnWaves, (L::D == 256 && NT == 2) ? 1 : 2) 
       if (threadIdx.x == 0) counters[w_first] = 0;                     // for the next call
     }
     if (write) {
-      const float unit = L::FMT == kNvfp4 ? *cache.v_ts : L::FMT == kInt4 ? 16777216.0f / 7.0f : 1.0f;
 #pragma unroll
       for (int ct = 0; ct < NT; ++ct) {
         const int h = ct * 16 + col;
@@ -691,7 +730,7 @@ __global__ __launch_bounds__(64 * kAttnWaves, (L::D == 256 && NT == 2) ? 1 : 2) 
             uint32_t two[L::PER / 2];
 #pragma unroll
             for (int j = 0; j < L::PER / 2; ++j)
-              two[j] = cvt_pk_bf16(res.acc[ct][g * L::PER + 2 * j][r] * inv * unit, res.acc[ct][g * L::PER + 2 * j + 1][r] * inv * unit);
+              two[j] = cvt_pk_bf16(res.acc[ct][g * L::PER + 2 * j][r] * inv * value_unit, res.acc[ct][g * L::PER + 2 * j + 1][r] * inv * value_unit);
             __builtin_memcpy(__builtin_assume_aligned(o + g * L::GV + (kq * 4 + r) * L::PER, L::PER >= 8 ? 16 : L::PER * 2), two, L::PER * 2);
           }
         if (a.lse && kq == 0)
@@ -722,15 +761,15 @@ size_t attn_decode_workspace_bytes(const pq_kv_cache& c, int64_t seqs, int q_hea
   int64_t workers = grid_of(c, seqs, q_heads, max_len, window);
   if (workers > kMaxSplits) workers = kMaxSplits;
   const int tiles = tiles_of(c, q_heads);
-  const size_t floats = tiles * (size_t)(c.head_dim / 16 * 256 + 32);
-  return PQ_ATTN_DECODE_ZERO_BYTES + (size_t)workers * 2 * floats * sizeof(float);
+  return PQ_ATTN_DECODE_ZERO_BYTES + (size_t)workers * 2 * tiles * (size_t)(c.head_dim / 16 * 1024 + 256);
 }
 
 int run_attn_decode(const pq_kv_cache& c, const AttnCall& a, hipStream_t st) {
   const int grid = (int)grid_of(c, a.seqs, a.q_heads, a.max_len, a.window), chunks = chunks_of(c, a.q_heads);
+  const uint32_t part_bytes = (uint32_t)(attn_decode_workspace_bytes(c, a.seqs, a.q_heads, a.max_len, a.window) - PQ_ATTN_DECODE_ZERO_BYTES);
   return kv_dispatch(c.fmt, c.group, c.head_dim, [&](auto l) {
-    if (tiles_of(c, a.q_heads) == 1) attn_decode_kernel<decltype(l), 1><<<grid, 64 * kAttnWaves, 0, st>>>(kv_view(c), a, chunks);
-    else attn_decode_kernel<decltype(l), 2><<<grid, 64 * kAttnWaves, 0, st>>>(kv_view(c), a, chunks);
+    if (tiles_of(c, a.q_heads) == 1) attn_decode_kernel<decltype(l), 1><<<grid, 64 * kAttnWaves, 0, st>>>(kv_view(c), a, chunks, part_bytes);
+    else attn_decode_kernel<decltype(l), 2><<<grid, 64 * kAttnWaves, 0, st>>>(kv_view(c), a, chunks, part_bytes);
     return check_hip(hipGetLastError(), "pq_attn_decode");
   });
 }
