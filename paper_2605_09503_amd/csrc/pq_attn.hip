@@ -22,9 +22,10 @@ typedef uint16_t ushort2_t __attribute__((ext_vector_type(2)));
 typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
 
 constexpr int kAttnWaves = 4;            // of a workgroup; they take a segment's blocks in turn
-constexpr int kWorkers = 512;            // workgroups that share all blocks evenly: two a compute unit
+constexpr int kUnits = 256;              // compute units
 constexpr int kMaxSplits = 1024;         // workgroups that may hold a part of a pair: counters in the workspace
 constexpr int kLeastBlocks = 4;          // of a workgroup
+constexpr int kMostParts = 64;           // of a pair: one workgroup joins them
 
 constexpr float kNoReference = -1e38f;   // M before the first token
 // A weight with its value's scale stays below 2^15 (fp16); M follows when it would not, to 2^7 and less: seldom, so that neither the
@@ -42,6 +43,12 @@ __device__ __forceinline__ float4_t mfma(const uint4_t& a, const uint4_t& b, con
 __device__ __forceinline__ uint32_t cvt_pk_f16(float lo, float hi) {
   typedef float f32x2_t __attribute__((ext_vector_type(2)));
   return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2_t){lo, hi}, half2_t));
+}
+
+// a value that the compiler takes for new: what follows from it is not kept in registers across the loops before
+__device__ __forceinline__ int renewed(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
 }
 
 // over the four lanes of a column (16 apart)
@@ -121,7 +128,7 @@ struct Values : Part<L> {
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int t = s * 16 + q * 4 + r;
-        const bool keep = t >= lo && t < hi;
+        const bool keep = (t >= lo) & (t < hi);
         if constexpr (L::FMT == kBf16) {
 #pragma unroll
           for (int w = 0; w < L::D / 32; ++w) {
@@ -314,7 +321,7 @@ __device__ __forceinline__ void block_outputs(Values<L>& x, float4_t (&s_)[NT][2
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const int t = (i >> 2) * 16 + kq * 4 + (i & 3);
-        if (t < lo || t >= hi) s_[ct][i >> 2][i & 3] = -1e38f;
+        s_[ct][i >> 2][i & 3] = ((t < lo) | (t >= hi)) ? -1e38f : s_[ct][i >> 2][i & 3];
       }
     }
     float top = fmaxf(s_[ct][0][0], s_[ct][0][1]);
@@ -335,7 +342,7 @@ __device__ __forceinline__ void block_outputs(Values<L>& x, float4_t (&s_)[NT][2
       float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s_[ct][i >> 2][i & 3], query.c[ct], -out.m[ct]));
       if (__builtin_expect(part, 0)) {
         const int t = (i >> 2) * 16 + kq * 4 + (i & 3);
-        w = t < lo || t >= hi ? 0.0f : w;
+        w = ((t < lo) | (t >= hi)) ? 0.0f : w;
       }
       p[ct][i >> 2][i & 3] = w;
       out.l[ct] += w;
@@ -446,24 +453,16 @@ __device__ __forceinline__ Lengths lengths_of(const AttnCall& a, int length) {
   r.n = max(1, (r.end + kKvBlock - 1) / kKvBlock - r.first);
   return r;
 }
-__device__ __forceinline__ int wave_sum_i32(int v) {
-#pragma unroll
-  for (int off = 32; off; off >>= 1) v += __shfl_xor(v, off);
-  return v;
+// sums over the lanes up to each, by exchanges inside rows of 16 lanes and broadcasts of a row's last lane: no LDS round trips
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);      // row_shr 1, 2, 4, 8
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);      // row_bcast 15 into rows 1 and 3
+  return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);   // row_bcast 31 into rows 2 and 3
 }
-__device__ __forceinline__ int wave_max_i32(int v) {
-#pragma unroll
-  for (int off = 32; off; off >>= 1) v = max(v, __shfl_xor(v, off));
-  return v;
-}
-__device__ __forceinline__ int wave_scan_i32(int v, int lane) {        // inclusive
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const int o = __shfl_up(v, off);
-    if (lane >= off) v += o;
-  }
-  return v;
-}
+__device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
 
 // a part's outputs, then (M, l) of its heads
 template <class L, int NT>
@@ -472,13 +471,9 @@ constexpr uint32_t part_bytes_of() { return NT * (L::NJ * 1024 + 256); }
 // the part of a pair that worker w holds, first the one that began it
 __device__ __forceinline__ int part_slot(int w, int w_first) { return w == w_first ? 2 * w + 1 : 2 * w; }
 
-// blocks that a wave has loads in flight for
-template <class L>
-constexpr int depth_of() {
-  constexpr int r = 2 * Part<L>::registers;
-  return r <= 24 ? 4 : r <= 32 ? 3 : r <= 48 ? 2 : 1;
-}
-
+// Waves a SIMD, and with them the registers of a wave.
+template <class L, int NT>
+constexpr int waves_of() { return L::D == 256 && (NT == 2 || L::FMT == kBf16) ? 1 : 2; }
 // the part buffer is written and read by workgroups of different chiplets in one launch: past the caches that they do not share
 constexpr int kAgent = 16;               // sc1 of a buffer instruction
 __device__ __forceinline__ void put_part(__amdgpu_buffer_rsrc_t buf, uint32_t at, const float4_t& v) {
@@ -489,14 +484,14 @@ __device__ __forceinline__ float4_t get_part(__amdgpu_buffer_rsrc_t buf, uint32_
 }
 
 template <class L, int NT>
-__global__ __launch_bounds__(64 * kAttnWaves, (L::D == 256 && NT == 2) ? 1 : 2) void attn_decode_kernel(KvView cache, AttnCall a,
-                                                                                                       int chunks, uint32_t part_bytes) {
-  constexpr int NJ = L::NJ, PD = depth_of<L>();
-  __shared__ float4_t shared_acc[2][NT * NJ][64];
-  __shared__ float shared_ml[2][NT][2][64];
+__global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L, NT>())) void attn_decode_kernel(KvView cache, AttnCall a,
+                                                                                                       int chunks, int longest, uint32_t part_bytes) {
+  constexpr int NJ = L::NJ, NW = kAttnWaves;
+  constexpr int kWorkers = kUnits * waves_of<L, NT>();                  // workgroups that share all blocks evenly: what is resident
+  __shared__ float4_t shared_acc[NW / 2][NT * NJ][64];
+  __shared__ float shared_ml[NW / 2][NT][2][64];
   __shared__ int last_one;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kq = lane >> 4, col = lane & 15;
   const int per_head = a.q_heads / cache.heads, pairs = cache.heads * chunks;      // pairs of a sequence
   int* counters = static_cast<int*>(a.ws);
   const auto parts = __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t*>(a.ws) + PQ_ATTN_DECODE_ZERO_BYTES, 0, part_bytes, 0x00027000);
@@ -506,26 +501,32 @@ __global__ __launch_bounds__(64 * kAttnWaves, (L::D == 256 && NT == 2) ? 1 : 2) 
   // the plan: the same in every wave
   const int length0 = lane < a.seqs ? a.lengths[lane] : 0;             // of the first 64 sequences: often of all
   auto length_at = [&](int b0) { return b0 == 0 ? length0 : b0 + lane < a.seqs ? a.lengths[b0 + lane] : 0; };
-  int blocks = 0, longest = 0;
-  for (int b0 = 0; b0 < a.seqs; b0 += 64) {
-    const int n = b0 + lane < a.seqs ? lengths_of(a, length_at(b0)).n : 0;
-    blocks += wave_sum_i32(n);
-    longest = max(longest, wave_max_i32(n));
-  }
-  blocks = __builtin_amdgcn_readfirstlane(blocks);
-  longest = __builtin_amdgcn_readfirstlane(longest);
-  int per = max((blocks * pairs + kWorkers - 1) / kWorkers, kLeastBlocks);         // blocks a worker
-  bool padded = per < 16;
-  if (padded) {
+  auto blocks_at = [&](int b0) { return b0 + lane < a.seqs ? lengths_of(a, length_at(b0)).n : 0; };
+  int blocks = 0;
+  for (int b0 = 0; b0 < a.seqs; b0 += 64) blocks += last_lane(wave_scan(blocks_at(b0)));
+  auto items_of = [&](int per) {                                       // workers of padded pairs
     int items = 0;
-    for (int b0 = 0; b0 < a.seqs; b0 += 64)
-      items += wave_sum_i32(b0 + lane < a.seqs ? (lengths_of(a, length_at(b0)).n + per - 1) / per : 0);
-    items = __builtin_amdgcn_readfirstlane(items) * pairs;
-    if (items > (int)gridDim.x || items > kMaxSplits) padded = false;
+    for (int b0 = 0; b0 < a.seqs; b0 += 64) items += last_lane(wave_scan((blocks_at(b0) + per - 1) / per));
+    return items * pairs;
+  };
+  const int even = max(max((blocks * pairs + kWorkers - 1) / kWorkers, kLeastBlocks), (longest + kMostParts - 1) / kMostParts);
+  int per = even;
+  bool padded = false;
+  if (a.seqs * pairs <= kWorkers) {                                    // up to half as much again for a pair a worker
+#pragma unroll 1
+    for (int more = 0; more <= 4 && !padded; ++more) {
+      per = even + even * more / 8;
+      padded = items_of(per) <= min(kWorkers, (int)gridDim.x);
+    }
   }
-  if (!padded && a.seqs * pairs >= 4 * kWorkers) {                     // pairs enough: one a worker
-    per = longest;
-    padded = true;
+  if (!padded) {
+    per = even;
+    if (a.seqs * pairs >= 4 * kWorkers) {                              // pairs enough: one a worker
+      per = longest;
+      padded = true;
+    } else if (even < 16) {
+      padded = items_of(per) <= min(kMaxSplits, (int)gridDim.x);
+    }
   }
   auto counted = [&](int n) { return padded ? (n + per - 1) / per * per : n; };
 
@@ -533,16 +534,15 @@ __global__ __launch_bounds__(64 * kAttnWaves, (L::D == 256 && NT == 2) ? 1 : 2) 
   int u = u_begin, base = 0, b = 0;                                    // the sequence that holds block u, its first block `base`
   for (int b0 = 0;; b0 += 64) {
     if (b0 >= a.seqs) return;                                          // workgroups past the last block
-    const int n = b0 + lane < a.seqs ? counted(lengths_of(a, length_at(b0)).n) * pairs : 0;
-    const int incl = wave_scan_i32(n, lane);
+    const int n = counted(blocks_at(b0)) * pairs, incl = wave_scan(n);
     const uint64_t past = __ballot(base + incl > u);
     if (past) {
-      const int at = __ffsll((unsigned long long)past) - 1;
+      const int at = __builtin_ctzll(past);
       base += __builtin_amdgcn_readlane(incl - n, at);
       b = b0 + at;
       break;
     }
-    base += __builtin_amdgcn_readlane(incl, 63);
+    base += last_lane(incl);
   }
 
   while (u < u_end && b < a.seqs) {
@@ -565,11 +565,11 @@ __global__ __launch_bounds__(64 * kAttnWaves, (L::D == 256 && NT == 2) ? 1 : 2) 
     const int head = __builtin_amdgcn_readfirstlane(pair / chunks), h0 = (pair - head * chunks) * 16 * NT;
     const int count = min(per_head - h0, 16 * NT);
     const int32_t* table = a.table + seq * a.table_ld;
-    const int n_mine = (t1 - t0 - wave + kAttnWaves - 1) / kAttnWaves, block0 = len.first + t0 + wave;
+    const int n_mine = (t1 - t0 - wave + NW - 1) / NW, block0 = len.first + t0 + wave;
     // pages of this wave's blocks, a lane each, 64 blocks in a register: of even and odd runs of 64
     int pages[2];
     auto fetch_pages = [&](int run) {
-      const int token = (block0 + (run * 64 + lane) * kAttnWaves) * kKvBlock;
+      const int token = (block0 + (run * 64 + lane) * NW) * kKvBlock;
       int p = -1;
       if (run * 64 + lane < n_mine && token < len.end) p = table[token >> cache.page_log2];
       return p < cache.pages ? p : -1;
@@ -579,41 +579,34 @@ __global__ __launch_bounds__(64 * kAttnWaves, (L::D == 256 && NT == 2) ? 1 : 2) 
       return i & 64 ? odd : even;
     };
     auto address = [&](int i) {
-      const int page = max(page_of(i), 0), in_page = (block0 + i * kAttnWaves) & ((1 << (cache.page_log2 - 5)) - 1);
+      const int page = max(page_of(i), 0), in_page = (block0 + i * NW) & ((1 << (cache.page_log2 - 5)) - 1);
       return cache.data + ((((int64_t)page * cache.heads + head) << (cache.page_log2 - 5)) + in_page) * L::bytes;
     };
     Query<L, NT> query;
     query.fetch(a, a.q + seq * a.q_ld + (int64_t)(head * per_head + h0) * a.q_head, count, lane);
-    Keys<L> keys[PD];
-    Values<L> values[PD];
-    if (n_mine > 0) {
-      pages[0] = fetch_pages(0);
-      pages[1] = fetch_pages(1);
-#pragma unroll
-      for (int d = 0; d < PD; ++d) {
-        const uint8_t* p = address(min(d, n_mine - 1));
-        keys[d].load(p, lane);
-        values[d].load(p, lane);
-      }
-    }
-    query.convert(a, key_unit);
     Result<L, NT> res;
     res.clear();
-    for (int i0 = 0; i0 < n_mine; i0 += PD) {
-#pragma unroll
-      for (int d = 0; d < PD; ++d) {
-        const int i = i0 + d;
-        if (i >= n_mine) break;
-        if (i && (i & 63) == 0) pages[(i >> 6) + 1 & 1] = fetch_pages((i >> 6) + 1);
-        // the block after next ones replaces this one; past the end the last once more, so that the loads in flight are always as many
-        const uint8_t* next = address(min(i + PD, n_mine - 1));
+    if (n_mine > 0) {
+      Keys<L> keys;
+      Values<L> values;
+      pages[0] = fetch_pages(0);
+      pages[1] = fetch_pages(1);
+      const uint8_t* block = address(0);
+      keys.load(block, lane);
+      values.load(block, lane);
+      query.convert(a, key_unit);
+      for (int i = 0; i < n_mine; ++i) {
+        if (i && (i & 63) == 0) pages[((i >> 6) + 1) & 1] = fetch_pages((i >> 6) + 1);
+        // the next block's keys replace this one's as soon as the scores are there, its values the same; past the end the last
+        // block once more, so that the loads in flight are always as many
+        block = address(min(i + 1, n_mine - 1));
         float4_t s[NT][2];
-        block_scores<L, NT>(keys[d], query, s);
-        keys[d].load(next, lane);
-        const int token = (block0 + i * kAttnWaves) * kKvBlock;
+        block_scores<L, NT>(keys, query, s);
+        keys.load(block, lane);
+        const int token = (block0 + i * NW) * kKvBlock;
         const int lo = page_of(i) >= 0 ? max(0, len.first_token - token) : kKvBlock, hi = min(kKvBlock, len.end - token);
-        block_outputs<L, NT>(values[d], s, query, res, lane, lo, hi);
-        values[d].load(next, lane);
+        block_outputs<L, NT>(values, s, query, res, lane, lo, hi);
+        values.load(block, lane);
       }
     }
     if constexpr (L::FMT == kInt4)                                     // the odd codes came 16 times as large
@@ -624,39 +617,45 @@ __global__ __launch_bounds__(64 * kAttnWaves, (L::D == 256 && NT == 2) ? 1 : 2) 
 #pragma unroll
     for (int ct = 0; ct < NT; ++ct) res.l[ct] = column_sum(res.l[ct]);
 
-    // join the waves: 2, 3 into 0, 1, then 1 into 0
+    // join the waves: the upper half into the lower one, and so on
+    const int lane_now = renewed(lane), kq = lane_now >> 4, col = lane_now & 15;
     auto put = [&](int at) {
 #pragma unroll
       for (int ct = 0; ct < NT; ++ct) {
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) shared_acc[at][ct * NJ + j][lane] = res.acc[ct][j];
-        shared_ml[at][ct][0][lane] = res.m[ct];
-        shared_ml[at][ct][1][lane] = res.l[ct];
+        for (int j = 0; j < NJ; ++j) shared_acc[at][ct * NJ + j][lane_now] = res.acc[ct][j];
+        shared_ml[at][ct][0][lane_now] = res.m[ct];
+        shared_ml[at][ct][1][lane_now] = res.l[ct];
       }
     };
     auto take = [&](int at) {
 #pragma unroll
       for (int ct = 0; ct < NT; ++ct) {
-        const float om = shared_ml[at][ct][0][lane], ol = shared_ml[at][ct][1][lane];
+        const float om = shared_ml[at][ct][0][lane_now], ol = shared_ml[at][ct][1][lane_now];
         const float m = fmaxf(res.m[ct], om);
         const float f = __builtin_amdgcn_exp2f(res.m[ct] - m), g = __builtin_amdgcn_exp2f(om - m);
         res.m[ct] = m;
         res.l[ct] = res.l[ct] * f + ol * g;
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) res.acc[ct][j] = res.acc[ct][j] * f + shared_acc[at][ct * NJ + j][lane] * g;
+        for (int j = 0; j < NJ; ++j) res.acc[ct][j] = res.acc[ct][j] * f + shared_acc[at][ct * NJ + j][lane_now] * g;
       }
     };
-    __syncthreads();                                                   // the last segment's reads are over
-    if (wave >= 2) put(wave - 2);
-    __syncthreads();
-    if (wave < 2) take(wave);
-    if (wave == 1) put(1);
-    __syncthreads();
-    if (wave == 0) take(1);
+    auto join_waves = [&](int held) {                                  // the first `held` hold something: uniform
+#pragma unroll
+      for (int half = NW / 2; half >= 1; half /= 2) {
+        if (held <= half) continue;
+        __syncthreads();                                               // reads of the last join are over
+        if (wave >= half && wave < 2 * half) put(wave - half);
+        __syncthreads();
+        if (wave < half) take(wave);
+      }
+    };
+    join_waves(t1 - t0);
 
     bool write = wave == 0;
     if (w_first != w_last) {                                           // a part of a pair: the last worker to finish joins them
       constexpr uint32_t kPart = part_bytes_of<L, NT>();
+      constexpr int kJoin = NJ < 8 ? NJ : 8;
       if (wave == 0) {
         const uint32_t part = part_slot(blockIdx.x, w_first) * kPart;
 #pragma unroll
@@ -665,54 +664,72 @@ __global__ __launch_bounds__(64 * kAttnWaves, (L::D == 256 && NT == 2) ? 1 : 2) 
           if (col < heads) {
             const uint32_t at = part + ct * (NJ * 1024 + 256);
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) put_part(parts, at + ((j * 4 + kq) * heads + col) * 16, res.acc[ct][j]);
+            for (int j = 0; j < NJ; ++j) put_part(parts, at + lane_now * 16 + j * 1024, res.acc[ct][j]);
             if (kq == 0) put_part(parts, at + NJ * 1024 + col * 16, (float4_t){res.m[ct], res.l[ct], 0.0f, 0.0f});
           }
         }
         // the stores have reached memory before the counter says so
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (lane == 0)
+        if (lane_now == 0)
           last_one = __hip_atomic_fetch_add(counters + w_first, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == w_last - w_first;
       }
       __syncthreads();
       if (!__builtin_amdgcn_readfirstlane(last_one)) continue;
-      // the common reference and the sum of the weights, then the outputs; the waves take the parts in turn
+      // The waves take the parts in turn, and where a part has fewer than sixteen heads, so do the runs of lanes that would hold
+      // the others; the next part's loads are in flight while one is added.
 #pragma unroll
       for (int ct = 0; ct < NT; ++ct) {
         const int heads = min(16, count - ct * 16);
-        float m = kNoReference, l = 0.0f;
-        float4_t acc[NJ];
+        const int run_log2 = heads > 8 ? 4 : heads > 4 ? 3 : heads > 2 ? 2 : heads > 1 ? 1 : 0, runs = 16 >> run_log2;
+        const int mine = col & ((1 << run_log2) - 1), step = NW * runs;
+        const int w0 = w_first + wave * runs + (col >> run_log2);
+        // eight instructions' outputs at a time: what two parts' loads leave room for
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) acc[j] = (float4_t){0.0f, 0.0f, 0.0f, 0.0f};
-        if (col < heads) {
-          for (int w = w_first + kq; w <= w_last; w += 4)
-            m = fmaxf(m, get_part(parts, part_slot(w, w_first) * kPart + ct * (NJ * 1024 + 256) + NJ * 1024 + col * 16)[0]);
-        }
-        m = column_max(m);
-        if (col < heads) {
-#pragma unroll 2
-          for (int w = w_first + wave; w <= w_last; w += kAttnWaves) {
-            const uint32_t at = part_slot(w, w_first) * kPart + ct * (NJ * 1024 + 256);
-            const float4_t ml = get_part(parts, at + NJ * 1024 + col * 16);
-            const float f = __builtin_amdgcn_exp2f(ml[0] - m);
-            l += ml[1] * f;
+        for (int j0 = 0; j0 < NJ; j0 += kJoin) {
+          float m = kNoReference, l = 0.0f;
+          float4_t acc[kJoin];
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) acc[j] += get_part(parts, at + ((j * 4 + kq) * heads + col) * 16) * f;
+          for (int j = 0; j < kJoin; ++j) acc[j] = (float4_t){0.0f, 0.0f, 0.0f, 0.0f};
+          struct Loaded {
+            float4_t ml, acc[kJoin];
+          };
+          auto fetch = [&](Loaded& x, int w) {
+            const bool ok = w <= w_last && mine < heads;               // others read past the buffer: zeros
+            const uint32_t at = ok ? part_slot(w, w_first) * kPart + ct * (NJ * 1024 + 256) : 0x80000000u;
+            x.ml = get_part(parts, at + NJ * 1024 + mine * 16);
+#pragma unroll
+            for (int j = 0; j < kJoin; ++j) x.acc[j] = get_part(parts, at + (kq * 16 + mine) * 16 + (j0 + j) * 1024);
+            if (!ok) x.ml[0] = kNoReference;
+          };
+          auto add = [&](float om, float ol, auto&& other) {
+            const float top = fmaxf(m, om), f = __builtin_amdgcn_exp2f(m - top), g = __builtin_amdgcn_exp2f(om - top);
+            m = top;
+            l = l * f + ol * g;
+#pragma unroll
+            for (int j = 0; j < kJoin; ++j) acc[j] = acc[j] * f + other(j) * g;
+          };
+          Loaded x, y;
+          fetch(x, w0);
+#pragma unroll 1
+          for (int w = 0; w <= w_last - w_first; w += 2 * step) {      // uniform
+            fetch(y, w0 + w + step);
+            add(x.ml[0], x.ml[1], [&](int j) { return x.acc[j]; });
+            fetch(x, w0 + w + 2 * step);
+            add(y.ml[0], y.ml[1], [&](int j) { return y.acc[j]; });
           }
-        }
-        res.m[ct] = m;
-        res.l[ct] = l;
+#pragma unroll 1
+          for (int off = 1 << run_log2; off < 16; off <<= 1)
+            add(__shfl_xor(m, off), __shfl_xor(l, off), [&](int j) {
+              return (float4_t){__shfl_xor(acc[j][0], off), __shfl_xor(acc[j][1], off), __shfl_xor(acc[j][2], off), __shfl_xor(acc[j][3], off)};
+            });
+          res.m[ct] = m;
+          res.l[ct] = l;
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) res.acc[ct][j] = acc[j];
+          for (int j = 0; j < kJoin; ++j) res.acc[ct][j0 + j] = acc[j];
+        }
       }
-      __syncthreads();
-      if (wave >= 2) put(wave - 2);
-      __syncthreads();
-      if (wave < 2) take(wave);
-      if (wave == 1) put(1);
-      __syncthreads();
-      if (wave == 0) take(1);
+      join_waves(NW);
       if (threadIdx.x == 0) counters[w_first] = 0;                     // for the next call
     }
     if (write) {
@@ -746,12 +763,15 @@ int chunks_of(const pq_kv_cache& c, int q_heads) {
   const int width = 16 * tiles_of(c, q_heads);
   return (q_heads / c.kv_heads + width - 1) / width;
 }
+int64_t longest_of(int64_t max_len, int64_t window) {                  // blocks of the longest sequence
+  int64_t n = (max_len + kKvBlock - 1) / kKvBlock;
+  if (window && n > window / kKvBlock + 2) n = window / kKvBlock + 2;
+  return n < 1 ? 1 : n;
+}
 int64_t grid_of(const pq_kv_cache& c, int64_t seqs, int q_heads, int64_t max_len, int64_t window) {
   const int64_t pairs = seqs * c.kv_heads * chunks_of(c, q_heads);
-  int64_t n = (max_len + kKvBlock - 1) / kKvBlock;                     // blocks of the longest sequence
-  if (window) n = n < window / kKvBlock + 2 ? n : window / kKvBlock + 2;
-  if (n < 1) n = 1;
-  const int64_t parts = pairs * ((n + kLeastBlocks - 1) / kLeastBlocks), most = pairs > kMaxSplits ? pairs : kMaxSplits;
+  const int64_t parts = pairs * ((longest_of(max_len, window) + kLeastBlocks - 1) / kLeastBlocks);
+  const int64_t most = pairs > kMaxSplits ? pairs : kMaxSplits;
   return parts < most ? parts : most;
 }
 
@@ -766,10 +786,11 @@ size_t attn_decode_workspace_bytes(const pq_kv_cache& c, int64_t seqs, int q_hea
 
 int run_attn_decode(const pq_kv_cache& c, const AttnCall& a, hipStream_t st) {
   const int grid = (int)grid_of(c, a.seqs, a.q_heads, a.max_len, a.window), chunks = chunks_of(c, a.q_heads);
+  const int longest = (int)longest_of(a.max_len, a.window);
   const uint32_t part_bytes = (uint32_t)(attn_decode_workspace_bytes(c, a.seqs, a.q_heads, a.max_len, a.window) - PQ_ATTN_DECODE_ZERO_BYTES);
   return kv_dispatch(c.fmt, c.group, c.head_dim, [&](auto l) {
-    if (tiles_of(c, a.q_heads) == 1) attn_decode_kernel<decltype(l), 1><<<grid, 64 * kAttnWaves, 0, st>>>(kv_view(c), a, chunks, part_bytes);
-    else attn_decode_kernel<decltype(l), 2><<<grid, 64 * kAttnWaves, 0, st>>>(kv_view(c), a, chunks, part_bytes);
+    if (tiles_of(c, a.q_heads) == 1) attn_decode_kernel<decltype(l), 1><<<grid, 64 * kAttnWaves, 0, st>>>(kv_view(c), a, chunks, longest, part_bytes);
+    else attn_decode_kernel<decltype(l), 2><<<grid, 64 * kAttnWaves, 0, st>>>(kv_view(c), a, chunks, longest, part_bytes);
     return check_hip(hipGetLastError(), "pq_attn_decode");
   });
 }
