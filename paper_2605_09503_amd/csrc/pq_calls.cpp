@@ -10,6 +10,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <ATen/ops/empty.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -22,6 +23,8 @@ namespace {
 PyObject* g_raise = nullptr;        // raise(rc): raises the error of the last call
 PyObject* g_operand = nullptr;      // operand(fmt, group, rows, K, like) -> tensor
 PyObject* g_workspace = nullptr;    // workspace(op, fmt, group, M, N, K, n_batches, like) -> tensor or None
+PyObject* g_refuse = nullptr;       // refuse(message): raises the error of arguments that do not fit
+PyObject* g_attn_workspace = nullptr;   // attn_workspace(cache, seqs, q_heads, max_len, window) -> tensor
 
 // thrown when a Python error is set
 struct PyFailed {};
@@ -337,15 +340,140 @@ PQ_CALL(calib_moments) {
   });
 }
 
+// ---- key-value cache: tensors are checked as pq.py's functions check them (a wrong type or size would be read past its end)
+template <class... A>
+[[noreturn]] void refuse(const char* format, A... a) {
+  Ref text(PyUnicode_FromFormat(format, a...));
+  Ref unused(PyObject_CallFunctionObjArgs(g_refuse, text.p, nullptr));
+  fail(PyExc_RuntimeError, "arguments do not fit");                     // not reached: refuse() raises
+}
+
+struct Cache {
+  const pq_kv_cache* c;
+  c10::Device device;
+};
+Cache cache_of(PyObject* o) {
+  Ref address(PyObject_GetAttrString(o, "_address")), data(PyObject_GetAttrString(o, "data"));
+  const at::Tensor* t = tensor(data.p);
+  if (!t) fail(PyExc_TypeError, "the cache's data must be a tensor");
+  return Cache{(const pq_kv_cache*)PyLong_AsVoidPtr(address.p), t->device()};
+}
+const at::Tensor& as_tensor(PyObject* o, const char* name) {
+  const at::Tensor* t = THPVariable_Check(o) ? &THPVariable_Unpack(o) : nullptr;
+  if (!t) PyErr_Format(PyExc_TypeError, "%s must be a tensor", name), throw PyFailed{};
+  return *t;
+}
+
+// bf16 [rows, heads, head_dim]; strides of one row or head do not matter
+struct HeadRows {
+  void* p;
+  int64_t ld, head;
+};
+HeadRows head_rows(const Cache& c, const char* name, const at::Tensor& t, int64_t rows, int64_t heads) {
+  if (t.scalar_type() != at::kBFloat16 || t.dim() != 3 || t.size(0) != rows || t.size(1) != heads || t.size(2) != c.c->head_dim ||
+      t.stride(2) != 1 || t.device() != c.device)
+    refuse("%s must be bfloat16 [%lld, %lld, %d] with adjacent channels, on the cache's device", name, (long long)rows, (long long)heads,
+           c.c->head_dim);
+  return HeadRows{t.data_ptr(), rows > 1 ? t.stride(0) : 0, heads > 1 ? t.stride(1) : 0};
+}
+void* indices(const Cache& c, const char* name, const at::Tensor& t, at::ScalarType type, const char* type_name, int64_t dims) {
+  if (t.scalar_type() != type || t.dim() != dims || (t.numel() > 1 && t.stride(dims - 1) != 1) || t.device() != c.device)
+    refuse("%s must be %s with %lld dimension%s, the last one contiguous, on the cache's device", name, type_name, (long long)dims,
+           dims > 1 ? "s" : "");
+  return t.data_ptr();
+}
+void* stream_of(const Cache& c) {
+  if (!c.device.is_cuda()) refuse("the cache must lie in GPU memory");
+  return stream();
+}
+at::Tensor new_rows(const Cache& c, int64_t rows, int64_t heads) {
+  return at::empty({rows, heads, c.c->head_dim}, at::TensorOptions().dtype(at::kBFloat16).device(c.device));
+}
+
+PQ_CALL(kv_write) {
+  return guarded([&] {
+    PQ_TAKE(pq_kv_write, 4, "cache", "k", "v", "slots");
+    const Cache c = cache_of(a[0]);
+    const at::Tensor &slots = as_tensor(a[3], "slots"), &k = as_tensor(a[1], "k"), &v = as_tensor(a[2], "v");
+    const int64_t* s = (const int64_t*)indices(c, "slots", slots, at::kLong, "torch.int64", 1);
+    const int64_t n = slots.size(0);
+    const HeadRows kr = head_rows(c, "k", k, n, c.c->kv_heads), vr = head_rows(c, "v", v, n, c.c->kv_heads);
+    void* st = stream_of(c);
+    call([&] { return pq_kv_write(c.c, kr.p, kr.ld, kr.head, vr.p, vr.ld, vr.head, s, n, st); });
+    return none();
+  });
+}
+
+PQ_CALL(kv_read) {
+  return guarded([&] {
+    PQ_TAKE(pq_kv_read, 2, "cache", "slots", "k", "v");
+    const Cache c = cache_of(a[0]);
+    const at::Tensor& slots = as_tensor(a[1], "slots");
+    const int64_t* s = (const int64_t*)indices(c, "slots", slots, at::kLong, "torch.int64", 1);
+    const int64_t n = slots.size(0);
+    const at::Tensor k = given(a[2]) ? as_tensor(a[2], "k") : new_rows(c, n, c.c->kv_heads);
+    const at::Tensor v = given(a[3]) ? as_tensor(a[3], "v") : new_rows(c, n, c.c->kv_heads);
+    const HeadRows kr = head_rows(c, "k", k, n, c.c->kv_heads), vr = head_rows(c, "v", v, n, c.c->kv_heads);
+    void* st = stream_of(c);
+    call([&] { return pq_kv_read(c.c, s, n, kr.p, kr.ld, kr.head, vr.p, vr.ld, vr.head, st); });
+    Ref ko(THPVariable_Wrap(k)), vo(THPVariable_Wrap(v));
+    return PyTuple_Pack(2, ko.p, vo.p);
+  });
+}
+
+PQ_CALL(attn_decode) {
+  return guarded([&] {
+    PQ_TAKE(pq_attn_decode, 6, "cache", "q", "table", "lengths", "max_len", "scale", "out", "lse", "window", "workspace");
+    const Cache c = cache_of(a[0]);
+    const at::Tensor &q = as_tensor(a[1], "q"), &table = as_tensor(a[2], "table"), &lengths = as_tensor(a[3], "lengths");
+    if (q.dim() != 3) refuse("q must be bfloat16 [seqs, q_heads, head_dim]");
+    const int64_t seqs = q.size(0), q_heads = q.size(1), max_len = as_int(a[4]), window = given(a[8]) ? as_int(a[8]) : 0;
+    const float scale = (float)PyFloat_AsDouble(a[5]);
+    if (PyErr_Occurred()) throw PyFailed{};
+    const HeadRows qr = head_rows(c, "q", q, seqs, q_heads);
+    const int32_t* tab = (const int32_t*)indices(c, "table", table, at::kInt, "torch.int32", 2);
+    const int32_t* len = (const int32_t*)indices(c, "lengths", lengths, at::kInt, "torch.int32", 1);
+    if (table.size(0) != seqs || lengths.size(0) != seqs || table.size(1) * c.c->page < max_len)
+      refuse("table and lengths must have a row for each of %lld sequences, and table the pages of %lld tokens", (long long)seqs,
+             (long long)max_len);
+    float* lse = nullptr;
+    if (given(a[7])) {
+      const at::Tensor& t = as_tensor(a[7], "lse");
+      if (t.scalar_type() != at::kFloat || t.dim() != 2 || t.size(0) != seqs || t.size(1) != q_heads || !t.is_contiguous() ||
+          t.device() != c.device)
+        refuse("lse must be contiguous float32 [%lld, %lld] on the cache's device", (long long)seqs, (long long)q_heads);
+      lse = (float*)t.data_ptr();
+    }
+    const at::Tensor out = given(a[6]) ? as_tensor(a[6], "out") : new_rows(c, seqs, q_heads);
+    const HeadRows outr = head_rows(c, "out", out, seqs, q_heads);
+    PyObject* w = nullptr;
+    if (given(a[9])) {
+      w = a[9];
+      Py_INCREF(w);
+    } else {
+      w = PyObject_CallFunction(g_attn_workspace, "OLLLL", a[0], (long long)seqs, (long long)q_heads, (long long)max_len, (long long)window);
+    }
+    Ref ws(w);
+    const at::Tensor& wt = as_tensor(ws.p, "workspace");
+    void *wp = wt.data_ptr(), *st = stream_of(c);
+    const size_t bytes = wt.numel() * wt.element_size();
+    const int64_t table_ld = seqs > 1 ? table.stride(0) : table.size(1);
+    call([&] {
+      return pq_attn_decode(c.c, qr.p, qr.ld, qr.head, tab, table_ld, len, seqs, (int)q_heads, max_len, window, scale, outr.p, outr.ld,
+                            outr.head, lse, wp, bytes, st);
+    });
+    return THPVariable_Wrap(out);
+  });
+}
+
 PyObject* bind(PyObject*, PyObject* args) {
-  PyObject *raise, *operand, *workspace;
-  if (!PyArg_ParseTuple(args, "OOO", &raise, &operand, &workspace)) return nullptr;
-  Py_INCREF(raise);
-  Py_INCREF(operand);
-  Py_INCREF(workspace);
-  Py_XSETREF(g_raise, raise);
-  Py_XSETREF(g_operand, operand);
-  Py_XSETREF(g_workspace, workspace);
+  PyObject* given_by[5];
+  if (!PyArg_ParseTuple(args, "OOOOO", &given_by[0], &given_by[1], &given_by[2], &given_by[3], &given_by[4])) return nullptr;
+  PyObject** const slots[5] = {&g_raise, &g_operand, &g_workspace, &g_refuse, &g_attn_workspace};
+  for (int i = 0; i < 5; ++i) {
+    Py_INCREF(given_by[i]);
+    Py_XSETREF(*slots[i], given_by[i]);
+  }
   Py_RETURN_NONE;
 }
 
@@ -374,7 +502,13 @@ PyMethodDef methods[] = {
               "y[M, N] (bf16) = dequant(A) @ dequant(W)^T."),
     PQ_METHOD(calib_moments, "(x, sumsq, absmax=None, workspace=None, rows=None, K=None, ld=None)",
               "sumsq[K] (float64, in/out) += column sums of squares of bf16 x[rows, ld]."),
-    {"bind", bind, METH_VARARGS, "bind(raise_, operand, workspace): the helpers of pq.py"},
+    PQ_METHOD(kv_write, "(cache, k, v, slots)",
+              "Quantizes keys and values, bf16 [n, kv_heads, head_dim] (slices of a fused projection's rows are), into the slots (int64 [n])."),
+    PQ_METHOD(kv_read, "(cache, slots, k=None, v=None)", "(k, v) of the slots as bf16 [n, kv_heads, head_dim] (allocated unless given)."),
+    PQ_METHOD(attn_decode, "(cache, q, table, lengths, max_len, scale, out=None, lse=None, window=0, workspace=None)",
+              "Attention of one new token a sequence, q bf16 [seqs, q_heads, head_dim], over the lengths[b] (int32) tokens whose pages\n"
+              "table[b] (int32) names; out like q (allocated unless given), lse float32 [seqs, q_heads].  max_len: no sequence is longer."),
+    {"bind", bind, METH_VARARGS, "bind(raise_, operand, workspace, refuse, attn_workspace): the helpers of pq.py"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pq_calls", "Hot calls of the binding (see pq.py).", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

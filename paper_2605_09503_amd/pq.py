@@ -179,7 +179,8 @@ def _stream():
 # (csrc/pq_calls.cpp): it takes the place of the functions of these names below, which do the same and serve where the module
 # is not built (it needs a host compiler and the interpreter's headers) or was built for another torch.
 _CALLS = ("pq_quantize_act", "pq_quantize_act_packed", "pq_norm_quantize_act_packed", "pq_hadamard_quantize_act_packed",
-          "pq_qgemm", "pq_qgemm_packed", "pq_qgemm_packed_f32", "pq_qgemm_packed_bias", "pq_calib_moments")
+          "pq_qgemm", "pq_qgemm_packed", "pq_qgemm_packed_f32", "pq_qgemm_packed_bias", "pq_calib_moments", "pq_kv_write",
+          "pq_kv_read", "pq_attn_decode")
 _CALLS_PATH = os.path.join(os.path.dirname(_LIB_PATH), "_pq_calls.so")
 _calls = None           # the module, or False where it cannot be had
 
@@ -194,6 +195,10 @@ def _refuse(msg: str):
 
 def _new_operand(fmt: int, group: int, rows: int, K: int, like: torch.Tensor) -> torch.Tensor:
     return torch.empty(max(pq_operand_bytes(fmt, group, rows, K), 16), dtype=torch.uint8, device=like.device)
+
+
+def _new_attn_workspace(cache, seqs: int, q_heads: int, max_len: int, window: int) -> torch.Tensor:
+    return pq_attn_decode_workspace(cache, seqs, q_heads, max_len, window)
 
 
 def _new_workspace(op: int, fmt: int, group: int, M: int, N: int, K: int, n_batches: int, like: torch.Tensor):
@@ -212,7 +217,7 @@ def _bind_calls():
         loader = importlib.machinery.ExtensionFileLoader("_pq_calls", _CALLS_PATH)
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_pq_calls", loader))
         loader.exec_module(module)
-        module.bind(_raise, _new_operand, _new_workspace)
+        module.bind(_raise, _new_operand, _new_workspace, _refuse, _new_attn_workspace)
         bound = {name: getattr(module, name) for name in _CALLS}
     except (ImportError, AttributeError, OSError) as e:
         warnings.warn("the native binding of the hot calls cannot be used, ctypes takes 2 us more a call (%s); build it with "
@@ -726,12 +731,18 @@ def _indices(cache: KVCache, name: str, t: torch.Tensor, dtype, dims: int):
     return t.data_ptr()
 
 
+def _stream_of(cache: KVCache):
+    if not cache.data.is_cuda:
+        _refuse("the cache must lie in GPU memory")
+    return _stream()
+
+
 def pq_kv_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
     """Quantizes keys and values, bf16 [n, kv_heads, head_dim] (slices of a fused projection's rows are), into the slots (int64 [n])."""
     s = _indices(cache, "slots", slots, torch.int64, 1)
     n = slots.shape[0]
     kr, vr = (_head_rows(cache, name, t, n, cache.kv_heads) for name, t in (("k", k), ("v", v)))
-    _check(load().pq_kv_write(cache._address, *kr, *vr, s, n, _stream()))
+    _check(load().pq_kv_write(cache._address, *kr, *vr, s, n, _stream_of(cache)))
 
 
 def pq_kv_read(cache: KVCache, slots: torch.Tensor, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
@@ -741,7 +752,7 @@ def pq_kv_read(cache: KVCache, slots: torch.Tensor, k: Optional[torch.Tensor] = 
     k, v = (torch.empty((n, cache.kv_heads, cache.head_dim), dtype=torch.bfloat16, device=cache.data.device) if t is None else t
             for t in (k, v))
     kr, vr = (_head_rows(cache, name, t, n, cache.kv_heads) for name, t in (("k", k), ("v", v)))
-    _check(load().pq_kv_read(cache._address, s, n, *kr, *vr, _stream()))
+    _check(load().pq_kv_read(cache._address, s, n, *kr, *vr, _stream_of(cache)))
     return k, v
 
 
@@ -783,7 +794,7 @@ def pq_attn_decode(cache: KVCache, q: torch.Tensor, table: torch.Tensor, lengths
     if workspace is None:
         workspace = pq_attn_decode_workspace(cache, seqs, q_heads, max_len, window)
     _check(load().pq_attn_decode(cache._address, *qr, tab, table.stride(0) if seqs > 1 else table.shape[1], n, seqs, q_heads, max_len, window,
-                                 float(scale), *outr, _ptr(lse), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()))
+                                 float(scale), *outr, _ptr(lse), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream_of(cache)))
     return out
 
 

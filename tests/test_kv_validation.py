@@ -1,4 +1,5 @@
 """Refusals of the cache's entry points: every check is the host's, before anything is launched (no GPU needed)."""
+import ast
 import ctypes as C
 
 import pytest
@@ -95,8 +96,25 @@ def test_attention(lib):  # noqa: F811
                 assert size(seqs, 4, top, window) <= size(seqs + 1, 4, top + 1, 0)
 
 
-def test_binding_refuses_other_tensors(lib, monkeypatch):  # noqa: F811
-    monkeypatch.setattr(pq, "_stream", lambda: None)
+def python_binding():
+    """pq.py alone, as it serves where the native module is not built."""
+    import importlib.util
+    spec = importlib.util.spec_from_file_location("pq_python", pq.__file__)
+    module = importlib.util.module_from_spec(spec)
+    import sys
+    sys.modules["pq_python"] = module
+    spec.loader.exec_module(module)
+    for name in ("pq_kv_write", "pq_kv_read", "pq_attn_decode"):
+        with open(pq.__file__) as f:
+            tree = ast.parse(f.read())
+        f = next(n for n in tree.body if isinstance(n, ast.FunctionDef) and n.name == name)
+        exec(compile(ast.Module([f], []), pq.__file__, "exec"), module.__dict__)
+    return module
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_binding_refuses_other_tensors(lib, native):  # noqa: F811
+    pq = globals()["pq"] if native else python_binding()
     c = pq.alloc_kv_cache(pq.FMT_INT4, 64, 2, 128, 64, 4, device="cpu")
     t = torch.zeros(3, 2, 128, dtype=torch.bfloat16)
     slots = torch.zeros(3, dtype=torch.int64)
@@ -128,9 +146,24 @@ def test_binding_refuses_other_tensors(lib, monkeypatch):  # noqa: F811
     refused(pq.pq_attn_decode, c, q, table, lengths, 200, 1.0, out=q[:, :2], workspace=ws)
     refused(pq.pq_attn_decode, c, q, table, lengths, 200, 1.0, lse=torch.zeros(3, 4, dtype=torch.float64), workspace=ws)
     refused(pq.pq_attn_decode, c, q, table, lengths, 200, 1.0, lse=torch.zeros(4, 3), workspace=ws)
-    with pytest.raises(pq.PQError) as e:
-        pq.pq_attn_decode(c, q, table, lengths, 200, 1.0, workspace=ws[:64])
-    assert e.value.code == PQ_ERR_WORKSPACE
+    refused(pq.pq_attn_decode, c, q, table, lengths, 200, 1.0, workspace=ws)                # all fits, in host memory
+    refused(pq.pq_kv_write, c, t, t, slots)
+    refused(pq.pq_kv_read, c, slots)
     for kw in (dict(data=c.data[:100]), dict(data=c.data.view(torch.int8)), dict(fmt=0, group=16), dict(page=33), dict(fmt=2, group=32)):
         with pytest.raises(pq.PQError):
             pq.KVCache(**{**{f: getattr(c, f) for f in ("fmt", "group", "kv_heads", "head_dim", "page", "pages", "data")}, **kw})
+
+
+SIGNATURES = {
+    "pq_kv_write": "(cache, k, v, slots)",
+    "pq_kv_read": "(cache, slots, k=None, v=None)",
+    "pq_attn_decode": "(cache, q, table, lengths, max_len, scale, out=None, lse=None, window=0, workspace=None)",
+}
+
+
+@pytest.mark.parametrize("name", sorted(SIGNATURES))
+def test_native_and_python_signatures(lib, name):  # noqa: F811
+    import inspect
+    assert str(inspect.signature(getattr(pq, name))) == SIGNATURES[name]
+    python = inspect.signature(getattr(python_binding(), name))
+    assert [str(p.replace(annotation=p.empty)) for p in python.parameters.values()] == SIGNATURES[name][1:-1].split(", ")
