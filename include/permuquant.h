@@ -526,7 +526,7 @@ int pq_hadamard_quantize_act_packed(const int32_t* perm, pq_format fmt, int grou
  *
  *   fmt, group   PQ_FMT_NVFP4 with 16; PQ_FMT_INT4 with 32, 64, 128 or 256, at most head_dim; PQ_FMT_BF16 with 0 (unquantized)
  *   head_dim     64, 128 or 256
- *   page         32, 64, 128, 256, 512 or 1024
+ *   page         32, 64, 128, 256, 512 or 1024; pages * (page / 32) * kv_heads below 2^31
  *   data         device memory, 16-byte aligned; need not be initialised
  *   k_tensor_scale, v_tensor_scale   float [1] device each, NVFP4 only (T of the header comment, one for all keys, one for all
  *                values; magnitudes above 2688 T saturate); ignored by the other formats

@@ -685,7 +685,8 @@ static const char* kv_cache_error(pq_format fmt, int group, int kv_heads, int he
   if (kv_heads <= 0 || kv_heads > 4096) return "kv_heads must be 1 .. 4096";
   if (page != 32 && page != 64 && page != 128 && page != 256 && page != 512 && page != 1024)
     return "page must be 32, 64, 128, 256, 512 or 1024 tokens";
-  if (pages <= 0 || pages > INT32_MAX) return "pages must be 1 .. 2^31 - 1";
+  if (pages <= 0 || pages > INT32_MAX || pages * (page / 32) * kv_heads > INT32_MAX)
+    return "pages must be 1 .. 2^31 - 1, and blocks of 32 tokens of all heads fewer than 2^31";
   *code = PQ_OK;
   return nullptr;
 }
@@ -729,7 +730,9 @@ static int check_kv_rows(const char* who, const pq_kv_cache* cache, const void* 
                          int64_t v_ld, int64_t v_head, const int64_t* slots, int64_t n, bool out) {
   int rc = check_kv_cache(who, cache);
   if (rc) return rc;
-  if (n < 0 || n > INT32_MAX) return fail(PQ_ERR_SHAPE, "%s: n=%lld outside 0 .. 2^31 - 1", who, (long long)n);
+  if (n < 0 || n > INT32_MAX || (n / 32 + 1) * cache->kv_heads > INT32_MAX)
+    return fail(PQ_ERR_SHAPE, "%s: n=%lld tokens of %d heads outside 0 .. 2^31 - 1 tokens, or 2^36 of all heads", who, (long long)n,
+                cache->kv_heads);
   if (n == 0) return PQ_OK;
   if (!k || !v || !slots) return fail(PQ_ERR_NULL, "%s: a required pointer is NULL", who);
   rc = check_head_rows(who, "k", k, k_ld, k_head, n, cache->kv_heads, cache->head_dim, out);

@@ -148,17 +148,6 @@ struct Values : Part<L> {
   }
 };
 
-// eight codes, two quads (of two tokens' values, or a key's chunk): the codes a of both as a pair of fp16 subnormals, the odd ones
-// 16 times as large
-struct IntCodes {
-  uint32_t d, swapped;
-  __device__ __forceinline__ explicit IntCodes(uint32_t x) : d(x), swapped(__builtin_amdgcn_perm(0u, x, 0x02030001u)) {}
-  __device__ __forceinline__ uint32_t pair(int a) const {
-    const uint32_t x = a & 2 ? swapped : d;
-    return a & 1 ? (x << 1) & 0x80708070u : x & 0x80078007u;
-  }
-};
-
 // The queries as the second operand, and what else the loop keeps of a pair.
 template <class L, int NT>
 struct Query {

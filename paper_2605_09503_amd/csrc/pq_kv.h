@@ -78,15 +78,44 @@ struct KvLayout {
 // INT4: code c (0 .. 3) of a quad
 __device__ __forceinline__ constexpr int int_mag_at(int c) { return (c & 2) * 4 + (c & 1) * 3; }       // 0, 3, 8, 11
 __device__ __forceinline__ constexpr int int_sign_at(int c) { return 15 - (c & 2) * 4 - (c & 1); }     // 15, 14, 7, 6
-// rounded x * inv (ties to even) as a code of a quad; |x * inv| < 7.5
-__device__ __forceinline__ uint32_t int_encode(float x, float inv, int c) {
-  const uint32_t m = as_u32(fabsf(x * inv) + 8388608.0f) & 7u;
-  return m << int_mag_at(c) | (as_u32(x) >> 31) << int_sign_at(c);
+// Two quads side by side, from eight values (pairs of bf16, values 2 i and 2 i + 1 in x[i]; quads of values 0 .. 3 and 4 .. 7):
+// x * inv (an inverse a pair) rounded to the nearest integer (ties to even), below 7.5 in magnitude.  Adding 2^23 leaves the integer in the low bits
+// under a constant; the words are summed at the codes' places, the constants taken off once.  Signs go two at a time.
+__device__ __forceinline__ uint32_t int_encode8(const uint32_t (&x)[4], const float (&inv)[4]) {
+  constexpr uint32_t kBase = 0x4B000000u;                              // bits of 2^23
+  uint32_t mags = 0, bases = 0, signs = 0;
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    const float v = c & 1 ? bf16_hi(x[c / 2]) : bf16_lo(x[c / 2]);
+    const int at = int_mag_at(c & 3) + (c & 4) * 4;
+    mags += as_u32(fabsf(v * inv[c / 2]) + 8388608.0f) << at;
+    bases += kBase << at;
+  }
+#pragma unroll
+  for (int c = 0; c < 4; ++c) {                                        // values c and c + 4: signs at bits 15 and 31
+    const uint32_t two = __builtin_amdgcn_perm(x[c / 2 + 2], x[c / 2], c & 1 ? 0x07060302u : 0x05040100u);
+    signs |= (two >> (15 - int_sign_at(c))) & (0x00010001u << int_sign_at(c));
+  }
+  return (mags - bases) | signs;
 }
-__device__ __forceinline__ float int_decode(uint32_t quad, int c) {
-  const float m = (float)((quad >> int_mag_at(c)) & 7u);
-  return (quad >> int_sign_at(c)) & 1u ? -m : m;
-}
+
+// Two quads side by side: codes a of both as a pair of fp16 subnormals, the odd ones 16 times as large.
+struct IntCodes {
+  uint32_t d, swapped;
+  __device__ __forceinline__ explicit IntCodes(uint32_t x) : d(x), swapped(__builtin_amdgcn_perm(0u, x, 0x02030001u)) {}
+  __device__ __forceinline__ uint32_t pair(int a) const {
+    const uint32_t x = a & 2 ? swapped : d;
+    return a & 1 ? (x << 1) & 0x80708070u : x & 0x80078007u;
+  }
+  // the integers
+  __device__ __forceinline__ void values(int a, float& lo, float& hi) const {
+    typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+    const half2 h = __builtin_bit_cast(half2, pair(a));
+    const float unit = a & 1 ? 1048576.0f : 16777216.0f;
+    lo = __builtin_fmaf((float)h.x, unit, 0.0f);
+    hi = __builtin_fmaf((float)h.y, unit, 0.0f);
+  }
+};
 
 // what the kernels need of a pq_kv_cache
 struct KvView {
@@ -101,9 +130,9 @@ struct KvView {
 // the block of a slot and the token's place in it
 template <class L>
 __device__ __forceinline__ uint8_t* kv_block(const KvView& c, int64_t slot, int head) {
-  const int64_t page = slot >> c.page_log2;
-  const int in_page = (int)(slot & ((1 << c.page_log2) - 1));
-  return c.data + (((page * c.heads + head) << (c.page_log2 - 5)) + (in_page >> 5)) * (int64_t)L::bytes;
+  const uint32_t page = (uint32_t)(slot >> c.page_log2), in_page = (uint32_t)slot & ((1u << c.page_log2) - 1);
+  const uint32_t block = ((page * c.heads + head) << (c.page_log2 - 5)) + (in_page >> 5);      // fewer than 2^31 in a cache
+  return c.data + (uint64_t)block * L::bytes;
 }
 
 // f(KvLayout) for a format, group and head size that check_kv_cache let through

@@ -18,11 +18,11 @@ def test_cache_bytes(lib):  # noqa: F811
     assert f(pq.FMT_INT4, 64, 8, 128, 64, 10) == tokens * 2 * (64 + 4)
     assert f(pq.FMT_INT4, 256, 8, 256, 64, 10) == tokens * 2 * (128 + 2)
     assert f(pq.FMT_BF16, 0, 8, 64, 64, 10) == tokens * 256
-    assert f(pq.FMT_INT4, 32, 1, 64, 1024, (1 << 31) - 1) == ((1 << 31) - 1) * 1024 * 72
+    assert f(pq.FMT_INT4, 32, 1, 64, 1024, (1 << 26) - 1) == ((1 << 26) - 1) * 1024 * 72
     for bad in [(pq.FMT_INT3, 32, 8, 128, 64, 1), (pq.FMT_NVFP4, 32, 8, 128, 64, 1), (pq.FMT_INT4, 16, 8, 128, 64, 1),
                 (pq.FMT_INT4, 128, 8, 64, 64, 1), (pq.FMT_BF16, 16, 8, 64, 64, 1), (pq.FMT_INT4, 32, 0, 64, 64, 1),
                 (pq.FMT_INT4, 32, 8, 96, 64, 1), (pq.FMT_INT4, 32, 8, 64, 48, 1), (pq.FMT_INT4, 32, 8, 64, 16, 1),
-                (pq.FMT_INT4, 32, 8, 64, 2048, 1), (pq.FMT_INT4, 32, 8, 64, 64, 0), (pq.FMT_INT4, 32, 8, 64, 64, 1 << 31),
+                (pq.FMT_INT4, 32, 8, 64, 2048, 1), (pq.FMT_INT4, 32, 8, 64, 64, 0), (pq.FMT_INT4, 32, 8, 64, 64, 1 << 31), (pq.FMT_INT4, 32, 1, 64, 1024, 1 << 26),
                 (9, 32, 8, 64, 64, 1)]:
         assert f(*bad) == 0, bad
         assert "pq_kv_cache_bytes" in pq.pq_last_error()
