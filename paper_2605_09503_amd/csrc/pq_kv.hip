@@ -49,34 +49,94 @@ __device__ __forceinline__ void write_key(const KvView& cache, uint8_t* block, i
   }
 }
 
-// a lane's channels of a value (pairs of them in x)
+// A lane's runs are PER channels, 4 bytes with groups of 32.  Rows are read and written in pieces of up to 16 bytes instead: TS
+// neighbouring lanes hold, before (after) an exchange, one run's channels of all of them each.  4-byte stores against this: reading
+// back 12 sequences up to 9001 tokens, INT4 groups of 32 in heads of 64, 24.6 against 23.2 us.
 template <class L>
-__device__ __forceinline__ void write_value(const KvView& cache, uint8_t* block, int t, int lane, bool ok, const uint32_t (&x)[L::NJ / 2],
+struct Pieces {
+  static constexpr int RUNS = L::NJ / L::PER, TS = L::PER >= 8 ? 1 : 8 / L::PER < RUNS ? 8 / L::PER : RUNS;
+  static constexpr int N = RUNS / TS, WORDS = L::PER * TS / 2, UNIT = L::PER / 2;
+  // channel of piece p of a lane
+  static __device__ __forceinline__ int channel(int p, int lane) { return (p * TS + (lane & (TS - 1))) * L::GV + (lane & ~(TS - 1)) * L::PER; }
+  static __device__ __forceinline__ void exchange(uint32_t (&x)[L::NJ / 2], int lane) {
+    if constexpr (TS > 1) swap<1, 0xB1>(x, lane);              // quad_perm [1,0,3,2]
+    if constexpr (TS > 2) swap<2, 0x4E>(x, lane);              // quad_perm [2,3,0,1]
+  }
+
+  // INT4: the largest magnitude of the group of piece p (before the exchange), in every lane that holds some of it
+  static __device__ __forceinline__ float group_maximum(const uint32_t (&x)[L::NJ / 2], int p) {
+    float a = 0.0f;
+#pragma unroll
+    for (int w = 0; w < WORDS; ++w) a = fmaxf(a, fmaxf(fabsf(bf16_lo(x[p * WORDS + w])), fabsf(bf16_hi(x[p * WORDS + w]))));
+    uint32_t u = as_u32(a);                                    // magnitudes order like their bits
+    u = max(u, dpp_u32<0x128>(u));                             // row_ror 8, 4, 2, 1: lanes TS apart
+    u = max(u, dpp_u32<0x124>(u));
+    if constexpr (TS <= 2) u = max(u, dpp_u32<0x122>(u));
+    if constexpr (TS == 1) u = max(u, dpp_u32<0x121>(u));
+    return as_f32(u);
+  }
+  // a piece's value in lane k of every TS
+  template <int K>
+  static __device__ __forceinline__ float of_lane(float v) {
+    if constexpr (TS == 4) return dpp_f32<K * 0x55>(v);        // quad_perm [k,k,k,k]
+    else if constexpr (TS == 2) return dpp_f32<K ? 0xF5 : 0xA0>(v);   // [0,0,2,2], [1,1,3,3]
+    else return v;
+  }
+
+ private:
+  template <int S, int CTRL>
+  static __device__ __forceinline__ void swap(uint32_t (&x)[L::NJ / 2], int lane) {
+    const bool upper = lane & S;
+#pragma unroll
+    for (int r = 0; r < RUNS; ++r) {
+      if (r & S) continue;
+#pragma unroll
+      for (int d = 0; d < UNIT; ++d) {
+        uint32_t &a = x[r * UNIT + d], &b = x[(r + S) * UNIT + d];
+        const uint32_t got = dpp_u32<CTRL>(upper ? a : b);
+        if (upper) a = got;
+        else b = got;
+      }
+    }
+  }
+};
+
+// a lane's pieces of a value
+template <class L>
+__device__ __forceinline__ void write_value(const KvView& cache, uint8_t* block, int t, int lane, bool ok, uint32_t (&x)[L::NJ / 2],
                                             float T, float encT) {
-  constexpr int PER = L::PER, RUNS = L::NJ / PER, PAIRS = PER / 2;       // runs of PER adjacent channels
+  typedef Pieces<L> P;
+  constexpr int PER = L::PER, RUNS = P::RUNS, PAIRS = PER / 2;
   if constexpr (L::FMT == kBf16) {
     if (ok)
 #pragma unroll
       for (int w = 0; w < L::NJ / 2; ++w) *reinterpret_cast<uint32_t*>(block + L::v_pair(t, lane, w)) = x[w];
   } else {
-    uint32_t codes[(L::NJ + 7) / 8] = {};
     float invs[RUNS];
-#pragma unroll
-    for (int g = 0; g < RUNS; ++g) {
+    if constexpr (L::FMT == kNvfp4) {
       float a = 0.0f;
 #pragma unroll
-      for (int j = 0; j < PAIRS; ++j) a = fmaxf(a, fmaxf(fabsf(bf16_lo(x[g * PAIRS + j])), fabsf(bf16_hi(x[g * PAIRS + j]))));
+      for (int j = 0; j < PAIRS; ++j) a = fmaxf(a, fmaxf(fabsf(bf16_lo(x[j])), fabsf(bf16_hi(x[j]))));
       constexpr int LPG = L::G / PER;                          // lanes of a group
-      a = group_max<LPG>(a);
-      if constexpr (L::FMT == kNvfp4) {
-        const Nv4Scale sc = nv4_scale(a, T, encT);
-        invs[g] = sc.inv;
-        if (ok && lane % LPG == 0) block[L::v_byte_at(t, lane / LPG)] = (uint8_t)sc.byte;
-      } else {
-        invs[g] = int_scale<kInt4>(a).inv;
-        if (ok && lane == 0) *reinterpret_cast<uint16_t*>(block + L::v_at + L::int_scale_at(t, g)) = (uint16_t)(as_u32(a) >> 16);
+      const Nv4Scale sc = nv4_scale(group_max<LPG>(a), T, encT);
+      invs[0] = sc.inv;
+      if (ok && lane % LPG == 0) block[L::v_byte_at(t, lane / LPG)] = (uint8_t)sc.byte;
+    } else {
+#pragma unroll
+      for (int p = 0; p < P::N; ++p) {
+        const float a = P::group_maximum(x, p), inv = int_scale<kInt4>(a).inv;
+        if (ok && lane < P::TS)
+          *reinterpret_cast<uint16_t*>(block + L::v_at + L::int_scale_at(t, p * P::TS + lane)) = (uint16_t)(as_u32(a) >> 16);
+        invs[p * P::TS] = P::template of_lane<0>(inv);
+        if constexpr (P::TS > 1) invs[p * P::TS + 1] = P::template of_lane<1>(inv);
+        if constexpr (P::TS > 2) {
+          invs[p * P::TS + 2] = P::template of_lane<2>(inv);
+          invs[p * P::TS + 3] = P::template of_lane<3>(inv);
+        }
       }
+      P::exchange(x, lane);
     }
+    uint32_t codes[(L::NJ + 7) / 8] = {};
 #pragma unroll
     for (int w = 0; w < L::NJ / 2; w += 4) {                   // eight channels (of heads of 64: four)
       uint32_t four[4] = {};
@@ -99,38 +159,6 @@ __device__ __forceinline__ void write_value(const KvView& cache, uint8_t* block,
         *reinterpret_cast<uint16_t*>(block + L::v_quad(t, lane, jq)) = (uint16_t)(codes[jq / 2] >> (jq % 2 * 16));
   }
 }
-
-// A lane's runs are PER channels, 4 bytes with groups of 32.  Rows are read and written in pieces of up to 16 bytes instead: TS
-// neighbouring lanes hold, before (after) an exchange, one run's channels of all of them each.  4-byte stores against this: reading
-// back 12 sequences up to 9001 tokens, INT4 groups of 32 in heads of 64, 24.6 against @@ us.
-template <class L>
-struct Pieces {
-  static constexpr int RUNS = L::NJ / L::PER, TS = L::PER >= 8 ? 1 : 8 / L::PER < RUNS ? 8 / L::PER : RUNS;
-  static constexpr int N = RUNS / TS, WORDS = L::PER * TS / 2, UNIT = L::PER / 2;
-  // channel of piece p of a lane
-  static __device__ __forceinline__ int channel(int p, int lane) { return (p * TS + (lane & (TS - 1))) * L::GV + (lane & ~(TS - 1)) * L::PER; }
-  static __device__ __forceinline__ void exchange(uint32_t (&x)[L::NJ / 2], int lane) {
-    if constexpr (TS > 1) swap<1, 0xB1>(x, lane);              // quad_perm [1,0,3,2]
-    if constexpr (TS > 2) swap<2, 0x4E>(x, lane);              // quad_perm [2,3,0,1]
-  }
-
- private:
-  template <int S, int CTRL>
-  static __device__ __forceinline__ void swap(uint32_t (&x)[L::NJ / 2], int lane) {
-    const bool upper = lane & S;
-#pragma unroll
-    for (int r = 0; r < RUNS; ++r) {
-      if (r & S) continue;
-#pragma unroll
-      for (int d = 0; d < UNIT; ++d) {
-        uint32_t &a = x[r * UNIT + d], &b = x[(r + S) * UNIT + d];
-        const uint32_t got = dpp_u32<CTRL>(upper ? a : b);
-        if (upper) a = got;
-        else b = got;
-      }
-    }
-  }
-};
 
 typedef uint32_t words4 __attribute__((ext_vector_type(4)));
 typedef uint32_t words2 __attribute__((ext_vector_type(2)));
@@ -216,7 +244,6 @@ __global__ __launch_bounds__(kKvThreads) void kv_write_kernel(KvView cache, KvRo
 #pragma unroll
   for (int i = 0; i < VI; ++i) {
     const bool ok = v_slot[i] >= 0 && v_slot[i] < n_slots;
-    Pieces<L>::exchange(vx[i], threadIdx.x % 16);
     write_value<L>(cache, kv_block<L>(cache, ok ? v_slot[i] : 0, head), (int)v_slot[i] & (kKvBlock - 1),
                    (threadIdx.x + i * kKvThreads) % 16, ok, vx[i], vT, vE);
   }
