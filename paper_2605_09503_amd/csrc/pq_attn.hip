@@ -477,8 +477,9 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L, NT>())) void attn_d
                                                                                                        int chunks, int longest, uint32_t part_bytes) {
   constexpr int NJ = L::NJ, NW = kAttnWaves;
   constexpr int kWorkers = kUnits * waves_of<L, NT>();                  // workgroups that share all blocks evenly: what is resident
-  __shared__ float4_t shared_acc[NW / 2][NT * NJ][64];
-  __shared__ float shared_ml[NW / 2][NT][2][64];
+  constexpr int JW = NJ / NW;                                          // instructions' outputs that a wave joins
+  __shared__ float4_t shared_acc[NW][NT * NJ][64];
+  __shared__ float2 shared_ml[NW][NT][16];
   __shared__ int last_one;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int per_head = a.q_heads / cache.heads, pairs = cache.heads * chunks;      // pairs of a sequence
@@ -606,142 +607,131 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L, NT>())) void attn_d
 #pragma unroll
     for (int ct = 0; ct < NT; ++ct) res.l[ct] = column_sum(res.l[ct]);
 
-    // join the waves: the upper half into the lower one, and so on
-    const int lane_now = renewed(lane), kq = lane_now >> 4, col = lane_now & 15;
-    auto put = [&](int at) {
+    // Join the waves: every wave takes JW instructions' outputs of all of them, and keeps them to the end.
+    const int lane_now = renewed(lane), kq = lane_now >> 4, col = lane_now & 15, j0 = wave * JW;
+    const int held = min(t1 - t0, NW);                                 // waves that hold anything
+    float m[NT], l[NT];
+    float4_t acc[NT][JW];
+    auto add = [&](int ct, float om, float ol, auto&& other) {
+      const float top = fmaxf(m[ct], om), f = __builtin_amdgcn_exp2f(m[ct] - top), g = __builtin_amdgcn_exp2f(om - top);
+      m[ct] = top;
+      l[ct] = l[ct] * f + ol * g;
+#pragma unroll
+      for (int j = 0; j < JW; ++j) acc[ct][j] = acc[ct][j] * f + other(j) * g;
+    };
+    auto clear = [&] {
 #pragma unroll
       for (int ct = 0; ct < NT; ++ct) {
+        m[ct] = kNoReference;
+        l[ct] = 0.0f;
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) shared_acc[at][ct * NJ + j][lane_now] = res.acc[ct][j];
-        shared_ml[at][ct][0][lane_now] = res.m[ct];
-        shared_ml[at][ct][1][lane_now] = res.l[ct];
+        for (int j = 0; j < JW; ++j) acc[ct][j] = (float4_t){0.0f, 0.0f, 0.0f, 0.0f};
       }
     };
-    auto take = [&](int at) {
+    __syncthreads();                                                   // reads of the last join are over
+    if (wave < held) {
 #pragma unroll
       for (int ct = 0; ct < NT; ++ct) {
-        const float om = shared_ml[at][ct][0][lane_now], ol = shared_ml[at][ct][1][lane_now];
-        const float m = fmaxf(res.m[ct], om);
-        const float f = __builtin_amdgcn_exp2f(res.m[ct] - m), g = __builtin_amdgcn_exp2f(om - m);
-        res.m[ct] = m;
-        res.l[ct] = res.l[ct] * f + ol * g;
+        if (ct * 16 + col >= count) continue;
 #pragma unroll
-        for (int j = 0; j < NJ; ++j) res.acc[ct][j] = res.acc[ct][j] * f + shared_acc[at][ct * NJ + j][lane_now] * g;
+        for (int j = 0; j < NJ; ++j) shared_acc[wave][ct * NJ + j][lane_now] = res.acc[ct][j];
+        if (kq == 0) shared_ml[wave][ct][col] = make_float2(res.m[ct], res.l[ct]);
       }
-    };
-    auto join_waves = [&](int held) {                                  // the first `held` hold something: uniform
+    }
+    __syncthreads();
+    clear();
+    for (int w = 0; w < held; ++w) {
 #pragma unroll
-      for (int half = NW / 2; half >= 1; half /= 2) {
-        if (held <= half) continue;
-        __syncthreads();                                               // reads of the last join are over
-        if (wave >= half && wave < 2 * half) put(wave - half);
-        __syncthreads();
-        if (wave < half) take(wave);
+      for (int ct = 0; ct < NT; ++ct) {
+        const float2 ml = shared_ml[w][ct][col];                       // columns past the queries: whatever lies there, not used
+        add(ct, ml.x, ml.y, [&](int j) { return shared_acc[w][ct * NJ + j0 + j][lane_now]; });
       }
-    };
-    join_waves(t1 - t0);
+    }
 
-    bool write = wave == 0;
     if (w_first != w_last) {                                           // a part of a pair: the last worker to finish joins them
       constexpr uint32_t kPart = part_bytes_of<L, NT>();
-      constexpr int kJoin = NJ < 8 ? NJ : 8;
-      if (wave == 0) {
-        const uint32_t part = part_slot(blockIdx.x, w_first) * kPart;
+      const uint32_t part = part_slot(blockIdx.x, w_first) * kPart;
 #pragma unroll
-        for (int ct = 0; ct < NT; ++ct) {
-          const int heads = min(16, count - ct * 16);
-          if (col < heads) {
-            const uint32_t at = part + ct * (NJ * 1024 + 256);
+      for (int ct = 0; ct < NT; ++ct) {
+        if (ct * 16 + col >= count) continue;
+        const uint32_t at = part + ct * (NJ * 1024 + 256);
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) put_part(parts, at + lane_now * 16 + j * 1024, res.acc[ct][j]);
-            if (kq == 0) put_part(parts, at + NJ * 1024 + col * 16, (float4_t){res.m[ct], res.l[ct], 0.0f, 0.0f});
-          }
-        }
-        // the stores have reached memory before the counter says so
-        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        if (lane_now == 0)
-          last_one = __hip_atomic_fetch_add(counters + w_first, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == w_last - w_first;
+        for (int j = 0; j < JW; ++j) put_part(parts, at + lane_now * 16 + (j0 + j) * 1024, acc[ct][j]);
+        if (wave == 0 && kq == 0) put_part(parts, at + NJ * 1024 + col * 16, (float4_t){m[ct], l[ct], 0.0f, 0.0f});
       }
+      // every wave's stores have reached memory before the counter says so
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();
+      if (threadIdx.x == 0)
+        last_one = __hip_atomic_fetch_add(counters + w_first, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == w_last - w_first;
       __syncthreads();
       if (!__builtin_amdgcn_readfirstlane(last_one)) continue;
-      // The waves take the parts in turn, and where a part has fewer than sixteen heads, so do the runs of lanes that would hold
-      // the others; the next part's loads are in flight while one is added.
+      if (threadIdx.x == 0) counters[w_first] = 0;                     // for the next call
+      // Where a part has fewer than sixteen heads, the lanes that would hold the others take further parts; the next parts' loads are
+      // in flight while some are added.  The order is the workers': the same bits whoever comes last.
+      constexpr int B = JW <= 2 ? 4 : 2;
+      clear();
 #pragma unroll
       for (int ct = 0; ct < NT; ++ct) {
         const int heads = min(16, count - ct * 16);
         const int run_log2 = heads > 8 ? 4 : heads > 4 ? 3 : heads > 2 ? 2 : heads > 1 ? 1 : 0, runs = 16 >> run_log2;
-        const int mine = col & ((1 << run_log2) - 1), step = NW * runs;
-        const int w0 = w_first + wave * runs + (col >> run_log2);
-        // eight instructions' outputs at a time: what two parts' loads leave room for
+        const int mine = col & ((1 << run_log2) - 1), first = w_first + (col >> run_log2);
+        struct Loaded {
+          float4_t ml[B], acc[B][JW];
+        };
+        auto fetch = [&](Loaded& x, int w) {
 #pragma unroll
-        for (int j0 = 0; j0 < NJ; j0 += kJoin) {
-          float m = kNoReference, l = 0.0f;
-          float4_t acc[kJoin];
+          for (int b = 0; b < B; ++b) {
+            const int worker = first + w + b * runs;
+            const bool ok = worker <= w_last && mine < heads;          // others read past the buffer: zeros
+            const uint32_t at = ok ? part_slot(worker, w_first) * kPart + ct * (NJ * 1024 + 256) : 0x80000000u;
+            x.ml[b] = get_part(parts, at + NJ * 1024 + mine * 16);
 #pragma unroll
-          for (int j = 0; j < kJoin; ++j) acc[j] = (float4_t){0.0f, 0.0f, 0.0f, 0.0f};
-          struct Loaded {
-            float4_t ml, acc[kJoin];
-          };
-          auto fetch = [&](Loaded& x, int w) {
-            const bool ok = w <= w_last && mine < heads;               // others read past the buffer: zeros
-            const uint32_t at = ok ? part_slot(w, w_first) * kPart + ct * (NJ * 1024 + 256) : 0x80000000u;
-            x.ml = get_part(parts, at + NJ * 1024 + mine * 16);
-#pragma unroll
-            for (int j = 0; j < kJoin; ++j) x.acc[j] = get_part(parts, at + (kq * 16 + mine) * 16 + (j0 + j) * 1024);
-            if (!ok) x.ml[0] = kNoReference;
-          };
-          auto add = [&](float om, float ol, auto&& other) {
-            const float top = fmaxf(m, om), f = __builtin_amdgcn_exp2f(m - top), g = __builtin_amdgcn_exp2f(om - top);
-            m = top;
-            l = l * f + ol * g;
-#pragma unroll
-            for (int j = 0; j < kJoin; ++j) acc[j] = acc[j] * f + other(j) * g;
-          };
-          Loaded x, y;
-          fetch(x, w0);
-#pragma unroll 1
-          for (int w = 0; w <= w_last - w_first; w += 2 * step) {      // uniform
-            fetch(y, w0 + w + step);
-            add(x.ml[0], x.ml[1], [&](int j) { return x.acc[j]; });
-            fetch(x, w0 + w + 2 * step);
-            add(y.ml[0], y.ml[1], [&](int j) { return y.acc[j]; });
+            for (int j = 0; j < JW; ++j) x.acc[b][j] = get_part(parts, at + (kq * 16 + mine) * 16 + (j0 + j) * 1024);
+            if (!ok) x.ml[b][0] = kNoReference;
           }
-#pragma unroll 1
-          for (int off = 1 << run_log2; off < 16; off <<= 1)
-            add(__shfl_xor(m, off), __shfl_xor(l, off), [&](int j) {
-              return (float4_t){__shfl_xor(acc[j][0], off), __shfl_xor(acc[j][1], off), __shfl_xor(acc[j][2], off), __shfl_xor(acc[j][3], off)};
-            });
-          res.m[ct] = m;
-          res.l[ct] = l;
+        };
+        auto add_all = [&](const Loaded& x) {
 #pragma unroll
-          for (int j = 0; j < kJoin; ++j) res.acc[ct][j0 + j] = acc[j];
+          for (int b = 0; b < B; ++b) add(ct, x.ml[b][0], x.ml[b][1], [&](int j) { return x.acc[b][j]; });
+        };
+        Loaded x, y;
+        fetch(x, 0);
+#pragma unroll 1
+        for (int w = 0; w <= w_last - w_first; w += 2 * B * runs) {    // uniform
+          fetch(y, w + B * runs);
+          add_all(x);
+          fetch(x, w + 2 * B * runs);
+          add_all(y);
         }
+#pragma unroll 1
+        for (int off = 1 << run_log2; off < 16; off <<= 1)
+          add(ct, __shfl_xor(m[ct], off), __shfl_xor(l[ct], off), [&](int j) {
+            const float4_t v = acc[ct][j];
+            return (float4_t){__shfl_xor(v[0], off), __shfl_xor(v[1], off), __shfl_xor(v[2], off), __shfl_xor(v[3], off)};
+          });
       }
-      join_waves(NW);
-      if (threadIdx.x == 0) counters[w_first] = 0;                     // for the next call
     }
-    if (write) {
 #pragma unroll
-      for (int ct = 0; ct < NT; ++ct) {
-        const int h = ct * 16 + col;
-        if (h >= count) continue;
-        const int64_t q_head = head * per_head + h0 + h;
-        const float inv = res.l[ct] > 0.0f ? 1.0f / res.l[ct] : 0.0f;
-        uint16_t* o = a.out + seq * a.out_ld + q_head * a.out_head;
+    for (int ct = 0; ct < NT; ++ct) {
+      const int h = ct * 16 + col;
+      if (h >= count) continue;
+      const int64_t q_head = head * per_head + h0 + h;
+      const float inv = l[ct] > 0.0f ? 1.0f / l[ct] : 0.0f;
+      uint16_t* o = a.out + seq * a.out_ld + q_head * a.out_head;
+      constexpr int RUN = L::PER < JW ? L::PER : JW;                   // adjacent channels of a lane and wave
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+      for (int r = 0; r < 4; ++r)
 #pragma unroll
-          for (int g = 0; g < NJ / L::PER; ++g) {
-            uint32_t two[L::PER / 2];
+        for (int g = 0; g < JW; g += RUN) {
+          uint16_t v[RUN];
 #pragma unroll
-            for (int j = 0; j < L::PER / 2; ++j)
-              two[j] = cvt_pk_bf16(res.acc[ct][g * L::PER + 2 * j][r] * inv * value_unit, res.acc[ct][g * L::PER + 2 * j + 1][r] * inv * value_unit);
-            __builtin_memcpy(__builtin_assume_aligned(o + g * L::GV + (kq * 4 + r) * L::PER, L::PER >= 8 ? 16 : L::PER * 2), two, L::PER * 2);
-          }
-        if (a.lse && kq == 0)
-          a.lse[(int64_t)seq * a.q_heads + q_head] = res.l[ct] > 0.0f ? (res.m[ct] + log2f(res.l[ct])) * 0.6931471805599453f : -INFINITY;
-      }
+          for (int j = 0; j < RUN; ++j) v[j] = (uint16_t)cvt_pk_bf16(acc[ct][g + j][r] * inv * value_unit, 0.0f);
+          __builtin_memcpy(__builtin_assume_aligned(o + L::v_channel(kq * 4 + r, j0 + g), RUN * 2), v, RUN * 2);
+        }
+      if (a.lse && kq == 0 && wave == 0)
+        a.lse[(int64_t)seq * a.q_heads + q_head] = l[ct] > 0.0f ? (m[ct] + log2f(l[ct])) * 0.6931471805599453f : -INFINITY;
     }
   }
 }
