@@ -465,11 +465,11 @@ template <class L, int NT>
 constexpr int waves_of() { return L::D == 256 && (NT == 2 || L::FMT == kBf16) ? 1 : 2; }
 // the part buffer is written and read by workgroups of different chiplets in one launch: past the caches that they do not share
 constexpr int kAgent = 16;               // sc1 of a buffer instruction
-__device__ __forceinline__ void put_part(__amdgpu_buffer_rsrc_t buf, uint32_t at, const float4_t& v) {
-  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4_t, v), buf, at, 0, kAgent);
+__device__ __forceinline__ void put_part(__amdgpu_buffer_rsrc_t buf, uint32_t at, uint32_t uniform, const float4_t& v) {
+  __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(uint4_t, v), buf, at, uniform, kAgent);
 }
-__device__ __forceinline__ float4_t get_part(__amdgpu_buffer_rsrc_t buf, uint32_t at) {
-  return __builtin_bit_cast(float4_t, __builtin_amdgcn_raw_buffer_load_b128(buf, at, 0, kAgent));
+__device__ __forceinline__ float4_t get_part(__amdgpu_buffer_rsrc_t buf, uint32_t at, uint32_t uniform) {
+  return __builtin_bit_cast(float4_t, __builtin_amdgcn_raw_buffer_load_b128(buf, at, uniform, kAgent));
 }
 
 template <class L, int NT>
@@ -593,10 +593,12 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L, NT>())) void attn_d
         float4_t s[NT][2];
         block_scores<L, NT>(keys, query, s);
         keys.load(block, lane);
+        __builtin_amdgcn_sched_barrier(0);                             // loads stay where they are: early
         const int token = (block0 + i * NW) * kKvBlock;
         const int lo = page_of(i) >= 0 ? max(0, len.first_token - token) : kKvBlock, hi = min(kKvBlock, len.end - token);
         block_outputs<L, NT>(values, s, query, res, lane, lo, hi);
         values.load(block, lane);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     if constexpr (L::FMT == kInt4)                                     // the odd codes came 16 times as large
@@ -654,10 +656,10 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L, NT>())) void attn_d
 #pragma unroll
       for (int ct = 0; ct < NT; ++ct) {
         if (ct * 16 + col >= count) continue;
-        const uint32_t at = part + ct * (NJ * 1024 + 256);
+        const uint32_t at = part + ct * (NJ * 1024 + 256), heads = min(16, count - ct * 16);
 #pragma unroll
-        for (int j = 0; j < JW; ++j) put_part(parts, at + lane_now * 16 + (j0 + j) * 1024, acc[ct][j]);
-        if (wave == 0 && kq == 0) put_part(parts, at + NJ * 1024 + col * 16, (float4_t){m[ct], l[ct], 0.0f, 0.0f});
+        for (int j = 0; j < JW; ++j) put_part(parts, (kq * heads + col) * 16, at + (j0 + j) * heads * 64, acc[ct][j]);
+        if (wave == 0 && kq == 0) put_part(parts, col * 16, at + NJ * 1024, (float4_t){m[ct], l[ct], 0.0f, 0.0f});
       }
       // every wave's stores have reached memory before the counter says so
       __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
@@ -686,11 +688,12 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L, NT>())) void attn_d
             const int worker = first + w + b * runs;
             const bool ok = worker <= w_last && mine < heads;          // others read past the buffer: zeros
             const uint32_t at = ok ? part_slot(worker, w_first) * kPart + ct * (NJ * 1024 + 256) : 0x80000000u;
-            x.ml[b] = get_part(parts, at + NJ * 1024 + mine * 16);
+            x.ml[b] = get_part(parts, at + mine * 16, NJ * 1024);
 #pragma unroll
-            for (int j = 0; j < JW; ++j) x.acc[b][j] = get_part(parts, at + (kq * 16 + mine) * 16 + (j0 + j) * 1024);
+            for (int j = 0; j < JW; ++j) x.acc[b][j] = get_part(parts, at + (kq * heads + mine) * 16, (j0 + j) * heads * 64);
             if (!ok) x.ml[b][0] = kNoReference;
           }
+          __builtin_amdgcn_sched_barrier(0);                           // the loads stay in front of what follows
         };
         auto add_all = [&](const Loaded& x) {
 #pragma unroll
