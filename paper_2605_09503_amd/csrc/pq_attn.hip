@@ -24,8 +24,10 @@ typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
 constexpr int kAttnWaves = 4;            // of a workgroup; they take a segment's blocks in turn
 constexpr int kUnits = 256;              // compute units
 constexpr int kMaxSplits = 1024;         // workgroups that may hold a part of a pair: counters in the workspace
-constexpr int kLeastBlocks = 4;          // of a workgroup
-constexpr int kMostParts = 64;           // of a pair: one workgroup joins them
+constexpr int kLeastBlocks = 4;          // of a workgroup that holds a part of a pair
+constexpr int kWholeBlocks = 20;         // a pair up to which stays whole: parts cost a join
+constexpr int kMostParts = 64;           // of a pair
+constexpr int kSoloBlocks = 8;          // see the plan
 
 constexpr float kNoReference = -1e38f;   // M before the first token
 // A weight with its value's scale stays below 2^15 (fp16); M follows when it would not, to 2^7 and less: seldom, so that neither the
@@ -149,61 +151,56 @@ struct Values : Part<L> {
 };
 
 // The queries as the second operand, and what else the loop keeps of a pair.
-template <class L, int NT>
+template <class L>
 struct Query {
-  uint4_t q[NT][L::NK];
-  float c[NT];                         // scores to powers of two
+  uint4_t q[L::NK];
+  float c;                         // scores to powers of two
 
   // count queries of the key head; columns past them are zeros
   __device__ __forceinline__ void fetch(const AttnCall& a, const uint16_t* __restrict__ src, int count, int lane) {
     const int kq = lane >> 4, n = lane & 15;
 #pragma unroll
-    for (int ct = 0; ct < NT; ++ct)
-#pragma unroll
-      for (int kk = 0; kk < L::NK; ++kk) {
-        q[ct][kk] = (uint4_t){0u, 0u, 0u, 0u};
-        if (ct * 16 + n < count) q[ct][kk] = *reinterpret_cast<const uint4_t*>(src + (ct * 16 + n) * a.q_head + kk * 32 + kq * 8);
-      }
+    for (int kk = 0; kk < L::NK; ++kk) {
+      q[kk] = (uint4_t){0u, 0u, 0u, 0u};
+      if (n < count) q[kk] = *reinterpret_cast<const uint4_t*>(src + (n) * a.q_head + kk * 32 + kq * 8);
+    }
   }
   __device__ __forceinline__ void convert(const AttnCall& a, float key_unit) {
     const uint32_t flip = a.scale < 0.0f ? 0x80008000u : 0u;           // c is positive: the sign goes to the query
     const float scale = fabsf(a.scale) * 1.4426950408889634f * key_unit;
+    uint4_t x[L::NK];
+    float top = 0.0f;
 #pragma unroll
-    for (int ct = 0; ct < NT; ++ct) {
-      uint4_t x[L::NK];
-      float top = 0.0f;
+    for (int kk = 0; kk < L::NK; ++kk) x[kk] = q[kk] ^ flip;
+    if constexpr (L::FMT == kBf16) {
+      c = scale;
 #pragma unroll
-      for (int kk = 0; kk < L::NK; ++kk) x[kk] = q[ct][kk] ^ flip;
-      if constexpr (L::FMT == kBf16) {
-        c[ct] = scale;
+      for (int kk = 0; kk < L::NK; ++kk) q[kk] = x[kk];
+    } else {
+      // fp16, the head's largest in [2^13, 2^14): bf16's eight bits stay exact down to 2^-27 of it
 #pragma unroll
-        for (int kk = 0; kk < L::NK; ++kk) q[ct][kk] = x[kk];
-      } else {
-        // fp16, the head's largest in [2^13, 2^14): bf16's eight bits stay exact down to 2^-27 of it
+      for (int kk = 0; kk < L::NK; ++kk)
 #pragma unroll
-        for (int kk = 0; kk < L::NK; ++kk)
+        for (int w = 0; w < 4; ++w) top = fmaxf(top, fmaxf(fabsf(bf16_lo(x[kk][w])), fabsf(bf16_hi(x[kk][w]))));
+      const int e = max((int)(as_u32(column_max(top)) >> 23) - 127, -100);
+      const float down = as_f32((uint32_t)(127 + 13 - e) << 23);
+      c = ldexpf(scale, e - 13);
 #pragma unroll
-          for (int w = 0; w < 4; ++w) top = fmaxf(top, fmaxf(fabsf(bf16_lo(x[kk][w])), fabsf(bf16_hi(x[kk][w]))));
-        const int e = max((int)(as_u32(column_max(top)) >> 23) - 127, -100);
-        const float down = as_f32((uint32_t)(127 + 13 - e) << 23);
-        c[ct] = ldexpf(scale, e - 13);
+      for (int kk = 0; kk < L::NK; ++kk) {
+        float f[8];
 #pragma unroll
-        for (int kk = 0; kk < L::NK; ++kk) {
-          float f[8];
+        for (int w = 0; w < 4; ++w) {
+          f[2 * w] = bf16_lo(x[kk][w]) * down;
+          f[2 * w + 1] = bf16_hi(x[kk][w]) * down;
+        }
+        if constexpr (L::FMT == kNvfp4) {
 #pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            f[2 * w] = bf16_lo(x[kk][w]) * down;
-            f[2 * w + 1] = bf16_hi(x[kk][w]) * down;
-          }
-          if constexpr (L::FMT == kNvfp4) {
+          for (int w = 0; w < 4; ++w) q[kk][w] = cvt_pk_f16(f[2 * w], f[2 * w + 1]);
+        } else {
 #pragma unroll
-            for (int w = 0; w < 4; ++w) q[ct][kk][w] = cvt_pk_f16(f[2 * w], f[2 * w + 1]);
-          } else {
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {                              // the order of IntCodes, and its factor
-              const float m = w & 1 ? 0.0625f : 1.0f;
-              q[ct][kk][w] = cvt_pk_f16(f[w] * m, f[w + 4] * m);
-            }
+          for (int w = 0; w < 4; ++w) {                              // the order of IntCodes, and its factor
+            const float m = w & 1 ? 0.0625f : 1.0f;
+            q[kk][w] = cvt_pk_f16(f[w] * m, f[w + 4] * m);
           }
         }
       }
@@ -212,33 +209,26 @@ struct Query {
 };
 
 // The running result of a wave: O[channel n = 4 q + r of instruction j, head] and the sums of the weights, both times 2^M.
-template <class L, int NT>
+template <class L>
 struct Result {
-  float4_t acc[NT][L::NJ];
-  float m[NT], l[NT];
+  float4_t acc[L::NJ];
+  float m, l;
 
   __device__ __forceinline__ void clear() {
+    m = kNoReference;
+    l = 0.0f;
 #pragma unroll
-    for (int ct = 0; ct < NT; ++ct) {
-      m[ct] = kNoReference;
-      l[ct] = 0.0f;
-#pragma unroll
-      for (int j = 0; j < L::NJ; ++j) acc[ct][j] = (float4_t){0.0f, 0.0f, 0.0f, 0.0f};
-    }
+    for (int j = 0; j < L::NJ; ++j) acc[j] = (float4_t){0.0f, 0.0f, 0.0f, 0.0f};
   }
 };
 
 // scores of a block's tokens, 16 s + 4 q + r in s_[.][s][r]
-template <class L, int NT>
-__device__ __forceinline__ void block_scores(const Keys<L>& x, const Query<L, NT>& query, float4_t (&s_)[NT][2]) {
+template <class L>
+__device__ __forceinline__ void block_scores(const Keys<L>& x, const Query<L>& query, float4_t (&s_)[2]) {
   constexpr IntC<L::FMT == kBf16> kType{};
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
-    float4_t sum[NT][L::NG];
-#pragma unroll
-    for (int ct = 0; ct < NT; ++ct)
-#pragma unroll
-      for (int g = 0; g < (L::FMT == kInt4 ? L::NG : 1); ++g) sum[ct][g] = (float4_t){0.0f, 0.0f, 0.0f, 0.0f};
+    float4_t sum;
 #pragma unroll
     for (int kk = 0; kk < L::NK; ++kk) {
       const int e = s * L::NK + kk;
@@ -262,30 +252,24 @@ __device__ __forceinline__ void block_scores(const Keys<L>& x, const Query<L, NT
           a[3] = h2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d, 1.0f, 3) * sc);
         }
       }
-      const int g = L::FMT == kInt4 ? kk * 32 / (L::G ? L::G : 1) : 0;
-#pragma unroll
-      for (int ct = 0; ct < NT; ++ct) sum[ct][g] = mfma(a, query.q[ct][kk], sum[ct][g], kType);
-    }
-#pragma unroll
-    for (int ct = 0; ct < NT; ++ct) {
+      // INT4: a group's sum is scaled as soon as it is there
+      constexpr int KG = L::FMT == kInt4 ? L::G / 32 : L::NK;
+      sum = mfma(a, query.q[kk], kk % KG ? sum : (float4_t){0.0f, 0.0f, 0.0f, 0.0f}, kType);
+      if (kk % KG != KG - 1) continue;
       if constexpr (L::FMT == kInt4) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          float v = x.h(s, r, 0) * sum[ct][0][r];
-#pragma unroll
-          for (int g = 1; g < L::NG; ++g) v = __builtin_fmaf(x.h(s, r, g), sum[ct][g][r], v);
-          s_[ct][s][r] = v;
-        }
+        for (int r = 0; r < 4; ++r)
+          s_[s][r] = kk / KG ? __builtin_fmaf(x.h(s, r, kk / KG), sum[r], s_[s][r]) : x.h(s, r, 0) * sum[r];
       } else {
-        s_[ct][s] = sum[ct][0];
+        s_[s] = sum;
       }
     }
   }
 }
 
 // their weights, and the values' sums; tokens outside [lo, hi) are left out
-template <class L, int NT>
-__device__ __forceinline__ void block_outputs(Values<L>& x, float4_t (&s_)[NT][2], const Query<L, NT>& query, Result<L, NT>& out, int lane,
+template <class L>
+__device__ __forceinline__ void block_outputs(Values<L>& x, float4_t (&s_)[2], const Query<L>& query, Result<L>& out, int lane,
                                               int lo, int hi) {
   constexpr IntC<L::FMT == kBf16> kType{};
   const int kq = lane >> 4;
@@ -303,69 +287,62 @@ __device__ __forceinline__ void block_outputs(Values<L>& x, float4_t (&s_)[NT][2
     eb = (float)(max((int)max(top.x, top.y) >> 7, 127 - 80) - 126);
   }
   // weights
-  float p[NT][2][4];
-#pragma unroll
-  for (int ct = 0; ct < NT; ++ct) {
-    if (__builtin_expect(part, 0)) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int t = (i >> 2) * 16 + kq * 4 + (i & 3);
-        s_[ct][i >> 2][i & 3] = ((t < lo) | (t >= hi)) ? -1e38f : s_[ct][i >> 2][i & 3];
-      }
-    }
-    float top = fmaxf(s_[ct][0][0], s_[ct][0][1]);
-#pragma unroll
-    for (int i = 2; i < 8; ++i) top = fmaxf(top, s_[ct][i >> 2][i & 3]);
-    const float bound = top * query.c[ct] + eb;
-    if (__builtin_expect(__any(bound > out.m[ct] + kHeadroom), 0)) {
-      const float b = column_max(bound);
-      const float m = b > out.m[ct] + kHeadroom ? b - kStart : out.m[ct];
-      const float f = __builtin_amdgcn_exp2f(out.m[ct] - m);
-      out.m[ct] = m;
-      out.l[ct] *= f;
-#pragma unroll
-      for (int j = 0; j < L::NJ; ++j) out.acc[ct][j] *= f;
-    }
+  float p[2][4];
+  if (__builtin_expect(part, 0)) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s_[ct][i >> 2][i & 3], query.c[ct], -out.m[ct]));
-      if (__builtin_expect(part, 0)) {
-        const int t = (i >> 2) * 16 + kq * 4 + (i & 3);
-        w = ((t < lo) | (t >= hi)) ? 0.0f : w;
-      }
-      p[ct][i >> 2][i & 3] = w;
-      out.l[ct] += w;
+      const int t = (i >> 2) * 16 + kq * 4 + (i & 3);
+      s_[i >> 2][i & 3] = ((t < lo) | (t >= hi)) ? -1e38f : s_[i >> 2][i & 3];
     }
+  }
+  float top = fmaxf(s_[0][0], s_[0][1]);
+#pragma unroll
+  for (int i = 2; i < 8; ++i) top = fmaxf(top, s_[i >> 2][i & 3]);
+  const float bound = top * query.c + eb;
+  if (__builtin_expect(__any(bound > out.m + kHeadroom), 0)) {
+    const float b = column_max(bound);
+    const float m = b > out.m + kHeadroom ? b - kStart : out.m;
+    const float f = __builtin_amdgcn_exp2f(out.m - m);
+    out.m = m;
+    out.l *= f;
+#pragma unroll
+    for (int j = 0; j < L::NJ; ++j) out.acc[j] *= f;
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float w = __builtin_amdgcn_exp2f(__builtin_fmaf(s_[i >> 2][i & 3], query.c, -out.m));
+    if (__builtin_expect(part, 0)) {
+      const int t = (i >> 2) * 16 + kq * 4 + (i & 3);
+      w = ((t < lo) | (t >= hi)) ? 0.0f : w;
+    }
+    p[i >> 2][i & 3] = w;
+    out.l += w;
   }
   // outputs
   if constexpr (L::FMT == kInt4) {
-    uint4_t w[NT][L::NG];
 #pragma unroll
-    for (int ct = 0; ct < NT; ++ct)
-#pragma unroll
-      for (int g = 0; g < L::NG; ++g)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int s = i >> 1, r = (i & 1) * 2;
-          w[ct][g][i] = cvt_pk_f16(p[ct][s][r] * x.h(s, r, g), p[ct][s][r + 1] * x.h(s, r + 1, g));
-        }
-#pragma unroll
-    for (int j = 0; j < L::NJ; ++j) {
-      uint4_t a;
+    for (int g = 0; g < L::NG; ++g) {
+      uint4_t w;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int f = i * L::NQ + j / 4;
-        a[i] = IntCodes(x.c[f >> 2][f & 3]).pair(j & 3);
+        const int s = i >> 1, r = (i & 1) * 2;
+        w[i] = cvt_pk_f16(p[s][r] * x.h(s, r, g), p[s][r + 1] * x.h(s, r + 1, g));
       }
 #pragma unroll
-      for (int ct = 0; ct < NT; ++ct) out.acc[ct][j] = mfma(a, w[ct][j / L::PER], out.acc[ct][j], kType);
+      for (int j = g * L::PER; j < (g + 1) * L::PER; ++j) {
+        uint4_t a;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int f = i * L::NQ + j / 4;
+          a[i] = IntCodes(x.c[f >> 2][f & 3]).pair(j & 3);
+        }
+        out.acc[j] = mfma(a, w, out.acc[j], kType);
+      }
     }
   } else if constexpr (L::FMT == kNvfp4) {
-    uint4_t w[NT];
+    uint4_t w;
 #pragma unroll
-    for (int ct = 0; ct < NT; ++ct)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[ct][i] = cvt_pk_f16(p[ct][i >> 1][i & 1], p[ct][i >> 1][(i & 1) + 2]);
+    for (int i = 0; i < 4; ++i) w[i] = cvt_pk_f16(p[i >> 1][i & 1], p[i >> 1][(i & 1) + 2]);
     half2_t sc[4];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -390,8 +367,7 @@ __device__ __forceinline__ void block_outputs(Values<L>& x, float4_t (&s_)[NT][2
           a[2 * s] = h2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d[s], 1.0f, B) * sc[2 * s]);
           a[2 * s + 1] = h2_bits(__builtin_amdgcn_cvt_scalef32_pk_f16_fp4(d[s], 1.0f, B + 2) * sc[2 * s + 1]);
         }
-#pragma unroll
-        for (int ct = 0; ct < NT; ++ct) out.acc[ct][j] = mfma(a, w[ct], out.acc[ct][j], kType);
+        out.acc[j] = mfma(a, w, out.acc[j], kType);
       };
       channel(even, IntC<0>{}, jq * 4);
       channel(odd, IntC<0>{}, jq * 4 + 1);
@@ -400,16 +376,14 @@ __device__ __forceinline__ void block_outputs(Values<L>& x, float4_t (&s_)[NT][2
     }
   } else {
     // the weights as two bf16 each, 16 bits: one would add as much error as the output's own rounding
-    uint4_t w[NT][2];
+    uint4_t w[2];
 #pragma unroll
-    for (int ct = 0; ct < NT; ++ct)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float p0 = p[ct][i >> 1][(i & 1) * 2], p1 = p[ct][i >> 1][(i & 1) * 2 + 1];
-        const uint32_t two = cvt_pk_bf16(p0, p1);
-        w[ct][0][i] = two;
-        w[ct][1][i] = cvt_pk_bf16(p0 - bf16_lo(two), p1 - bf16_hi(two));
-      }
+    for (int i = 0; i < 4; ++i) {
+      const float p0 = p[i >> 1][(i & 1) * 2], p1 = p[i >> 1][(i & 1) * 2 + 1];
+      const uint32_t two = cvt_pk_bf16(p0, p1);
+      w[0][i] = two;
+      w[1][i] = cvt_pk_bf16(p0 - bf16_lo(two), p1 - bf16_hi(two));
+    }
 #pragma unroll
     for (int j = 0; j < L::NJ; ++j) {
       uint4_t a;
@@ -418,11 +392,8 @@ __device__ __forceinline__ void block_outputs(Values<L>& x, float4_t (&s_)[NT][2
         const int f0 = (i * 2) * (L::D / 32) + j / 2, f1 = f0 + L::D / 32;
         a[i] = __builtin_amdgcn_perm(x.c[f1 >> 2][f1 & 3], x.c[f0 >> 2][f0 & 3], j & 1 ? 0x07060302u : 0x05040100u);
       }
-#pragma unroll
-      for (int ct = 0; ct < NT; ++ct) {
-        out.acc[ct][j] = mfma(a, w[ct][0], out.acc[ct][j], kType);
-        out.acc[ct][j] = mfma(a, w[ct][1], out.acc[ct][j], kType);
-      }
+      out.acc[j] = mfma(a, w[0], out.acc[j], kType);
+      out.acc[j] = mfma(a, w[1], out.acc[j], kType);
     }
   }
 }
@@ -454,15 +425,15 @@ __device__ __forceinline__ int wave_scan(int v) {
 __device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
 
 // a part's outputs, then (M, l) of its heads
-template <class L, int NT>
-constexpr uint32_t part_bytes_of() { return NT * (L::NJ * 1024 + 256); }
+template <class L>
+constexpr uint32_t part_bytes_of() { return L::NJ * 1024 + 256; }
 
 // the part of a pair that worker w holds, first the one that began it
 __device__ __forceinline__ int part_slot(int w, int w_first) { return w == w_first ? 2 * w + 1 : 2 * w; }
 
 // Waves a SIMD, and with them the registers of a wave.
-template <class L, int NT>
-constexpr int waves_of() { return L::D == 256 && (NT == 2 || L::FMT == kBf16) ? 1 : 2; }
+template <class L>
+constexpr int waves_of() { return L::D == 256 && (L::FMT == kBf16 || L::G == 32) ? 1 : 2; }
 // the part buffer is written and read by workgroups of different chiplets in one launch: past the caches that they do not share
 constexpr int kAgent = 16;               // sc1 of a buffer instruction
 __device__ __forceinline__ void put_part(__amdgpu_buffer_rsrc_t buf, uint32_t at, uint32_t uniform, const float4_t& v) {
@@ -472,17 +443,18 @@ __device__ __forceinline__ float4_t get_part(__amdgpu_buffer_rsrc_t buf, uint32_
   return __builtin_bit_cast(float4_t, __builtin_amdgcn_raw_buffer_load_b128(buf, at, uniform, kAgent));
 }
 
-template <class L, int NT>
-__global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L, NT>())) void attn_decode_kernel(KvView cache, AttnCall a,
+template <class L>
+__global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L>())) void attn_decode_kernel(KvView cache, AttnCall a,
                                                                                                        int chunks, int longest, uint32_t part_bytes) {
   constexpr int NJ = L::NJ, NW = kAttnWaves;
-  constexpr int kWorkers = kUnits * waves_of<L, NT>();                  // workgroups that share all blocks evenly: what is resident
+  constexpr int kWorkers = kUnits * waves_of<L>();                  // workgroups that share all blocks evenly: what is resident
   constexpr int JW = NJ / NW;                                          // instructions' outputs that a wave joins
-  __shared__ float4_t shared_acc[NW][NT * NJ][64];
-  __shared__ float2 shared_ml[NW][NT][16];
+  __shared__ float4_t shared_acc[NW][NJ][64];
+  __shared__ float2 shared_ml[NW][16];
   __shared__ int last_one;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int per_head = a.q_heads / cache.heads, pairs = cache.heads * chunks;      // pairs of a sequence
+  const int width = (per_head + chunks - 1) / chunks;                  // queries of a pair
   int* counters = static_cast<int*>(a.ws);
   const auto parts = __builtin_amdgcn_make_buffer_rsrc(static_cast<uint8_t*>(a.ws) + PQ_ATTN_DECODE_ZERO_BYTES, 0, part_bytes, 0x00027000);
   const float key_unit = L::FMT == kNvfp4 ? *cache.k_ts : L::FMT == kInt4 ? 16777216.0f / 7.0f : 1.0f;
@@ -494,14 +466,15 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L, NT>())) void attn_d
   auto blocks_at = [&](int b0) { return b0 + lane < a.seqs ? lengths_of(a, length_at(b0)).n : 0; };
   int blocks = 0;
   for (int b0 = 0; b0 < a.seqs; b0 += 64) blocks += last_lane(wave_scan(blocks_at(b0)));
+  auto parts_of = [&](int n, int per) { return n <= kWholeBlocks ? 1 : (n + per - 1) / per; };
   auto items_of = [&](int per) {                                       // workers of padded pairs
     int items = 0;
-    for (int b0 = 0; b0 < a.seqs; b0 += 64) items += last_lane(wave_scan((blocks_at(b0) + per - 1) / per));
+    for (int b0 = 0; b0 < a.seqs; b0 += 64) items += last_lane(wave_scan(b0 + lane < a.seqs ? parts_of(blocks_at(b0), per) : 0));
     return items * pairs;
   };
   const int even = max(max((blocks * pairs + kWorkers - 1) / kWorkers, kLeastBlocks), (longest + kMostParts - 1) / kMostParts);
   int per = even;
-  bool padded = false;
+  bool padded = false, solo = false;
   if (a.seqs * pairs <= kWorkers) {                                    // up to half as much again for a pair a worker
 #pragma unroll 1
     for (int more = 0; more <= 4 && !padded; ++more) {
@@ -511,20 +484,23 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L, NT>())) void attn_d
   }
   if (!padded) {
     per = even;
-    if (a.seqs * pairs >= 4 * kWorkers) {                              // pairs enough: one a worker
+    // many pairs, or short ones: a wave each, without a join
+    solo = a.seqs * pairs >= kWorkers && (int64_t)longest * kWorkers <= (int64_t)kSoloBlocks * a.seqs * pairs;
+    if (solo || a.seqs * pairs >= 4 * kWorkers) {                      // pairs enough: one a worker
       per = longest;
       padded = true;
     } else if (even < 16) {
       padded = items_of(per) <= min(kMaxSplits, (int)gridDim.x);
     }
   }
-  auto counted = [&](int n) { return padded ? (n + per - 1) / per * per : n; };
+  const int worker = solo ? blockIdx.x * NW + wave : blockIdx.x;
+  auto counted = [&](int n) { return padded ? (per == longest ? per : parts_of(n, per) * per) : n; };
 
-  const int u_begin = blockIdx.x * per, u_end = u_begin + per;         // seqs * pairs * blocks fit 31 bits
+  const int u_begin = worker * per, u_end = u_begin + per;             // seqs * pairs * blocks fit 31 bits
   int u = u_begin, base = 0, b = 0;                                    // the sequence that holds block u, its first block `base`
   for (int b0 = 0;; b0 += 64) {
-    if (b0 >= a.seqs) return;                                          // workgroups past the last block
-    const int n = counted(blocks_at(b0)) * pairs, incl = wave_scan(n);
+    if (b0 >= a.seqs) return;                                          // workers past the last block
+    const int n = b0 + lane < a.seqs ? counted(blocks_at(b0)) * pairs : 0, incl = wave_scan(n);
     const uint64_t past = __ballot(base + incl > u);
     if (past) {
       const int at = __builtin_ctzll(past);
@@ -542,7 +518,7 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L, NT>())) void attn_d
     int t0 = t_at, t1 = min(np, t_at + u_end - u);
     int w_first = __builtin_amdgcn_readfirstlane(pair_base / per), w_last = __builtin_amdgcn_readfirstlane((pair_base + np - 1) / per);
     if (padded) {                                                      // even parts
-      const int k = blockIdx.x - w_first, of = w_last - w_first + 1, each = __builtin_amdgcn_readfirstlane(len.n / of), more = len.n - each * of;
+      const int k = worker - w_first, of = w_last - w_first + 1, each = __builtin_amdgcn_readfirstlane(len.n / of), more = len.n - each * of;
       t0 = k * each + min(k, more);
       t1 = t0 + each + (k < more);
     }
@@ -552,14 +528,16 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L, NT>())) void attn_d
       ++b;
     }
 
-    const int head = __builtin_amdgcn_readfirstlane(pair / chunks), h0 = (pair - head * chunks) * 16 * NT;
-    const int count = min(per_head - h0, 16 * NT);
+    const int head = __builtin_amdgcn_readfirstlane(pair / chunks), h0 = (pair - head * chunks) * width;
+    const int count = min(per_head - h0, width);
     const int32_t* table = a.table + seq * a.table_ld;
-    const int n_mine = (t1 - t0 - wave + NW - 1) / NW, block0 = len.first + t0 + wave;
+    // this wave's blocks: all in solo, else every NW-th
+    const int stride = solo ? 1 : NW, block0 = len.first + t0 + (solo ? 0 : wave);
+    const int n_mine = solo ? t1 - t0 : (t1 - t0 - wave + NW - 1) / NW;
     // pages of this wave's blocks, a lane each, 64 blocks in a register: of even and odd runs of 64
     int pages[2];
     auto fetch_pages = [&](int run) {
-      const int token = (block0 + (run * 64 + lane) * NW) * kKvBlock;
+      const int token = (block0 + (run * 64 + lane) * stride) * kKvBlock;
       int p = -1;
       if (run * 64 + lane < n_mine && token < len.end) p = table[token >> cache.page_log2];
       return p < cache.pages ? p : -1;
@@ -569,12 +547,12 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L, NT>())) void attn_d
       return i & 64 ? odd : even;
     };
     auto address = [&](int i) {
-      const int page = max(page_of(i), 0), in_page = (block0 + i * NW) & ((1 << (cache.page_log2 - 5)) - 1);
+      const int page = max(page_of(i), 0), in_page = (block0 + i * stride) & ((1 << (cache.page_log2 - 5)) - 1);
       return cache.data + ((((int64_t)page * cache.heads + head) << (cache.page_log2 - 5)) + in_page) * L::bytes;
     };
-    Query<L, NT> query;
+    Query<L> query;
     query.fetch(a, a.q + seq * a.q_ld + (int64_t)(head * per_head + h0) * a.q_head, count, lane);
-    Result<L, NT> res;
+    Result<L> res;
     res.clear();
     if (n_mine > 0) {
       Keys<L> keys;
@@ -590,161 +568,169 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L, NT>())) void attn_d
         // the next block's keys replace this one's as soon as the scores are there, its values the same; past the end the last
         // block once more, so that the loads in flight are always as many
         block = address(min(i + 1, n_mine - 1));
-        float4_t s[NT][2];
-        block_scores<L, NT>(keys, query, s);
+        float4_t s[2];
+        block_scores<L>(keys, query, s);
         keys.load(block, lane);
         __builtin_amdgcn_sched_barrier(0);                             // loads stay where they are: early
-        const int token = (block0 + i * NW) * kKvBlock;
+        const int token = (block0 + i * stride) * kKvBlock;
         const int lo = page_of(i) >= 0 ? max(0, len.first_token - token) : kKvBlock, hi = min(kKvBlock, len.end - token);
-        block_outputs<L, NT>(values, s, query, res, lane, lo, hi);
+        block_outputs<L>(values, s, query, res, lane, lo, hi);
         values.load(block, lane);
         __builtin_amdgcn_sched_barrier(0);
       }
     }
     if constexpr (L::FMT == kInt4)                                     // the odd codes came 16 times as large
 #pragma unroll
-      for (int ct = 0; ct < NT; ++ct)
-#pragma unroll
-        for (int j = 1; j < NJ; j += 2) res.acc[ct][j] *= 0.0625f;
-#pragma unroll
-    for (int ct = 0; ct < NT; ++ct) res.l[ct] = column_sum(res.l[ct]);
+      for (int j = 1; j < NJ; j += 2) res.acc[j] *= 0.0625f;
+    res.l = column_sum(res.l);
 
-    // Join the waves: every wave takes JW instructions' outputs of all of them, and keeps them to the end.
-    const int lane_now = renewed(lane), kq = lane_now >> 4, col = lane_now & 15, j0 = wave * JW;
-    const int held = min(t1 - t0, NW);                                 // waves that hold anything
-    float m[NT], l[NT];
-    float4_t acc[NT][JW];
-    auto add = [&](int ct, float om, float ol, auto&& other) {
-      const float top = fmaxf(m[ct], om), f = __builtin_amdgcn_exp2f(m[ct] - top), g = __builtin_amdgcn_exp2f(om - top);
-      m[ct] = top;
-      l[ct] = l[ct] * f + ol * g;
+    const int lane_now = renewed(lane), kq = lane_now >> 4, col = lane_now & 15;
+    float m, l;
+    float4_t acc[JW];                                              // JW instructions' outputs at a time
+    auto add = [&](float om, float ol, auto&& other) {
+      const float top = fmaxf(m, om), f = __builtin_amdgcn_exp2f(m - top), g = __builtin_amdgcn_exp2f(om - top);
+      m = top;
+      l = l * f + ol * g;
 #pragma unroll
-      for (int j = 0; j < JW; ++j) acc[ct][j] = acc[ct][j] * f + other(j) * g;
+      for (int j = 0; j < JW; ++j) acc[j] = acc[j] * f + other(j) * g;
     };
     auto clear = [&] {
+      m = kNoReference;
+      l = 0.0f;
 #pragma unroll
-      for (int ct = 0; ct < NT; ++ct) {
-        m[ct] = kNoReference;
-        l[ct] = 0.0f;
-#pragma unroll
-        for (int j = 0; j < JW; ++j) acc[ct][j] = (float4_t){0.0f, 0.0f, 0.0f, 0.0f};
-      }
+      for (int j = 0; j < JW; ++j) acc[j] = (float4_t){0.0f, 0.0f, 0.0f, 0.0f};
     };
-    __syncthreads();                                                   // reads of the last join are over
-    if (wave < held) {
+    auto put_wave = [&] {
+      if (col >= count) return;
 #pragma unroll
-      for (int ct = 0; ct < NT; ++ct) {
-        if (ct * 16 + col >= count) continue;
-#pragma unroll
-        for (int j = 0; j < NJ; ++j) shared_acc[wave][ct * NJ + j][lane_now] = res.acc[ct][j];
-        if (kq == 0) shared_ml[wave][ct][col] = make_float2(res.m[ct], res.l[ct]);
-      }
-    }
-    __syncthreads();
-    clear();
-    for (int w = 0; w < held; ++w) {
-#pragma unroll
-      for (int ct = 0; ct < NT; ++ct) {
-        const float2 ml = shared_ml[w][ct][col];                       // columns past the queries: whatever lies there, not used
-        add(ct, ml.x, ml.y, [&](int j) { return shared_acc[w][ct * NJ + j0 + j][lane_now]; });
-      }
-    }
-
-    if (w_first != w_last) {                                           // a part of a pair: the last worker to finish joins them
-      constexpr uint32_t kPart = part_bytes_of<L, NT>();
-      const uint32_t part = part_slot(blockIdx.x, w_first) * kPart;
-#pragma unroll
-      for (int ct = 0; ct < NT; ++ct) {
-        if (ct * 16 + col >= count) continue;
-        const uint32_t at = part + ct * (NJ * 1024 + 256), heads = min(16, count - ct * 16);
-#pragma unroll
-        for (int j = 0; j < JW; ++j) put_part(parts, (kq * heads + col) * 16, at + (j0 + j) * heads * 64, acc[ct][j]);
-        if (wave == 0 && kq == 0) put_part(parts, col * 16, at + NJ * 1024, (float4_t){m[ct], l[ct], 0.0f, 0.0f});
-      }
-      // every wave's stores have reached memory before the counter says so
-      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
-      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-      __syncthreads();
-      if (threadIdx.x == 0)
-        last_one = __hip_atomic_fetch_add(counters + w_first, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == w_last - w_first;
-      __syncthreads();
-      if (!__builtin_amdgcn_readfirstlane(last_one)) continue;
-      if (threadIdx.x == 0) counters[w_first] = 0;                     // for the next call
-      // Where a part has fewer than sixteen heads, the lanes that would hold the others take further parts; the next parts' loads are
-      // in flight while some are added.  The order is the workers': the same bits whoever comes last.
-      constexpr int B = JW <= 2 ? 4 : 2;
-      clear();
-#pragma unroll
-      for (int ct = 0; ct < NT; ++ct) {
-        const int heads = min(16, count - ct * 16);
-        const int run_log2 = heads > 8 ? 4 : heads > 4 ? 3 : heads > 2 ? 2 : heads > 1 ? 1 : 0, runs = 16 >> run_log2;
-        const int mine = col & ((1 << run_log2) - 1), first = w_first + (col >> run_log2);
-        struct Loaded {
-          float4_t ml[B], acc[B][JW];
-        };
-        auto fetch = [&](Loaded& x, int w) {
-#pragma unroll
-          for (int b = 0; b < B; ++b) {
-            const int worker = first + w + b * runs;
-            const bool ok = worker <= w_last && mine < heads;          // others read past the buffer: zeros
-            const uint32_t at = ok ? part_slot(worker, w_first) * kPart + ct * (NJ * 1024 + 256) : 0x80000000u;
-            x.ml[b] = get_part(parts, at + mine * 16, NJ * 1024);
-#pragma unroll
-            for (int j = 0; j < JW; ++j) x.acc[b][j] = get_part(parts, at + (kq * heads + mine) * 16, (j0 + j) * heads * 64);
-            if (!ok) x.ml[b][0] = kNoReference;
-          }
-          __builtin_amdgcn_sched_barrier(0);                           // the loads stay in front of what follows
-        };
-        auto add_all = [&](const Loaded& x) {
-#pragma unroll
-          for (int b = 0; b < B; ++b) add(ct, x.ml[b][0], x.ml[b][1], [&](int j) { return x.acc[b][j]; });
-        };
-        Loaded x, y;
-        fetch(x, 0);
-#pragma unroll 1
-        for (int w = 0; w <= w_last - w_first; w += 2 * B * runs) {    // uniform
-          fetch(y, w + B * runs);
-          add_all(x);
-          fetch(x, w + 2 * B * runs);
-          add_all(y);
-        }
-#pragma unroll 1
-        for (int off = 1 << run_log2; off < 16; off <<= 1)
-          add(ct, __shfl_xor(m[ct], off), __shfl_xor(l[ct], off), [&](int j) {
-            const float4_t v = acc[ct][j];
-            return (float4_t){__shfl_xor(v[0], off), __shfl_xor(v[1], off), __shfl_xor(v[2], off), __shfl_xor(v[3], off)};
-          });
-      }
-    }
-#pragma unroll
-    for (int ct = 0; ct < NT; ++ct) {
-      const int h = ct * 16 + col;
-      if (h >= count) continue;
-      const int64_t q_head = head * per_head + h0 + h;
-      const float inv = l[ct] > 0.0f ? 1.0f / l[ct] : 0.0f;
+      for (int j = 0; j < NJ; ++j) shared_acc[wave][j][lane_now] = res.acc[j];
+      if (kq == 0) shared_ml[wave][col] = make_float2(res.m, res.l);
+    };
+    auto add_wave = [&](int w, int j0) {                               // columns past the queries: whatever lies there, not used
+      const float2 ml = shared_ml[w][col];
+      add(ml.x, ml.y, [&](int j) { return shared_acc[w][j0 + j][lane_now]; });
+    };
+    auto emit = [&](int j0) {
+      if (col >= count) return;
+      const int64_t q_head = head * per_head + h0 + col;
+      const float inv = l > 0.0f ? 1.0f / l : 0.0f;
       uint16_t* o = a.out + seq * a.out_ld + q_head * a.out_head;
-      constexpr int RUN = L::PER < JW ? L::PER : JW;                   // adjacent channels of a lane and wave
+      constexpr int RUN = L::PER < JW ? L::PER : JW;                 // adjacent channels of a lane
 #pragma unroll
       for (int r = 0; r < 4; ++r)
 #pragma unroll
         for (int g = 0; g < JW; g += RUN) {
           uint16_t v[RUN];
 #pragma unroll
-          for (int j = 0; j < RUN; ++j) v[j] = (uint16_t)cvt_pk_bf16(acc[ct][g + j][r] * inv * value_unit, 0.0f);
+          for (int j = 0; j < RUN; ++j) v[j] = (uint16_t)cvt_pk_bf16(acc[g + j][r] * inv * value_unit, 0.0f);
           __builtin_memcpy(__builtin_assume_aligned(o + L::v_channel(kq * 4 + r, j0 + g), RUN * 2), v, RUN * 2);
         }
-      if (a.lse && kq == 0 && wave == 0)
-        a.lse[(int64_t)seq * a.q_heads + q_head] = l[ct] > 0.0f ? (m[ct] + log2f(l[ct])) * 0.6931471805599453f : -INFINITY;
+      if (a.lse && kq == 0 && j0 == 0)
+        a.lse[(int64_t)seq * a.q_heads + q_head] = l > 0.0f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+    };
+
+    if (solo) {                                                        // nothing to join; through LDS for one way of storing
+      put_wave();
+      __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll 1
+      for (int j0 = 0; j0 < NJ; j0 += JW) {
+        clear();
+        add_wave(wave, j0);
+        emit(j0);
+      }
+      continue;                                                        // one pair a wave: the loop ends
     }
+
+    // Join the waves: every wave takes JW instructions' outputs of all of them, and keeps them to the end.
+    const int held = min(t1 - t0, NW), j0 = wave * JW;                 // waves that hold anything
+    __syncthreads();                                                   // reads of the last join are over
+    if (wave < held) put_wave();
+    __syncthreads();
+    clear();
+    for (int w = 0; w < held; ++w) add_wave(w, j0);
+
+    // A part of a pair: groups of `fan` parts, then of their sums, are joined by the one of their workers that is last to come.
+    int entry = worker - w_first, entries = w_last - w_first + 1, step = 1, level = 0;
+    bool done = true;
+    const int fan = count > 4 ? 8 : 16;                                // parts that a workgroup joins at a time
+    while (entries > 1) {
+      constexpr uint32_t kPart = part_bytes_of<L>();
+      const int first = entry / fan * fan, n = min(fan, entries - first);     // of the group
+      auto slot = [&](int e) { return (uint32_t)part_slot(w_first + e * step, w_first) * kPart; };
+      if (n > 1) {
+        if (col < count) {
+          const uint32_t at = slot(entry);
+#pragma unroll
+          for (int j = 0; j < JW; ++j) put_part(parts, (kq * count + col) * 16, at + (j0 + j) * count * 64, acc[j]);
+          if (wave == 0 && kq == 0) put_part(parts, col * 16, at + NJ * 1024, (float4_t){m, l, 0.0f, 0.0f});
+        }
+        // Every wave's stores have reached memory before the counter says so.  Counters of different groups and levels differ: a group
+        // of two and more at a level reaches past the worker `level` behind its first.
+        int* counter = counters + w_first + first * step + level;
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup");
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __syncthreads();
+        if (threadIdx.x == 0) {
+          last_one = __hip_atomic_fetch_add(counter, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == n - 1;
+          if (last_one) __hip_atomic_store(counter, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);      // for the next call
+        }
+        __syncthreads();
+        done = __builtin_amdgcn_readfirstlane(last_one);
+        if (!done) break;
+        // Where a part has fewer than sixteen heads, the lanes that would hold the others take further parts.  The order is the
+        // workers': the same bits whoever comes last.
+        constexpr int B = JW <= 2 ? 4 : 2;
+        clear();
+        const int run_log2 = count > 8 ? 4 : count > 4 ? 3 : count > 2 ? 2 : count > 1 ? 1 : 0, runs = 16 >> run_log2;
+        const int mine = col & ((1 << run_log2) - 1), run = col >> run_log2;
+        struct Loaded {
+          float4_t ml[B], acc[B][JW];
+        };
+        auto fetch = [&](Loaded& x, int e0) {
+#pragma unroll
+          for (int b = 0; b < B; ++b) {
+            const int e = e0 + b * runs + run;
+            const bool ok = e < n && mine < count;                   // others read past the buffer: zeros
+            const uint32_t at = ok ? slot(first + e) : 0x80000000u;
+            x.ml[b] = get_part(parts, at + mine * 16, NJ * 1024);
+#pragma unroll
+            for (int j = 0; j < JW; ++j) x.acc[b][j] = get_part(parts, at + (kq * count + mine) * 16, (j0 + j) * count * 64);
+            if (!ok) x.ml[b][0] = kNoReference;
+          }
+          __builtin_amdgcn_sched_barrier(0);                         // the loads stay in front of what follows
+        };
+        auto add_all = [&](const Loaded& x) {
+#pragma unroll
+          for (int b = 0; b < B; ++b) add(x.ml[b][0], x.ml[b][1], [&](int j) { return x.acc[b][j]; });
+        };
+#pragma unroll 1
+        for (int e = 0; e < n; e += B * runs) {                      // uniform
+          Loaded x;
+          fetch(x, e);
+          add_all(x);
+        }
+#pragma unroll 1
+        for (int off = 1 << run_log2; off < 16; off <<= 1)
+          add(__shfl_xor(m, off), __shfl_xor(l, off), [&](int j) {
+            const float4_t v = acc[j];
+            return (float4_t){__shfl_xor(v[0], off), __shfl_xor(v[1], off), __shfl_xor(v[2], off), __shfl_xor(v[3], off)};
+          });
+      }
+      entry /= fan;
+      entries = (entries + fan - 1) / fan;
+      step *= fan;
+      ++level;
+    }
+    if (done) emit(j0);
   }
 }
 
-// queries of a key head that share a pass: two tiles of columns where one does not hold them
-int tiles_of(const pq_kv_cache& c, int q_heads) { return q_heads / c.kv_heads > 16 ? 2 : 1; }
-int chunks_of(const pq_kv_cache& c, int q_heads) {
-  const int width = 16 * tiles_of(c, q_heads);
-  return (q_heads / c.kv_heads + width - 1) / width;
-}
+// Queries of a key head that share a pass: sixteen columns of the products; more take as many passes, of about as many queries each.
+// (Two tiles of columns a pass read the cache once for up to 32, but leave a wave too few registers: 20 queries a key head, 16
+// sequences up to 8000 tokens, INT4 in heads of 128: 24.6 us against 20.8, of 256: 46 against 29.)
+int chunks_of(const pq_kv_cache& c, int q_heads) { return (q_heads / c.kv_heads + 15) / 16; }
 int64_t longest_of(int64_t max_len, int64_t window) {                  // blocks of the longest sequence
   int64_t n = (max_len + kKvBlock - 1) / kKvBlock;
   if (window && n > window / kKvBlock + 2) n = window / kKvBlock + 2;
@@ -762,8 +748,7 @@ int64_t grid_of(const pq_kv_cache& c, int64_t seqs, int q_heads, int64_t max_len
 size_t attn_decode_workspace_bytes(const pq_kv_cache& c, int64_t seqs, int q_heads, int64_t max_len, int64_t window) {
   int64_t workers = grid_of(c, seqs, q_heads, max_len, window);
   if (workers > kMaxSplits) workers = kMaxSplits;
-  const int tiles = tiles_of(c, q_heads);
-  return PQ_ATTN_DECODE_ZERO_BYTES + (size_t)workers * 2 * tiles * (size_t)(c.head_dim / 16 * 1024 + 256);
+  return PQ_ATTN_DECODE_ZERO_BYTES + (size_t)workers * 2 * (size_t)(c.head_dim / 16 * 1024 + 256);
 }
 
 int run_attn_decode(const pq_kv_cache& c, const AttnCall& a, hipStream_t st) {
@@ -771,8 +756,7 @@ int run_attn_decode(const pq_kv_cache& c, const AttnCall& a, hipStream_t st) {
   const int longest = (int)longest_of(a.max_len, a.window);
   const uint32_t part_bytes = (uint32_t)(attn_decode_workspace_bytes(c, a.seqs, a.q_heads, a.max_len, a.window) - PQ_ATTN_DECODE_ZERO_BYTES);
   return kv_dispatch(c.fmt, c.group, c.head_dim, [&](auto l) {
-    if (tiles_of(c, a.q_heads) == 1) attn_decode_kernel<decltype(l), 1><<<grid, 64 * kAttnWaves, 0, st>>>(kv_view(c), a, chunks, longest, part_bytes);
-    else attn_decode_kernel<decltype(l), 2><<<grid, 64 * kAttnWaves, 0, st>>>(kv_view(c), a, chunks, longest, part_bytes);
+    attn_decode_kernel<decltype(l)><<<grid, 64 * kAttnWaves, 0, st>>>(kv_view(c), a, chunks, longest, part_bytes);
     return check_hip(hipGetLastError(), "pq_attn_decode");
   });
 }
