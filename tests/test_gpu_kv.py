@@ -245,6 +245,20 @@ def test_one_long_sequence(fmt, group, dim):
     run_case(fmt, group, dim, [30011], heads=1, per=4, page=256)
 
 
+@pytest.mark.parametrize("fmt,group,dim", [(I4, 64, 64), (NV, 16, 128), (BF, 0, 256)])
+def test_one_long_sequence_of_many_queries(fmt, group, dim):
+    run_case(fmt, group, dim, [40003], heads=1, per=11, page=1024)
+
+
+@pytest.mark.parametrize("fmt,group,dim", [(I4, 32, 64), (NV, 16, 64), (BF, 0, 64), (I4, 128, 128)])
+def test_more_pairs_than_workgroups(fmt, group, dim):
+    # sequences of a server's batch: workgroups that end one pair and begin the next
+    rng = np.random.default_rng(21)
+    run_case(fmt, group, dim, [int(m) for m in rng.integers(1, 1500, 130)] + [1500], heads=4, per=2, page=64)
+    # many pairs, one of them long: a workgroup each
+    run_case(fmt, group, dim, [1200] + [int(m) for m in rng.integers(0, 70, 89)], heads=24, per=1, page=64, lse=False)
+
+
 @pytest.mark.parametrize("fmt,group,dim", [(I4, 64, 128), (NV, 16, 128), (BF, 0, 128)])
 def test_sharp_and_flat_scores(fmt, group, dim):
     run_case(fmt, group, dim, [500, 33], scale=1.0, q_scale=4.0)            # one token takes nearly all
@@ -299,33 +313,35 @@ def test_no_sequences():
     assert out.shape == (0, 4, 64)
 
 
+@pytest.mark.parametrize("n", [120, 4000])                 # one workgroup a pair; several that join
 @pytest.mark.parametrize("fmt,group", [(I4, 64), (NV, 16), (BF, 0)])
-def test_graph_replays_and_other_streams(fmt, group):
+def test_graph_replays_and_other_streams(fmt, group, n):
     """A decode step (write, attention) captured once: replays follow the lengths and slots in device memory, and a second stream
     with a workspace of its own gives the same."""
     rng = np.random.default_rng(14)
-    dim, heads, page, n = 128, 2, 32, 120
+    dim, heads, page = 128, 2, 32
+    pages = (n + 40) // page
     k, v = rows(rng, n, heads, dim), rows(rng, n, heads, dim)
-    cache, (kt, vt) = make_cache(fmt, group, heads, dim, page, 4, k, v)
+    cache, (kt, vt) = make_cache(fmt, group, heads, dim, page, pages, k, v)
     pq.pq_kv_write(cache, k, v, torch.arange(n, device=DEV))
     q = torch.randn(1, 8, dim, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).to(DEV)
-    table = torch.arange(4, dtype=torch.int32, device=DEV)[None]
+    table = torch.arange(pages, dtype=torch.int32, device=DEV)[None]
     lengths, slot = torch.tensor([n - 4], dtype=torch.int32, device=DEV), torch.tensor([n - 5], device=DEV)
     kn, vn = k[:1].clone(), v[:1].clone()
-    ws = pq.pq_attn_decode_workspace(cache, 1, 8, 128)
+    ws = pq.pq_attn_decode_workspace(cache, 1, 8, n + 8)
     out = torch.empty_like(q)
     other = torch.cuda.Stream()
 
     def step(o, w):
         pq.pq_kv_write(cache, kn, vn, slot)
-        pq.pq_attn_decode(cache, q, table, lengths, 128, 0.1, out=o, workspace=w)
+        pq.pq_attn_decode(cache, q, table, lengths, n + 8, 0.1, out=o, workspace=w)
 
     step(out, ws)
     torch.cuda.synchronize()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         step(out, ws)
-    ws2 = pq.pq_attn_decode_workspace(cache, 1, 8, 128)
+    ws2 = pq.pq_attn_decode_workspace(cache, 1, 8, n + 8)
     for i in range(4):
         kn.copy_(k[10 + i:11 + i])
         vn.copy_(v[20 + i:21 + i])
@@ -345,3 +361,18 @@ def test_graph_replays_and_other_streams(fmt, group):
         rk, rv = pq.pq_kv_read(cache, slot)
         same_bits(rk, OK.read_back(fmt, group, f64(kn), kt))
         same_bits(rv, OK.read_back(fmt, group, f64(vn), vt))
+
+
+@pytest.mark.parametrize("fmt", ["nvfp4", "int4", "bf16"])
+def test_example(fmt):
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "decode_cache.py")
+    spec = importlib.util.spec_from_file_location("decode_cache", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    worst, x = module.run(fmt, steps=3)
+    assert bool(torch.isfinite(x.float()).all())
+    # 4-bit keys and values of normal variates: codes are off by up to a seventh of a group's largest, some 2.5 standard deviations,
+    # so an output may be off by as much as it is large; the unquantized cache gives the same bits
+    assert worst <= (0.0 if fmt == "bf16" else 2.0)
