@@ -7,6 +7,17 @@
 //   outputs  O[channel, head] += V' P   the same instruction, 16 channels x 32 tokens; the scores' result layout (lane 16 q + h
 //                                       holds tokens 4 q .. 4 q + 3 of head h) is the operand layout of the weights
 // Nothing goes through LDS or between lanes in the loop.
+//
+// Bound by the reading of the cache where it is long: two flops a stored number and query are far below what the matrix unit gives, and
+// a block's vector work (unpacking, eight exponentials a lane) fits beside its loads.  Measured (MI355X, a copy runs at 4.9 TB/s):
+//   64 sequences up to 24 000 tokens, 8 heads of 128, INT4/64: 1.05 GB in 192 us, 5.5 TB/s
+//   one of 131 000 tokens, 8 heads of 128, INT4/128:         138 MB in 35 us, 3.9 TB/s
+//   8 up to 4600 tokens, 24 heads of 128, bf16:          304 MB in 62 us, 4.9 TB/s
+// Short work is bound by the chain of what waits for one another: launch, lengths, plan 2 us; pages, queries, first block 2; the
+// waves' join 1; a part's store, counter and fetch 3.  The smallest call takes 4.4 us of kernel.
+//
+// Each wave keeps one block ahead in registers.  Two ahead (4-bit formats, heads up to 128) cost 10 to 30 % in short sequences and
+// gave nothing in long ones; eight waves a workgroup, three or four a SIMD gave less than they cost elsewhere.
 #include "pq_kv.h"
 #include "pq_qgemm_common.h"
 
@@ -24,10 +35,8 @@ typedef uint32_t uint4_t __attribute__((ext_vector_type(4)));
 constexpr int kAttnWaves = 4;            // of a workgroup; they take a segment's blocks in turn
 constexpr int kUnits = 256;              // compute units
 constexpr int kMaxSplits = 1024;         // workgroups that may hold a part of a pair: counters in the workspace
-constexpr int kLeastBlocks = 4;          // of a workgroup that holds a part of a pair
-constexpr int kWholeBlocks = 20;         // a pair up to which stays whole: parts cost a join
-constexpr int kMostParts = 64;           // of a pair
-constexpr int kSoloBlocks = 8;          // see the plan
+// The limits of the plan below (what they say and what they are worth is told there).
+constexpr int kLeastBlocks = 4, kWholeBlocks = 20, kMostParts = 64, kSoloBlocks = 8, kExtraBlocks = 64, kPartBlocks = 32;
 
 constexpr float kNoReference = -1e38f;   // M before the first token
 // A weight with its value's scale stays below 2^15 (fp16); M follows when it would not, to 2^7 and less: seldom, so that neither the
@@ -162,7 +171,7 @@ struct Query {
 #pragma unroll
     for (int kk = 0; kk < L::NK; ++kk) {
       q[kk] = (uint4_t){0u, 0u, 0u, 0u};
-      if (n < count) q[kk] = *reinterpret_cast<const uint4_t*>(src + (n) * a.q_head + kk * 32 + kq * 8);
+      if (n < count) q[kk] = *reinterpret_cast<const uint4_t*>(src + n * a.q_head + kk * 32 + kq * 8);
     }
   }
   __device__ __forceinline__ void convert(const AttnCall& a, float key_unit) {
@@ -399,9 +408,24 @@ __device__ __forceinline__ void block_outputs(Values<L>& x, float4_t (&s_)[2], c
 }
 
 // ------------------------------------------------------------------------ which blocks are whose
-// All blocks of all pairs (sequence, key head, sixteen or thirty-two of its queries) are numbered sequence by sequence, pair by pair.
-// A worker takes `per` of them in a row: the work is even whatever the lengths.  Where `per` is small, or the pairs are many, each
-// pair's blocks are padded to a multiple of it instead: no worker then holds two pairs.
+// A pair is a sequence and up to sixteen queries of one key head; workers (workgroups, or waves) share the blocks of all pairs.  Every
+// wave works the plan out from the lengths, so that it holds for the lengths of this call, whatever the grid was sized for (one
+// sequence of 2000 tokens where max_len is 131 072: 9.4 us; sized by max_len 18.0).  With `even` = all blocks / resident workers:
+//
+//   parts    where pairs are few: every pair in equal parts of up to `per` blocks, per = even to 1.5 even, the least with which each
+//            part finds a resident worker: no worker then holds two pairs.  (48 sequences up to 5000 tokens, 2 heads: 14.5 us; per =
+//            even only 18.3.)  A pair up to kWholeBlocks stays whole (128 pairs up to 300 tokens: 8.7 us, parted 10.0; but 64 pairs up
+//            to 2000 with 40: 13.9, 12.2 with 20), a part is at least kLeastBlocks (8 pairs of 1500 tokens: 9.3 us; of 2 blocks 11.4, of
+//            8 9.8), and a pair has at most kMostParts (4 pairs of 60 000 tokens, 8 queries each: 17.7 us; 32 parts 21.6, 128 20.0).
+//   solo     a wave a pair, nothing to join, where pairs fill the workers and are short for their number: blocks of the longest <=
+//            kSoloBlocks pairs / workers (2160 pairs up to 40 tokens: 10.8 us, a workgroup each 20.7; 2400 up to 1200 with a limit of
+//            12: 105, 90 with 8).
+//   whole    a worker a pair, where the longest has at most kExtraBlocks more than `even`: 600 pairs up to 800 tokens 18.9 us, in a row
+//            26.9; 480 up to 3000 37.7, with 32 more 41.8; 400 up to 5000 with 128 more 33.6, 32.0 with 64.
+//   parts    again, up to kMaxSplits of them, more than are resident, where `even` is below kPartBlocks: 800 pairs up to 300 tokens
+//            but 8 of 3000 20.5 us, in a row 25.2; a bound of 64: 55.6 against 52.9 with 2400 pairs, 8 of them of 10 000 tokens.
+//   in a row blocks numbered sequence by sequence, pair by pair, `even` of them a worker: the same work whatever the lengths, at up to
+//            two joins a worker (512 pairs up to 24 000 tokens: 197 us, whole 232).
 struct Lengths {           // of a sequence: first attended token and end, first block, blocks (at least one)
   int first_token, end, first, n;
 };
@@ -422,16 +446,26 @@ __device__ __forceinline__ int wave_scan(int v) {
   v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);      // row_bcast 15 into rows 1 and 3
   return v + __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);   // row_bcast 31 into rows 2 and 3
 }
+// the largest of all lanes (none is negative)
+__device__ __forceinline__ int wave_max(int v) {
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false));
+  v = max(v, __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false));
+  return __builtin_amdgcn_readlane(max(v, __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false)), 63);
+}
 __device__ __forceinline__ int last_lane(int v) { return __builtin_amdgcn_readlane(v, 63); }
 
-// a part's outputs, then (M, l) of its heads
+// a part's outputs, then (M, l) of its queries
 template <class L>
 constexpr uint32_t part_bytes_of() { return L::NJ * 1024 + 256; }
 
 // the part of a pair that worker w holds, first the one that began it
 __device__ __forceinline__ int part_slot(int w, int w_first) { return w == w_first ? 2 * w + 1 : 2 * w; }
 
-// Waves a SIMD, and with them the registers of a wave.
+// Waves a SIMD, and with them the registers of a wave: one where a block and the results pass 256 (16 sequences up to 8000 tokens,
+// 4 heads of 256, INT4/32: 36.5 us, with two and what that spills 76.5).
 template <class L>
 constexpr int waves_of() { return L::D == 256 && (L::FMT == kBf16 || L::G == 32) ? 1 : 2; }
 // the part buffer is written and read by workgroups of different chiplets in one launch: past the caches that they do not share
@@ -444,10 +478,10 @@ __device__ __forceinline__ float4_t get_part(__amdgpu_buffer_rsrc_t buf, uint32_
 }
 
 template <class L>
-__global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L>())) void attn_decode_kernel(KvView cache, AttnCall a,
-                                                                                                       int chunks, int longest, uint32_t part_bytes) {
+__global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L>())) void attn_decode_kernel(KvView cache, AttnCall a, int chunks,
+                                                                                          uint32_t part_bytes) {
   constexpr int NJ = L::NJ, NW = kAttnWaves;
-  constexpr int kWorkers = kUnits * waves_of<L>();                  // workgroups that share all blocks evenly: what is resident
+  constexpr int kWorkers = kUnits * waves_of<L>();                     // what is resident
   constexpr int JW = NJ / NW;                                          // instructions' outputs that a wave joins
   __shared__ float4_t shared_acc[NW][NJ][64];
   __shared__ float2 shared_ml[NW][16];
@@ -460,12 +494,15 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L>())) void attn_decod
   const float key_unit = L::FMT == kNvfp4 ? *cache.k_ts : L::FMT == kInt4 ? 16777216.0f / 7.0f : 1.0f;
   const float value_unit = L::FMT == kNvfp4 ? *cache.v_ts : L::FMT == kInt4 ? 16777216.0f / 7.0f : 1.0f;
 
-  // the plan: the same in every wave
+  // the plan
   const int length0 = lane < a.seqs ? a.lengths[lane] : 0;             // of the first 64 sequences: often of all
   auto length_at = [&](int b0) { return b0 == 0 ? length0 : b0 + lane < a.seqs ? a.lengths[b0 + lane] : 0; };
   auto blocks_at = [&](int b0) { return b0 + lane < a.seqs ? lengths_of(a, length_at(b0)).n : 0; };
-  int blocks = 0;
-  for (int b0 = 0; b0 < a.seqs; b0 += 64) blocks += last_lane(wave_scan(blocks_at(b0)));
+  int blocks = 0, longest = 0;                                         // of a pair of each sequence
+  for (int b0 = 0; b0 < a.seqs; b0 += 64) {
+    blocks += last_lane(wave_scan(blocks_at(b0)));
+    longest = max(longest, wave_max(blocks_at(b0)));
+  }
   auto parts_of = [&](int n, int per) { return n <= kWholeBlocks ? 1 : (n + per - 1) / per; };
   auto items_of = [&](int per) {                                       // workers of padded pairs
     int items = 0;
@@ -475,7 +512,7 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L>())) void attn_decod
   const int even = max(max((blocks * pairs + kWorkers - 1) / kWorkers, kLeastBlocks), (longest + kMostParts - 1) / kMostParts);
   int per = even;
   bool padded = false, solo = false;
-  if (a.seqs * pairs <= kWorkers) {                                    // up to half as much again for a pair a worker
+  if (a.seqs * pairs <= kWorkers) {
 #pragma unroll 1
     for (int more = 0; more <= 4 && !padded; ++more) {
       per = even + even * more / 8;
@@ -484,16 +521,16 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L>())) void attn_decod
   }
   if (!padded) {
     per = even;
-    // many pairs, or short ones: a wave each, without a join
     solo = a.seqs * pairs >= kWorkers && (int64_t)longest * kWorkers <= (int64_t)kSoloBlocks * a.seqs * pairs;
-    if (solo || a.seqs * pairs >= 4 * kWorkers) {                      // pairs enough: one a worker
+    if (solo || longest <= even + kExtraBlocks) {
       per = longest;
       padded = true;
-    } else if (even < 16) {
+    } else if (even < kPartBlocks) {
       padded = items_of(per) <= min(kMaxSplits, (int)gridDim.x);
     }
   }
   const int worker = solo ? blockIdx.x * NW + wave : blockIdx.x;
+  // blocks of a pair in the numbering: padded to whole workers
   auto counted = [&](int n) { return padded ? (per == longest ? per : parts_of(n, per) * per) : n; };
 
   const int u_begin = worker * per, u_end = u_begin + per;             // seqs * pairs * blocks fit 31 bits
@@ -586,7 +623,7 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L>())) void attn_decod
 
     const int lane_now = renewed(lane), kq = lane_now >> 4, col = lane_now & 15;
     float m, l;
-    float4_t acc[JW];                                              // JW instructions' outputs at a time
+    float4_t acc[JW];                                                  // JW instructions' outputs at a time
     auto add = [&](float om, float ol, auto&& other) {
       const float top = fmaxf(m, om), f = __builtin_amdgcn_exp2f(m - top), g = __builtin_amdgcn_exp2f(om - top);
       m = top;
@@ -615,7 +652,7 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L>())) void attn_decod
       const int64_t q_head = head * per_head + h0 + col;
       const float inv = l > 0.0f ? 1.0f / l : 0.0f;
       uint16_t* o = a.out + seq * a.out_ld + q_head * a.out_head;
-      constexpr int RUN = L::PER < JW ? L::PER : JW;                 // adjacent channels of a lane
+      constexpr int RUN = L::PER < JW ? L::PER : JW;                   // adjacent channels of a lane
 #pragma unroll
       for (int r = 0; r < 4; ++r)
 #pragma unroll
@@ -654,7 +691,9 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L>())) void attn_decod
     // A part of a pair: groups of `fan` parts, then of their sums, are joined by the one of their workers that is last to come.
     int entry = worker - w_first, entries = w_last - w_first + 1, step = 1, level = 0;
     bool done = true;
-    const int fan = count > 4 ? 8 : 16;                                // parts that a workgroup joins at a time
+    // Parts that a workgroup joins at a time: a level costs 2 to 3 us, but so do more loads than a wave has in flight (8 pairs of
+    // 1500 tokens, 4 queries each: 9.3 us, with 8 at a time 11.2; 4 pairs of 30 000, 16 queries: 16.8 us, with 16 at a time 18.1).
+    const int fan = count > 4 ? 8 : 16;
     while (entries > 1) {
       constexpr uint32_t kPart = part_bytes_of<L>();
       const int first = entry / fan * fan, n = min(fan, entries - first);     // of the group
@@ -692,21 +731,21 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L>())) void attn_decod
 #pragma unroll
           for (int b = 0; b < B; ++b) {
             const int e = e0 + b * runs + run;
-            const bool ok = e < n && mine < count;                   // others read past the buffer: zeros
+            const bool ok = e < n && mine < count;                     // others read past the buffer: zeros
             const uint32_t at = ok ? slot(first + e) : 0x80000000u;
             x.ml[b] = get_part(parts, at + mine * 16, NJ * 1024);
 #pragma unroll
             for (int j = 0; j < JW; ++j) x.acc[b][j] = get_part(parts, at + (kq * count + mine) * 16, (j0 + j) * count * 64);
             if (!ok) x.ml[b][0] = kNoReference;
           }
-          __builtin_amdgcn_sched_barrier(0);                         // the loads stay in front of what follows
+          __builtin_amdgcn_sched_barrier(0);                           // the loads stay in front of what follows
         };
         auto add_all = [&](const Loaded& x) {
 #pragma unroll
           for (int b = 0; b < B; ++b) add(x.ml[b][0], x.ml[b][1], [&](int j) { return x.acc[b][j]; });
         };
 #pragma unroll 1
-        for (int e = 0; e < n; e += B * runs) {                      // uniform
+        for (int e = 0; e < n; e += B * runs) {                        // uniform
           Loaded x;
           fetch(x, e);
           add_all(x);
@@ -753,10 +792,9 @@ size_t attn_decode_workspace_bytes(const pq_kv_cache& c, int64_t seqs, int q_hea
 
 int run_attn_decode(const pq_kv_cache& c, const AttnCall& a, hipStream_t st) {
   const int grid = (int)grid_of(c, a.seqs, a.q_heads, a.max_len, a.window), chunks = chunks_of(c, a.q_heads);
-  const int longest = (int)longest_of(a.max_len, a.window);
   const uint32_t part_bytes = (uint32_t)(attn_decode_workspace_bytes(c, a.seqs, a.q_heads, a.max_len, a.window) - PQ_ATTN_DECODE_ZERO_BYTES);
   return kv_dispatch(c.fmt, c.group, c.head_dim, [&](auto l) {
-    attn_decode_kernel<decltype(l)><<<grid, 64 * kAttnWaves, 0, st>>>(kv_view(c), a, chunks, longest, part_bytes);
+    attn_decode_kernel<decltype(l)><<<grid, 64 * kAttnWaves, 0, st>>>(kv_view(c), a, chunks, part_bytes);
     return check_hip(hipGetLastError(), "pq_attn_decode");
   });
 }

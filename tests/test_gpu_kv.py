@@ -259,6 +259,25 @@ def test_more_pairs_than_workgroups(fmt, group, dim):
     run_case(fmt, group, dim, [1200] + [int(m) for m in rng.integers(0, 70, 89)], heads=24, per=1, page=64, lse=False)
 
 
+@pytest.mark.parametrize("fmt,group,dim", [(I4, 32, 64), (NV, 16, 64), (BF, 0, 64), (I4, 64, 128)])
+def test_shares_of_pairs(fmt, group, dim):
+    # three pairs a sequence (33 queries of one key head)
+    rng = np.random.default_rng(33)
+    some = lambda lo, hi, n: [int(m) for m in rng.integers(lo, hi, n)]
+    run_case(fmt, group, dim, some(300, 1500, 133), heads=1, per=33, page=64)              # fewer pairs than workgroups, each whole
+    run_case(fmt, group, dim, some(300, 1000, 132) + [4000], heads=1, per=33, page=64)     # one much longer: equal parts of pairs
+    run_case(fmt, group, dim, [6000] + some(900, 1700, 200), heads=1, per=33, page=64, lse=False)    # blocks in a row
+    run_case(fmt, group, dim, some(0, 60, 180) + [3000], heads=1, per=33, page=64, lse=False)        # many short ones
+
+
+@pytest.mark.parametrize("fmt,group,dim", [(I4, 64, 128), (NV, 16, 64), (BF, 0, 128)])
+def test_short_sequences_of_a_large_capacity(fmt, group, dim):
+    run_case(fmt, group, dim, [0, 900, 1, 33, 400], max_len=20000, page=64)
+    run_case(fmt, group, dim, [900, 70], max_len=20000, page=1024, window=300)
+    rng = np.random.default_rng(34)
+    run_case(fmt, group, dim, [int(m) for m in rng.integers(0, 200, 300)], heads=2, per=1, max_len=2000, page=64, lse=False)
+
+
 @pytest.mark.parametrize("fmt,group,dim", [(I4, 64, 128), (NV, 16, 128), (BF, 0, 128)])
 def test_sharp_and_flat_scores(fmt, group, dim):
     run_case(fmt, group, dim, [500, 33], scale=1.0, q_scale=4.0)            # one token takes nearly all
