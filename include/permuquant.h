@@ -8,7 +8,9 @@
  * the paper describes next to it: the normalisation layer that absorbs the activation reorder
  * (App. C), the Hadamard variant PermuQuant-H (App. D), the layer-output reading of the
  * calibration metric, a dynamic NVFP4 tensor scale, the layer's bias in the GEMM epilogue and
- * the alternative reorder criteria of the ablation (Tab. 2a).
+ * the alternative reorder criteria of the ablation (Tab. 2a).  For models that generate token by
+ * token it keeps the keys and values of the attention between such layers in the same formats:
+ * a paged cache quantized as it is written, read back, and attended to by one new token a sequence.
  *
  * Conventions
  *   - X is [M, K] row-major (tokens x input channels), W is [N, K] row-major (output x input

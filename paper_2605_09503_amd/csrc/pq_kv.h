@@ -79,8 +79,8 @@ struct KvLayout {
 __device__ __forceinline__ constexpr int int_mag_at(int c) { return (c & 2) * 4 + (c & 1) * 3; }       // 0, 3, 8, 11
 __device__ __forceinline__ constexpr int int_sign_at(int c) { return 15 - (c & 2) * 4 - (c & 1); }     // 15, 14, 7, 6
 // Two quads side by side, from eight values (pairs of bf16, values 2 i and 2 i + 1 in x[i]; quads of values 0 .. 3 and 4 .. 7):
-// x * inv (an inverse a pair) rounded to the nearest integer (ties to even), below 7.5 in magnitude.  Adding 2^23 leaves the integer in the low bits
-// under a constant; the words are summed at the codes' places, the constants taken off once.  Signs go two at a time.
+// x * inv (an inverse a pair) rounded to the nearest integer (ties to even), below 7.5 in magnitude.  Adding 2^23 leaves the integer in
+// the low bits under a constant; the words are summed at the codes' places, the constants taken off once.  Signs go two at a time.
 __device__ __forceinline__ uint32_t int_encode8(const uint32_t (&x)[4], const float (&inv)[4]) {
   constexpr uint32_t kBase = 0x4B000000u;                              // bits of 2^23
   uint32_t mags = 0, bases = 0, signs = 0;

@@ -1,6 +1,9 @@
 // Keys and values quantized into a cache's pages as they are produced, and read back (layout: pq_kv.h; the arithmetic is the
 // pinned quantizer's of pq_quantize.hip, so a cache holds what pq_quantize_act would).  Bound by HBM: 2 bytes an element on
-// one side, 0.5 and the scales on the other.
+// one side, 0.5 and the scales on the other.  Measured (MI355X; a copy of 4 GiB runs at 4.9 TB/s):
+//   65 000 tokens, 8 heads of 128, NVFP4, 341 MB each way: written in 70 us (4.9 TB/s), read back in 53 (6.4)
+//   14 400 tokens, 8 heads of 128, INT4/32, 75 MB:         written in 19 us (4.0 TB/s), read back in 17 (4.4)
+// One token of 16 sequences takes 3.3 us, 650 tokens read back 4.2: a launch and three loads in a row (slot, row, scale).
 #include "pq_kv.h"
 #include "pq_qgemm_common.h"
 
@@ -13,16 +16,28 @@ struct KvRows {                          // rows of [token][head][D] bf16; strid
   int64_t ld, head;
 };
 
-// A workgroup takes 32 tokens of one head, keys and values; workgroups next to each other take the heads of the same tokens.  Neighbouring lanes hold neighbouring channels of a token, so a wave
-// reads (or writes) whole rows, and the codes of neighbouring tokens meet in the L2; all of a thread's loads are in flight together.
+// A workgroup takes 32 tokens of one head, keys and values; workgroups next to each other take the heads of the same tokens, whose
+// rows lie next to each other.  Neighbouring lanes hold neighbouring channels of a token, so a wave reads (or writes) whole rows, and
+// the codes of neighbouring tokens meet in the L2 (bytes read and written in HBM: the tensors' own to 2 %); all of a thread's loads
+// are in flight together.  With a head after the other and a load at a time the 65 000 tokens took 195 us for both ways.
 constexpr int kKvThreads = 256;
 template <class L>
 constexpr int key_items() { return kKvBlock * L::D / 8 / kKvThreads; }   // of a thread: a row's 8 channels each
 constexpr int kValueItems = kKvBlock * 16 / kKvThreads;                   // a row's lane each
 
+// The 32 tokens of a workgroup often lie in two blocks, and the next workgroup of the head has the rest of the second: both
+// belong on one chiplet, whose L2 then reads (fills) the block once.  Workgroups go round the eight chiplets, so with a multiple of
+// eight heads they do by themselves (and runs of tiles a chiplet are 1 to 3 % slower: 127.0 -> 128.8 us for 65 000 tokens both ways);
+// else chiplets take runs: 4 heads of 64, INT4/32, 71 000 tokens read back 21.1 -> 20.1 us, 2 of 64 written and read 20.4 -> 19.1, 20
+// 37.1 -> 36.3 (5 heads of 256 46.5 -> 47.2).  The grid's size follows from arguments
+// that are there: read from gridDim, a pass of two small calls took 9.8 us in place of 8.0.
+__device__ __forceinline__ uint32_t tile_of_workgroup(int heads, int64_t n) {
+  return heads & 7 ? (uint32_t)block_by_chiplet(blockIdx.x, (int)((n + kKvBlock - 1) / kKvBlock) * heads) : blockIdx.x;
+}
+
 // eight channels of keys, a lane each
 template <class L>
-__device__ __forceinline__ void write_key(const KvView& cache, uint8_t* block, int t, int c, bool ok, const uint4& x, float T, float encT) {
+__device__ __forceinline__ void write_key(uint8_t* block, int t, int c, bool ok, const uint4& x, float T, float encT) {
   if constexpr (L::FMT == kBf16) {
     if (ok) *reinterpret_cast<uint4*>(block + L::k_chunk(t, c)) = x;
   } else {
@@ -103,8 +118,7 @@ struct Pieces {
 
 // a lane's pieces of a value
 template <class L>
-__device__ __forceinline__ void write_value(const KvView& cache, uint8_t* block, int t, int lane, bool ok, uint32_t (&x)[L::NJ / 2],
-                                            float T, float encT) {
+__device__ __forceinline__ void write_value(uint8_t* block, int t, int lane, bool ok, uint32_t (&x)[L::NJ / 2], float T, float encT) {
   typedef Pieces<L> P;
   constexpr int PER = L::PER, RUNS = P::RUNS, PAIRS = PER / 2;
   if constexpr (L::FMT == kBf16) {
@@ -203,8 +217,9 @@ template <class L>
 __global__ __launch_bounds__(kKvThreads) void kv_write_kernel(KvView cache, KvRows k, KvRows v, const int64_t* __restrict__ slots,
                                                               int64_t n) {
   constexpr int LPR = L::D / 8, KI = key_items<L>(), VI = kValueItems;
-  const int head = blockIdx.x % cache.heads;
-  const int64_t t0 = (int64_t)(blockIdx.x / cache.heads) * kKvBlock, n_slots = cache.slots();
+  const uint32_t tile = tile_of_workgroup(cache.heads, n);
+  const int head = tile % cache.heads;
+  const int64_t t0 = (int64_t)(tile / cache.heads) * kKvBlock, n_slots = cache.slots();
   int64_t k_slot[KI], v_slot[VI];
   uint4 kx[KI];
   uint32_t vx[VI][L::NJ / 2];
@@ -238,23 +253,25 @@ __global__ __launch_bounds__(kKvThreads) void kv_write_kernel(KvView cache, KvRo
 #pragma unroll
   for (int i = 0; i < KI; ++i) {
     const bool ok = k_slot[i] >= 0 && k_slot[i] < n_slots;     // other slots keep nothing
-    write_key<L>(cache, kv_block<L>(cache, ok ? k_slot[i] : 0, head), (int)k_slot[i] & (kKvBlock - 1),
+    write_key<L>(kv_block<L>(cache, ok ? k_slot[i] : 0, head), (int)k_slot[i] & (kKvBlock - 1),
                  (threadIdx.x + i * kKvThreads) % LPR, ok, kx[i], kT, kE);
   }
 #pragma unroll
   for (int i = 0; i < VI; ++i) {
     const bool ok = v_slot[i] >= 0 && v_slot[i] < n_slots;
-    write_value<L>(cache, kv_block<L>(cache, ok ? v_slot[i] : 0, head), (int)v_slot[i] & (kKvBlock - 1),
+    write_value<L>(kv_block<L>(cache, ok ? v_slot[i] : 0, head), (int)v_slot[i] & (kKvBlock - 1),
                    (threadIdx.x + i * kKvThreads) % 16, ok, vx[i], vT, vE);
   }
 }
 
 // values: INT4 z * s, NVFP4 value * s_b * T, every step one binary32 operation
 template <class L>
-__global__ __launch_bounds__(kKvThreads) void kv_read_kernel(KvView cache, const int64_t* __restrict__ slots, int64_t n, KvRows k, KvRows v) {
+__global__ __launch_bounds__(kKvThreads) void kv_read_kernel(KvView cache, const int64_t* __restrict__ slots, int64_t n, KvRows k,
+                                                             KvRows v) {
   constexpr int LPR = L::D / 8, KI = key_items<L>(), VI = kValueItems, PER = L::PER, RUNS = L::NJ / PER, PAIRS = PER / 2;
-  const int head = blockIdx.x % cache.heads;
-  const int64_t t0 = (int64_t)(blockIdx.x / cache.heads) * kKvBlock, n_slots = cache.slots();
+  const uint32_t tile = tile_of_workgroup(cache.heads, n);
+  const int head = tile % cache.heads;
+  const int64_t t0 = (int64_t)(tile / cache.heads) * kKvBlock, n_slots = cache.slots();
   int64_t k_slot[KI], v_slot[VI];
 #pragma unroll
   for (int i = 0; i < KI; ++i) {
@@ -333,7 +350,8 @@ __global__ __launch_bounds__(kKvThreads) void kv_read_kernel(KvView cache, const
       }
       y = make_uint4(cvt_pk_bf16(f[0], f[1]), cvt_pk_bf16(f[2], f[3]), cvt_pk_bf16(f[4], f[5]), cvt_pk_bf16(f[6], f[7]));
     }
-    if (row < n) __builtin_nontemporal_store((words4){y.x, y.y, y.z, y.w}, reinterpret_cast<words4*>(k.p + row * k.ld + head * k.head + u % LPR * 8));
+    if (row < n)
+      __builtin_nontemporal_store((words4){y.x, y.y, y.z, y.w}, reinterpret_cast<words4*>(k.p + row * k.ld + head * k.head + u % LPR * 8));
   }
 #pragma unroll
   for (int i = 0; i < VI; ++i) {
@@ -394,8 +412,8 @@ int run_kv_write(const pq_kv_cache& c, const void* k, int64_t k_ld, int64_t k_he
                  const int64_t* slots, int64_t n, hipStream_t st) {
   return kv_dispatch(c.fmt, c.group, c.head_dim, [&](auto l) {
     const unsigned grid = (unsigned)((n + kKvBlock - 1) / kKvBlock * c.kv_heads);
-    kv_write_kernel<decltype(l)><<<grid, kKvThreads, 0, st>>>(kv_view(c), KvRows{(uint16_t*)k, k_ld, k_head}, KvRows{(uint16_t*)v, v_ld, v_head},
-                                                      slots, n);
+    kv_write_kernel<decltype(l)><<<grid, kKvThreads, 0, st>>>(kv_view(c), KvRows{(uint16_t*)k, k_ld, k_head},
+                                                              KvRows{(uint16_t*)v, v_ld, v_head}, slots, n);
     return check_hip(hipGetLastError(), "pq_kv_write");
   });
 }
@@ -405,7 +423,7 @@ int run_kv_read(const pq_kv_cache& c, const int64_t* slots, int64_t n, void* k, 
   return kv_dispatch(c.fmt, c.group, c.head_dim, [&](auto l) {
     const unsigned grid = (unsigned)((n + kKvBlock - 1) / kKvBlock * c.kv_heads);
     kv_read_kernel<decltype(l)><<<grid, kKvThreads, 0, st>>>(kv_view(c), slots, n, KvRows{(uint16_t*)k, k_ld, k_head},
-                                                     KvRows{(uint16_t*)v, v_ld, v_head});
+                                                             KvRows{(uint16_t*)v, v_ld, v_head});
     return check_hip(hipGetLastError(), "pq_kv_read");
   });
 }
