@@ -14,7 +14,7 @@
 //   one of 131 000 tokens, 8 heads of 128, INT4/128:         138 MB in 35 us, 3.9 TB/s
 //   8 up to 4600 tokens, 24 heads of 128, bf16:          304 MB in 62 us, 4.9 TB/s
 // Short work is bound by the chain of what waits for one another: launch, lengths, plan 2 us; pages, queries, first block 2; the
-// waves' join 1; a part's store, counter and fetch 3.  The smallest call takes 4.4 us of kernel.
+// waves' join 1; a part's store, counter and fetch 3.  A call over 19 tokens takes 6 us.
 //
 // Each wave keeps one block ahead in registers.  Two ahead (4-bit formats, heads up to 128) cost 10 to 30 % in short sequences and
 // gave nothing in long ones; eight waves a workgroup, three or four a SIMD gave less than they cost elsewhere.

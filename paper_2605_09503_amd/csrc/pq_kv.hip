@@ -18,8 +18,9 @@ struct KvRows {                          // rows of [token][head][D] bf16; strid
 
 // A workgroup takes 32 tokens of one head, keys and values; workgroups next to each other take the heads of the same tokens, whose
 // rows lie next to each other.  Neighbouring lanes hold neighbouring channels of a token, so a wave reads (or writes) whole rows, and
-// the codes of neighbouring tokens meet in the L2 (bytes read and written in HBM: the tensors' own to 2 %); all of a thread's loads
-// are in flight together.  With a head after the other and a load at a time the 65 000 tokens took 195 us for both ways.
+// the codes of neighbouring tokens meet in the L2 (65 000 tokens: HBM reads 271 MB for 266 and 79 for 75, the slots by eight chiplets
+// included, and writes what there is); all of a thread's loads are in flight together.  With a head after the other and a load at a
+// time the 65 000 tokens took 195 us for both ways.
 constexpr int kKvThreads = 256;
 template <class L>
 constexpr int key_items() { return kKvBlock * L::D / 8 / kKvThreads; }   // of a thread: a row's 8 channels each
@@ -29,8 +30,8 @@ constexpr int kValueItems = kKvBlock * 16 / kKvThreads;                   // a r
 // belong on one chiplet, whose L2 then reads (fills) the block once.  Workgroups go round the eight chiplets, so with a multiple of
 // eight heads they do by themselves (and runs of tiles a chiplet are 1 to 3 % slower: 127.0 -> 128.8 us for 65 000 tokens both ways);
 // else chiplets take runs: 4 heads of 64, INT4/32, 71 000 tokens read back 21.1 -> 20.1 us, 2 of 64 written and read 20.4 -> 19.1, 20
-// 37.1 -> 36.3 (5 heads of 256 46.5 -> 47.2).  The grid's size follows from arguments
-// that are there: read from gridDim, a pass of two small calls took 9.8 us in place of 8.0.
+// 37.1 -> 36.3 (5 heads of 256 46.5 -> 47.2).  The grid's size follows from arguments that are there: read from gridDim, a pass of two
+// small calls took 9.8 us in place of 8.0.
 __device__ __forceinline__ uint32_t tile_of_workgroup(int heads, int64_t n) {
   return heads & 7 ? (uint32_t)block_by_chiplet(blockIdx.x, (int)((n + kKvBlock - 1) / kKvBlock) * heads) : blockIdx.x;
 }
