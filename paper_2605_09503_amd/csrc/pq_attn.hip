@@ -533,7 +533,9 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L>())) void attn_decod
   // blocks of a pair in the numbering: padded to whole workers
   auto counted = [&](int n) { return padded ? (per == longest ? per : parts_of(n, per) * per) : n; };
 
-  const int u_begin = worker * per, u_end = u_begin + per;             // seqs * pairs * blocks fit 31 bits
+  // All blocks and the last worker's share fit 31 bits (the host's limit is 2^30 before padding); idle workers' numbers may not.
+  if ((int64_t)worker * per > INT32_MAX - per) return;
+  const int u_begin = worker * per, u_end = u_begin + per;
   int u = u_begin, base = 0, b = 0;                                    // the sequence that holds block u, its first block `base`
   for (int b0 = 0;; b0 += 64) {
     if (b0 >= a.seqs) return;                                          // workers past the last block

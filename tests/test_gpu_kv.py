@@ -278,6 +278,22 @@ def test_short_sequences_of_a_large_capacity(fmt, group, dim):
     run_case(fmt, group, dim, [int(m) for m in rng.integers(0, 200, 300)], heads=2, per=1, max_len=2000, page=64, lse=False)
 
 
+def test_blocks_near_the_limit_of_a_call():
+    # 262 140 pairs of 2501 blocks, over 2^29 in all (sequences that share their pages): numbers of idle waves would pass 31 bits
+    rng = np.random.default_rng(35)
+    n, seqs, heads = 2500 * 32 + 5, 65535, 4
+    k, v = rows(rng, n, heads, 64), rows(rng, n, heads, 64)
+    cache, _ = make_cache(I4, 64, heads, 64, 1024, 79, k, v)
+    pq.pq_kv_write(cache, k, v, torch.arange(n, device=DEV))
+    table = torch.arange(79, dtype=torch.int32, device=DEV).repeat(seqs, 1)
+    q = torch.randn(1, heads, 64, generator=torch.Generator().manual_seed(2)).to(torch.bfloat16).to(DEV)
+    lengths = torch.full((seqs,), n, dtype=torch.int32, device=DEV)
+    out = pq.pq_attn_decode(cache, q.repeat(seqs, 1, 1), table, lengths, n, 0.125)
+    assert torch.equal(out, out[:1].expand_as(out))
+    ks, vs = OK.stored(I4, 64, f64(k[:, :2]), None), OK.stored(I4, 64, f64(v[:, :2]), None)
+    check(f64(out[0, :2]), None, f64(q[0, :2]), ks, vs, 0.125)
+
+
 @pytest.mark.parametrize("fmt,group,dim", [(I4, 64, 128), (NV, 16, 128), (BF, 0, 128)])
 def test_sharp_and_flat_scores(fmt, group, dim):
     run_case(fmt, group, dim, [500, 33], scale=1.0, q_scale=4.0)            # one token takes nearly all
