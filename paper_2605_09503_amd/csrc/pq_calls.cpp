@@ -455,6 +455,7 @@ PQ_CALL(attn_decode) {
     }
     Ref ws(w);
     const at::Tensor& wt = as_tensor(ws.p, "workspace");
+    if (!wt.is_contiguous() || wt.device() != c.device) refuse("workspace must be contiguous, on the cache's device");
     void *wp = wt.data_ptr(), *st = stream_of(c);
     const size_t bytes = wt.numel() * wt.element_size();
     const int64_t table_ld = seqs > 1 ? table.stride(0) : table.size(1);

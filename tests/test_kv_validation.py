@@ -104,6 +104,10 @@ def python_binding():
     import sys
     sys.modules["pq_python"] = module
     spec.loader.exec_module(module)
+    pq.load()
+    module.load()                            # binds the native module, one a process, to this copy's helpers, and its calls here
+    if pq._calls:
+        pq._calls.bind(pq._raise, pq._new_operand, pq._new_workspace, pq._refuse, pq._new_attn_workspace)
     for name in ("pq_kv_write", "pq_kv_read", "pq_attn_decode"):
         with open(pq.__file__) as f:
             tree = ast.parse(f.read())
@@ -152,6 +156,17 @@ def test_binding_refuses_other_tensors(lib, native):  # noqa: F811
     for kw in (dict(data=c.data[:100]), dict(data=c.data.view(torch.int8)), dict(fmt=0, group=16), dict(page=33), dict(fmt=2, group=32)):
         with pytest.raises(pq.PQError):
             pq.KVCache(**{**{f: getattr(c, f) for f in ("fmt", "group", "kv_heads", "head_dim", "page", "pages", "data")}, **kw})
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_binding_refuses_other_workspaces(lib, native):  # noqa: F811
+    # a strided one would be written past its end, one in host memory from the GPU
+    pq = globals()["pq"] if native else python_binding()
+    c = pq.alloc_kv_cache(pq.FMT_INT4, 64, 2, 128, 64, 4, device="cpu")
+    q, table, lengths = torch.zeros(3, 4, 128, dtype=torch.bfloat16), torch.zeros(3, 4, dtype=torch.int32), torch.zeros(3, dtype=torch.int32)
+    for ws in (torch.zeros(1 << 21, dtype=torch.uint8)[::2], torch.zeros(1 << 20, dtype=torch.uint8, device="meta")):
+        with pytest.raises(pq.PQError, match="workspace"):
+            pq.pq_attn_decode(c, q, table, lengths, 200, 1.0, workspace=ws)
 
 
 SIGNATURES = {
