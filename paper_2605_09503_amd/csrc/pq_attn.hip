@@ -652,7 +652,7 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L>())) void attn_decod
     auto emit = [&](int j0) {
       if (col >= count) return;
       const int64_t q_head = head * per_head + h0 + col;
-      const float inv = l > 0.0f ? 1.0f / l : 0.0f;
+      const float inv = l == 0.0f ? 0.0f : 1.0f / l;                   // NaN stays
       uint16_t* o = a.out + seq * a.out_ld + q_head * a.out_head;
       constexpr int RUN = L::PER < JW ? L::PER : JW;                   // adjacent channels of a lane
 #pragma unroll
@@ -665,7 +665,7 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L>())) void attn_decod
           __builtin_memcpy(__builtin_assume_aligned(o + L::v_channel(kq * 4 + r, j0 + g), RUN * 2), v, RUN * 2);
         }
       if (a.lse && kq == 0 && j0 == 0)
-        a.lse[(int64_t)seq * a.q_heads + q_head] = l > 0.0f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+        a.lse[(int64_t)seq * a.q_heads + q_head] = l == 0.0f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
     };
 
     if (solo) {                                                        // nothing to join; through LDS for one way of storing

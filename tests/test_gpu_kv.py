@@ -330,6 +330,31 @@ def test_pages_outside_are_left_out(fmt, group, dim):
     assert np.all(f64(out)[1] == 0) and bool((lse[1] == -np.inf).all())
 
 
+@pytest.mark.parametrize("n", [5, 120, 4000])              # tokens a sequence: within a block, a workgroup a pair, parts that join
+@pytest.mark.parametrize("fmt,group", [(I4, 64), (NV, 16), (BF, 0)])
+def test_nan_stays_in_its_row(fmt, group, n):
+    rng = np.random.default_rng(14)
+    heads, per, pages = 2, 3, 2 * ((n + 63) // 64)
+    k, v = rows(rng, 2 * n, heads, 128), rows(rng, 2 * n, heads, 128)
+    cache, _ = make_cache(fmt, group, heads, 128, 64, pages, k, v)
+    table = torch.arange(pages, dtype=torch.int32, device=DEV).reshape(2, -1)
+    slots = torch.cat([torch.arange(n), pages // 2 * 64 + torch.arange(n)]).to(DEV)
+    pq.pq_kv_write(cache, k, v, slots)
+    q = torch.randn(2, heads * per, 128, generator=torch.Generator().manual_seed(4)).to(torch.bfloat16).to(DEV)
+    lens = torch.full((2,), n, dtype=torch.int32, device=DEV)
+
+    def call(q):
+        lse = torch.empty(2, heads * per, device=DEV)
+        return pq.pq_attn_decode(cache, q, table, lens, n, 0.09, lse=lse), lse
+    want, want_lse = call(q)
+    q[0, 4, 17] = float("nan")
+    got, lse = call(q)
+    assert bool(got[0, 4].isnan().all()) and bool(lse[0, 4].isnan())       # a part of a context that is NaN may not weigh nothing
+    hit = torch.zeros(2, heads * per, dtype=torch.bool, device=DEV)
+    hit[0, 4] = True
+    assert torch.equal(got[~hit], want[~hit]) and torch.equal(lse[~hit], want_lse[~hit])
+
+
 def test_lengths_beyond_max_len_are_cut():
     rng = np.random.default_rng(13)
     k, v = rows(rng, 96, 1, 64), rows(rng, 96, 1, 64)
