@@ -20,7 +20,6 @@ import torch
 
 FMT_NVFP4, FMT_INT4, FMT_INT3 = 0, 1, 2
 FMT_BF16 = 3            # of a key-value cache only
-FMT_BF16 = 3            # of a key-value cache only
 OP_CALIB_MOMENTS, OP_SELECT_PERM, OP_QUANTIZE_WEIGHTS, OP_QUANTIZE_ACT, OP_QGEMM, OP_QUANT_ERROR, \
     OP_SELECT_PERM_OUTPUT, OP_CHANNEL_STATS, OP_ORDER = range(9)
 CRIT_VARIANCE, CRIT_ABSMAX = 0, 1
@@ -52,12 +51,6 @@ class NormParams(C.Structure):
 class OutputPlan(C.Structure):
     """pq_output_plan of the header."""
     _fields_ = [(n, C.c_int) for n in ("batches", "orders", "tile_m", "tile_n", "tile_waves")]
-
-
-class _KVCacheStruct(C.Structure):
-    """pq_kv_cache of the header."""
-    _fields_ = [("fmt", C.c_int), ("group", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int), ("page", C.c_int),
-                ("pages", C.c_int64), ("data", C.c_void_p), ("k_tensor_scale", C.c_void_p), ("v_tensor_scale", C.c_void_p)]
 
 
 class _KVCacheStruct(C.Structure):
@@ -150,13 +143,6 @@ def _declare(lib):
     lib.pq_attn_decode_workspace_bytes.restype = sz
     lib.pq_attn_decode_workspace_bytes.argtypes = [vp, i64, i32, i64, i64]
     lib.pq_attn_decode.argtypes = [vp, vp, i64, i64, vp, i64, vp, i64, i32, i64, i64, C.c_float, vp, i64, i64, vp, vp, sz, vp]
-    lib.pq_kv_cache_bytes.restype = sz
-    lib.pq_kv_cache_bytes.argtypes = [i32, i32, i32, i32, i32, i64]
-    lib.pq_kv_write.argtypes = [vp, vp, i64, i64, vp, i64, i64, vp, i64, vp]
-    lib.pq_kv_read.argtypes = [vp, vp, i64, vp, i64, i64, vp, i64, i64, vp]
-    lib.pq_attn_decode_workspace_bytes.restype = sz
-    lib.pq_attn_decode_workspace_bytes.argtypes = [vp, i64, i32, i64, i64]
-    lib.pq_attn_decode.argtypes = [vp, vp, i64, i64, vp, i64, vp, i64, i32, i64, i64, C.c_float, vp, i64, i64, vp, vp, sz, vp]
     lib.pq_probe_stream.argtypes = [vp, sz, vp, sz, vp]
     lib.pq_qgemm_check_int_scales.argtypes = [i32, i32, vp, i64, i64, C.POINTER(C.c_int64), vp, sz, vp]
     lib.pq_probe_mfma.argtypes = [i32, vp, C.POINTER(C.c_double), vp]
@@ -201,10 +187,6 @@ _calls = None           # the module, or False where it cannot be had
 
 def _raise(rc: int):
     raise PQError(rc, load().pq_last_error().decode())
-
-
-def _refuse(msg: str):
-    raise PQError(-2, msg)
 
 
 def _refuse(msg: str):
@@ -815,124 +797,6 @@ def pq_attn_decode(cache: KVCache, q: torch.Tensor, table: torch.Tensor, lengths
         _refuse("workspace must be contiguous, on the cache's device")
     _check(load().pq_attn_decode(cache._address, *qr, tab, table.stride(0) if seqs > 1 else table.shape[1], n, seqs, q_heads, max_len, window,
                                  float(scale), *outr, _ptr(lse), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream_of(cache)))
-    return out
-
-
-# ------------------------------------------------------------------------ key-value cache and the attention over it
-@dataclass(frozen=True)
-class KVCache:
-    """A key-value cache (pq_kv_cache of the header): `data` holds pages * page tokens of kv_heads heads."""
-    fmt: int
-    group: int
-    kv_heads: int
-    head_dim: int
-    page: int
-    pages: int
-    data: torch.Tensor
-    k_tensor_scale: Optional[torch.Tensor] = None
-    v_tensor_scale: Optional[torch.Tensor] = None
-
-    def __post_init__(self):
-        need = pq_kv_cache_bytes(self.fmt, self.group, self.kv_heads, self.head_dim, self.page, self.pages)
-        if need == 0:
-            raise PQError(-2, pq_last_error())
-        if self.data.dtype != torch.uint8 or not self.data.is_contiguous() or self.data.numel() < need:
-            _refuse("a cache of %d contiguous bytes is needed" % need)
-        for t in (self.k_tensor_scale, self.v_tensor_scale):
-            if self.fmt == FMT_NVFP4 and (t is None or t.dtype != torch.float32 or t.numel() != 1 or t.device != self.data.device):
-                _refuse("NVFP4 needs the tensor scales of keys and values, one float32 each, on the cache's device")
-        struct = _KVCacheStruct(self.fmt, self.group, self.kv_heads, self.head_dim, self.page, self.pages, self.data.data_ptr(),
-                                _ptr(self.k_tensor_scale), _ptr(self.v_tensor_scale))
-        object.__setattr__(self, "_struct", struct)
-        object.__setattr__(self, "_address", C.addressof(struct))
-
-
-def pq_kv_cache_bytes(fmt: int, group: int, kv_heads: int, head_dim: int, page: int, pages: int) -> int:
-    return int(load().pq_kv_cache_bytes(fmt, group, kv_heads, head_dim, page, pages))
-
-
-def alloc_kv_cache(fmt: int, group: int, kv_heads: int, head_dim: int, page: int, pages: int,
-                   k_tensor_scale: Optional[torch.Tensor] = None, v_tensor_scale: Optional[torch.Tensor] = None,
-                   device="cuda") -> KVCache:
-    """A cache of `pages` pages of `page` tokens; the tensor scales (float32 [1]) are NVFP4's."""
-    need = pq_kv_cache_bytes(fmt, group, kv_heads, head_dim, page, pages)
-    if need == 0:
-        raise PQError(-2, pq_last_error())
-    return KVCache(fmt, group, kv_heads, head_dim, page, pages, torch.empty(need, dtype=torch.uint8, device=device),
-                   k_tensor_scale, v_tensor_scale)
-
-
-def _head_rows(cache: KVCache, name: str, t: torch.Tensor, rows: int, heads: int):
-    """(pointer, stride of a row, stride of a head) of bf16 [rows, heads, head_dim]; strides of one row or head do not matter."""
-    if t.dtype != torch.bfloat16 or tuple(t.shape) != (rows, heads, cache.head_dim) or t.stride(2) != 1 or t.device != cache.data.device:
-        _refuse("%s must be bfloat16 [%d, %d, %d] with adjacent channels, on the cache's device" % (name, rows, heads, cache.head_dim))
-    return t.data_ptr(), t.stride(0) if rows > 1 else 0, t.stride(1) if heads > 1 else 0
-
-
-def _indices(cache: KVCache, name: str, t: torch.Tensor, dtype, dims: int):
-    if t.dtype != dtype or t.dim() != dims or (t.numel() > 1 and t.stride(-1) != 1) or t.device != cache.data.device:
-        _refuse("%s must be %s with %d dimension%s, the last one contiguous, on the cache's device" % (name, dtype, dims, "s" * (dims > 1)))
-    return t.data_ptr()
-
-
-def pq_kv_write(cache: KVCache, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
-    """Quantizes keys and values, bf16 [n, kv_heads, head_dim] (slices of a fused projection's rows are), into the slots (int64 [n])."""
-    s = _indices(cache, "slots", slots, torch.int64, 1)
-    n = slots.shape[0]
-    kr, vr = (_head_rows(cache, name, t, n, cache.kv_heads) for name, t in (("k", k), ("v", v)))
-    _check(load().pq_kv_write(cache._address, *kr, *vr, s, n, _stream()))
-
-
-def pq_kv_read(cache: KVCache, slots: torch.Tensor, k: Optional[torch.Tensor] = None, v: Optional[torch.Tensor] = None):
-    """(k, v) of the slots as bf16 [n, kv_heads, head_dim] (allocated unless given)."""
-    s = _indices(cache, "slots", slots, torch.int64, 1)
-    n = slots.shape[0]
-    k, v = (torch.empty((n, cache.kv_heads, cache.head_dim), dtype=torch.bfloat16, device=cache.data.device) if t is None else t
-            for t in (k, v))
-    kr, vr = (_head_rows(cache, name, t, n, cache.kv_heads) for name, t in (("k", k), ("v", v)))
-    _check(load().pq_kv_read(cache._address, s, n, *kr, *vr, _stream()))
-    return k, v
-
-
-ATTN_DECODE_ZERO_BYTES = 4096       # PQ_ATTN_DECODE_ZERO_BYTES of the header
-
-
-def pq_attn_decode_workspace_bytes(cache: KVCache, seqs: int, q_heads: int, max_len: int, window: int = 0) -> int:
-    return int(load().pq_attn_decode_workspace_bytes(cache._address, seqs, q_heads, max_len, window))
-
-
-def pq_attn_decode_workspace(cache: KVCache, seqs: int, q_heads: int, max_len: int, window: int = 0) -> torch.Tensor:
-    """A workspace for pq_attn_decode with these arguments, or smaller ones: for one stream, call after call."""
-    need = pq_attn_decode_workspace_bytes(cache, seqs, q_heads, max_len, window)
-    if need == 0:
-        raise PQError(-2, pq_last_error())
-    ws = torch.empty(need, dtype=torch.uint8, device=cache.data.device)
-    ws[:ATTN_DECODE_ZERO_BYTES].zero_()
-    return ws
-
-
-def pq_attn_decode(cache: KVCache, q: torch.Tensor, table: torch.Tensor, lengths: torch.Tensor, max_len: int, scale: float,
-                   out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None, window: int = 0,
-                   workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
-    """Attention of one new token a sequence, q bf16 [seqs, q_heads, head_dim], over the lengths[b] (int32) tokens whose pages
-    table[b] (int32) names; out like q (allocated unless given), lse float32 [seqs, q_heads].  max_len: no sequence is longer."""
-    if q.dim() != 3:
-        _refuse("q must be bfloat16 [seqs, q_heads, head_dim]")
-    seqs, q_heads = q.shape[0], q.shape[1]
-    qr = _head_rows(cache, "q", q, seqs, q_heads)
-    tab, n = _indices(cache, "table", table, torch.int32, 2), _indices(cache, "lengths", lengths, torch.int32, 1)
-    if table.shape[0] != seqs or lengths.shape[0] != seqs or table.shape[1] * cache.page < max_len:
-        _refuse("table and lengths must have a row for each of %d sequences, and table the pages of %d tokens" % (seqs, max_len))
-    if lse is not None and (lse.dtype != torch.float32 or tuple(lse.shape) != (seqs, q_heads) or not lse.is_contiguous()
-                            or lse.device != cache.data.device):
-        _refuse("lse must be contiguous float32 [%d, %d] on the cache's device" % (seqs, q_heads))
-    if out is None:
-        out = torch.empty((seqs, q_heads, cache.head_dim), dtype=torch.bfloat16, device=cache.data.device)
-    outr = _head_rows(cache, "out", out, seqs, q_heads)
-    if workspace is None:
-        workspace = pq_attn_decode_workspace(cache, seqs, q_heads, max_len, window)
-    _check(load().pq_attn_decode(cache._address, *qr, tab, table.stride(0) if seqs > 1 else table.shape[1], n, seqs, q_heads, max_len, window,
-                                 float(scale), *outr, _ptr(lse), _ptr(workspace), workspace.numel() * workspace.element_size(), _stream()))
     return out
 
 
