@@ -701,6 +701,12 @@ __global__ __launch_bounds__((64 * kAttnWaves), (waves_of<L>())) void attn_decod
       const int first = entry / fan * fan, n = min(fan, entries - first);     // of the group
       auto slot = [&](int e) { return (uint32_t)part_slot(w_first + e * step, w_first) * kPart; };
       if (n > 1) {
+        // A sum goes to its first part's slot.  Every wave has read that part's (M, l) at the level below before wave 0 stores the sum's;
+        // outputs are read and stored by the same wave.
+        if (level > 0) {
+          asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+          __syncthreads();
+        }
         if (col < count) {
           const uint32_t at = slot(entry);
 #pragma unroll

@@ -250,6 +250,34 @@ def test_one_long_sequence_of_many_queries(fmt, group, dim):
     run_case(fmt, group, dim, [40003], heads=1, per=11, page=1024)
 
 
+@pytest.mark.parametrize("per", [3, 16])                   # sixteen parts joined at a time, and eight
+@pytest.mark.parametrize("fmt,group,dim", [(I4, 64, 128), (NV, 16, 64), (BF, 0, 64), (I4, 128, 256)])
+def test_parts_joined_over_levels(fmt, group, dim, per):
+    # up to 64 parts a pair: sums of parts are joined again, out of the slots that they were read from
+    rng = np.random.default_rng(41)
+    lengths, heads, page = [20011, 9000], 3, 256
+    per_seq = (max(lengths) + page - 1) // page
+    k, v = rows(rng, sum(lengths), heads, dim), rows(rng, sum(lengths), heads, dim)
+    cache, (kt, vt) = make_cache(fmt, group, heads, dim, page, 2 * per_seq, k, v)
+    table = torch.arange(2 * per_seq, dtype=torch.int32, device=DEV).reshape(2, per_seq)
+    slots = torch.cat([b * per_seq * page + torch.arange(n) for b, n in enumerate(lengths)]).to(DEV)
+    pq.pq_kv_write(cache, k, v, slots)
+    q = torch.randn(2, heads * per, dim, generator=torch.Generator().manual_seed(5)).to(torch.bfloat16).to(DEV)
+    lens, ws = torch.tensor(lengths, dtype=torch.int32, device=DEV), pq.pq_attn_decode_workspace(cache, 2, heads * per, max(lengths))
+    results = []
+    for _ in range(100):
+        lse = torch.empty(2, heads * per, device=DEV)
+        results.append((pq.pq_attn_decode(cache, q, table, lens, max(lengths), dim ** -0.5, lse=lse, workspace=ws), lse))
+    out, lse = results[0]
+    for o, l in results[1:]:
+        assert torch.equal(o.view(torch.int16), out.view(torch.int16)) and torch.equal(l, lse)
+    ks, vs = OK.stored(fmt, group, f64(k), kt), OK.stored(fmt, group, f64(v), vt)
+    got, q64, at = f64(out), f64(q), 0
+    for b, n in enumerate(lengths):
+        check(got[b], lse[b].cpu().numpy().astype(np.float64), q64[b], ks[at:at + n], vs[at:at + n], dim ** -0.5, "sequence %d" % b)
+        at += n
+
+
 @pytest.mark.parametrize("fmt,group,dim", [(I4, 32, 64), (NV, 16, 64), (BF, 0, 64), (I4, 128, 128)])
 def test_more_pairs_than_workgroups(fmt, group, dim):
     # sequences of a server's batch: workgroups that end one pair and begin the next
