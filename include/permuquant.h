@@ -554,7 +554,7 @@ size_t pq_kv_cache_bytes(pq_format fmt, int group, int kv_heads, int head_dim, i
  * Quantizes the keys and values of n tokens into the cache: k, v bf16, element (token, head, channel) at
  * token * ld + head * head_ld + channel (slices of the rows of a fused projection are read where they are); strides multiples of 8,
  * pointers 16-byte aligned.  slots: int64 [n] device, distinct; a slot outside 0 .. pages * page - 1 (-1 for a row of padding)
- * keeps nothing.  n may be 0.  Other slots of a page keep what they held: pages fill token by token.
+ * keeps nothing.  n may be 0; ceil(n / 32) * kv_heads < 2^24.  Other slots of a page keep what they held: pages fill token by token.
  */
 int pq_kv_write(const pq_kv_cache* cache, const void* k_bf16, int64_t k_ld, int64_t k_head_ld, const void* v_bf16, int64_t v_ld,
                 int64_t v_head_ld, const int64_t* slots, int64_t n, void* stream);
@@ -577,7 +577,8 @@ int pq_kv_read(const pq_kv_cache* cache, const int64_t* slots, int64_t n, void* 
  * 16-byte aligned.  table: int32 device, (seq, i) at seq * table_ld + i; entries past a sequence's last page are not read.
  * lengths: int32 [seqs] device.  max_len: no length is longer (host; a longer one is cut to it); max_len <= page * table_ld.
  * A page outside 0 .. pages - 1 is not read: its tokens are left out.  What lies in a page behind a sequence's last token or in
- * front of its window does not matter, NaN included.  q_heads: a multiple of kv_heads; seqs * q_heads * (max_len / 32 + 32) <= 2^30.
+ * front of its window does not matter, NaN included.  q_heads: a multiple of kv_heads.  Limits: seqs and
+ * q_heads below 2^16; seqs * q_heads * (max_len / 32 + 32) <= 2^30; seqs * kv_heads * ceil(q_heads / kv_heads / 16) < 2^24.
  * lse: float [seqs, q_heads] or NULL: ln of the sum of exp(scale * q . k), with which outputs over parts of a context are joined.
  * Scores, the softmax's sums and the outputs' are held in fp32; out is rounded once to bf16.
  * NaN in a query or in an attended key gives NaN outputs and lse of that head.

@@ -668,6 +668,9 @@ int pq_qgemm_check_int_scales(pq_format fmt, int group, const void* scales, int6
   return run_check_int_scales(fmt, group, scales, rows, K, bad_count, workspace, as_stream(stream));
 }
 
+// Workgroups of 256 threads that a launch takes: a grid has fewer than 2^32 threads.
+static constexpr int64_t kMostWorkgroups = (1 << 24) - 1;
+
 static const char* kv_cache_error(pq_format fmt, int group, int kv_heads, int head_dim, int page, int64_t pages, int* code) {
   *code = PQ_ERR_FORMAT;
   if (fmt == PQ_FMT_NVFP4) {
@@ -730,8 +733,8 @@ static int check_kv_rows(const char* who, const pq_kv_cache* cache, const void* 
                          int64_t v_ld, int64_t v_head, const int64_t* slots, int64_t n, bool out) {
   int rc = check_kv_cache(who, cache);
   if (rc) return rc;
-  if (n < 0 || n > INT32_MAX || (n / 32 + 1) * cache->kv_heads > INT32_MAX)
-    return fail(PQ_ERR_SHAPE, "%s: n=%lld tokens of %d heads outside 0 .. 2^31 - 1 tokens, or 2^36 of all heads", who, (long long)n,
+  if (n < 0 || n > INT32_MAX || (n + 31) / 32 * cache->kv_heads > kMostWorkgroups)
+    return fail(PQ_ERR_SHAPE, "%s: n=%lld tokens of %d heads: blocks of 32 tokens of all heads must be fewer than 2^24", who, (long long)n,
                 cache->kv_heads);
   if (n == 0) return PQ_OK;
   if (!k || !v || !slots) return fail(PQ_ERR_NULL, "%s: a required pointer is NULL", who);
@@ -761,6 +764,9 @@ static int check_attn_shape(const char* who, const pq_kv_cache* c, int64_t seqs,
   if (seqs < 0 || seqs > 65535) return fail(PQ_ERR_SHAPE, "%s: seqs=%lld outside 0 .. 65535", who, (long long)seqs);
   if (q_heads <= 0 || q_heads > 65535 || q_heads % c->kv_heads)
     return fail(PQ_ERR_SHAPE, "%s: q_heads=%d must be a positive multiple of kv_heads=%d", who, q_heads, c->kv_heads);
+  if (seqs * c->kv_heads * ((q_heads / c->kv_heads + 15) / 16) > kMostWorkgroups)
+    return fail(PQ_ERR_SHAPE, "%s: seqs=%lld sequences of %d heads with %d queries each: sixteens of queries must be fewer than 2^24", who,
+                (long long)seqs, c->kv_heads, q_heads / c->kv_heads);
   if (max_len < 0 || max_len > (1 << 30)) return fail(PQ_ERR_SHAPE, "%s: max_len=%lld outside 0 .. 2^30", who, (long long)max_len);
   if (window < 0) return fail(PQ_ERR_SHAPE, "%s: window=%lld is negative", who, (long long)window);
   if (seqs * q_heads * (max_len / 32 + 32) > (int64_t)1 << 30)

@@ -135,6 +135,20 @@ def test_nothing_to_write():
     assert k.shape == v.shape == (0, 2, 64)
 
 
+def test_the_largest_launch():
+    # 2^24 - 1 workgroups but for a few; every head of every token is the same row, and all but two tokens are padding
+    heads, n, dim = 4095, 4097 * 32, 64
+    x = torch.randn(2, dim, generator=torch.Generator().manual_seed(3)).to(torch.bfloat16).to(DEV)
+    k, v = (t.expand(n, heads, dim) for t in x)
+    cache = pq.alloc_kv_cache(I4, 32, heads, dim, 32, 1)
+    slots = torch.full((n,), -1, dtype=torch.int64, device=DEV)
+    slots[1], slots[n - 1] = 30, 4
+    pq.pq_kv_write(cache, k, v, slots)
+    for got, row in zip(pq.pq_kv_read(cache, torch.tensor([4, 30], device=DEV)), x):
+        want = OK.read_back(I4, 32, f64(row))
+        assert np.array_equal(np.where(bits(got) == 0x8000, 0, bits(got)), np.broadcast_to(np.where(want == 0x8000, 0, want), got.shape))
+
+
 # ------------------------------------------------------------------------ attention
 
 def check(got, got_lse, q64, ks, vs, scale, label=""):

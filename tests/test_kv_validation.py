@@ -182,3 +182,18 @@ def test_native_and_python_signatures(lib, name):  # noqa: F811
     assert str(inspect.signature(getattr(pq, name))) == SIGNATURES[name]
     python = inspect.signature(getattr(python_binding(), name))
     assert [str(p.replace(annotation=p.empty)) for p in python.parameters.values()] == SIGNATURES[name][1:-1].split(", ")
+
+
+def test_more_than_a_launch_takes(lib):  # noqa: F811
+    # 2^24 workgroups of 256 threads are refused by name (the largest that are not go on to the next check)
+    for heads, n in ((1, (1 << 29) - 32), (8, (1 << 26) - 32), (4095, 4097 * 32)):
+        c = cache(kv_heads=heads)
+        w = lambda n: lib.pq_kv_write(c, None, 256, 128, None, 256, 128, None, n, None)
+        r = lambda n: lib.pq_kv_read(c, None, n, None, 256, 128, None, 256, 128, None)
+        for f in (w, r):
+            assert f(n) == PQ_ERR_NULL
+            assert f(n + 1) == PQ_ERR_SHAPE and "2^24" in pq.pq_last_error()
+    size = lambda kv, q, seqs=65535: lib.pq_attn_decode_workspace_bytes(cache(kv_heads=kv), seqs, q, 31, 0)
+    assert size(256, 256) > 0 and size(1, 512) > 0
+    assert size(257, 257) == 0 and "2^24" in pq.pq_last_error()
+    assert size(129, 129 * 3, 65535) > 0 and size(300, 300, 60000) == 0
