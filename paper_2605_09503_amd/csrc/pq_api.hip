@@ -714,8 +714,8 @@ static int check_head_rows(const char* who, const char* name, const void* p, int
   if (!aligned16(p) || ld % 8 || head_ld % 8)
     return fail(PQ_ERR_SHAPE, "%s: %s must be 16-byte aligned and its strides (%lld, %lld) multiples of 8", who, name, (long long)ld,
                 (long long)head_ld);
-  if (ld < 0 || head_ld < 0 || (heads > 1 && head_ld < dim && out) ||
-      (rows > 1 && out && ld < (heads - 1) * head_ld + dim && head_ld < (rows - 1) * ld + dim))
+  if (ld < 0 || head_ld < 0 || (out && heads > 1 && head_ld < dim) || (out && rows > 1 && ld < dim) ||
+      (out && rows > 1 && heads > 1 && ld < (heads - 1) * head_ld + dim && head_ld < (rows - 1) * ld + dim))
     return fail(PQ_ERR_SHAPE, "%s: the rows of %s overlap (strides %lld, %lld)", who, name, (long long)ld, (long long)head_ld);
   return PQ_OK;
 }

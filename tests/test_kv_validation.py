@@ -197,3 +197,18 @@ def test_more_than_a_launch_takes(lib):  # noqa: F811
     assert size(256, 256) > 0 and size(1, 512) > 0
     assert size(257, 257) == 0 and "2^24" in pq.pq_last_error()
     assert size(129, 129 * 3, 65535) > 0 and size(300, 300, 60000) == 0
+
+
+def test_rows_that_overlap(lib):  # noqa: F811
+    # tokens of a head that overlap each other, however far apart the heads lie; heads outermost is a layout like another
+    def read(ld, head, n=3, heads=2):
+        return lib.pq_kv_read(cache(kv_heads=heads), FAKE, n, FAKE, ld, head, ODD, 4096, 512, None)      # v's address ends those that pass
+    for bad in ((64, 1024), (0, 1024), (120, 4096)):
+        assert read(*bad) == PQ_ERR_SHAPE and "rows of k overlap" in pq.pq_last_error(), bad
+    for bad in ((64, 1024), (0, 1 << 20)):
+        assert read(*bad, heads=1) == PQ_ERR_SHAPE and "rows of k overlap" in pq.pq_last_error(), bad
+    for good in ((256, 128), (128, 384), (264, 136), (128, 1024)):
+        assert read(*good) == PQ_ERR_SHAPE and "v must be 16-byte aligned" in pq.pq_last_error(), good
+    assert read(128, 0, heads=1) == read(0, 128, n=1) == PQ_ERR_SHAPE and "v must be 16-byte aligned" in pq.pq_last_error()
+    assert lib.pq_attn_decode(cache(), FAKE, 512, 128, FAKE, 4, FAKE, 3, 4, 200, 0, 1.0, FAKE, 64, 4096, None, FAKE, 1 << 40, None) == PQ_ERR_SHAPE
+    assert "rows of out overlap" in pq.pq_last_error()
