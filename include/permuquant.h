@@ -581,7 +581,8 @@ int pq_kv_read(const pq_kv_cache* cache, const int64_t* slots, int64_t n, void* 
  * q_heads below 2^16; seqs * q_heads * (max_len / 32 + 32) <= 2^30; seqs * kv_heads * ceil(q_heads / kv_heads / 16) < 2^24.
  * lse: float [seqs, q_heads] or NULL: ln of the sum of exp(scale * q . k), with which outputs over parts of a context are joined.
  * Scores, the softmax's sums and the outputs' are held in fp32; out is rounded once to bf16.
- * NaN in a query or in an attended key gives NaN outputs and lse of that head.
+ * NaN in a query gives NaN outputs and lse of that head; in a BF16 cache NaN in an attended key gives them for all queries of its
+ * key head (what the 4-bit formats make of NaN is unspecified, as everywhere).
  * workspace: pq_attn_decode_workspace_bytes(cache, seqs, q_heads, max_len, window) bytes, 16-byte aligned; its first
  * PQ_ATTN_DECODE_ZERO_BYTES must be zero before the first call, and every call leaves them zero.  Calls that may overlap need
  * workspaces of their own.  seqs may be 0.  May be captured into a HIP graph; results are the same bits from run to run.

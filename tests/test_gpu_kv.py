@@ -397,6 +397,34 @@ def test_nan_stays_in_its_row(fmt, group, n):
     assert torch.equal(got[~hit], want[~hit]) and torch.equal(lse[~hit], want_lse[~hit])
 
 
+@pytest.mark.parametrize("n", [5, 120, 4000, 20011])
+def test_nan_in_a_key_of_a_bf16_cache(n):
+    # all queries of its key head, in its sequence, and no others; across parts that join
+    rng = np.random.default_rng(15)
+    heads, per, pages = 2, 3, 2 * ((n + 63) // 64)
+    k, v = rows(rng, 2 * n, heads, 128), rows(rng, 2 * n, heads, 128)
+    cache, _ = make_cache(BF, 0, heads, 128, 64, pages, k, v)
+    table = torch.arange(pages, dtype=torch.int32, device=DEV).reshape(2, -1)
+    slots = torch.cat([torch.arange(n), pages // 2 * 64 + torch.arange(n)]).to(DEV)
+    pq.pq_kv_write(cache, k, v, slots)
+    q = torch.randn(2, heads * per, 128, generator=torch.Generator().manual_seed(6)).to(torch.bfloat16).to(DEV)
+    lens = torch.full((2,), n, dtype=torch.int32, device=DEV)
+
+    def call():
+        lse = torch.empty(2, heads * per, device=DEV)
+        return pq.pq_attn_decode(cache, q, table, lens, n, 0.09, lse=lse), lse
+    want, want_lse = call()
+    at = n + n // 2                                            # a token of the second sequence
+    bad = k[at:at + 1].clone()
+    bad[0, 0, 5] = float("nan")
+    pq.pq_kv_write(cache, bad, v[at:at + 1], slots[at:at + 1])
+    got, lse = call()
+    hit = torch.zeros(2, heads * per, dtype=torch.bool, device=DEV)
+    hit[1, :per] = True
+    assert bool(got[hit].isnan().all()) and bool(lse[hit].isnan().all())
+    assert torch.equal(got[~hit], want[~hit]) and torch.equal(lse[~hit], want_lse[~hit])
+
+
 def test_lengths_beyond_max_len_are_cut():
     rng = np.random.default_rng(13)
     k, v = rows(rng, 96, 1, 64), rows(rng, 96, 1, 64)
