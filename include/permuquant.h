@@ -580,7 +580,12 @@ int pq_kv_read(const pq_kv_cache* cache, const int64_t* slots, int64_t n, void* 
  * front of its window does not matter, NaN included.  q_heads: a multiple of kv_heads.  Limits: seqs and
  * q_heads below 2^16; seqs * q_heads * (max_len / 32 + 32) <= 2^30; seqs * kv_heads * ceil(q_heads / kv_heads / 16) < 2^24.
  * lse: float [seqs, q_heads] or NULL: ln of the sum of exp(scale * q . k), with which outputs over parts of a context are joined.
- * Scores, the softmax's sums and the outputs' are held in fp32; out is rounded once to bf16.
+ * Scores, the softmax's sums and the outputs' are held in fp32; out is rounded once to bf16.  The weights of the product with the
+ * values are rounded: to fp16 (11 bits) by NVFP4 caches, to fp16 after multiplication with the scale of the value's group by INT4
+ * caches, to 16 bits by BF16 caches.  Weights of INT4 lose further bits where weight and scale together are below 2^-20 of the
+ * head's largest (a group of channels at 2^-22 of the largest: 0.5 % of itself, at 2^-26 10 %).  This holds for values of magnitudes
+ * from 2^-80 to 2^90 and products q . k within fp32's range: weighted sums of larger values may overflow, and larger scales of INT4
+ * take bits from lse.
  * NaN in a query gives NaN outputs and lse of that head; in a BF16 cache NaN in an attended key gives them for all queries of its
  * key head (what the 4-bit formats make of NaN is unspecified, as everywhere).
  * workspace: pq_attn_decode_workspace_bytes(cache, seqs, q_heads, max_len, window) bytes, 16-byte aligned; its first

@@ -327,7 +327,10 @@ __device__ __forceinline__ void block_outputs(Values<L>& x, float4_t (&s_)[2], c
     p[i >> 2][i & 3] = w;
     out.l += w;
   }
-  // outputs
+  // Outputs.  The 4-bit formats take a weight (INT4: times its value's scale) in fp16: an error of at most 2^-11 of a token's share,
+  // an eighth of what rounding the output to bf16 may add.  A second fp16 for the rest costs 3 to 6 % (64 sequences up to 24 000 tokens
+  // 192 -> 201 us, 32 up to 4099 27.0 -> 28.4, one of 131 000 35.4 -> 36.4).  Where weight and scale fall below 2^-20 of the largest,
+  // fp16's subnormals take further bits.
   if constexpr (L::FMT == kInt4) {
 #pragma unroll
     for (int g = 0; g < L::NG; ++g) {

@@ -352,6 +352,13 @@ def test_sizes_of_values(fmt, group, dim, big):
     run_case(fmt, group, dim, [500, 33, 1], big=big)
 
 
+@pytest.mark.parametrize("fmt,group,dim", [(I4, 64, 128), (I4, 256, 256), (NV, 16, 128), (BF, 0, 64)])
+@pytest.mark.parametrize("exponent", [-70, 78])            # values of rows() lie some 2^10 to both sides
+def test_ends_of_the_values_range(fmt, group, dim, exponent):
+    run_case(fmt, group, dim, [20011, 33, 1], big=2.0 ** exponent, page=256, heads=1)
+    run_case(fmt, group, dim, [900], big=2.0 ** exponent, scale=0.0)
+
+
 @pytest.mark.parametrize("fmt,group,dim", [(I4, 64, 128), (NV, 16, 128), (BF, 0, 128)])
 def test_pages_outside_are_left_out(fmt, group, dim):
     rng = np.random.default_rng(12)
