@@ -356,7 +356,10 @@ Cache cache_of(PyObject* o) {
   Ref address(PyObject_GetAttrString(o, "_address")), data(PyObject_GetAttrString(o, "data"));
   const at::Tensor* t = tensor(data.p);
   if (!t) fail(PyExc_TypeError, "the cache's data must be a tensor");
-  return Cache{(const pq_kv_cache*)PyLong_AsVoidPtr(address.p), t->device()};
+  const auto* c = (const pq_kv_cache*)PyLong_AsVoidPtr(address.p);
+  if (PyErr_Occurred()) throw PyFailed{};
+  if (!c) fail(PyExc_TypeError, "a key-value cache is required");
+  return Cache{c, t->device()};
 }
 const at::Tensor& as_tensor(PyObject* o, const char* name) {
   const at::Tensor* t = THPVariable_Check(o) ? &THPVariable_Unpack(o) : nullptr;

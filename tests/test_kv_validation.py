@@ -212,3 +212,18 @@ def test_rows_that_overlap(lib):  # noqa: F811
     assert read(128, 0, heads=1) == read(0, 128, n=1) == PQ_ERR_SHAPE and "v must be 16-byte aligned" in pq.pq_last_error()
     assert lib.pq_attn_decode(cache(), FAKE, 512, 128, FAKE, 4, FAKE, 3, 4, 200, 0, 1.0, FAKE, 64, 4096, None, FAKE, 1 << 40, None) == PQ_ERR_SHAPE
     assert "rows of out overlap" in pq.pq_last_error()
+
+
+def test_what_is_no_cache(lib):  # noqa: F811
+    # read as an address and not asked whether it is one, these ended the process
+    import types
+    t, i = torch.zeros(3, 2, 128, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int64)
+    for address in ("no address", None, 0, 1.5):
+        c = types.SimpleNamespace(_address=address, data=torch.zeros(1, dtype=torch.uint8))
+        for f in (lambda: pq.pq_kv_write(c, t, t, i), lambda: pq.pq_kv_read(c, i),
+                  lambda: pq.pq_attn_decode(c, t, i[None].int(), i.int(), 3, 1.0)):
+            with pytest.raises((TypeError, AttributeError)):
+                f()
+    for c in (None, t):
+        with pytest.raises(AttributeError):
+            pq.pq_kv_write(c, t, t, i)
