@@ -148,6 +148,15 @@ void call(F&& f) {
   }
 }
 
+// torch.OutOfMemoryError, as torch's own allocations raise it
+void set_out_of_memory(const char* what) {
+  PyObject* torch = PyImport_ImportModule("torch");
+  PyObject* type = torch ? PyObject_GetAttrString(torch, "OutOfMemoryError") : nullptr;
+  if (type) PyErr_SetString(type, what);
+  Py_XDECREF(type);
+  Py_XDECREF(torch);
+}
+
 // runs a call's body; errors of the interpreter and C++ exceptions of torch become Python exceptions
 template <class F>
 PyObject* guarded(F&& f) {
@@ -157,6 +166,8 @@ PyObject* guarded(F&& f) {
     return nullptr;
   } catch (const c10::IndexError& e) {
     PyErr_SetString(PyExc_IndexError, e.what_without_backtrace());
+  } catch (const c10::OutOfMemoryError& e) {
+    set_out_of_memory(e.what_without_backtrace());
   } catch (const c10::Error& e) {
     PyErr_SetString(PyExc_RuntimeError, e.what_without_backtrace());
   } catch (const std::bad_alloc&) {

@@ -149,6 +149,19 @@ def test_the_largest_launch():
         assert np.array_equal(np.where(bits(got) == 0x8000, 0, bits(got)), np.broadcast_to(np.where(want == 0x8000, 0, want), got.shape))
 
 
+def test_outputs_that_memory_cannot_hold():
+    # what a program catches to give memory back and try again
+    cache = pq.alloc_kv_cache(BF, 0, 4095, 256, 32, 1)
+    slots = torch.full((4097 * 32,), -1, dtype=torch.int64, device=DEV)
+    torch.cuda.empty_cache()
+    torch.cuda.set_per_process_memory_fraction(0.1)
+    try:
+        with pytest.raises(torch.OutOfMemoryError):
+            pq.pq_kv_read(cache, slots)                       # 275 GB
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
+
+
 # ------------------------------------------------------------------------ attention
 
 def check(got, got_lse, q64, ks, vs, scale, label=""):
