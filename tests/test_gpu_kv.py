@@ -513,6 +513,48 @@ def test_graph_replays_and_other_streams(fmt, group, n):
         same_bits(rv, OK.read_back(fmt, group, f64(vn), vt))
 
 
+def example():
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "decode_cache.py")
+    spec = importlib.util.spec_from_file_location("decode_cache", path)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    return module
+
+
+@pytest.mark.parametrize("fmt", ["nvfp4", "int4", "bf16"])
+def test_attention_of_the_example(fmt):
+    """Every write and attention of the example, of its cache and the unquantized one, against the oracle over what was written."""
+    module, steps = example(), 3
+    held, calls = {}, []
+
+    class Watched:
+        def __getattr__(self, name):
+            return getattr(pq, name)
+
+        def pq_kv_write(self, cache, k, v, slots):
+            pq.pq_kv_write(cache, k, v, slots)
+            parts = held.setdefault(id(cache), {})
+            ts = [t.item() if cache.fmt == NV else None for t in (cache.k_tensor_scale, cache.v_tensor_scale)]
+            ks, vs = (OK.stored(cache.fmt, cache.group, f64(t), s) for t, s in zip((k, v), ts))
+            parts.update((int(s), (ks[i], vs[i])) for i, s in enumerate(slots.tolist()))
+
+        def pq_attn_decode(self, cache, q, table, lengths, max_len, scale, workspace):
+            out = pq.pq_attn_decode(cache, q, table, lengths, max_len, scale, workspace=workspace)
+            calls.append(cache.fmt)
+            got, q64, parts = f64(out), f64(q), held[id(cache)]
+            for b, n in enumerate(lengths.tolist()):
+                slots = [int(table[b, t // cache.page]) * cache.page + t % cache.page for t in range(n)]
+                ks, vs = (np.stack([parts[s][i] for s in slots]) for i in (0, 1))
+                check(got[b], None, q64[b], ks, vs, scale, "sequence %d of %d tokens" % (b, n))
+            return out
+
+    module.pq = Watched()
+    module.run(fmt, steps=steps)
+    assert len(calls) == 2 * steps and calls.count(BF) == (2 if fmt == "bf16" else 1) * steps
+
+
 @pytest.mark.parametrize("fmt", ["nvfp4", "int4", "bf16"])
 def test_example(fmt):
     import importlib.util
