@@ -579,6 +579,8 @@ int pq_kv_read(const pq_kv_cache* cache, const int64_t* slots, int64_t n, void* 
  * A page outside 0 .. pages - 1 is not read: its tokens are left out.  What lies in a page behind a sequence's last token or in
  * front of its window does not matter, NaN included.  q_heads: a multiple of kv_heads.  Limits: seqs and
  * q_heads below 2^16; seqs * q_heads * (max_len / 32 + 32) <= 2^30; seqs * kv_heads * ceil(q_heads / kv_heads / 16) < 2^24.
+ * Every wave of a call goes through all lengths: batches of more than some 300 sequences are quicker in calls of about 256 each (1024
+ * sequences of 100 tokens, 8 heads: 131 us in one call, 17 for 256).
  * lse: float [seqs, q_heads] or NULL: ln of the sum of exp(scale * q . k), with which outputs over parts of a context are joined.
  * Scores, the softmax's sums and the outputs' are held in fp32; out is rounded once to bf16.  The weights of the product with the
  * values are rounded: to fp16 (11 bits) by NVFP4 caches, to fp16 after multiplication with the scale of the value's group by INT4

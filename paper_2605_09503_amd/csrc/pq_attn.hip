@@ -13,8 +13,9 @@
 //   64 sequences up to 24 000 tokens, 8 heads of 128, INT4/64: 1.05 GB in 192 us, 5.5 TB/s
 //   one of 131 000 tokens, 8 heads of 128, INT4/128:         138 MB in 35 us, 3.9 TB/s
 //   8 up to 4600 tokens, 24 heads of 128, bf16:          304 MB in 62 us, 4.9 TB/s
-// Short work is bound by the chain of what waits for one another: launch, lengths, plan 2 us; pages, queries, first block 2; the
-// waves' join 1; a part's store, counter and fetch 3.  A call over 19 tokens takes 6 us.
+// Short work is bound by the chain of what waits for one another, by clock stamps of every workgroup: lengths and plan 1.4 to 2.2 us,
+// pages 1.2, first block 0.7 to 2.4, the waves' join 0.6 to 1.8, a part's store and counter 1.1, fetch and sum of parts 1.1 to 2 a
+// level.  A call over 19 tokens takes 6 us.
 //
 // Each wave keeps one block ahead in registers.  Two ahead (4-bit formats, heads up to 128) cost 10 to 30 % in short sequences and
 // gave nothing in long ones; eight waves a workgroup, three or four a SIMD gave less than they cost elsewhere.
@@ -429,6 +430,11 @@ __device__ __forceinline__ void block_outputs(Values<L>& x, float4_t (&s_)[2], c
 //            but 8 of 3000 20.5 us, in a row 25.2; a bound of 64: 55.6 against 52.9 with 2400 pairs, 8 of them of 10 000 tokens.
 //   in a row blocks numbered sequence by sequence, pair by pair, `even` of them a worker: the same work whatever the lengths, at up to
 //            two joins a worker (512 pairs up to 24 000 tokens: 197 us, whole 232).
+//
+// Equal parts of long and short pairs leave an imbalance: 256 pairs up to 4099 tokens get up to 57 blocks a worker over a mean of 41
+// (27 us, and half of the workers have ended their blocks by 18).
+// Every wave goes through all lengths, so many sequences cost their number squared: 100 tokens, 8 heads, 32 queries, INT4: 256
+// sequences 17 us, 1024 131, 4096 1580, 16 384 27 000, 65 535 433 000.  Past some 300 sequences, calls of 256 each are quicker.
 struct Lengths {           // of a sequence: first attended token and end, first block, blocks (at least one)
   int first_token, end, first, n;
 };

@@ -3,6 +3,8 @@
 // one side, 0.5 and the scales on the other.  Measured (MI355X; a copy of 4 GiB runs at 4.9 TB/s):
 //   65 000 tokens, 8 heads of 128, NVFP4, 341 MB each way: written in 70 us (4.9 TB/s), read back in 53 (6.4)
 //   14 400 tokens, 8 heads of 128, INT4/32, 75 MB:         written in 19 us (4.0 TB/s), read back in 17 (4.4)
+//   65 000 tokens, 8 heads of 128, bf16, 532 MB:           written in 109 us (4.9 TB/s), read back in 101 (5.3)
+//   30 000 tokens, 4 heads of 256, bf16, 246 MB:           written in 63 us (3.9 TB/s), read back in 56 (4.4)
 // One token of 16 sequences takes 3.3 us, 650 tokens read back 4.2: a launch and three loads in a row (slot, row, scale).
 #include "pq_kv.h"
 #include "pq_qgemm_common.h"
