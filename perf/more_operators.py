@@ -202,15 +202,20 @@ def _keep(state):
     """What a program that uses the library keeps: weights in the product's layout, buffers of activations, a workspace."""
     from paper_2605_09503_amd import pq
     case = state["case"]
+    kind, K = case["kind"], case.get("K")
     state["pq"] = pq
-    if case["kind"] in ("quantize", "linear", "experts"):
-        state["act"] = pq.alloc_quantized(pq.FMT_MXFP4, BLOCK, state["x"].shape[0], case["K"])
-    if case["kind"] == "linear":
+    if kind == "quantize":
+        state["codes"], state["scales"] = pq.alloc_quantized(pq.FMT_MXFP4, BLOCK, case["M"], K)
+    elif kind == "linear":
         state["w"] = pq.pq_pack_operand(pq.FMT_MXFP4, BLOCK, state.pop("codes"), state.pop("scales"))
-    elif case["kind"] == "experts":
+    elif kind == "experts":
         state["w"] = pq.pack_experts(state.pop("codes"), state.pop("scales"), case["E"])
-    elif case["kind"] == "route":
+    elif kind == "route":
+        state["out"] = pq.alloc_route(case["T"], case["E"], case["k"])
         state["workspace"] = pq.pq_moe_route_workspace(case["T"], case["E"], case["k"])
+    if kind in ("linear", "experts"):
+        rows = state["x"].shape[0]
+        state["operand"] = torch.empty(pq.pq_operand_bytes(pq.FMT_MXFP4, BLOCK, rows, K), dtype=torch.uint8, device=DEV)
 
 
 # ------------------------------------------------------------------------ one pass
@@ -222,18 +227,26 @@ def run(state):
 def _run_own(state):
     case, pq = state["case"], state["pq"]
     kind = case["kind"]
+    if kind == "quantize":
+        pq.pq_quantize_act(pq.FMT_MXFP4, BLOCK, state["x"], None, None, state["codes"], state["scales"])
+        return pq.pq_dequantize(pq.FMT_MXFP4, BLOCK, state["codes"], state["scales"])
     if kind == "route":
-        r = pq.pq_moe_route(state["logits"], case["k"], renormalize=case["renormalize"], workspace=state["workspace"])
+        r = pq.pq_moe_route(state["logits"], case["k"], case["renormalize"], out=state["out"], workspace=state["workspace"])
         return r.ids, r.weights, r.offsets, r.rows, r.positions
     if kind == "combine":
         return pq.pq_moe_combine(state["y"], state["positions"], state["weights"], addend=state["addend"])
-    codes, scales = state["act"]
-    pq.pq_quantize_act(pq.FMT_MXFP4, BLOCK, state["x"], None, None, codes, scales)
-    if kind == "quantize":
-        return pq.pq_mx_dequantize(codes, scales)
-    if kind == "linear":
-        return pq.pq_mx_gemm(codes, scales, state["w"], case["N"], bias=state["bias"])
-    return pq.pq_mx_gemm_grouped(codes, scales, state["w"], case["N"], state["offsets"], rows=state["tokens"], bias=state["bias"])
+    N, K = case["N"], case["K"]
+    a = pq.pq_quantize_act_packed(pq.FMT_MXFP4, BLOCK, state["x"], None, state["operand"])
+    M = case["M"] if kind == "linear" else case["T"] * case["k"]
+    y = torch.empty(M, (N + 7) // 8 * 8, dtype=torch.bfloat16, device=DEV)[:, :N]
+    if kind == "experts":
+        pq.pq_qgemm_grouped(pq.FMT_MXFP4, BLOCK, a, state["x"].shape[0], state["w"], state["offsets"], y, N, K, rows=state["tokens"],
+                            bias=state["bias"])
+    elif case["bias"]:
+        pq.pq_qgemm_packed_bias(pq.FMT_MXFP4, BLOCK, a, None, state["w"], None, state["bias"], y, M, N, K)
+    else:
+        pq.pq_qgemm_packed(pq.FMT_MXFP4, BLOCK, a, None, state["w"], None, y, M, N, K)
+    return y
 
 
 # ---- plain form: elementary torch operations in 32 bits, rounded once at the end
