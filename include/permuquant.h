@@ -57,8 +57,8 @@
 extern "C" {
 #endif
 
-/* PQ_FMT_BF16 (the values as they are) is a format of the key-value cache only. */
-typedef enum { PQ_FMT_NVFP4 = 0, PQ_FMT_INT4 = 1, PQ_FMT_INT3 = 2, PQ_FMT_BF16 = 3 } pq_format;
+/* PQ_FMT_BF16 (the values as they are) is a format of the key-value cache only; PQ_FMT_MXFP4 one of the calls that name it. */
+typedef enum { PQ_FMT_NVFP4 = 0, PQ_FMT_INT4 = 1, PQ_FMT_INT3 = 2, PQ_FMT_BF16 = 3, PQ_FMT_MXFP4 = 4 } pq_format;
 
 typedef enum {
   PQ_OP_CALIB_MOMENTS = 0,
@@ -81,7 +81,7 @@ typedef enum {
 
 #define PQ_MAX_ALPHAS 15
 
-/* Offered (format, group) pairs: NVFP4 with 16; INT4 and INT3 with 32, 64, 128 or 256.
+/* Offered (format, group) pairs: NVFP4 with 16; INT4 and INT3 with 32, 64, 128 or 256; MXFP4 with 32.
  * K must be a multiple of the group size (hence of 16).                                     */
 
 /* Message of the last failure on this thread ("" if none). Never NULL. Host memory owned by
@@ -600,6 +600,74 @@ int pq_attn_decode(const pq_kv_cache* cache, const void* q_bf16, int64_t q_ld, i
                    int64_t table_ld, const int32_t* lengths, int64_t seqs, int q_heads, int64_t max_len, int64_t window, float scale,
                    void* out_bf16, int64_t out_ld, int64_t out_head_ld, float* lse, void* workspace, size_t workspace_bytes,
                    void* stream);
+
+/*
+ * MXFP4 (OCP microscaling formats, version 1.0), the 4-bit format that the matrix unit multiplies as it is stored: E2M1 elements as
+ * NVFP4's, one scale 2^(byte - 127) for 32 channels (byte 255: NaN), no tensor scale.
+ *   byte = clamp(floor(log2 amax) - 2 + 127, 0, 252),  code = sign(x) << 3 | E2M1_rne_sat(|x| / 2^(byte - 127))   (ties to the even code)
+ * exactly, for every finite bf16 value; a group of zeros has byte 0.  An infinity or a NaN gives its group byte 255: all of it, and the
+ * outputs that it takes part in, are NaN.  Stored as the other formats: codes [rows, K / 2], scales uint8 [rows, K / 32].
+ *
+ * The format of pq_quantize_act, pq_quantize_weights (tensor_scale_out receives 1), pq_operand_bytes, pq_pack_operand,
+ * pq_quantize_act_packed, pq_qgemm_packed, pq_qgemm_packed_bias and pq_qgemm_packed_f32, with group 32, any K that is a multiple of 32,
+ * tensor scales ignored, and of the calls below; other calls refuse it with PQ_ERR_FORMAT.  Its operands are panels of 256 channels,
+ * zero from K on (pq_operand_bytes counts them).
+ * Products are exact, sums fp32 over the whole of K, in an order that depends on M, N and K.
+ */
+
+/*
+ * The values that stored codes and scales stand for, as bf16 [rows, ldy]: code * scale (* tensor scale, NVFP4) in binary32, rounded to
+ * nearest even (MXFP4: exact below 2^128).  All formats; arguments as for pq_quantize_act.  rows and K at most 2^24; ldy >= K, a multiple
+ * of 8.
+ */
+int pq_dequantize(pq_format fmt, int group, const uint8_t* codes, const void* scales, const float* tensor_scale, int64_t rows, int64_t K,
+                  void* y_bf16, int64_t ldy, void* stream);
+
+/*
+ * Products grouped by expert (MXFP4): rows offsets[e] .. offsets[e + 1] - 1 of y are rows of A times expert e's weights,
+ *   y[i, n] = sum_k A[rows[i], k] W_e[n, k] (+ bias[e, n]),    rows[i] = i where rows is NULL,
+ * with the arithmetic of pq_qgemm_packed.
+ *
+ * a_operand: a_rows rows, as pq_quantize_act_packed leaves them (tokens once, however many experts they go to).
+ * w_operands: one operand an expert, as pq_pack_operand makes it of N rows, pq_operand_bytes(fmt, group, N, K) bytes apart.
+ * offsets: int32 [experts + 1] device, non-decreasing; values outside 0 .. M are cut to it.  Experts without rows cost nothing.
+ * rows: int32 [M] device or NULL (then a_rows >= M).  A row whose index is outside 0 .. a_rows - 1 is left as it was.
+ * M: rows of y, an upper bound of offsets[experts] (host); what lies outside offsets[0] .. offsets[experts] - 1 is left as it was.
+ * bias: bf16 [experts, N] or NULL.  y: bf16 [M, ldy].  M and a_rows may be 0; experts at most 65536.  May be captured into a graph.
+ */
+int pq_qgemm_grouped(pq_format fmt, int group, const void* a_operand, int64_t a_rows, const void* w_operands, int experts,
+                     const int32_t* offsets, const int32_t* rows, int64_t M, int64_t N, int64_t K, const void* bias_bf16, void* y_bf16,
+                     int64_t ldy, void* stream);
+
+/*
+ * Routing of tokens to experts.  Of every token's logits the k largest, largest first (equal logits: the lower index first), and the
+ * order in which the experts' rows stand:
+ *   ids[t, j]        the expert;  weights[t, j]  its softmax weight, over the chosen experts (renormalize != 0) or over all of them
+ *   offsets[e]       rows of experts before e (offsets[experts]: all rows)
+ *   positions[t, j]  the row of (t, j); rows of an expert are in the order of their tokens;  rows[positions[t, j]] = t
+ * An expert whose logit is -inf or NaN is not chosen.  Where fewer than k are left (none in a row of padding that is -inf throughout) the
+ * rest has id -1, weight 0 and position -1, and takes no row; rows from offsets[experts] on are -1.  Weights where a logit is +inf are
+ * unspecified.
+ *
+ * logits: float or bf16 [tokens, ld], ld >= experts.  ids, positions: int32 [tokens, k]; weights: float [tokens, k]; offsets: int32
+ * [experts + 1]; rows: int32 [tokens * k].  tokens 0 .. 2^24, experts 1 .. 1024, k 1 .. min(32, experts).  Softmax in binary32.
+ * workspace: pq_moe_route_workspace_bytes(...) bytes, need not be initialised; calls that may overlap need workspaces of their own.
+ * May be captured into a graph; the same bits from run to run.
+ */
+typedef enum { PQ_LOGITS_F32 = 0, PQ_LOGITS_BF16 = 1 } pq_logits;
+size_t pq_moe_route_workspace_bytes(int64_t tokens, int experts, int k);
+int pq_moe_route(pq_logits type, const void* logits, int64_t tokens, int experts, int64_t ld, int k, int renormalize, int32_t* ids,
+                 float* weights, int32_t* offsets, int32_t* rows, int32_t* positions, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * The weighted sum of the rows that a token's experts made, in binary32 (j ascending), rounded once to bf16:
+ *   out[t, n] = addend[t, n] + sum_j weights[t, j] * y[positions[t, j], n]          (addend NULL: 0)
+ * y: bf16 [rows, y_ld]; positions: int32 [tokens, k], outside 0 .. rows - 1: left out (NaN in other rows does not matter); weights: float
+ * [tokens, k]; addend, out: bf16 [tokens, ld]; strides >= N and multiples of 8.  out may be addend itself (the same strides), but
+ * overlaps neither it otherwise nor y.  tokens 0 .. 2^24, k 1 .. 32.
+ */
+int pq_moe_combine(const void* y_bf16, int64_t rows, int64_t y_ld, const int32_t* positions, const float* weights, int64_t tokens, int k,
+                   int64_t N, const void* addend_bf16, int64_t addend_ld, void* out_bf16, int64_t out_ld, void* stream);
 
 /*
  * Measurement aids (no part of the method and not covered by the version contract of the calls above:

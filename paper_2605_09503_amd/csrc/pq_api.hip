@@ -23,6 +23,7 @@ int check_hip(hipError_t e, const char* what) {
 }
 
 int check_format(pq_format fmt, int group, int64_t K) {
+  if (fmt == PQ_FMT_MXFP4) return fail(PQ_ERR_FORMAT, "MXFP4 is not a format of this call");
   if (fmt != PQ_FMT_NVFP4 && fmt != PQ_FMT_INT4 && fmt != PQ_FMT_INT3)
     return fail(PQ_ERR_FORMAT, "unknown format %d", (int)fmt);
   if (fmt == PQ_FMT_NVFP4) {
@@ -32,6 +33,13 @@ int check_format(pq_format fmt, int group, int64_t K) {
   }
   if (K <= 0) return fail(PQ_ERR_SHAPE, "K must be positive, got %lld", (long long)K);
   if (K % group) return fail(PQ_ERR_SHAPE, "K=%lld is not a multiple of group=%d", (long long)K, group);
+  return PQ_OK;
+}
+
+int check_linear_format(pq_format fmt, int group, int64_t K) {
+  if (fmt != PQ_FMT_MXFP4) return check_format(fmt, group, K);
+  if (group != 32) return fail(PQ_ERR_FORMAT, "MXFP4 uses groups of 32, got %d", group);
+  if (K <= 0 || K % 32) return fail(PQ_ERR_SHAPE, "K=%lld must be a positive multiple of 32", (long long)K);
   return PQ_OK;
 }
 
@@ -233,10 +241,10 @@ int pq_quantize_weights(pq_format fmt, int group, const void* w, int64_t N, int6
                         void* stream) {
   if (!w || !codes || !scales || !tensor_scale_out)
     return fail(PQ_ERR_NULL, "pq_quantize_weights: a required pointer is NULL");
-  int rc = check_format(fmt, group, K);
+  int rc = check_linear_format(fmt, group, K);
   if (rc) return rc;
   if (N <= 0) return fail(PQ_ERR_SHAPE, "pq_quantize_weights: N=%lld must be positive", (long long)N);
-  if (!aligned16(w) || !aligned16(codes) || !aligned16(scales))
+  if (!aligned16(w) || !aligned16(codes) || !aligned16(scales) || (fmt == PQ_FMT_MXFP4 && !aligned16(perm)))
     return fail(PQ_ERR_SHAPE, "pq_quantize_weights: tensors must be 16-byte aligned");
   hipStream_t st = as_stream(stream);
   if (fmt == PQ_FMT_NVFP4) {
@@ -245,6 +253,7 @@ int pq_quantize_weights(pq_format fmt, int group, const void* w, int64_t N, int6
     rc = launch_fill_float(tensor_scale_out, 1.0f, st);
   }
   if (rc) return rc;
+  if (fmt == PQ_FMT_MXFP4) return launch_mx_quantize_rows(w, N, K, K, perm, codes, scales, st);
   return launch_quantize_rows(fmt, group, w, N, K, K, perm, tensor_scale_out, codes, scales, st);
 }
 
@@ -252,7 +261,7 @@ int pq_quantize_act(pq_format fmt, int group, const void* x, int64_t M, int64_t 
                     const int32_t* perm, const float* tensor_scale, uint8_t* codes, void* scales,
                     void* stream) {
   if (!x || !codes || !scales) return fail(PQ_ERR_NULL, "pq_quantize_act: a required pointer is NULL");
-  int rc = check_format(fmt, group, K);
+  int rc = check_linear_format(fmt, group, K);
   if (rc) return rc;
   if (fmt == PQ_FMT_NVFP4 && !tensor_scale)
     return fail(PQ_ERR_NULL, "pq_quantize_act: NVFP4 needs the per-tensor scale");
@@ -262,6 +271,10 @@ int pq_quantize_act(pq_format fmt, int group, const void* x, int64_t M, int64_t 
                 (long long)ld, (long long)K);
   if (!aligned16(x) || !aligned16(codes) || !aligned16(scales))
     return fail(PQ_ERR_SHAPE, "pq_quantize_act: tensors must be 16-byte aligned");
+  if (fmt == PQ_FMT_MXFP4) {
+    if (!aligned16(perm)) return fail(PQ_ERR_SHAPE, "pq_quantize_act: perm must be 16-byte aligned");
+    return launch_mx_quantize_rows(x, M, K, ld, perm, codes, scales, as_stream(stream));
+  }
   return launch_quantize_rows(fmt, group, x, M, K, ld, perm, tensor_scale, codes, scales,
                               as_stream(stream));
 }
@@ -355,7 +368,8 @@ int pq_select_output_plan(pq_format fmt, int group, int64_t M, int64_t N, int64_
 }
 
 size_t pq_operand_bytes(pq_format fmt, int group, int64_t rows, int64_t K) {
-  if (check_format(fmt, group, K) || rows <= 0 || K % 32) return 0;
+  if (check_linear_format(fmt, group, K) || rows <= 0 || K % 32) return 0;
+  if (fmt == PQ_FMT_MXFP4) return rows > (1 << 24) || K > (1 << 24) ? 0 : mx_operand_bytes(rows, K);
   return operand_bytes(fmt, group, rows, K);
 }
 
@@ -363,16 +377,17 @@ static int pack_operand_common(const char* name, pq_format fmt, int group, const
                                int64_t rows, int64_t K, void* operand, size_t operand_size, bool dense3,
                                void* stream) {
   if (!codes || !scales || !operand) return fail(PQ_ERR_NULL, "%s: a required pointer is NULL", name);
-  int rc = check_format(fmt, group, K);
+  int rc = check_linear_format(fmt, group, K);
   if (rc) return rc;
   if (rows <= 0) return fail(PQ_ERR_SHAPE, "%s: rows=%lld must be positive", name, (long long)rows);
   if (K % 32) return fail(PQ_ERR_SHAPE, "%s: K=%lld must be a multiple of 32", name, (long long)K);
   if (rows > (1 << 24) || K > (1 << 24)) return fail(PQ_ERR_SHAPE, "%s: a dimension exceeds 2^24", name);
   if (!aligned16(codes) || !aligned16(scales) || !aligned16(operand))
     return fail(PQ_ERR_SHAPE, "%s: buffers must be 16-byte aligned", name);
-  const size_t need = operand_bytes(fmt, group, rows, K);
+  const size_t need = fmt == PQ_FMT_MXFP4 ? mx_operand_bytes(rows, K) : operand_bytes(fmt, group, rows, K);
   if (operand_size < need)
     return fail(PQ_ERR_WORKSPACE, "%s: operand buffer of %zu bytes needed, %zu given", name, need, operand_size);
+  if (fmt == PQ_FMT_MXFP4) return launch_mx_pack(codes, scales, rows, K, operand, as_stream(stream));
   return run_pack_operand(fmt, group, codes, scales, rows, K, operand, dense3, as_stream(stream));
 }
 
@@ -420,7 +435,7 @@ int pq_quantize_act_packed(pq_format fmt, int group, const void* x, int64_t M, i
   if (!x || !operand) return fail(PQ_ERR_NULL, "pq_quantize_act_packed: a required pointer is NULL");
   if ((codes == nullptr) != (scales == nullptr))
     return fail(PQ_ERR_NULL, "pq_quantize_act_packed: give both of codes and scales or neither");
-  int rc = check_format(fmt, group, K);
+  int rc = check_linear_format(fmt, group, K);
   if (rc) return rc;
   if (fmt == PQ_FMT_NVFP4 && !tensor_scale)
     return fail(PQ_ERR_NULL, "pq_quantize_act_packed: NVFP4 needs the per-tensor scale");
@@ -432,10 +447,11 @@ int pq_quantize_act_packed(pq_format fmt, int group, const void* x, int64_t M, i
                 (long long)ld, (long long)K);
   if (!aligned16(x) || !aligned16(operand) || !aligned16(codes) || !aligned16(scales))
     return fail(PQ_ERR_SHAPE, "pq_quantize_act_packed: buffers must be 16-byte aligned");
-  const size_t need = operand_bytes(fmt, group, M, K);
+  const size_t need = fmt == PQ_FMT_MXFP4 ? mx_operand_bytes(M, K) : operand_bytes(fmt, group, M, K);
   if (operand_size < need)
     return fail(PQ_ERR_WORKSPACE, "pq_quantize_act_packed: operand buffer of %zu bytes needed, %zu given", need,
                 operand_size);
+  if (fmt == PQ_FMT_MXFP4) return launch_mx_quantize_operand(x, M, K, ld, operand, codes, scales, as_stream(stream));
   return run_quantize_packed(fmt, group, x, M, K, ld, tensor_scale, operand, codes, scales, as_stream(stream));
 }
 
@@ -614,7 +630,7 @@ static int qgemm_packed_common(pq_format fmt, int group, const void* a_operand, 
                                const void* w_operand, const float* w_ts, int64_t M, int64_t N, int64_t K,
                                const void* bias, void* y, int64_t ldy, bool out_f32, void* stream) {
   if (!a_operand || !w_operand || !y) return fail(PQ_ERR_NULL, "pq_qgemm_packed: a required pointer is NULL");
-  int rc = check_format(fmt, group, K);
+  int rc = check_linear_format(fmt, group, K);
   if (rc) return rc;
   if (fmt == PQ_FMT_NVFP4 && (!a_ts || !w_ts))
     return fail(PQ_ERR_NULL, "pq_qgemm_packed: NVFP4 needs both per-tensor scales");
@@ -628,6 +644,10 @@ static int qgemm_packed_common(pq_format fmt, int group, const void* a_operand, 
                 (long long)ldy, (long long)N);
   if (!aligned16(a_operand) || !aligned16(w_operand) || !aligned16(y) || !aligned16(bias))
     return fail(PQ_ERR_SHAPE, "pq_qgemm_packed: buffers must be 16-byte aligned");
+  if (fmt == PQ_FMT_MXFP4)
+    return run_mx_gemm(MxCall{(const uint8_t*)a_operand, M, (const uint8_t*)w_operand, 0, 1, nullptr, nullptr, M, N, K, (const uint16_t*)bias, y,
+                              ldy, out_f32},
+                       as_stream(stream));
   return run_qgemm_packed(fmt, group, a_operand, a_ts, w_operand, w_ts, M, N, K, bias, y, ldy, out_f32,
                           as_stream(stream));
 }
@@ -805,6 +825,94 @@ int pq_attn_decode(const pq_kv_cache* cache, const void* q, int64_t q_ld, int64_
   const AttnCall a{(const uint16_t*)q, q_ld, q_head_ld, table, table_ld, lengths, (int)seqs, q_heads, (int)max_len,
                    window >= max_len ? 0 : (int)window, scale, (uint16_t*)out, out_ld, out_head_ld, lse, workspace};
   return run_attn_decode(*cache, a, as_stream(stream));
+}
+
+int pq_dequantize(pq_format fmt, int group, const uint8_t* codes, const void* scales, const float* tensor_scale, int64_t rows, int64_t K,
+                  void* y, int64_t ldy, void* stream) {
+  const char* who = "pq_dequantize";
+  if (!codes || !scales || !y) return fail(PQ_ERR_NULL, "%s: a required pointer is NULL", who);
+  int rc = check_linear_format(fmt, group, K);
+  if (rc) return rc;
+  if (fmt == PQ_FMT_NVFP4 && !tensor_scale) return fail(PQ_ERR_NULL, "%s: NVFP4 needs the per-tensor scale", who);
+  if (rows <= 0 || rows > (1 << 24) || K > (1 << 24))
+    return fail(PQ_ERR_SHAPE, "%s: rows=%lld K=%lld outside 1 .. 2^24", who, (long long)rows, (long long)K);
+  if (ldy < K || ldy % 8)
+    return fail(PQ_ERR_SHAPE, "%s: ldy=%lld must be >= K=%lld and a multiple of 8", who, (long long)ldy, (long long)K);
+  if (!aligned16(codes) || !aligned16(scales) || !aligned16(y)) return fail(PQ_ERR_SHAPE, "%s: tensors must be 16-byte aligned", who);
+  return launch_dequantize(fmt, group, codes, scales, tensor_scale, rows, K, y, ldy, as_stream(stream));
+}
+
+int pq_qgemm_grouped(pq_format fmt, int group, const void* a_operand, int64_t a_rows, const void* w_operands, int experts,
+                     const int32_t* offsets, const int32_t* rows, int64_t M, int64_t N, int64_t K, const void* bias, void* y, int64_t ldy,
+                     void* stream) {
+  const char* who = "pq_qgemm_grouped";
+  if (fmt != PQ_FMT_MXFP4) return fail(PQ_ERR_FORMAT, "%s: MXFP4 only, got format %d", who, (int)fmt);
+  int rc = check_linear_format(fmt, group, K);
+  if (rc) return rc;
+  if (experts <= 0 || experts > 65536) return fail(PQ_ERR_SHAPE, "%s: experts=%d outside 1 .. 65536", who, experts);
+  if (M < 0 || M > (1 << 24) || a_rows < 0 || a_rows > (1 << 24) || N <= 0 || N > (1 << 24) || K > (1 << 24))
+    return fail(PQ_ERR_SHAPE, "%s: M=%lld a_rows=%lld N=%lld K=%lld: M and a_rows 0 .. 2^24, N and K 1 .. 2^24", who, (long long)M,
+                (long long)a_rows, (long long)N, (long long)K);
+  if (!rows && a_rows < M)
+    return fail(PQ_ERR_SHAPE, "%s: a_rows=%lld rows cannot make M=%lld without an index", who, (long long)a_rows, (long long)M);
+  if (M == 0 || a_rows == 0) return PQ_OK;
+  if (!a_operand || !w_operands || !offsets || !y) return fail(PQ_ERR_NULL, "%s: a required pointer is NULL", who);
+  if (ldy < N || ldy % 8) return fail(PQ_ERR_SHAPE, "%s: ldy=%lld must be >= N=%lld and a multiple of 8", who, (long long)ldy, (long long)N);
+  if (!aligned16(a_operand) || !aligned16(w_operands) || !aligned16(y) || !aligned16(bias))
+    return fail(PQ_ERR_SHAPE, "%s: buffers must be 16-byte aligned", who);
+  if (((uintptr_t)offsets | (uintptr_t)rows) & 3) return fail(PQ_ERR_SHAPE, "%s: offsets and rows must be 4-byte aligned", who);
+  return run_mx_gemm(MxCall{(const uint8_t*)a_operand, a_rows, (const uint8_t*)w_operands, mx_operand_bytes(N, K), experts, offsets, rows, M, N,
+                            K, (const uint16_t*)bias, y, ldy, false},
+                     as_stream(stream));
+}
+
+static int check_route(const char* who, int64_t tokens, int experts, int k) {
+  if (tokens < 0 || tokens > (1 << 24)) return fail(PQ_ERR_SHAPE, "%s: tokens=%lld outside 0 .. 2^24", who, (long long)tokens);
+  if (experts <= 0 || experts > 1024) return fail(PQ_ERR_SHAPE, "%s: experts=%d outside 1 .. 1024", who, experts);
+  if (k <= 0 || k > 32 || k > experts) return fail(PQ_ERR_SHAPE, "%s: k=%d outside 1 .. 32, or above experts=%d", who, k, experts);
+  return PQ_OK;
+}
+
+size_t pq_moe_route_workspace_bytes(int64_t tokens, int experts, int k) {
+  return check_route("pq_moe_route_workspace_bytes", tokens, experts, k) ? 0 : moe_route_workspace_bytes(tokens, experts);
+}
+
+int pq_moe_route(pq_logits type, const void* logits, int64_t tokens, int experts, int64_t ld, int k, int renormalize, int32_t* ids,
+                 float* weights, int32_t* offsets, int32_t* rows, int32_t* positions, void* workspace, size_t workspace_bytes, void* stream) {
+  const char* who = "pq_moe_route";
+  if (type != PQ_LOGITS_F32 && type != PQ_LOGITS_BF16) return fail(PQ_ERR_FORMAT, "%s: unknown type of logits %d", who, (int)type);
+  int rc = check_route(who, tokens, experts, k);
+  if (rc) return rc;
+  if (!offsets || (tokens && (!logits || !ids || !weights || !rows || !positions)))
+    return fail(PQ_ERR_NULL, "%s: a required pointer is NULL", who);
+  if (ld < experts) return fail(PQ_ERR_SHAPE, "%s: ld=%lld < experts=%d", who, (long long)ld, experts);
+  if (((uintptr_t)logits & (type == PQ_LOGITS_F32 ? 3 : 1)) ||
+      (((uintptr_t)ids | (uintptr_t)weights | (uintptr_t)offsets | (uintptr_t)rows | (uintptr_t)positions) & 3))
+    return fail(PQ_ERR_SHAPE, "%s: every array must be aligned to its elements", who);
+  const size_t need = moe_route_workspace_bytes(tokens, experts);
+  if (!workspace || workspace_bytes < need)
+    return fail(PQ_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", who, need, workspace ? workspace_bytes : (size_t)0);
+  if (!aligned16(workspace)) return fail(PQ_ERR_SHAPE, "%s: workspace must be 16-byte aligned", who);
+  return run_moe_route(RouteCall{logits, type == PQ_LOGITS_BF16, tokens, ld, experts, k, renormalize != 0, ids, weights, offsets, rows, positions},
+                       workspace, as_stream(stream));
+}
+
+int pq_moe_combine(const void* y, int64_t rows, int64_t y_ld, const int32_t* positions, const float* weights, int64_t tokens, int k, int64_t N,
+                   const void* addend, int64_t addend_ld, void* out, int64_t out_ld, void* stream) {
+  const char* who = "pq_moe_combine";
+  if (tokens < 0 || tokens > (1 << 24) || rows < 0 || rows > INT32_MAX || k <= 0 || k > 32 || N <= 0 || N > (1 << 24))
+    return fail(PQ_ERR_SHAPE, "%s: tokens=%lld rows=%lld k=%d N=%lld: tokens 0 .. 2^24, rows 0 .. 2^31 - 1, k 1 .. 32, N 1 .. 2^24", who,
+                (long long)tokens, (long long)rows, k, (long long)N);
+  if (tokens == 0) return PQ_OK;
+  if ((rows && !y) || !positions || !weights || !out) return fail(PQ_ERR_NULL, "%s: a required pointer is NULL", who);
+  if (y_ld < N || y_ld % 8 || out_ld < N || out_ld % 8 || (addend && (addend_ld < N || addend_ld % 8)))
+    return fail(PQ_ERR_SHAPE, "%s: row strides %lld, %lld, %lld must be >= N=%lld and multiples of 8", who, (long long)y_ld, (long long)out_ld,
+                (long long)addend_ld, (long long)N);
+  if (!aligned16(y) || !aligned16(addend) || !aligned16(out)) return fail(PQ_ERR_SHAPE, "%s: tensors must be 16-byte aligned", who);
+  if (((uintptr_t)positions | (uintptr_t)weights) & 3) return fail(PQ_ERR_SHAPE, "%s: positions and weights must be 4-byte aligned", who);
+  return run_moe_combine(CombineCall{(const uint16_t*)y, rows, y_ld, positions, weights, tokens, k, N, (const uint16_t*)addend, addend_ld,
+                                     (uint16_t*)out, out_ld},
+                         as_stream(stream));
 }
 
 int pq_probe_stream(const void* src, size_t read_bytes, void* dst, size_t write_bytes, void* stream) {

@@ -23,6 +23,8 @@ inline size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 // PQ_OK, or the error for an unknown format / unsupported (format, group) pair / K % group.
 int check_format(pq_format fmt, int group, int64_t K);
+// the same for the calls that offer MXFP4 too
+int check_linear_format(pq_format fmt, int group, int64_t K);
 
 // Lets a kernel have more than 48 KB of dynamic LDS.  The attribute belongs to the kernel and the device, so it is set
 // once for each: `done` (one per kernel, a bit per device) says where it is; devices past the 64th set it every time.
@@ -184,6 +186,59 @@ struct AttnCall {
 };
 size_t attn_decode_workspace_bytes(const pq_kv_cache& c, int64_t seqs, int q_heads, int64_t max_len, int64_t window);
 int run_attn_decode(const pq_kv_cache& c, const AttnCall& a, hipStream_t st);
+
+// MXFP4 (pq_mx_quantize.hip, pq_mx_gemm.hip)
+size_t mx_operand_bytes(int64_t rows, int64_t K);
+int launch_mx_quantize_rows(const void* x, int64_t rows, int64_t K, int64_t ld, const int32_t* perm, uint8_t* codes, void* scales,
+                            hipStream_t st);
+int launch_mx_quantize_operand(const void* x, int64_t rows, int64_t K, int64_t ld, void* operand, uint8_t* codes, void* scales,
+                               hipStream_t st);
+int launch_mx_pack(const uint8_t* codes, const void* scales, int64_t rows, int64_t K, void* operand, hipStream_t st);
+int launch_dequantize(pq_format fmt, int group, const uint8_t* codes, const void* scales, const float* tensor_scale, int64_t rows, int64_t K,
+                      void* y, int64_t ldy, hipStream_t st);
+struct MxCall {
+  const uint8_t* a;                        // operand of a_rows rows
+  int64_t a_rows;
+  const uint8_t* w;                        // operands of N rows, w_next bytes apart
+  size_t w_next;
+  int experts;
+  const int32_t* offsets;                  // [experts + 1], or null: one group of all M rows
+  const int32_t* rows;                     // [M] rows of a, or null: row i of y is made from row i
+  int64_t M, N, K;
+  const uint16_t* bias;                    // [experts, N] or null
+  void* y;
+  int64_t ldy;
+  bool out_f32;
+};
+int run_mx_gemm(const MxCall& c, hipStream_t st);
+
+// routing to experts and the weighted sum of what they made (pq_moe.hip)
+struct RouteCall {
+  const void* logits;
+  bool bf16;                               // or binary32
+  int64_t tokens, ld;
+  int experts, k;
+  bool renormalize;
+  int32_t* ids;
+  float* weights;
+  int32_t *offsets, *rows, *positions;
+};
+size_t moe_route_workspace_bytes(int64_t tokens, int experts);
+int run_moe_route(const RouteCall& c, void* ws, hipStream_t st);
+struct CombineCall {
+  const uint16_t* y;
+  int64_t rows, y_ld;
+  const int32_t* positions;
+  const float* weights;
+  int64_t tokens;
+  int k;
+  int64_t N;
+  const uint16_t* addend;                  // or null
+  int64_t addend_ld;
+  uint16_t* out;
+  int64_t out_ld;
+};
+int run_moe_combine(const CombineCall& c, hipStream_t st);
 
 int run_check_int_scales(pq_format fmt, int group, const void* scales, int64_t rows, int64_t K, int64_t* bad_count,
                          void* ws, hipStream_t st);

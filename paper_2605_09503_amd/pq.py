@@ -14,12 +14,14 @@ import importlib.util
 import os
 import warnings
 from dataclasses import dataclass
-from typing import List, Optional, Sequence
+from typing import List, NamedTuple, Optional, Sequence
 
 import torch
 
 FMT_NVFP4, FMT_INT4, FMT_INT3 = 0, 1, 2
 FMT_BF16 = 3            # of a key-value cache only
+FMT_MXFP4 = 4           # of the quantizers, the packed products and the products grouped by expert
+LOGITS_F32, LOGITS_BF16 = 0, 1
 OP_CALIB_MOMENTS, OP_SELECT_PERM, OP_QUANTIZE_WEIGHTS, OP_QUANTIZE_ACT, OP_QGEMM, OP_QUANT_ERROR, \
     OP_SELECT_PERM_OUTPUT, OP_CHANNEL_STATS, OP_ORDER = range(9)
 CRIT_VARIANCE, CRIT_ABSMAX = 0, 1
@@ -143,6 +145,12 @@ def _declare(lib):
     lib.pq_attn_decode_workspace_bytes.restype = sz
     lib.pq_attn_decode_workspace_bytes.argtypes = [vp, i64, i32, i64, i64]
     lib.pq_attn_decode.argtypes = [vp, vp, i64, i64, vp, i64, vp, i64, i32, i64, i64, C.c_float, vp, i64, i64, vp, vp, sz, vp]
+    lib.pq_dequantize.argtypes = [i32, i32, vp, vp, vp, i64, i64, vp, i64, vp]
+    lib.pq_qgemm_grouped.argtypes = [i32, i32, vp, i64, vp, i32, vp, vp, i64, i64, i64, vp, vp, i64, vp]
+    lib.pq_moe_route_workspace_bytes.restype = sz
+    lib.pq_moe_route_workspace_bytes.argtypes = [i64, i32, i32]
+    lib.pq_moe_route.argtypes = [i32, vp, i64, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.pq_moe_combine.argtypes = [vp, i64, i64, vp, vp, i64, i32, i64, vp, i64, vp, i64, vp]
     lib.pq_probe_stream.argtypes = [vp, sz, vp, sz, vp]
     lib.pq_qgemm_check_int_scales.argtypes = [i32, i32, vp, i64, i64, C.POINTER(C.c_int64), vp, sz, vp]
     lib.pq_probe_mfma.argtypes = [i32, vp, C.POINTER(C.c_double), vp]
@@ -800,9 +808,151 @@ def pq_attn_decode(cache: KVCache, q: torch.Tensor, table: torch.Tensor, lengths
     return out
 
 
+# ------------------------------------------------------------------------ reading back, products by expert, routing
+def pq_dequantize(fmt: int, group: int, codes: torch.Tensor, scales: torch.Tensor, tensor_scale: Optional[torch.Tensor] = None,
+                  y: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The values that stored codes [rows, K/2] and scales stand for, bf16 [rows, K] (allocated unless given)."""
+    rows, K = codes.shape[0], codes.shape[1] * 2
+    if y is None:
+        y = torch.empty((rows, K), dtype=torch.bfloat16, device=codes.device)
+    _check(load().pq_dequantize(fmt, group, _ptr(codes), _ptr(scales), _ptr(tensor_scale), rows, K, _ptr(y), y.stride(0), _stream()))
+    return y
+
+
+def pack_experts(codes: torch.Tensor, scales: torch.Tensor, experts: int) -> torch.Tensor:
+    """MXFP4 weights of all experts, codes [experts * N, K/2] and scales [experts * N, K/32], as the operands of pq_qgemm_grouped:
+    uint8 [experts, pq_operand_bytes(FMT_MXFP4, 32, N, K)]."""
+    if codes.dim() != 2 or scales.dim() != 2 or experts <= 0 or codes.shape[0] % experts or scales.shape[0] != codes.shape[0]:
+        _refuse("codes and scales must have the same rows, a multiple of %d" % experts)
+    N, K = codes.shape[0] // experts, codes.shape[1] * 2
+    need = pq_operand_bytes(FMT_MXFP4, 32, N, K)
+    if need == 0:
+        raise PQError(-2, pq_last_error())
+    out = torch.empty((experts, need), dtype=torch.uint8, device=codes.device)
+    for e in range(experts):
+        # rows of K/32 bytes: an expert's may begin at an address that is not the call's 16-byte alignment
+        pq_pack_operand(FMT_MXFP4, 32, _aligned(codes[e * N:(e + 1) * N]), _aligned(scales[e * N:(e + 1) * N]), out[e])
+    return out
+
+
+def _aligned(t: torch.Tensor) -> torch.Tensor:
+    return t if t.data_ptr() % 16 == 0 and t.is_contiguous() else t.contiguous().clone()
+
+
+def _on_current_device(name: str, t: torch.Tensor, like: Optional[torch.Tensor] = None):
+    """The stream of a call on t: its device has to be the current one, or that of the call's other tensors."""
+    if not t.is_cuda or (t.device != like.device if like is not None else t.device.index != torch.cuda.current_device()):
+        _refuse("%s must lie in the memory of the current GPU, with the call's other tensors" % name)
+
+
+def _array(name: str, t: torch.Tensor, dtype, shape, like: torch.Tensor) -> int:
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        _refuse("%s must be contiguous %s %s" % (name, dtype, list(shape)))
+    _on_current_device(name, t, like)
+    return t.data_ptr()
+
+
+def _rows2(name: str, t: torch.Tensor, rows: int, width: int, like: Optional[torch.Tensor]):
+    """(pointer, row stride) of bf16 [rows, width] with adjacent columns; the stride of a single row does not matter."""
+    if t.dtype != torch.bfloat16 or tuple(t.shape) != (rows, width) or (width > 1 and t.stride(1) != 1):
+        _refuse("%s must be bfloat16 [%d, %d] with adjacent columns" % (name, rows, width))
+    _on_current_device(name, t, like)
+    return t.data_ptr(), t.stride(0) if rows > 1 else (width + 7) // 8 * 8
+
+
+def pq_qgemm_grouped(fmt: int, group: int, a_operand: torch.Tensor, a_rows: int, w_operands: torch.Tensor, offsets: torch.Tensor,
+                     y: torch.Tensor, N: int, K: int, rows: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None) -> None:
+    """y[i] (bf16 [M, N]) = row rows[i] (int32 [M], or i) of A times the weights of the expert whose rows offsets (int32 [experts + 1])
+    places i in, plus bias[expert] (bf16 [experts, N]).  w_operands: uint8 [experts, pq_operand_bytes(fmt, group, N, K)]."""
+    if w_operands.dim() != 2 or w_operands.dtype != torch.uint8 or not w_operands.is_contiguous():
+        _refuse("w_operands must be contiguous uint8 [experts, bytes of an operand]")
+    experts, M = w_operands.shape[0], y.shape[0]
+    need = pq_operand_bytes(fmt, group, N, K)
+    if need and w_operands.shape[1] != need:
+        _refuse("w_operands must hold %d bytes an expert" % need)
+    yp, ldy = _rows2("y", y, M, N, None)
+    _on_current_device("w_operands", w_operands, y)
+    _on_current_device("a_operand", a_operand, y)
+    if a_operand.dtype != torch.uint8 or not a_operand.is_contiguous() or a_operand.numel() < pq_operand_bytes(fmt, group, a_rows, K):
+        _refuse("a_operand must be contiguous uint8 and hold an operand of %d rows" % a_rows)
+    op = _array("offsets", offsets, torch.int32, (experts + 1,), y)
+    rp = None if rows is None else _array("rows", rows, torch.int32, (M,), y)
+    bp = None if bias is None else _array("bias", bias, torch.bfloat16, (experts, N), y)
+    _check(load().pq_qgemm_grouped(fmt, group, _ptr(a_operand), a_rows, _ptr(w_operands), experts, op, rp, M, N, K, bp, yp, ldy, _stream()))
+
+
+class Route(NamedTuple):
+    """What pq_moe_route leaves: see pq_moe_route of the header."""
+    ids: torch.Tensor           # int32 [tokens, k]
+    weights: torch.Tensor       # float32 [tokens, k]
+    offsets: torch.Tensor       # int32 [experts + 1]
+    rows: torch.Tensor          # int32 [tokens * k]
+    positions: torch.Tensor     # int32 [tokens, k]
+
+
+def alloc_route(tokens: int, experts: int, k: int, device="cuda") -> Route:
+    ints = lambda *shape: torch.empty(shape, dtype=torch.int32, device=device)
+    return Route(ints(tokens, k), torch.empty((tokens, k), dtype=torch.float32, device=device), ints(experts + 1), ints(tokens * k),
+                 ints(tokens, k))
+
+
+def pq_moe_route_workspace_bytes(tokens: int, experts: int, k: int) -> int:
+    return int(load().pq_moe_route_workspace_bytes(tokens, experts, k))
+
+
+def pq_moe_route_workspace(tokens: int, experts: int, k: int, device="cuda") -> torch.Tensor:
+    """A workspace for pq_moe_route with these arguments, or fewer tokens: for one stream, call after call."""
+    need = pq_moe_route_workspace_bytes(tokens, experts, k)
+    if need == 0:
+        raise PQError(-2, pq_last_error())
+    return torch.empty(need, dtype=torch.uint8, device=device)
+
+
+def pq_moe_route(logits: torch.Tensor, k: int, renormalize: bool = True, out: Optional[Route] = None,
+                 workspace: Optional[torch.Tensor] = None) -> Route:
+    """The k largest of every row of logits (float32 or bf16 [tokens, experts]), their softmax weights, and the order of the rows by
+    expert (allocated unless given)."""
+    if logits.dim() != 2 or logits.dtype not in (torch.float32, torch.bfloat16) or (logits.shape[1] > 1 and logits.stride(1) != 1):
+        _refuse("logits must be float32 or bfloat16 [tokens, experts] with adjacent experts")
+    tokens, experts = logits.shape
+    _on_current_device("logits", logits)
+    if workspace is None:
+        workspace = pq_moe_route_workspace(tokens, experts, k, logits.device)
+    if not workspace.is_contiguous():
+        _refuse("workspace must be contiguous")
+    _on_current_device("workspace", workspace, logits)
+    if out is None:
+        out = alloc_route(tokens, experts, k, logits.device)
+    shapes = ((tokens, k), (tokens, k), (experts + 1,), (tokens * k,), (tokens, k))
+    ptrs = [_array(name, t, torch.float32 if name == "weights" else torch.int32, shape, logits)
+            for name, t, shape in zip(Route._fields, out, shapes)]
+    _check(load().pq_moe_route(LOGITS_BF16 if logits.dtype == torch.bfloat16 else LOGITS_F32, _ptr(logits), tokens, experts,
+                               logits.stride(0) if tokens > 1 else experts, k, int(renormalize), *ptrs, _ptr(workspace),
+                               workspace.numel() * workspace.element_size(), _stream()))
+    return out
+
+
+def pq_moe_combine(y: torch.Tensor, positions: torch.Tensor, weights: torch.Tensor, addend: Optional[torch.Tensor] = None,
+                   out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """out[t] = addend[t] + sum_j weights[t, j] * y[positions[t, j]], bf16 [tokens, N] (allocated unless given); y bf16 [rows, N],
+    positions int32 and weights float32 [tokens, k]."""
+    if y.dim() != 2 or positions.dim() != 2:
+        _refuse("y must be bfloat16 [rows, N], positions int32 [tokens, k]")
+    (rows, N), (tokens, k) = y.shape, positions.shape
+    yp, y_ld = _rows2("y", y, rows, N, None)
+    pp = _array("positions", positions, torch.int32, (tokens, k), y)
+    wp = _array("weights", weights, torch.float32, (tokens, k), y)
+    ap, a_ld = (None, 0) if addend is None else _rows2("addend", addend, tokens, N, y)
+    if out is None:
+        out = torch.empty((tokens, (N + 7) // 8 * 8), dtype=torch.bfloat16, device=y.device)[:, :N]
+    outp, o_ld = _rows2("out", out, tokens, N, y)
+    _check(load().pq_moe_combine(yp, rows, y_ld, pp, wp, tokens, k, N, ap, a_ld, outp, o_ld, _stream()))
+    return out
+
+
 # ------------------------------------------------------------------------ allocation helpers
 def scale_dtype(fmt: int):
-    return torch.uint8 if fmt == FMT_NVFP4 else torch.float32
+    return torch.uint8 if fmt in (FMT_NVFP4, FMT_MXFP4) else torch.float32
 
 
 def alloc_quantized(fmt: int, group: int, rows: int, K: int, device="cuda"):

@@ -1,0 +1,462 @@
+"""MXFP4 quantizers and products, routing and the weighted sum against the oracle in 64 bits.
+
+Tolerances.  Codes, scales and read-back values are exact.  A product's terms are exact; a 32 x 32 x 64 instruction adds 64 of them to
+an fp32 sum, and each of its additions is taken to lose at most 2^-23 of the terms' absolute sum (2^-24 rounded, twice that cut off): K / 64
+instructions in turn and some 8 additions that join parts give (K / 64 + 8) 2^-23 of sum |terms|.  A bias adds 2^-24 of what it gives; bf16
+outputs are rounded once (2^-8 of themselves).  Weights: e^x of an argument that is off by 2^-24 of itself (|x| < 100) and a few
+roundings in sum and quotient: 1e-5.  The weighted sum: k + 1 fused steps of 2^-24 of the terms' absolute sum, then bf16's 2^-8."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import formats as OF
+from oracle import mx
+from oracle import quantize as OQ
+from paper_2605_09503_amd import pq
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+MX = pq.FMT_MXFP4
+
+
+def bits(t):
+    return t.contiguous().view(torch.int16).cpu().numpy().view(np.uint16)
+
+
+def f64(t):
+    return OF.bf16_bits_to_f64(bits(t)) if t.dtype == torch.bfloat16 else t.cpu().double().numpy()
+
+
+def rows_of(rng, rows, K, gap=0, odd=True):
+    """bf16 [rows, K], a slice of wider rows where gap > 0: channels of uneven sizes, zeros, groups of subnormals and of huge values."""
+    x = rng.standard_normal((rows, K)) * np.exp(rng.standard_normal(K))
+    x[rng.random((rows, K)) < 0.02] *= 30.0
+    if odd:
+        x[rng.random((rows, K)) < 0.05] = 0.0
+        g = x.reshape(rows, K // 32, 32)
+        g[rng.random(g.shape[:2]) < 0.03] = 0.0
+        g[rng.random(g.shape[:2]) < 0.03] *= 2.0 ** -20
+    wide = np.full((rows, K + 2 * gap), 7.0)
+    wide[:, gap:gap + K] = x
+    return pq.bf16_from_bits(OF.f64_to_bf16_bits_rne(wide), DEV)[:, gap:gap + K]
+
+
+def stored(q):
+    return torch.from_numpy(mx.packed_codes(q)).to(DEV), torch.from_numpy(q.scale).to(DEV)
+
+
+def operand(x):
+    return pq.pq_quantize_act_packed(MX, 32, x, None)
+
+
+def bound(K, mag):
+    return (K / 64 + 8) * 2.0 ** -23 * mag
+
+
+def close(got, ref, err, rounding=2.0 ** -8):
+    got = f64(got)
+    nan = np.isnan(ref)
+    assert np.array_equal(np.isnan(got), nan)
+    off, allowed = np.abs(got - ref)[~nan], (err + rounding * (np.abs(ref) + err) + 2.0 ** -133)[~nan]
+    worst = (off / allowed).max(initial=0.0)
+    assert worst <= 1.0, worst
+
+
+EXTREMES = [0.0, -0.0, 2.0 ** -133, -2.0 ** -126, 2.0 ** -127, 2.0 ** -120, 1.0, -1.75, 3.5, 5.0, -7.0, 7.96875, 2.0 ** 120, -2.0 ** 127 * 1.9921875]
+
+
+# ------------------------------------------------------------------------ quantizers
+
+@pytest.mark.parametrize("rows,K,gap", [(1, 32, 0), (3, 96, 8), (64, 256, 0), (37, 288, 16), (129, 2016, 8), (5, 10240, 0)])
+def test_quantize_stored(rows, K, gap):
+    rng = np.random.default_rng(rows + K)
+    x = rows_of(rng, rows, K, gap)
+    want = mx.quantize(f64(x))
+    codes, scales = pq.alloc_quantized(MX, 32, rows, K)
+    pq.pq_quantize_act(MX, 32, x, None, None, codes, scales)
+    assert np.array_equal(codes.cpu().numpy(), mx.packed_codes(want)) and np.array_equal(scales.cpu().numpy(), want.scale)
+    y = pq.pq_dequantize(MX, 32, codes, scales)
+    assert np.array_equal(f64(y), mx.dequantize(want))
+    wide = torch.full((rows, K + 24), 3.0, dtype=torch.bfloat16, device=DEV)
+    pq.pq_dequantize(MX, 32, codes, scales, y=wide[:, 8:8 + K])
+    assert torch.equal(wide[:, 8:8 + K], y) and bool((wide[:, :8] == 3).all()) and bool((wide[:, 8 + K:] == 3).all())
+    perm = torch.from_numpy(rng.permutation(K).astype(np.int32)).to(DEV)
+    pq.pq_quantize_act(MX, 32, x, perm, None, codes, scales)
+    want = mx.quantize(f64(x)[:, perm.cpu().numpy()])
+    assert np.array_equal(codes.cpu().numpy(), mx.packed_codes(want)) and np.array_equal(scales.cpu().numpy(), want.scale)
+    one = torch.zeros(1, device=DEV)
+    codes.zero_()
+    pq.pq_quantize_weights(MX, 32, x.contiguous(), perm, codes, scales, one)
+    assert np.array_equal(codes.cpu().numpy(), mx.packed_codes(want)) and one.item() == 1.0
+
+
+def test_every_bf16_value():
+    # each finite value as the largest of its group, with a spread of smaller ones, and next to infinities and NaN
+    rng = np.random.default_rng(7)
+    values = np.arange(65536, dtype=np.uint16)
+    x = rng.permutation(np.tile(values, 8))                    # 16384 groups of any values: most hold one that is not finite
+    lone = np.zeros((65536, 32), dtype=np.uint16)
+    lone[:, 3] = values
+    e = OF.f64_to_bf16_bits_rne(np.ldexp(rng.standard_normal((40, 32 * 32)), np.repeat(rng.integers(-140, 127, (40, 32)), 32, axis=1)).clip(-3e38, 3e38))
+    for b in (x.reshape(128, -1), lone.reshape(1024, -1), e):
+        t = pq.bf16_from_bits(b, DEV)
+        want = mx.quantize(f64(t))
+        codes, scales = pq.alloc_quantized(MX, 32, *t.shape)
+        pq.pq_quantize_act(MX, 32, t, None, None, codes, scales)
+        assert np.array_equal(scales.cpu().numpy(), want.scale)
+        ok = np.repeat(want.scale != 255, 16, axis=1)            # codes of a NaN group do not matter
+        assert np.array_equal(codes.cpu().numpy()[ok], mx.packed_codes(want)[ok])
+        got, ref = f64(pq.pq_dequantize(MX, 32, codes, scales)), mx.dequantize(want)
+        assert np.array_equal(got, ref, equal_nan=True)
+
+
+@pytest.mark.parametrize("rows,K,gap", [(1, 32, 0), (3, 96, 8), (64, 256, 0), (37, 288, 16), (129, 2016, 8), (300, 544, 0)])
+def test_operand_is_the_packed_stored_form(rows, K, gap):
+    rng = np.random.default_rng(rows * K)
+    x = rows_of(rng, rows, K, gap)
+    want = mx.quantize(f64(x))
+    codes, scales = stored(want)
+    need = pq.pq_operand_bytes(MX, 32, rows, K)
+    a, b = (torch.full((need,), 0xFF, dtype=torch.uint8, device=DEV) for _ in range(2))
+    got_codes, got_scales = pq.alloc_quantized(MX, 32, rows, K)
+    pq.pq_pack_operand(MX, 32, codes, scales, a)
+    pq.pq_quantize_act_packed(MX, 32, x, None, b, got_codes, got_scales)
+    assert torch.equal(got_codes, codes) and torch.equal(got_scales, scales)
+    # what lies between the parts to make them multiples of 256 bytes is nobody's
+    panels = (K + 255) // 256
+    at = (panels * rows * 128 + 255) // 256 * 256
+    for part in (slice(0, panels * rows * 128), slice(at, at + panels * rows * 8)):
+        assert torch.equal(a[part], b[part])
+
+
+@pytest.mark.parametrize("fmt,group", [(pq.FMT_NVFP4, 16), (pq.FMT_INT4, 32), (pq.FMT_INT4, 128), (pq.FMT_INT3, 64)])
+def test_dequantize_other_formats(fmt, group):
+    rng = np.random.default_rng(11)
+    x = rows_of(rng, 19, 384)
+    ts = torch.full((1,), float(np.float32(np.abs(f64(x)).max() / 2688)), device=DEV)
+    codes, scales = pq.alloc_quantized(fmt, group, 19, 384)
+    pq.pq_quantize_act(fmt, group, x, None, ts, codes, scales)
+    q = OQ.quantize(fmt, group, f64(x), np.float32(ts.item()))
+    want = OF.f64_to_bf16_bits_rne(OF.fl32(OQ.dequantize(fmt, group, q)))
+    got = bits(pq.pq_dequantize(fmt, group, codes, scales, ts))
+    assert np.array_equal(np.where(got == 0x8000, 0, got), np.where(want == 0x8000, 0, want))
+
+
+# ------------------------------------------------------------------------ products
+
+SHAPES = [(1, 1, 32), (1, 8, 96), (1, 300, 4096), (2, 517, 1056), (16, 64, 256), (17, 40, 288), (31, 136, 512), (33, 1000, 544), (64, 257, 2016), (65, 128, 1024),
+          (100, 333, 800), (128, 128, 128), (129, 200, 2560), (250, 512, 768), (257, 260, 320), (300, 1030, 1312), (777, 520, 640), (1025, 515, 2080)]
+
+
+@pytest.mark.parametrize("M,N,K", SHAPES)
+def test_product(M, N, K):
+    rng = np.random.default_rng(M * 7 + N + K)
+    x, w = rows_of(rng, M, K, 8), rows_of(rng, N, K)
+    xq, wq = (mx.dequantize(mx.quantize(f64(t))) for t in (x, w))
+    ref, mag = xq @ wq.T, np.abs(xq) @ np.abs(wq).T
+    a, b = operand(x), pq.pq_pack_operand(MX, 32, *stored(mx.quantize(f64(w))))
+    ldy = (N + 7) // 8 * 8 + 8
+    y = torch.full((M + 1, ldy), 5.0, device=DEV)
+    pq.pq_qgemm_packed_f32(MX, 32, a, None, b, None, y[:M], M, N, K)
+    close(y[:M, :N], ref, bound(K, mag), 0.0)
+    assert bool((y[M:] == 5).all()) and bool((y[:, N:] == 5).all())
+    y = torch.full((M + 1, ldy), 5.0, dtype=torch.bfloat16, device=DEV)
+    pq.pq_qgemm_packed(MX, 32, a, None, b, None, y[:M], M, N, K)
+    close(y[:M, :N], ref, bound(K, mag))
+    assert bool((y[M:] == 5).all()) and bool((y[:, N:] == 5).all())
+    bias = rows_of(rng, 1, (N + 31) // 32 * 32, odd=False)[0, :N].clone()
+    pq.pq_qgemm_packed_bias(MX, 32, a, None, b, None, bias, y[:M], M, N, K)
+    ref = ref + f64(bias[None])
+    close(y[:M, :N], ref, bound(K, mag) + 2.0 ** -24 * np.abs(ref))
+    assert bool((y[M:] == 5).all()) and bool((y[:, N:] == 5).all())
+
+
+@pytest.mark.parametrize("M,N,K", [(5, 70, 288), (200, 300, 512), (600, 700, 320)])
+def test_product_of_extremes(M, N, K):
+    # the largest and smallest scales; a group with an infinity or a NaN makes its row (or column) NaN and nothing else
+    rng = np.random.default_rng(M)
+    x, w = rows_of(rng, M, K), rows_of(rng, N, K)
+    x[0, :32] = torch.tensor(EXTREMES + [0.0] * (32 - len(EXTREMES)), dtype=torch.bfloat16)
+    x[M // 2] *= 2.0 ** 100
+    w[1] *= 2.0 ** -110
+    x[1, 33] = float("inf")
+    x[M - 1, K - 1] = float("nan")
+    w[N - 2, 5] = -float("inf")
+    w[0, :32] = 0.0                                                       # what meets the extremes of row 0: fp32 holds the rest
+    w[1:, :32] = torch.where(w[1:, :32].abs() > 1, torch.zeros_like(w[1:, :32]), w[1:, :32])
+    xq, wq = (mx.dequantize(mx.quantize(f64(t))) for t in (x, w))
+    with np.errstate(invalid="ignore", over="ignore"):
+        ref, mag = xq @ wq.T, np.abs(xq) @ np.abs(wq).T
+    keep = np.isnan(ref) | (np.abs(mag) < 2.0 ** 120)
+    y = torch.empty(M, (N + 7) // 8 * 8, device=DEV)
+    pq.pq_qgemm_packed_f32(MX, 32, operand(x), None, operand(w), None, y, M, N, K)
+    got = y[:, :N].cpu().double().numpy()
+    assert np.array_equal(np.isnan(got)[keep], np.isnan(ref)[keep])
+    fine = keep & ~np.isnan(ref)
+    assert (np.abs(got - ref)[fine] <= (bound(K, mag) + 2.0 ** -126)[fine]).all()
+
+
+def test_product_repeats_its_bits():
+    rng = np.random.default_rng(1)
+    for M, N, K in ((3, 700, 4096), (70, 900, 2048), (700, 900, 1024)):
+        a, b = operand(rows_of(rng, M, K)), operand(rows_of(rng, N, K))
+        y = [torch.empty(M, (N + 7) // 8 * 8, device=DEV) for _ in range(3)]
+        for t in y:
+            pq.pq_qgemm_packed_f32(MX, 32, a, None, b, None, t, M, N, K)
+        assert torch.equal(y[0][:, :N], y[1][:, :N]) and torch.equal(y[0][:, :N], y[2][:, :N])
+
+
+# ------------------------------------------------------------------------ products by expert
+
+def experts_case(rng, sizes, a_rows, N, K, gather, bias, first=0, behind=0):
+    E, M = len(sizes), first + sum(sizes) + behind
+    x, w = rows_of(rng, a_rows, K), rows_of(rng, E * N, K)
+    xq, wq = mx.dequantize(mx.quantize(f64(x))), mx.dequantize(mx.quantize(f64(w)))
+    rows = rng.integers(0, a_rows, M).astype(np.int32) if gather else None
+    b = rng.standard_normal((E, N)) if bias else np.zeros((E, N))
+    b = OF.bf16_bits_to_f64(OF.f64_to_bf16_bits_rne(b))
+    offsets = first + np.concatenate([[0], np.cumsum(sizes)])
+    ref, err = np.full((M, N), 5.0), np.zeros((M, N))
+    for e in range(E):
+        for i in range(offsets[e], offsets[e + 1]):
+            r = rows[i] if gather else i
+            part = wq[e * N:(e + 1) * N]
+            ref[i] = part @ xq[r] + b[e]
+            err[i] = bound(K, np.abs(part) @ np.abs(xq[r])) + 2.0 ** -24 * np.abs(ref[i])
+    t = lambda v: None if v is None else torch.from_numpy(np.ascontiguousarray(v)).to(DEV)
+    codes, scales = stored(mx.quantize(f64(w)))
+    return dict(a=operand(x), w=pq.pack_experts(codes, scales, E), offsets=t(offsets.astype(np.int32)), rows=t(rows),
+                bias=pq.bf16_from_bits(OF.f64_to_bf16_bits_rne(b), DEV) if bias else None, ref=ref, err=err, M=M)
+
+
+def grouped(c, a_rows, N, K, **kw):
+    y = torch.full((c["M"], (N + 7) // 8 * 8 + 8), 5.0, dtype=torch.bfloat16, device=DEV)
+    pq.pq_qgemm_grouped(MX, 32, c["a"], a_rows, c["w"], c["offsets"], y[:, :N], N, K, rows=kw.get("rows", c["rows"]), bias=c["bias"])
+    assert bool((y[:, N:] == 5).all())
+    return y[:, :N]
+
+
+@pytest.mark.parametrize("sizes,a_rows,N,K,gather,bias", [
+    ([1], 1, 8, 32, True, False), ([0, 0, 3, 0], 5, 40, 288, True, True), ([5, 1, 0, 33, 2], 41, 72, 512, False, True),
+    ([1] * 70, 9, 33, 96, True, True), ([0] * 130 + [17] + [0] * 65, 17, 64, 256, False, False), ([64, 0, 128, 31, 200], 50, 260, 544, True, True),
+    ([300, 1, 257, 0, 512], 1100, 264, 320, False, False), ([700, 30], 300, 520, 1056, True, True), ([3, 4, 2, 7, 0, 1, 5, 2], 8, 1000, 2016, True, False),
+    ([20] * 40, 200, 136, 640, True, True)])
+def test_grouped(sizes, a_rows, N, K, gather, bias):
+    rng = np.random.default_rng(len(sizes) + a_rows + N)
+    c = experts_case(rng, sizes, a_rows, N, K, gather, bias, first=0 if gather is False else 2, behind=0 if gather is False else 3)
+    close(grouped(c, a_rows, N, K), c["ref"], c["err"])
+
+
+def test_grouped_leaves_other_rows():
+    rng = np.random.default_rng(3)
+    a_rows, N, K = 20, 48, 288
+    c = experts_case(rng, [4, 0, 40, 3], a_rows, N, K, True, True, first=1, behind=2)
+    rows = c["rows"].clone()
+    rows[6], rows[11], rows[44] = -1, a_rows, 1 << 30                     # unknown rows: left as they were
+    ref = c["ref"].copy()
+    ref[[6, 11, 44]] = 5.0
+    err = c["err"].copy()
+    err[[6, 11, 44]] = 0.0
+    close(grouped(c, a_rows, N, K, rows=rows), ref, err)
+    # offsets beyond M and below 0 are cut
+    c["offsets"] = torch.tensor([-7, 5, 5, 45, 1 << 30], dtype=torch.int32, device=DEV)
+    y = grouped(c, a_rows, N, K)
+    close(y[1:48], c["ref"][1:48], c["err"][1:48])
+    assert not bool((y[0] == 5).all()) and not bool((y[48:] == 5).all())
+    # nothing at all
+    c["offsets"] = torch.full((5,), 9, dtype=torch.int32, device=DEV)
+    assert bool((grouped(c, a_rows, N, K) == 5).all())
+    c["M"] = 0
+    c["rows"] = c["rows"][:0]
+    assert grouped(c, a_rows, N, K).numel() == 0
+
+
+def test_grouped_of_one_expert_is_the_product():
+    rng = np.random.default_rng(4)
+    for M, N, K in ((3, 100, 512), (90, 300, 800), (520, 520, 256)):
+        x, w = rows_of(rng, M, K), rows_of(rng, N, K)
+        a, b = operand(x), operand(w)
+        y, z = (torch.empty(M, (N + 7) // 8 * 8, dtype=torch.bfloat16, device=DEV)[:, :N] for _ in range(2))
+        pq.pq_qgemm_packed(MX, 32, a, None, b, None, y, M, N, K)
+        pq.pq_qgemm_grouped(MX, 32, a, M, b[None], torch.tensor([0, M], dtype=torch.int32, device=DEV), z, N, K)
+        ref = mx.dequantize(mx.quantize(f64(x))) @ mx.dequantize(mx.quantize(f64(w))).T
+        mag = np.abs(mx.dequantize(mx.quantize(f64(x)))) @ np.abs(mx.dequantize(mx.quantize(f64(w)))).T
+        close(y, ref, bound(K, mag))
+        close(z, ref, bound(K, mag))
+
+
+# ------------------------------------------------------------------------ routing, weighted sum
+
+def check_route(r, want, exact_weights=False):
+    for name in ("ids", "offsets", "rows", "positions"):
+        assert np.array_equal(getattr(r, name).cpu().numpy(), getattr(want, name)), name
+    assert np.abs(r.weights.cpu().double().numpy() - want.weights).max(initial=0.0) <= 1e-5
+
+
+@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 64, 6), (5, 3, 3), (7, 65, 8), (64, 16, 2), (65, 128, 4), (200, 300, 10), (130, 1024, 32), (1000, 256, 8)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("renormalize", [True, False])
+def test_route(T, E, k, dtype, renormalize):
+    rng = np.random.default_rng(T + E)
+    x = rng.standard_normal((T, E)) * 2
+    x[rng.random((T, E)) < 0.1] = -np.inf
+    x[rng.random((T, E)) < 0.02] = np.nan
+    x[rng.random(T) < 0.1] = -np.inf                                      # padding
+    x[rng.random(T) < 0.1, :min(E, 7)] = 3.0                              # ties
+    wide = torch.full((T, E + 5), 1e30, dtype=dtype, device=DEV)
+    wide[:, 3:3 + E] = torch.from_numpy(x).to(dtype)
+    logits = wide[:, 3:3 + E]
+    r = pq.alloc_route(T, E, k)
+    for t in r:
+        t.fill_(77)
+    pq.pq_moe_route(logits, k, renormalize, out=r)
+    check_route(r, mx.route(logits.double().cpu().numpy(), k, renormalize))
+    again = pq.pq_moe_route(logits, k, renormalize)
+    assert all(torch.equal(a, b) for a, b in zip(r, again))
+
+
+def test_route_no_tokens_and_no_choices():
+    r = pq.pq_moe_route(torch.empty(0, 9, device=DEV), 2)
+    assert r.offsets.tolist() == [0] * 10 and r.rows.numel() == 0
+    r = pq.pq_moe_route(torch.full((70, 9), -float("inf"), device=DEV), 2)
+    assert r.offsets.tolist() == [0] * 10 and bool((r.rows == -1).all()) and bool((r.ids == -1).all()) and bool((r.weights == 0).all())
+    big = torch.zeros(3, 4, device=DEV)
+    big[:, 1] = 3e38
+    big[:, 2] = -3e38
+    r = pq.pq_moe_route(big, 4)
+    assert r.ids.tolist() == [[1, 0, 3, 2]] * 3 and r.weights.tolist() == [[1.0, 0.0, 0.0, 0.0]] * 3
+
+
+@pytest.mark.parametrize("T,E,k", [(33000, 8, 2), (70001, 33, 3)])
+def test_route_of_many_tokens(T, E, k):
+    # more tokens than one pass of all workgroups
+    x = torch.randn(T, E, generator=torch.Generator(device=DEV).manual_seed(T), device=DEV)
+    r = pq.pq_moe_route(x, k)
+    ids = torch.sort(x, dim=1, descending=True, stable=True).indices[:, :k]
+    assert torch.equal(r.ids.long(), ids)
+    order = torch.argsort(ids.reshape(-1), stable=True)
+    assert torch.equal(r.rows.long(), order // k)
+    place = torch.empty_like(order)
+    place[order] = torch.arange(T * k, device=DEV)
+    assert torch.equal(r.positions.long().reshape(-1), place)
+    assert torch.equal(r.offsets.long()[1:], torch.bincount(ids.reshape(-1), minlength=E).cumsum(0))
+
+
+@pytest.mark.parametrize("T,k,N", [(1, 1, 1), (3, 2, 8), (7, 4, 13), (50, 8, 264), (33, 32, 100), (4, 3, 5000)])
+@pytest.mark.parametrize("addend", [False, True])
+def test_combine(T, k, N, addend):
+    rng = np.random.default_rng(T * k + N)
+    R = T * k + 2
+    bf = lambda a: pq.bf16_from_bits(OF.f64_to_bf16_bits_rne(a), DEV)
+    y = rng.standard_normal((R, N + 9))
+    y[R - 1] = np.nan                                                     # no token's
+    y = bf(y)
+    ld = (N + 7) // 8 * 8 + 8
+    wide = torch.full((R, ld), 9.0, dtype=torch.bfloat16, device=DEV)
+    wide[:, :N] = y[:, :N]
+    pos = rng.integers(-1, R - 1, (T, k)).astype(np.int32)                # the same row twice among them
+    pos[rng.random((T, k)) < 0.1] = R + 3
+    pos[0] = -1
+    weights = rng.standard_normal((T, k)).astype(np.float32)
+    add = torch.full((T, ld), 4.0, dtype=torch.bfloat16, device=DEV)
+    add[:, :N] = bf(rng.standard_normal((T, N)))
+    out = torch.full((T + 1, ld), 6.0, dtype=torch.bfloat16, device=DEV)
+    args = (wide[:, :N], torch.from_numpy(pos).to(DEV), torch.from_numpy(weights).to(DEV), add[:, :N] if addend else None)
+    pq.pq_moe_combine(*args, out=out[:T, :N])
+    ref, mag = mx.combine(f64(wide[:, :N]), pos, weights, f64(add[:, :N]) if addend else None)
+    close(out[:T, :N], ref, (k + 1) * 2.0 ** -24 * mag)
+    assert bool((out[T:] == 6).all()) and bool((out[:, N:] == 6).all())
+    assert torch.equal(pq.pq_moe_combine(*args), out[:T, :N])
+    if addend:                                                            # on top of the addend itself
+        pq.pq_moe_combine(*args, out=add[:, :N])
+        assert torch.equal(add[:, :N], out[:T, :N]) and bool((add[:, N:] == 4).all())
+
+
+# ------------------------------------------------------------------------ together
+
+class Layer:
+    """A layer of experts as a program holds it: two products an expert, the rows weighted and summed on top of the input."""
+
+    def __init__(self, rng, T, D, H, E, k):
+        self.k, self.D, self.H, self.E, self.T = k, D, H, E, T
+        self.w1, self.w2, self.router = rows_of(rng, E * H, D, odd=False), rows_of(rng, E * D, H, odd=False), rows_of(rng, E, D, odd=False)
+        pack = lambda w: pq.pack_experts(*stored(mx.quantize(f64(w))), E)
+        self.p1, self.p2 = pack(self.w1), pack(self.w2)
+        self.route = pq.alloc_route(T, E, k)
+        self.ws = pq.pq_moe_route_workspace(T, E, k)
+        self.a1 = torch.empty(pq.pq_operand_bytes(MX, 32, T, D), dtype=torch.uint8, device=DEV)
+        self.a2 = torch.empty(pq.pq_operand_bytes(MX, 32, T * k, H), dtype=torch.uint8, device=DEV)
+        self.h, self.z = (torch.zeros(T * k, n, dtype=torch.bfloat16, device=DEV) for n in (H, D))
+        self.out = torch.empty(T, D, dtype=torch.bfloat16, device=DEV)
+
+    def __call__(self, x, logits):
+        r = pq.pq_moe_route(logits, self.k, out=self.route, workspace=self.ws)
+        pq.pq_quantize_act_packed(MX, 32, x, None, self.a1)
+        pq.pq_qgemm_grouped(MX, 32, self.a1, self.T, self.p1, r.offsets, self.h, self.H, self.D, rows=r.rows)
+        pq.pq_quantize_act_packed(MX, 32, torch.relu(self.h), None, self.a2)
+        pq.pq_qgemm_grouped(MX, 32, self.a2, self.T * self.k, self.p2, r.offsets, self.z, self.D, self.H)
+        return pq.pq_moe_combine(self.z, r.positions, r.weights, x, self.out)
+
+    def check(self, x, logits):
+        """Step by step, each step's input as the step before left it."""
+        want = mx.route(logits.double().cpu().numpy(), self.k, True)
+        check_route(self.route, want)
+        value = lambda t: mx.dequantize(mx.quantize(f64(t)))
+        total = want.offsets[-1]
+        for a, w, y, n, rows in ((value(x), value(self.w1), self.h, self.H, want.rows), (value(torch.relu(self.h)), value(self.w2), self.z, self.D, np.arange(self.T * self.k))):
+            for e in range(self.E):
+                at = slice(want.offsets[e], want.offsets[e + 1])
+                part, rr = w[e * n:(e + 1) * n], rows[at]
+                close(y[at.start:at.stop], a[rr] @ part.T, bound(a.shape[1], np.abs(a[rr]) @ np.abs(part).T))
+        ref, mag = mx.combine(f64(self.z), want.positions, self.route.weights.cpu().numpy(), f64(x))
+        close(self.out, ref, (self.k + 1) * 2.0 ** -24 * mag)
+        return total
+
+
+@pytest.mark.parametrize("T,D,H,E,k", [(1, 64, 96, 8, 2), (40, 288, 160, 6, 3), (300, 512, 544, 16, 4)])
+def test_layer_of_experts(T, D, H, E, k):
+    rng = np.random.default_rng(T)
+    layer = Layer(rng, T, D, H, E, k)
+    x = rows_of(rng, T, D, odd=False)
+    logits = torch.from_numpy(rng.standard_normal((T, E))).float().to(DEV)
+    logits[T // 2 + 1:T // 2 + 3] = -float("inf")                          # padding
+    layer(x, logits)
+    layer.check(x, logits)
+
+
+def test_layer_in_graphs_and_streams():
+    rng = np.random.default_rng(8)
+    T, D, H, E, k = 30, 256, 288, 8, 2
+    layers = [Layer(rng, T, D, H, E, k) for _ in range(2)]
+    inputs = [(rows_of(rng, T, D, odd=False), torch.from_numpy(rng.standard_normal((T, E))).float().to(DEV)) for _ in range(4)]
+    x, logits = inputs[0][0].clone(), inputs[0][1].clone()
+    for layer in layers:
+        layer(x, logits)
+    torch.cuda.synchronize()
+    graphs = []
+    for layer in layers:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            layer(x, logits)
+        graphs.append(g)
+    for new_x, new_logits in inputs[1:]:
+        x.copy_(new_x)
+        logits.copy_(new_logits)
+        for layer, g in zip(layers, graphs):
+            g.replay()
+            torch.cuda.synchronize()
+            layer.check(x, logits)
+            got = layer.out.clone()
+            assert torch.equal(layer(x, logits), got)                     # eager work between the replays
+    streams = [torch.cuda.Stream() for _ in layers]
+    want = [layer.out.clone() for layer in layers]
+    for layer in layers:
+        layer.out.zero_()
+    torch.cuda.synchronize()
+    for layer, st in zip(layers, streams):
+        with torch.cuda.stream(st):
+            for _ in range(5):
+                layer(x, logits)
+    torch.cuda.synchronize()
+    for layer, w in zip(layers, want):
+        assert torch.equal(layer.out, w)
