@@ -610,7 +610,7 @@ int pq_attn_decode(const pq_kv_cache* cache, const void* q_bf16, int64_t q_ld, i
  *
  * The format of pq_quantize_act, pq_quantize_weights (tensor_scale_out receives 1), pq_operand_bytes, pq_pack_operand,
  * pq_quantize_act_packed, pq_qgemm_packed, pq_qgemm_packed_bias and pq_qgemm_packed_f32, with group 32, any K that is a multiple of 32,
- * tensor scales ignored, and of the calls below; other calls refuse it with PQ_ERR_FORMAT.  Its operands are panels of 256 channels,
+ * tensor scales ignored, and of the calls below; other calls refuse it with PQ_ERR_FORMAT.  Its operands are panels of 128 channels,
  * zero from K on (pq_operand_bytes counts them).
  * Products are exact, sums fp32 over the whole of K, in an order that depends on M, N and K.
  */

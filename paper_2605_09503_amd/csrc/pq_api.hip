@@ -644,6 +644,7 @@ static int qgemm_packed_common(pq_format fmt, int group, const void* a_operand, 
                 (long long)ldy, (long long)N);
   if (!aligned16(a_operand) || !aligned16(w_operand) || !aligned16(y) || !aligned16(bias))
     return fail(PQ_ERR_SHAPE, "pq_qgemm_packed: buffers must be 16-byte aligned");
+  if (fmt == PQ_FMT_MXFP4 && ldy > (1 << 24)) return fail(PQ_ERR_SHAPE, "pq_qgemm_packed: ldy=%lld exceeds 2^24", (long long)ldy);
   if (fmt == PQ_FMT_MXFP4)
     return run_mx_gemm(MxCall{(const uint8_t*)a_operand, M, (const uint8_t*)w_operand, 0, 1, nullptr, nullptr, M, N, K, (const uint16_t*)bias, y,
                               ldy, out_f32},
@@ -857,7 +858,8 @@ int pq_qgemm_grouped(pq_format fmt, int group, const void* a_operand, int64_t a_
     return fail(PQ_ERR_SHAPE, "%s: a_rows=%lld rows cannot make M=%lld without an index", who, (long long)a_rows, (long long)M);
   if (M == 0 || a_rows == 0) return PQ_OK;
   if (!a_operand || !w_operands || !offsets || !y) return fail(PQ_ERR_NULL, "%s: a required pointer is NULL", who);
-  if (ldy < N || ldy % 8) return fail(PQ_ERR_SHAPE, "%s: ldy=%lld must be >= N=%lld and a multiple of 8", who, (long long)ldy, (long long)N);
+  if (ldy < N || ldy % 8 || ldy > (1 << 24))
+    return fail(PQ_ERR_SHAPE, "%s: ldy=%lld must be >= N=%lld, a multiple of 8 and at most 2^24", who, (long long)ldy, (long long)N);
   if (!aligned16(a_operand) || !aligned16(w_operands) || !aligned16(y) || !aligned16(bias))
     return fail(PQ_ERR_SHAPE, "%s: buffers must be 16-byte aligned", who);
   if (((uintptr_t)offsets | (uintptr_t)rows) & 3) return fail(PQ_ERR_SHAPE, "%s: offsets and rows must be 4-byte aligned", who);

@@ -46,10 +46,10 @@ __device__ __forceinline__ uint32_t mx_quantize8(const uint4& x, uint32_t& byte)
 }
 
 // ---------------------------------------------------------------- operand of the product
-// Panels of 256 channels: codes[panel][row][128 bytes], scales[panel][row][8 bytes], channels from K on zero (codes and scales).
-// A row's piece of a panel is one 128-byte line, so gathered rows read whole lines, and the rows of a tile lie next to each
-// other whatever K is (rows K / 2 bytes apart would meet in few channels of the caches where K is a power of two).
-constexpr int kMxPanel = 256;
+// Panels of 128 channels: codes[panel][row][64 bytes], scales[panel][row][4 bytes], channels from K on zero (codes and scales).
+// The rows of a tile lie next to each other whatever K is: whole lines are read (rows K / 2 bytes apart would meet in few channels of
+// the caches where K is a power of two), and a gathered row's piece is still half a line.
+constexpr int kMxPanel = 128;
 constexpr int kMxRowBytes = kMxPanel / 2, kMxRowScales = kMxPanel / kMxBlock;
 __host__ __device__ __forceinline__ int64_t mx_panels(int64_t K) { return (K + kMxPanel - 1) / kMxPanel; }
 __host__ __device__ __forceinline__ size_t mx_scales_at(int64_t rows, int64_t K) {

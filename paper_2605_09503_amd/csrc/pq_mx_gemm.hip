@@ -9,6 +9,7 @@ namespace {
 
 typedef int int4v __attribute__((ext_vector_type(4)));
 typedef int int8v __attribute__((ext_vector_type(8)));
+typedef uint32_t uint4v __attribute__((ext_vector_type(4)));
 typedef float float16v __attribute__((ext_vector_type(16)));
 
 // ---------------------------------------------------------------- which tile a workgroup computes
@@ -29,53 +30,99 @@ __device__ __forceinline__ int wave_scan(int v) {
   return v;
 }
 
-// Tiles of `bm` rows are counted through the experts in turn, each expert's rows start one.  Workgroups go round the eight
-// chiplets in turn; each chiplet takes a contiguous eighth of the tiles that there are (the launch has as many workgroups as there
-// could be), in blocks of eight tiles of rows, so that what its workgroups read at a time meets in its L2.
-// False where the workgroup has no tile.  Uniform; every wave does it for itself.
-__device__ __forceinline__ bool locate(const MxCall& c, int bm, int bn, Tile& t) {
-  const int lane = threadIdx.x & 63, M = (int)c.M, across = (int)((c.N + bn - 1) / bn);
-  const auto tiles_of = [&](int e, int& from, int& to) {
-    from = to = 0;
-    if (e < c.experts) {
-      from = min(max(c.offsets[e], 0), M);
-      to = min(max(c.offsets[e + 1], 0), M);
-    }
-    return to > from ? (to - from + bm - 1) / bm : 0;
-  };
-  int from, to, total = (M + bm - 1) / bm;
-  if (c.offsets) {
-    total = 0;
-    for (int e = 0; e < c.experts; e += 64) total += __builtin_amdgcn_readlane(wave_scan(tiles_of(e + lane, from, to)), 63);
+// rows from .. to - 1 of expert e, and how many tiles of bm they take: each expert's rows start one
+__device__ __forceinline__ int tiles_of(const MxCall& c, int bm, int e, int& from, int& to) {
+  from = to = 0;
+  if (e < c.experts) {
+    from = min(max(c.offsets[e], 0), (int)c.M);
+    to = min(max(c.offsets[e + 1], 0), (int)c.M);
   }
-  const int64_t all = (int64_t)total * across;
-  const int64_t per = all >> 3, extra = all & 7, chiplet = blockIdx.x & 7, at = blockIdx.x >> 3;
-  if (at >= per + (chiplet < extra ? 1 : 0)) return false;
-  const int64_t flat = chiplet * per + min(chiplet, extra) + at;
-  const int64_t block = (int64_t)8 * across, b = flat / block, in = flat - b * block;
-  const int high = min(8, total - (int)b * 8);
-  int mt = (int)(b * 8 + in % high);
-  t.n0 = in / high * bn;
-  if (!c.offsets) {
+  return to > from ? (to - from + bm - 1) / bm : 0;
+}
+// The tiles a workgroup computes.  Workgroups go round the eight chiplets in turn; each chiplet takes a contiguous eighth of the
+// tiles, in blocks of eight tiles of rows, and its workgroups go through it side by side: what they read at a time meets in its L2.
+template <bool GROUPED>
+struct Tiles {
+  // A table in LDS for up to kTable experts: tiles of the experts up to each one, and their offsets cut to 0 .. M.  What a search
+  // in memory waits for would hold up the loads that are on their way.
+  static constexpr int kTable = GROUPED ? 1024 : 0, kTableBytes = GROUPED ? (2 * kTable + 4) * 4 : 0;
+  int total, across, next, step, end;         // tiles of rows and of columns; numbers of this workgroup's tiles
+  const int32_t* table;                       // or null
+  __device__ __forceinline__ Tiles(const MxCall& c, int bm, int bn, int32_t* lds) {
+    table = nullptr;
+    if constexpr (GROUPED) {
+      const int lane = threadIdx.x & 63;
+      table = lds && c.experts <= kTable ? lds : nullptr;
+      total = 0;
+      for (int e = 0; e < c.experts; e += 64) {
+        int from, to;
+        const int upto = total + wave_scan(tiles_of(c, bm, e + lane, from, to));
+        if (table) {                                             // every wave writes the same
+          lds[e + lane] = upto;
+          lds[kTable + e + lane] = from;
+          if (e + lane == c.experts - 1) lds[kTable + e + lane + 1] = to;
+        }
+        total = __builtin_amdgcn_readlane(upto, 63);
+      }
+      if (table) __syncthreads();
+    } else {
+      total = (int)((c.M + bm - 1) / bm);
+    }
+    across = (int)((c.N + bn - 1) / bn);
+    const int all = total * across, per = all >> 3, extra = all & 7, chiplet = blockIdx.x & 7;
+    const int start = chiplet * per + min(chiplet, extra);
+    next = start + (int)(blockIdx.x >> 3);
+    step = (int)((gridDim.x + 7 - chiplet) >> 3);
+    end = start + per + (chiplet < extra ? 1 : 0);
+  }
+  // tile number `flat` (uniform)
+  __device__ __forceinline__ Tile at(const MxCall& c, int bm, int bn, int flat) const {
+    Tile t;
+    const int block = 8 * across, b = flat / block, in = flat - b * block, high = min(8, total - b * 8);
+    const int mt = b * 8 + in % high;
+    t.n0 = (int64_t)(in / high) * bn;
     t.first = (int64_t)mt * bm;
     t.end = min(t.first + bm, c.M);
     t.expert = 0;
-    return true;
-  }
-  for (int e = 0; e < c.experts; e += 64) {
-    const int n = tiles_of(e + lane, from, to), upto = wave_scan(n);
-    const uint64_t past = __ballot(upto > mt);
-    if (past) {
-      const int l = __builtin_ctzll(past);
-      const int start = __builtin_amdgcn_readlane(from, l) + (mt - (__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(n, l))) * bm;
-      t.first = start;
-      t.end = min(start + bm, __builtin_amdgcn_readlane(to, l));
-      t.expert = e + l;
-      return true;
+    if constexpr (!GROUPED) return t;
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+    for (int e = 0; e < c.experts; e += 64) {
+      int from = 0, to = 0, upto;
+      if (table)
+        upto = e + lane < c.experts ? table[e + lane] : total;
+      else
+        upto = before + wave_scan(tiles_of(c, bm, e + lane, from, to));
+      const uint64_t past = __ballot(upto > mt);
+      if (past) {
+        const int l = __builtin_ctzll(past);
+        if (table) {
+          from = table[kTable + e + l];
+          to = table[kTable + e + l + 1];
+          before = e + l ? table[e + l - 1] : 0;
+          from = __builtin_amdgcn_readfirstlane(from);
+          to = __builtin_amdgcn_readfirstlane(to);
+          before = __builtin_amdgcn_readfirstlane(before);
+        } else {
+          if (l) before = __builtin_amdgcn_readlane(upto, l - 1);
+          from = __builtin_amdgcn_readlane(from, l);
+          to = __builtin_amdgcn_readlane(to, l);
+        }
+        t.first = from + (int64_t)(mt - before) * bm;
+        t.end = min(t.first + bm, (int64_t)to);
+        t.expert = e + l;
+        break;
+      }
+      before = __builtin_amdgcn_readlane(upto, 63);
     }
-    mt -= __builtin_amdgcn_readlane(upto, 63);
+    return t;
   }
-  return false;
+};
+
+// a value that the compiler computes anew from here on: what is derived from it does not stay in registers across a loop
+__device__ __forceinline__ int opaque(int v) {
+  asm volatile("" : "+v"(v));
+  return v;
 }
 
 // the row of A that row m of y is made from, -1 where the index is none of A's
@@ -93,6 +140,13 @@ __device__ __forceinline__ void load16_to_lds(uint32_t to, const uint8_t* base, 
 __device__ __forceinline__ void load4_to_lds(uint32_t to, const uint8_t* base, uint32_t offset) {
   asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, %2" ::"{m0}"(to), "v"(offset), "s"(base) : "memory");
 }
+__device__ __forceinline__ void load4_to_lds(uint32_t to, const uint8_t* from) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dword %1, off" ::"{m0}"(to), "v"(from) : "memory");
+}
+// two bytes a lane, which take four in LDS
+__device__ __forceinline__ void load2_to_lds(uint32_t to, const uint8_t* base, uint32_t offset) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_ushort %1, %2" ::"{m0}"(to), "v"(offset), "s"(base) : "memory");
+}
 // all but the last N loads of this wave have arrived and its LDS reads are done
 template <int N>
 __device__ __forceinline__ void arrived() {
@@ -100,9 +154,9 @@ __device__ __forceinline__ void arrived() {
 }
 __device__ __forceinline__ void meet() { asm volatile("s_barrier" ::: "memory"); }
 
-// A row's piece of a panel is 128 bytes of LDS, its 16-byte blocks permuted by (row / 2) % 8: the 16 rows that a read takes at a
+// A row's piece of a panel is 64 bytes of LDS, its 16-byte blocks permuted by (row / 4) % 4: the 16 rows that a read takes at a
 // time then have a block in every bank.
-__device__ __forceinline__ int block_at(int row, int block) { return (block ^ ((row >> 1) & 7)) * 16; }
+__device__ __forceinline__ int block_at(int row, int block) { return (block ^ ((row >> 2) & 3)) * 16; }
 
 template <int SEL>
 __device__ __forceinline__ float16v mfma(const int4v& w, const int4v& a, const float16v& acc, int w_scale, int a_scale) {
@@ -115,18 +169,12 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
   return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)a) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)b) << 16;
 }
 // outputs n .. n + 7 of row m, n a multiple of 8
-__device__ __forceinline__ void store8(const MxCall& c, int64_t m, int64_t n, const float (&v)[8]) {
-  if (c.out_f32) {
-    float* y = (float*)c.y + m * c.ldy + n;
-    for (int e = 0; e < 8; ++e)
-      if (n + e < c.N) y[e] = v[e];
-    return;
-  }
+__device__ __forceinline__ void store8(const MxCall& c, int64_t m, int64_t n, const uint4& v) {
   uint16_t* y = (uint16_t*)c.y + m * c.ldy + n;
-  const uint32_t w[4] = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
   if (n + 7 < c.N) {
-    *reinterpret_cast<uint4*>(y) = make_uint4(w[0], w[1], w[2], w[3]);
+    *reinterpret_cast<uint4*>(y) = v;
   } else {
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
     for (int e = 0; e < 7; ++e)
       if (n + e < c.N) y[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
@@ -138,169 +186,303 @@ template <int BM, int BN, int WM, int WN>
 struct Shared {
   static constexpr int waves = WM * WN, fm = BM / WM / 32, fn = BN / WN / 32;       // fragments of 32 a wave
   static constexpr int a_scales = (BM + BN) * kMxRowBytes, w_scales = a_scales + BM * kMxRowScales;
-  static constexpr int stage = (BM + BN) * (kMxRowBytes + kMxRowScales), lds = 2 * stage;
-  static constexpr int a_loads = BM / 8 / waves, w_loads = BN / 8 / waves;           // of 8 rows
-  static constexpr int as_loads = BM / 32, ws_loads = BN / 32;                        // of 32 rows' scales, over all waves
-  static constexpr int pitch = fn * 32 + 4;                                           // floats a row of outputs
-  static_assert(waves * 32 * pitch * 4 <= lds, "32 rows of every wave's outputs");
-  static_assert((as_loads + ws_loads) % waves == 0, "every wave issues as many loads");
+  static constexpr int stages = 4, stage = (BM + BN) * (kMxRowBytes + kMxRowScales);
+  static constexpr int a_loads = BM / 16 / waves, w_loads = BN / 16 / waves;         // of 16 rows
+  static constexpr int as_loads = BM / 64, ws_loads = BN / 64;                        // of 64 rows' scales, over all waves
+  static constexpr int s_loads = (as_loads + ws_loads) / waves, loads = a_loads + w_loads + s_loads;
+  static constexpr int stores = fm * fn * 2;                                          // of a wave, a tile
+  // behind the stages, for this tile and the next: bias of its columns, a word each, and (grouped) the index of its rows; the table
+  static constexpr int bias = stages * stage, index = bias + 2 * BN * 4, table = index + 2 * BM * 4;
+  static constexpr int lds(bool grouped) { return grouped ? table + Tiles<true>::kTableBytes : index; }
+  static constexpr int few = 5;            // panels: with fewer the loads reach past the next tile, whose bias and index are read as they are needed
+  static_assert(fn * 32 <= 64, "a lane a column");
+  static_assert((as_loads + ws_loads) % waves == 0 && as_loads % s_loads == 0, "every wave issues as many loads");
 };
 
-template <int BM, int BN, int WM, int WN>
+// A workgroup goes through its tiles, and through the panels of each, without a stop: three panels are on their way while one is
+// multiplied, also where they are the next tile's.
+template <int BM, int BN, int WM, int WN, bool GROUPED>
 __global__ __launch_bounds__(WM* WN * 64, 2) void mx_gemm_shared_kernel(const MxCall c) {
   using S = Shared<BM, BN, WM, WN>;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  Tile t;
-  if (!locate(c, BM, BN, t)) return;
+  const Tiles<GROUPED> tiles(c, BM, BN, reinterpret_cast<int32_t*>(lds + S::table));
+  if (tiles.next >= tiles.end) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wave_m = wave % WM, wave_n = wave / WM;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
-
-  // loader: a load takes 8 rows' pieces of a panel, lane l the block that belongs at place l % 8 of row l / 8; rows past the
-  // tile's last re-read it (their outputs are not stored)
-  const int a_last = (int)(t.end - t.first) - 1, w_last = (int)min((int64_t)BN, c.N - t.n0) - 1;
-  const uint8_t *a = c.a, *w = c.w + (size_t)t.expert * c.w_next + t.n0 * kMxRowBytes;
-  const uint8_t *as = c.a + mx_scales_at(c.a_rows, c.K), *ws = c.w + (size_t)t.expert * c.w_next + mx_scales_at(c.N, c.K) + t.n0 * kMxRowScales;
-  const size_t a_next = (size_t)c.a_rows, w_next = (size_t)c.N;
-  const auto a_row = [&](int row) { return (uint32_t)max(a_row_of(c, t.first + min(row, a_last)), 0); };
-  uint32_t a_at[S::a_loads], w_at[S::w_loads], s_at[(S::as_loads + S::ws_loads) / S::waves];
-#pragma unroll
-  for (int i = 0; i < S::a_loads; ++i) {
-    const int row = 8 * (S::waves * i + wave) + (lane >> 3);
-    a_at[i] = a_row(row) * kMxRowBytes + block_at(row, lane & 7);
-  }
-#pragma unroll
-  for (int i = 0; i < S::w_loads; ++i) {
-    const int row = 8 * (S::waves * i + wave) + (lane >> 3);
-    w_at[i] = (uint32_t)min(row, w_last) * kMxRowBytes + block_at(row, lane & 7);
-  }
-#pragma unroll
-  for (int i = 0; i < (S::as_loads + S::ws_loads) / S::waves; ++i) {
-    const int j = S::waves * i + wave, row = (j < S::as_loads ? j : j - S::as_loads) * 32 + (lane >> 1);
-    s_at[i] = (j < S::as_loads ? a_row(row) : (uint32_t)min(row, w_last)) * kMxRowScales + (lane & 1) * 4;
-  }
   const int panels = (int)mx_panels(c.K);
-  const auto load = [&](int p, int stage) {
-    const uint32_t to = lds0 + stage * S::stage;
+  const bool ahead = panels >= S::few, index_ahead = GROUPED && c.rows && ahead;
+  const size_t as_at = mx_scales_at(c.a_rows, c.K), ws_at = mx_scales_at(c.N, c.K);
+
+  // Loader: a load takes 16 rows' pieces of a panel, lane l the block that belongs at place l % 4 of row l / 4 (the same for all of a
+  // wave's loads); rows past the tile's last re-read it (their outputs are not stored).  The scale loads of the first waves are of A's
+  // rows, of those behind of W's.
+  const bool s_of_a = wave * S::s_loads < S::as_loads;
+  const int s_first = (wave * S::s_loads - (s_of_a ? 0 : S::as_loads)) * 64;
+  // Few instructions a panel: the matrix unit takes 32 cycles an instruction, and whatever else a wave issues between two costs 4.
+  int load_tile = tiles.next, load_panel = 0;
+  bool more = true, drain = false;                             // the last load() was of a panel; it was a tile's last
+  int load_slot = 0;
+  Tile lt;
+  const uint8_t *a_from, *w_from, *s_from;                     // of the next panel
+  const size_t a_step = (size_t)c.a_rows * kMxRowBytes, w_step = (size_t)c.N * kMxRowBytes;
+  const size_t s_step = (size_t)(s_of_a ? c.a_rows : c.N) * kMxRowScales;
+  uint32_t a_off[S::a_loads], w_off[S::w_loads], s_off[S::s_loads];
+  const uint32_t blk = block_at(16 * wave + (lane >> 2), lane & 3);
+  const auto aim = [&] {                                       // at tile load_tile
+    lt = tiles.at(c, BM, BN, load_tile);
+    const int l = opaque(lane), first = 16 * wave + (l >> 2);
+    const int a_last = (int)(lt.end - lt.first) - 1, w_last = (int)min((int64_t)BN, c.N - lt.n0) - 1;
+    a_from = c.a + (GROUPED ? 0 : lt.first * kMxRowBytes);
+    w_from = c.w + (size_t)lt.expert * c.w_next;
+    s_from = s_of_a ? c.a + as_at + (GROUPED ? 0 : lt.first * kMxRowScales) : w_from + ws_at + lt.n0 * kMxRowScales;
+    w_from += lt.n0 * kMxRowBytes;
+    load_slot ^= 1;
+    if (c.bias && ahead && wave * 64 < BN)
+      load2_to_lds(lds0 + S::bias + (load_slot * BN + wave * 64) * 4, (const uint8_t*)(c.bias + lt.expert * c.N + lt.n0), (uint32_t)min(wave * 64 + l, w_last) * 2);
+    if (index_ahead && wave * 64 < BM)
+      load4_to_lds(lds0 + S::index + (load_slot * BM + wave * 64) * 4, (const uint8_t*)(c.rows + lt.first), (uint32_t)min(wave * 64 + l, a_last) * 4);
+    // grouped: the rows as the index gives them, which load() makes offsets of before it first uses them
+    const auto a_row = [&](int row) {
+      row = min(row, a_last);
+      return !GROUPED ? (uint32_t)row : index_ahead ? 0u : c.rows ? (uint32_t)c.rows[lt.first + row] : (uint32_t)lt.first + row;
+    };
 #pragma unroll
-    for (int i = 0; i < S::a_loads; ++i) load16_to_lds(to + (S::waves * i + wave) * 1024, a + p * a_next * kMxRowBytes, a_at[i]);
+    for (int i = 0; i < S::a_loads; ++i) {
+      a_off[i] = a_row(first + 16 * S::waves * i);
+      if constexpr (!GROUPED) a_off[i] = a_off[i] * kMxRowBytes + blk;
+    }
 #pragma unroll
-    for (int i = 0; i < S::w_loads; ++i) load16_to_lds(to + BM * kMxRowBytes + (S::waves * i + wave) * 1024, w + p * w_next * kMxRowBytes, w_at[i]);
+    for (int i = 0; i < S::w_loads; ++i) w_off[i] = (uint32_t)min(first + 16 * S::waves * i, w_last) * kMxRowBytes + blk;
 #pragma unroll
-    for (int i = 0; i < (S::as_loads + S::ws_loads) / S::waves; ++i) {
-      const int j = S::waves * i + wave;
-      load4_to_lds(to + S::a_scales + j * 256, j < S::as_loads ? as + p * a_next * kMxRowScales : ws + p * w_next * kMxRowScales, s_at[i]);
+    for (int i = 0; i < S::s_loads; ++i) {
+      const int row = s_first + 64 * i + l;
+      s_off[i] = s_of_a ? a_row(row) : (uint32_t)min(row, w_last);
+      if constexpr (!GROUPED) s_off[i] *= kMxRowScales;
+    }
+  };
+  const auto load = [&](int stage) {
+    more = load_tile < tiles.end;
+    if (!more) return;
+    drain = false;
+    if (GROUPED && load_panel == 0) {
+      if (index_ahead) {
+        const uint32_t* rows = reinterpret_cast<const uint32_t*>(lds + S::index) + load_slot * BM;
+        const int l = opaque(lane);
+#pragma unroll
+        for (int i = 0; i < S::a_loads; ++i) a_off[i] = rows[16 * (S::waves * i + wave) + (l >> 2)];
+        if (s_of_a) {
+#pragma unroll
+          for (int i = 0; i < S::s_loads; ++i) s_off[i] = rows[s_first + 64 * i + l];
+        }
+      }
+      const auto known = [&](uint32_t r) { return r < (uint32_t)c.a_rows ? r : 0u; };
+#pragma unroll
+      for (int i = 0; i < S::a_loads; ++i) a_off[i] = known(a_off[i]) * kMxRowBytes + blk;
+#pragma unroll
+      for (int i = 0; i < S::s_loads; ++i) s_off[i] = (s_of_a ? known(s_off[i]) : s_off[i]) * kMxRowScales;
+    }
+    const uint32_t to = lds0 + stage * S::stage + wave * 1024;
+#pragma unroll
+    for (int i = 0; i < S::a_loads; ++i) load16_to_lds(to + S::waves * i * 1024, a_from, a_off[i]);
+#pragma unroll
+    for (int i = 0; i < S::w_loads; ++i) load16_to_lds(to + BM * kMxRowBytes + S::waves * i * 1024, w_from, w_off[i]);
+#pragma unroll
+    for (int i = 0; i < S::s_loads; ++i) load4_to_lds(lds0 + stage * S::stage + S::a_scales + (wave * S::s_loads + i) * 256, s_from, s_off[i]);
+    a_from += a_step;
+    w_from += w_step;
+    s_from += s_step;
+    if (++load_panel == panels) {
+      load_panel = 0;
+      load_tile += tiles.step;
+      if (load_tile < tiles.end) {
+        aim();
+        drain = index_ahead;
+      }
     }
   };
 
   // lane l multiplies row l % 32 of a fragment, channels 32 (l / 32) .. of every 64
   const int row = lane & 31, half = lane >> 5;
-  int block[4];
-#pragma unroll
-  for (int s = 0; s < 4; ++s) block[s] = block_at(row, 2 * s + half);
-  const int a_base = (wave_m * S::fm * 32 + row) * kMxRowBytes, w_base = (BM + wave_n * S::fn * 32 + row) * kMxRowBytes;
+  // block 2 s + half of the row: its place is that of block `half` with a bit flipped
+  const int a_base = (wave_m * S::fm * 32 + row) * kMxRowBytes + block_at(row, half);
+  const int w_base = (BM + wave_n * S::fn * 32 + row) * kMxRowBytes + block_at(row, half);
+  static_assert(S::stage % kMxRowBytes == 0, "rows of a stage are aligned to their size");
   const int as_base = S::a_scales + (wave_m * S::fm * 32 + row) * kMxRowScales, ws_base = S::w_scales + (wave_n * S::fn * 32 + row) * kMxRowScales;
 
   float16v acc[S::fn][S::fm];
-#pragma unroll
-  for (int i = 0; i < S::fn; ++i)
-#pragma unroll
-    for (int j = 0; j < S::fm; ++j) acc[i][j] = float16v{};
-
   int4v af[2][S::fm], wf[2][S::fn];
-  int asc[S::fm][2], wsc[S::fn][2];            // a row's scale bytes of 128 channels a word, this lane's blocks in bytes 0 and 2
-  const auto read = [&](int set, int stage, int s) {
-    const unsigned char* at = lds + stage * S::stage + block[s];
-#pragma unroll
-    for (int i = 0; i < S::fn; ++i) wf[set][i] = *reinterpret_cast<const int4v*>(at + w_base + i * 32 * kMxRowBytes);
-#pragma unroll
-    for (int j = 0; j < S::fm; ++j) af[set][j] = *reinterpret_cast<const int4v*>(at + a_base + j * 32 * kMxRowBytes);
-  };
-  const auto read_scales = [&](int stage, int (&sa)[S::fm][2], int (&sw)[S::fn][2]) {
-    const unsigned char* at = lds + stage * S::stage;
-#pragma unroll
-    for (int i = 0; i < S::fn; ++i) {
-      const uint2 v = *reinterpret_cast<const uint2*>(at + ws_base + i * 32 * kMxRowScales);
-      sw[i][0] = (int)(v.x >> (8 * half)), sw[i][1] = (int)(v.y >> (8 * half));
-    }
-#pragma unroll
-    for (int j = 0; j < S::fm; ++j) {
-      const uint2 v = *reinterpret_cast<const uint2*>(at + as_base + j * 32 * kMxRowScales);
-      sa[j][0] = (int)(v.x >> (8 * half)), sa[j][1] = (int)(v.y >> (8 * half));
-    }
-  };
-#define PQ_MULTIPLY(set, s)                                                                                             \
-  _Pragma("unroll") for (int i = 0; i < S::fn; ++i) _Pragma("unroll") for (int j = 0; j < S::fm; ++j) acc[i][j] =       \
-      mfma<2 * ((s) & 1)>(wf[set][i], af[set][j], acc[i][j], wsc[i][(s) >> 1], asc[j][(s) >> 1])
-
-  // The fragments of 64 channels are read while those before them are multiplied; the barrier stands before the last of a panel:
-  // behind it the next panel has arrived in the other stage, and this one's is free for the panel after that.
-  load(0, 0);
-  arrived<0>();
-  meet();
-  if (panels > 1) load(1, 1);
-  read_scales(0, asc, wsc);
-  read(0, 0, 0);
-  for (int p = 0; p < panels; ++p) {
-    const int stage = p & 1;
-    read(1, stage, 1);
-    PQ_MULTIPLY(0, 0);
-    __builtin_amdgcn_sched_barrier(0);
-    read(0, stage, 2);
-    PQ_MULTIPLY(1, 1);
-    __builtin_amdgcn_sched_barrier(0);
-    read(1, stage, 3);
-    PQ_MULTIPLY(0, 2);
-    if (p + 1 < panels) {
-      arrived<0>();
-      meet();
-      if (p + 2 < panels) load(p + 2, stage);
-      read(0, stage ^ 1, 0);
-      int na[S::fm][2], nw[S::fn][2];
-      read_scales(stage ^ 1, na, nw);
-      PQ_MULTIPLY(1, 3);
-#pragma unroll
-      for (int j = 0; j < S::fm; ++j) asc[j][0] = na[j][0], asc[j][1] = na[j][1];
-#pragma unroll
-      for (int i = 0; i < S::fn; ++i) wsc[i][0] = nw[i][0], wsc[i][1] = nw[i][1];
-    } else {
-      PQ_MULTIPLY(1, 3);
-    }
-  }
-#undef PQ_MULTIPLY
-
-  // A lane has row l % 32 of a fragment and columns 8 q + 4 (l / 32) + 0 .. 3.  Through LDS, 32 rows at a time in a part of the wave's
-  // own, a row's columns come together: whole lines are stored, eight columns a lane.
-  arrived<0>();
-  meet();
-  float* part = reinterpret_cast<float*>(lds) + wave * 32 * S::pitch;
-  constexpr int lanes = S::fn * 4, at_once = 64 / lanes;                // lanes a row, rows a store
-  const int64_t n = t.n0 + wave_n * S::fn * 32 + lane % lanes * 8;
-  float bias[8] = {};
-  if (c.bias) {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) bias[e] = bf16_to_f32(c.bias[t.expert * c.N + min(n + e, c.N - 1)]);
-  }
-#pragma unroll
-  for (int j = 0; j < S::fm; ++j) {
+  int asc[S::fm], wsc[S::fn];                  // scale bytes of this lane's two blocks of a panel: 0 and 2
+  const auto clear = [&] {
 #pragma unroll
     for (int i = 0; i < S::fn; ++i)
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        *reinterpret_cast<float4*>(part + row * S::pitch + 32 * i + 8 * q + 4 * half) =
-            make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-#pragma unroll 1
-    for (int r = lane / lanes; r < 32; r += at_once) {
-      const float* from = part + r * S::pitch + lane % lanes * 8;
-      const float4 x = *reinterpret_cast<const float4*>(from), z = *reinterpret_cast<const float4*>(from + 4);
-      const int64_t m = t.first + (wave_m * S::fm + j) * 32 + r;
-      if (m >= t.end || n >= c.N || a_row_of(c, m) < 0) continue;
-      store8(c, m, n, {x.x + bias[0], x.y + bias[1], x.z + bias[2], x.w + bias[3], z.x + bias[4], z.y + bias[5], z.z + bias[6], z.w + bias[7]});
+      for (int j = 0; j < S::fm; ++j) acc[i][j] = float16v{};
+  };
+  const auto read = [&](int set, int stage, int s) {
+    const unsigned char *wp = lds + ((stage * S::stage + w_base) ^ (32 * s)), *ap = lds + ((stage * S::stage + a_base) ^ (32 * s));
+#pragma unroll
+    for (int i = 0; i < S::fn; ++i) wf[set][i] = *reinterpret_cast<const int4v*>(wp + i * 32 * kMxRowBytes);
+#pragma unroll
+    for (int j = 0; j < S::fm; ++j) af[set][j] = *reinterpret_cast<const int4v*>(ap + j * 32 * kMxRowBytes);
+  };
+  const auto read_scales = [&](int stage, int (&sa)[S::fm], int (&sw)[S::fn]) {
+    const unsigned char* at = lds + stage * S::stage;
+#pragma unroll
+    for (int i = 0; i < S::fn; ++i) sw[i] = *reinterpret_cast<const int*>(at + ws_base + i * 32 * kMxRowScales);
+#pragma unroll
+    for (int j = 0; j < S::fm; ++j) sa[j] = *reinterpret_cast<const int*>(at + as_base + j * 32 * kMxRowScales);
+  };
+  const auto take_scales = [&](const int (&sa)[S::fm], const int (&sw)[S::fn]) {
+#pragma unroll
+    for (int i = 0; i < S::fn; ++i) wsc[i] = (int)((uint32_t)sw[i] >> (8 * half));
+#pragma unroll
+    for (int j = 0; j < S::fm; ++j) asc[j] = (int)((uint32_t)sa[j] >> (8 * half));
+  };
+#define PQ_MULTIPLY(s)                                                                                                  \
+  _Pragma("unroll") for (int i = 0; i < S::fn; ++i) _Pragma("unroll") for (int j = 0; j < S::fm; ++j) acc[i][j] =       \
+      mfma<2 * (s)>(wf[s][i], af[s][j], acc[i][j], wsc[i], asc[j]);                                                     \
+  pin()
+
+  // the products stay in front of what follows: moved behind the barrier they would hold the fragments of a whole panel
+  const auto pin = [&] {
+#pragma unroll
+    for (int i = 0; i < S::fn; ++i)
+#pragma unroll
+      for (int j = 0; j < S::fm; ++j) asm volatile("" : "+v"(acc[i][j]));
+  };
+
+  // A lane has row l % 32 of a fragment and columns 8 q + 4 (l / 32) + 0 .. 3; the two halves of the wave exchange what makes eight
+  // columns of a row, lanes below 32 of q = 0 and 2, those above of 1 and 3.  The stores are S::stores of a wave whatever they
+  // keep (what has no place goes past the buffer's end and is dropped), so that waits can count past them.
+  const auto store = [&](const Tile& t, int slot) {
+    if (c.out_f32) {                                           // for checks of the sums: no care taken of its speed
+      const int l = opaque(lane);
+#pragma unroll
+      for (int i = 0; i < S::fn; ++i)
+#pragma unroll
+        for (int j = 0; j < S::fm; ++j)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int64_t m = t.first + (wave_m * S::fm + j) * 32 + (l & 31), n = t.n0 + (wave_n * S::fn + i) * 32 + 8 * (e >> 2) + 4 * (l >> 5) + (e & 3);
+            if (m < t.end && n < c.N) ((float*)c.y)[m * c.ldy + n] = acc[i][j][e];
+          }
+      return;
     }
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    const int l = opaque(lane), h = l >> 5;
+    const int64_t n0 = t.n0 + wave_n * S::fn * 32;
+    const int cols = (int)min(c.N - n0, (int64_t)S::fn * 32);  // of this wave; may be none
+    if (c.bias && !ahead) {                                    // this wave's columns, as the loader would have left them
+      if (l < S::fn * 32)
+        reinterpret_cast<uint32_t*>(lds + S::bias)[slot * BN + wave_n * S::fn * 32 + l] = c.bias[t.expert * c.N + min(n0 + l, c.N - 1)];
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+    // added also where there is none (zeros): sums that a branch changes would be copied
+#pragma unroll
+    for (int i = 0; i < S::fn; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint4v b = *reinterpret_cast<const uint4v*>(lds + S::bias + (slot * BN + wave_n * S::fn * 32 + 32 * i + 8 * q + 4 * h) * 4);
+#pragma unroll
+        for (int j = 0; j < S::fm; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += as_f32(b[e] << 16);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    uint64_t kept[(S::fm + 1) / 2];                            // rows of this wave that have one of A's
+    if (GROUPED && c.rows) {
+#pragma unroll
+      for (int j = 0; j < (S::fm + 1) / 2; ++j) {
+        const int r = wave_m * S::fm * 32 + 64 * j + l;
+        const int64_t m = min(t.first + r, t.end - 1);
+        const uint32_t from = index_ahead ? reinterpret_cast<const uint32_t*>(lds + S::index)[slot * BM + min(r, BM - 1)] : (uint32_t)c.rows[m];
+        kept[j] = __ballot(from < (uint32_t)c.a_rows);
+      }
+    }
+    constexpr int kNowhere = 0x7FFFFFF0;
+#pragma unroll
+    for (int j = 0; j < S::fm; ++j) {
+      const int64_t m0 = t.first + (wave_m * S::fm + j) * 32;
+      const int rows = (int)min(t.end - m0, (int64_t)32), r = l & 31;
+      bool ok = r < rows;
+      if (GROUPED && c.rows) ok = ok && (kept[j / 2] >> (32 * (j & 1) + r) & 1);
+      uint16_t* y = (uint16_t*)c.y + m0 * c.ldy + n0;
+      const auto buf = __builtin_amdgcn_make_buffer_rsrc(y, 0, 0x7FFFFFF0, 0x00027000);
+      const int at = r * (int)c.ldy * 2 + 16 * h;
+#pragma unroll
+      for (int i = 0; i < S::fn; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; q += 2) {
+          const auto pack = [&](int g, int e) { return pack_bf16(acc[i][j][4 * g + e], acc[i][j][4 * g + e + 1]); };
+          const auto x = __builtin_amdgcn_permlane32_swap(pack(q, 0), pack(q + 1, 0), false, false);
+          const auto z = __builtin_amdgcn_permlane32_swap(pack(q, 2), pack(q + 1, 2), false, false);
+          const int col = 32 * i + 8 * q + 8 * h;
+          const uint4v v = {x[0], z[0], x[1], z[1]};
+          __builtin_amdgcn_raw_buffer_store_b128(v, buf, ok && col + 8 <= cols ? at + 64 * i + 16 * q : kNowhere, 0, 0);
+          if (c.N & 7) {                                       // uniform; the last columns of rows that end inside eight
+#pragma unroll
+            for (int e = 0; e < 7; ++e)
+              __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(v[e >> 1] >> (16 * (e & 1))), buf,
+                                                    ok && col + 8 > cols && col + e < cols ? at + 64 * i + 16 * q + 2 * e : kNowhere, 0, 0);
+          }
+        }
+    }
+  };
+
+  // The fragments of 64 channels are read while those before them are multiplied; the barrier stands before the last of a panel:
+  // behind it the next panel has arrived, and the stage of the one before this one is free for the panel three on.
+  if (!c.bias)
+    for (int i = tid; i < 2 * BN; i += S::waves * 64) reinterpret_cast<uint32_t*>(lds + S::bias)[i] = 0;
+  aim();
+  Tile t = lt;
+  int stage = 0, slot = load_slot;
+  if (index_ahead) {
+    arrived<0>();
+    meet();
   }
+#pragma unroll
+  for (int p = 0; p < S::stages - 1; ++p) load(p);
+  if (more && !drain)
+    arrived<(S::stages - 2) * S::loads>();
+  else
+    arrived<0>();
+  meet();
+  read_scales(0, asc, wsc);
+  take_scales(asc, wsc);
+  read(0, 0, 0);
+  bool stored = false;                                         // the tile before this one issued S::stores stores, and they may be under way
+  for (int tile = tiles.next; tile < tiles.end; tile += tiles.step) {
+    clear();
+    for (int p = 0; p < panels; ++p) {
+      load((stage + S::stages - 1) & (S::stages - 1));
+      read(1, stage, 1);
+      PQ_MULTIPLY(0);
+      __builtin_amdgcn_sched_barrier(0);
+      // What is waited for is the next panel.  Behind its loads come those of two more, and in a tile's first two panels the
+      // stores of the tile before.
+      if (!more || drain)
+        arrived<0>();
+      else if (stored && p < 2)
+        arrived<(S::stages - 2) * S::loads + S::stores>();
+      else
+        arrived<(S::stages - 2) * S::loads>();
+      meet();
+      stage = (stage + 1) & (S::stages - 1);
+      read(0, stage, 0);                                       // of no use behind the last panel of all
+      int na[S::fm], nw[S::fn];
+      read_scales(stage, na, nw);
+      PQ_MULTIPLY(1);
+      __builtin_amdgcn_sched_barrier(0);
+      take_scales(na, nw);
+    }
+    store(t, slot);
+    stored = panels >= 2 && !c.out_f32 && (c.N & 7) == 0;
+    slot ^= 1;
+    // the loads are up to three panels ahead, in the next tile where a tile has more than three
+    if (tile + tiles.step < tiles.end) t = panels > 3 ? lt : tiles.at(c, BM, BN, tile + tiles.step);
+  }
+#undef PQ_MULTIPLY
 }
 
 // ---------------------------------------------------------------- small tiles whose waves share K
@@ -309,19 +491,20 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void mx_gemm_shared_kernel(const Mx
 template <int FM, int KW>
 struct Split {
   static constexpr int bm = 32 * FM, bn = 32;
-  static constexpr int a_scales = (bm + bn) * kMxRowBytes, w_scales = a_scales + bm * kMxRowScales;
-  static constexpr int stage = (bm + bn) * (kMxRowBytes + kMxRowScales), own = 2 * stage, lds = KW * own;
-  static constexpr int loads = (bm + bn) / 8 + (bm + bn) / 32;
+  static constexpr int scales = (bm + bn) * kMxRowBytes;
+  static constexpr int stages = 4, stage = (bm + bn) * kMxRowBytes + FM * 256, own = stages * stage, lds = KW * own;
+  static constexpr int loads = (bm + bn) / 16 + FM;
   static constexpr int pitch = 36;                                     // floats a row of sums: rows start four banks apart
   static_assert(bm * pitch * 4 <= own, "the sums take a wave's own part");
 };
 
-template <int FM, int KW>
+template <int FM, int KW, bool GROUPED>
 __global__ __launch_bounds__(KW * 64) void mx_gemm_split_kernel(const MxCall c) {
   using S = Split<FM, KW>;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
-  Tile t;
-  if (!locate(c, S::bm, S::bn, t)) return;
+  const Tiles<GROUPED> tiles(c, S::bm, S::bn, nullptr);
+  if (tiles.next >= tiles.end) return;
+  const Tile t = tiles.at(c, S::bm, S::bn, tiles.next);
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   unsigned char* own = lds + wave * S::own;
@@ -332,30 +515,32 @@ __global__ __launch_bounds__(KW * 64) void mx_gemm_split_kernel(const MxCall c) 
   const uint8_t *as = c.a + mx_scales_at(c.a_rows, c.K), *ws = c.w + (size_t)t.expert * c.w_next + mx_scales_at(c.N, c.K) + t.n0 * kMxRowScales;
   const size_t a_next = (size_t)c.a_rows, w_next = (size_t)c.N;
   const auto a_row = [&](int row) { return (uint32_t)max(a_row_of(c, t.first + min(row, a_last)), 0); };
-  uint32_t a_at[4 * FM], w_at[4], as_at[FM], ws_at;
+  uint32_t a_at[2 * FM], w_at[2], s_at[FM];
 #pragma unroll
-  for (int i = 0; i < 4 * FM; ++i) {
-    const int row = 8 * i + (lane >> 3);
-    a_at[i] = a_row(row) * kMxRowBytes + block_at(row, lane & 7);
+  for (int i = 0; i < 2 * FM; ++i) {
+    const int row = 16 * i + (lane >> 2);
+    a_at[i] = a_row(row) * kMxRowBytes + block_at(row, lane & 3);
   }
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = 8 * i + (lane >> 3);
-    w_at[i] = (uint32_t)min(row, w_last) * kMxRowBytes + block_at(row, lane & 7);
+  for (int i = 0; i < 2; ++i) {
+    const int row = 16 * i + (lane >> 2);
+    w_at[i] = (uint32_t)min(row, w_last) * kMxRowBytes + block_at(row, lane & 3);
   }
+  // scales: W's 32 rows and A's first 32 in one load, A's other 32 (and W's again) in the next
+  const bool of_w = lane < 32;
 #pragma unroll
-  for (int i = 0; i < FM; ++i) as_at[i] = a_row(32 * i + (lane >> 1)) * kMxRowScales + (lane & 1) * 4;
-  ws_at = (uint32_t)min(lane >> 1, w_last) * kMxRowScales + (lane & 1) * 4;
+  for (int i = 0; i < FM; ++i) s_at[i] = (of_w ? (uint32_t)min(lane, w_last) : a_row(32 * i + lane - 32)) * kMxRowScales;
+  const uint8_t* s_base = of_w ? ws : as;
+  const size_t s_next = (of_w ? w_next : a_next) * kMxRowScales;
   const int panels = (int)mx_panels(c.K);
   const auto load = [&](int p, int stage) {
     const uint32_t to = lds0 + stage * S::stage;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) load16_to_lds(to + S::bm * kMxRowBytes + i * 1024, w + p * w_next * kMxRowBytes, w_at[i]);
-    load4_to_lds(to + S::w_scales, ws + p * w_next * kMxRowScales, ws_at);
+    for (int i = 0; i < 2; ++i) load16_to_lds(to + S::bm * kMxRowBytes + i * 1024, w + p * w_next * kMxRowBytes, w_at[i]);
 #pragma unroll
-    for (int i = 0; i < 4 * FM; ++i) load16_to_lds(to + i * 1024, a + p * a_next * kMxRowBytes, a_at[i]);
+    for (int i = 0; i < 2 * FM; ++i) load16_to_lds(to + i * 1024, a + p * a_next * kMxRowBytes, a_at[i]);
 #pragma unroll
-    for (int i = 0; i < FM; ++i) load4_to_lds(to + S::a_scales + i * 256, as + p * a_next * kMxRowScales, as_at[i]);
+    for (int i = 0; i < FM; ++i) load4_to_lds(to + S::scales + i * 256, s_base + p * s_next + s_at[i]);
   };
 
   const int row = lane & 31, half = lane >> 5;
@@ -364,39 +549,38 @@ __global__ __launch_bounds__(KW * 64) void mx_gemm_split_kernel(const MxCall c) 
   for (int j = 0; j < FM; ++j) acc[j] = float16v{};
   const auto multiply = [&](int stage) {
     const unsigned char* at = own + stage * S::stage;
-    int4v wf[4], af[4][FM];
-    uint2 sw = *reinterpret_cast<const uint2*>(at + S::w_scales + row * kMxRowScales), sa[FM];
-    const int wl = (int)(sw.x >> (8 * half)), wh = (int)(sw.y >> (8 * half));
+    int4v wf[2], af[2][FM];
+    const int sw = (int)(*reinterpret_cast<const uint32_t*>(at + S::scales + row * 4) >> (8 * half));
+    int sa[FM];
 #pragma unroll
-    for (int j = 0; j < FM; ++j) sa[j] = *reinterpret_cast<const uint2*>(at + S::a_scales + (32 * j + row) * kMxRowScales);
+    for (int j = 0; j < FM; ++j) sa[j] = (int)(*reinterpret_cast<const uint32_t*>(at + S::scales + j * 256 + 128 + row * 4) >> (8 * half));
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
+    for (int s = 0; s < 2; ++s) {
       wf[s] = *reinterpret_cast<const int4v*>(at + (S::bm + row) * kMxRowBytes + block_at(row, 2 * s + half));
 #pragma unroll
       for (int j = 0; j < FM; ++j) af[s][j] = *reinterpret_cast<const int4v*>(at + (32 * j + row) * kMxRowBytes + block_at(row, 2 * s + half));
     }
 #pragma unroll
     for (int j = 0; j < FM; ++j) {
-      const int al = (int)(sa[j].x >> (8 * half)), ah = (int)(sa[j].y >> (8 * half));
-      acc[j] = mfma<0>(wf[0], af[0][j], acc[j], wl, al);
-      acc[j] = mfma<2>(wf[1], af[1][j], acc[j], wl, al);
-      acc[j] = mfma<0>(wf[2], af[2][j], acc[j], wh, ah);
-      acc[j] = mfma<2>(wf[3], af[3][j], acc[j], wh, ah);
+      acc[j] = mfma<0>(wf[0], af[0][j], acc[j], sw, sa[j]);
+      acc[j] = mfma<2>(wf[1], af[1][j], acc[j], sw, sa[j]);
     }
   };
-  if (wave < panels) load(wave, 0);
-  if (wave + KW < panels) load(wave + KW, 1);
+#pragma unroll
+  for (int i = 0; i < S::stages; ++i)
+    if (wave + i * KW < panels) load(wave + i * KW, i);
   int stage = 0;
-  for (int p = wave; p < panels; p += KW, stage ^= 1) {
-    if (p + KW < panels)
-      arrived<S::loads>();
+  for (int p = wave; p < panels; p += KW) {
+    if (p + (S::stages - 1) * KW < panels)
+      arrived<(S::stages - 1) * S::loads>();
     else
       arrived<0>();
     multiply(stage);
-    if (p + 2 * KW < panels) {
-      arrived<S::loads>();                               // this stage's reads are done
-      load(p + 2 * KW, stage);
+    if (p + S::stages * KW < panels) {
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");       // this stage's reads are done
+      load(p + S::stages * KW, stage);
     }
+    stage = (stage + 1) % S::stages;
   }
   // sums: row m = l % 32, columns 8 q + 4 (l / 32) .. of this wave's part
   arrived<0>();
@@ -423,42 +607,60 @@ __global__ __launch_bounds__(KW * 64) void mx_gemm_split_kernel(const MxCall c) 
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += bf16_to_f32(c.bias[t.expert * c.N + min(n + e, c.N - 1)]);
     }
-    store8(c, m, n, v);
+    if (c.out_f32) {
+      for (int e = 0; e < 8; ++e)
+        if (n + e < c.N) ((float*)c.y)[m * c.ldy + n + e] = v[e];
+    } else {
+      store8(c, m, n, make_uint4(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])));
+    }
   }
 }
 
+// `most`: workgroups that run at a time and go through all tiles, or 0: one for every tile that there could be (those beyond the
+// tiles that there are end at once)
 template <class K>
-int launch(K kernel, const char* name, const MxCall& c, int bm, int bn, int waves, int lds, std::atomic<uint64_t>& allowed, hipStream_t st) {
+int launch(K kernel, const char* name, const MxCall& c, int bm, int bn, int waves, int lds, int most, std::atomic<uint64_t>& allowed,
+           hipStream_t st) {
   const int64_t tiles_m = (c.M + bm - 1) / bm + (c.offsets ? (c.experts < c.M ? c.experts : c.M) : 0), across = (c.N + bn - 1) / bn;
-  // a grid has fewer than 2^32 threads; workgroups beyond the tiles that there are end at once
+  // a grid has fewer than 2^32 threads
   if (tiles_m * across + 8 >= ((int64_t)1 << 26) / waves)
     return fail(PQ_ERR_SHAPE, "MXFP4 product: M=%lld N=%lld are too many tiles for one call", (long long)c.M, (long long)c.N);
   int rc = allow_lds((const void*)kernel, (size_t)lds, allowed, name);
   if (rc) return rc;
-  kernel<<<(unsigned)((tiles_m * across + 7) / 8 * 8), waves * 64, lds, st>>>(c);
+  const int64_t n = (tiles_m * across + 7) / 8 * 8;
+  kernel<<<(unsigned)(most && most < n ? most : n), waves * 64, lds, st>>>(c);
   return check_hip(hipGetLastError(), name);
 }
 
-template <int BM, int BN, int WM, int WN>
+constexpr int kUnits = 256;                  // compute units
+
+template <int BM, int BN, int WM, int WN, bool GROUPED>
 int launch_shared(const MxCall& c, hipStream_t st) {
+  using S = Shared<BM, BN, WM, WN>;
   static std::atomic<uint64_t> allowed{0};
-  return launch(mx_gemm_shared_kernel<BM, BN, WM, WN>, "mx_gemm_shared_kernel", c, BM, BN, WM * WN, Shared<BM, BN, WM, WN>::lds, allowed, st);
+  return launch(mx_gemm_shared_kernel<BM, BN, WM, WN, GROUPED>, "mx_gemm_shared_kernel", c, BM, BN, S::waves, S::lds(GROUPED),
+                kUnits * (160 * 1024 / S::lds(GROUPED)), allowed, st);
 }
-template <int FM, int KW>
+template <int FM, int KW, bool GROUPED>
 int launch_split(const MxCall& c, hipStream_t st) {
   static std::atomic<uint64_t> allowed{0};
-  return launch(mx_gemm_split_kernel<FM, KW>, "mx_gemm_split_kernel", c, 32 * FM, 32, KW, Split<FM, KW>::lds, allowed, st);
+  return launch(mx_gemm_split_kernel<FM, KW, GROUPED>, "mx_gemm_split_kernel", c, 32 * FM, 32, KW, Split<FM, KW>::lds, 0, allowed, st);
+}
+
+template <bool GROUPED>
+int run(const MxCall& c, hipStream_t st) {
+  const int64_t groups = GROUPED ? c.experts : 1, each = (c.M + groups - 1) / groups;
+  if (each <= 32) return launch_split<1, 4, GROUPED>(c, st);
+  if (each <= 64) return launch_split<2, 4, GROUPED>(c, st);
+  if (((each + 255) / 256) * ((c.N + 255) / 256) * groups < 200) return launch_shared<128, 128, 2, 2, GROUPED>(c, st);
+  return launch_shared<256, 256, 2, 4, GROUPED>(c, st);
 }
 
 }  // namespace
 
 int run_mx_gemm(const MxCall& c, hipStream_t st) {
   if (c.M == 0) return PQ_OK;
-  const int64_t each = c.offsets ? (c.M + c.experts - 1) / c.experts : c.M;
-  if (each <= 32) return launch_split<1, 4>(c, st);
-  if (each <= 64) return launch_split<2, 4>(c, st);
-  if (((each + 255) / 256) * ((c.N + 255) / 256) * (c.offsets ? c.experts : 1) < 200) return launch_shared<128, 128, 2, 2>(c, st);
-  return launch_shared<256, 256, 2, 4>(c, st);
+  return c.offsets ? run<true>(c, st) : run<false>(c, st);
 }
 
 }  // namespace pq

@@ -35,13 +35,13 @@ __global__ __launch_bounds__(kThreads) void mx_quantize_rows_kernel(const uint16
   }
 }
 
-// Operand layout: 32 lanes a row's piece of a panel.
+// Operand layout: 16 lanes a row's piece of a panel.
 __global__ __launch_bounds__(kThreads) void mx_quantize_operand_kernel(const uint16_t* __restrict__ x, int64_t rows, int64_t K, int64_t ld,
                                                                        uint8_t* __restrict__ operand, size_t scales_at,
                                                                        uint8_t* __restrict__ codes, uint8_t* __restrict__ scales) {
-  const int64_t n = mx_panels(K) * rows * 32;
+  const int64_t n = mx_panels(K) * rows * 16;
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) {
-    const int64_t piece = i >> 5, p = piece / rows, r = piece - p * rows, k = p * kMxPanel + (i & 31) * 8;
+    const int64_t piece = i >> 4, p = piece / rows, r = piece - p * rows, k = p * kMxPanel + (i & 15) * 8;
     uint32_t byte = 0, q = 0;
     if (k < K) {                                             // K is a multiple of 32: the four lanes of a group together
       q = mx_quantize8(*reinterpret_cast<const uint4*>(x + r * ld + k), byte);
@@ -126,7 +126,7 @@ int launch_mx_quantize_rows(const void* x, int64_t rows, int64_t K, int64_t ld, 
 
 int launch_mx_quantize_operand(const void* x, int64_t rows, int64_t K, int64_t ld, void* operand, uint8_t* codes, void* scales,
                                hipStream_t st) {
-  mx_quantize_operand_kernel<<<blocks_for(mx_panels(K) * rows * 32), kThreads, 0, st>>>((const uint16_t*)x, rows, K, ld, (uint8_t*)operand,
+  mx_quantize_operand_kernel<<<blocks_for(mx_panels(K) * rows * 16), kThreads, 0, st>>>((const uint16_t*)x, rows, K, ld, (uint8_t*)operand,
                                                                                         mx_scales_at(rows, K), codes, (uint8_t*)scales);
   return check_hip(hipGetLastError(), "mx_quantize_operand_kernel");
 }

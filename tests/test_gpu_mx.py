@@ -123,9 +123,9 @@ def test_operand_is_the_packed_stored_form(rows, K, gap):
     pq.pq_quantize_act_packed(MX, 32, x, None, b, got_codes, got_scales)
     assert torch.equal(got_codes, codes) and torch.equal(got_scales, scales)
     # what lies between the parts to make them multiples of 256 bytes is nobody's
-    panels = (K + 255) // 256
-    at = (panels * rows * 128 + 255) // 256 * 256
-    for part in (slice(0, panels * rows * 128), slice(at, at + panels * rows * 8)):
+    panels = (K + 127) // 128
+    at = (panels * rows * 64 + 255) // 256 * 256
+    for part in (slice(0, panels * rows * 64), slice(at, at + panels * rows * 4)):
         assert torch.equal(a[part], b[part])
 
 

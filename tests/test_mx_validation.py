@@ -14,10 +14,10 @@ MX = pq.FMT_MXFP4
 
 def test_operand_bytes(lib):  # noqa: F811
     f = pq.pq_operand_bytes
-    assert f(MX, 32, 64, 256) == 64 * (128 + 8)
-    assert f(MX, 32, 64, 288) == 2 * 64 * (128 + 8)               # panels of 256 channels
-    assert f(MX, 32, 3, 32) == 512 + 256                          # 384 and 24 bytes, each to a multiple of 256
-    assert f(MX, 32, 1 << 24, 1 << 24) == (1 << 16) * (1 << 24) * 136
+    assert f(MX, 32, 64, 128) == 64 * (64 + 4)
+    assert f(MX, 32, 64, 160) == 2 * 64 * (64 + 4)                # panels of 128 channels
+    assert f(MX, 32, 3, 32) == 256 + 256                          # 192 and 12 bytes, each to a multiple of 256
+    assert f(MX, 32, 1 << 24, 1 << 24) == (1 << 17) * (1 << 24) * 68
     for bad in [(MX, 16, 64, 256), (MX, 64, 64, 256), (MX, 32, 0, 256), (MX, 32, 64, 0), (MX, 32, 64, 48), (MX, 32, (1 << 24) + 1, 32),
                 (MX, 32, 1, (1 << 24) + 32), (5, 32, 64, 256)]:
         assert f(*bad) == 0, bad
