@@ -8,166 +8,339 @@ namespace pq {
 namespace {
 
 constexpr int kTile = 64;                                     // tokens a pass of a workgroup: a bit each of a 64-bit mask
-constexpr int kRouteWaves = 16;
+constexpr int kRouteWaves = 16, kRouteThreads = kRouteWaves * kWave;
 constexpr int kMaxBlocks = 512;                               // workgroups; more tokens mean more passes of each
 
-__device__ __forceinline__ float logit_at(const RouteCall& c, int64_t t, int e) {
-  return c.bf16 ? bf16_to_f32(((const uint16_t*)c.logits)[t * c.ld + e]) : ((const float*)c.logits)[t * c.ld + e];
+// ---------------------------------------------------------------- the k largest of a token's logits
+// A logit as an unsigned key that orders alike, 0 where the expert cannot be chosen (-inf, NaN); -0 counts as 0.
+__device__ __forceinline__ uint32_t key_of(float v) {
+  const uint32_t u = as_u32(v + 0.0f);
+  return v > -INFINITY ? (u & 0x80000000u ? ~u : u | 0x80000000u) : 0u;
+}
+__device__ __forceinline__ float value_of(uint32_t key) { return as_f32(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
+
+// largest over the wave, uniform: inside rows of 16 lanes by DPP exchanges, then the four rows on the scalar unit
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  v = max(v, dpp_u32<0xB1>(v));                               // quad_perm [1,0,3,2]
+  v = max(v, dpp_u32<0x4E>(v));                               // quad_perm [2,3,0,1]
+  v = max(v, dpp_u32<0x141>(v));                              // row_half_mirror
+  v = max(v, dpp_u32<0x140>(v));                              // row_mirror
+  const uint32_t a = __builtin_amdgcn_readlane(v, 0), b = __builtin_amdgcn_readlane(v, 16), c = __builtin_amdgcn_readlane(v, 32),
+                 d = __builtin_amdgcn_readlane(v, 48);
+  return max(max(a, b), max(c, d));
+}
+// the sum over the wave in a fixed order, in every lane
+__device__ __forceinline__ float wave_sum_f32(float v) {
+  v += dpp_f32<0xB1>(v);
+  v += dpp_f32<0x4E>(v);
+  v += dpp_f32<0x141>(v);
+  v += dpp_f32<0x140>(v);
+  const float a = as_f32(__builtin_amdgcn_readlane(as_u32(v), 0)), b = as_f32(__builtin_amdgcn_readlane(as_u32(v), 16)),
+              c = as_f32(__builtin_amdgcn_readlane(as_u32(v), 32)), d = as_f32(__builtin_amdgcn_readlane(as_u32(v), 48));
+  return (a + b) + (c + d);
 }
 
-template <class Op>
-__device__ __forceinline__ float wave_reduce(float v, Op op) {
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) v = op(v, __shfl_xor(v, d, kWave));
-  return v;
-}
-__device__ __forceinline__ int wave_min(int v) {
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) v = min(v, __shfl_xor(v, d, kWave));
-  return v;
-}
-
-// A wave a token.  The k largest one after another: the largest value over the wave, then the lowest index that holds it.
-// PER: experts a lane, lane + 64 i.
-template <int PER>
-__global__ __launch_bounds__(kRouteWaves* kWave) void route_topk_kernel(const RouteCall c, int per_block, uint16_t* __restrict__ hist) {
-  extern __shared__ uint32_t count[];                         // [experts]
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  for (int e = threadIdx.x; e < c.experts; e += blockDim.x) count[e] = 0;
-  __syncthreads();
-  const int64_t first = (int64_t)blockIdx.x * per_block, end = min(first + per_block, c.tokens);
-  for (int64_t t = first + wave; t < end; t += kRouteWaves) {
-    float v[PER];
-#pragma unroll
-    for (int i = 0; i < PER; ++i) {
-      const int e = lane + 64 * i;
-      v[i] = e < c.experts ? logit_at(c, t, e) : -INFINITY;
-      if (!(v[i] > -INFINITY)) v[i] = -INFINITY;              // NaN too: never chosen
-    }
-    float top = -INFINITY, total = 0.0f;
-    float kept = -INFINITY;                                   // lane j: the j-th largest
-    int kept_id = -1;
-    for (int j = 0; j < c.k; ++j) {
-      float best = v[0];
-#pragma unroll
-      for (int i = 1; i < PER; ++i) best = fmaxf(best, v[i]);
-      const float max = wave_reduce(best, [](float a, float b) { return fmaxf(a, b); });
-      if (j == 0) {
-        top = max;
-        if (!c.renormalize) {
-          float part = 0.0f;
-#pragma unroll
-          for (int i = 0; i < PER; ++i) part += v[i] > -INFINITY ? expf(v[i] - top) : 0.0f;
-          total = wave_reduce(part, [](float a, float b) { return a + b; });
-        }
-      }
-      if (max == -INFINITY) break;                            // uniform: none left
-      int at = 0x7FFFFFFF;
-#pragma unroll
-      for (int i = PER - 1; i >= 0; --i)
-        if (v[i] == max) at = lane + 64 * i;
-      const int id = wave_min(at);
-#pragma unroll
-      for (int i = 0; i < PER; ++i)
-        if (lane + 64 * i == id) v[i] = -INFINITY;
-      if (lane == j) kept = max, kept_id = id;
-    }
-    const float p = kept_id >= 0 ? expf(kept - top) : 0.0f;
-    if (c.renormalize) total = wave_reduce(p, [](float a, float b) { return a + b; });
-    if (lane < c.k) {
-      c.ids[t * c.k + lane] = kept_id;
-      c.weights[t * c.k + lane] = kept_id >= 0 ? p / total : 0.0f;
-      if (kept_id >= 0) atomicAdd(&count[kept_id], 1u);
+// A lane's PER experts, lane + 64 i, largest first: a wave's largest is then one of the lanes' first, and the lane that has it moves
+// on to its next.  A bf16 logit and its expert fit one word (the expert's complement below, so that equal logits order by
+// expert); binary32 logits keep the expert beside the key.
+template <int PER, bool BF16>
+struct Sorted {
+  uint32_t key[PER], low[BF16 ? 1 : PER];                     // low: complement of the expert
+  __device__ __forceinline__ void order(int i, int j) {       // the larger of two to place i
+    if constexpr (BF16) {
+      const uint32_t a = max(key[i], key[j]), b = min(key[i], key[j]);
+      key[i] = a, key[j] = b;
+    } else {
+      const uint64_t a = (uint64_t)key[i] << 32 | low[i], b = (uint64_t)key[j] << 32 | low[j];
+      const bool swap = b > a;
+      const uint32_t k = key[i], l = low[i];
+      key[i] = swap ? key[j] : k, low[i] = swap ? low[j] : l;
+      key[j] = swap ? k : key[j], low[j] = swap ? l : low[j];
     }
   }
-  __syncthreads();
-  for (int e = threadIdx.x; e < c.experts; e += blockDim.x) hist[(int64_t)blockIdx.x * c.experts + e] = (uint16_t)count[e];
+  __device__ __forceinline__ void sort() {                    // odd-even merges
+#pragma unroll
+    for (int p = 1; p < PER; p *= 2)
+#pragma unroll
+      for (int k = p; k >= 1; k /= 2)
+#pragma unroll
+        for (int j = k % p; j + k < PER; j += 2 * k)
+#pragma unroll
+          for (int i = 0; i < k; ++i)
+            if (i + j + k < PER && (i + j) / (2 * p) == (i + j + k) / (2 * p)) order(i + j, i + j + k);
+  }
+  // the wave's largest: its key (0: none is left) and expert, uniform; it is taken out
+  __device__ __forceinline__ uint32_t pop(int lane, int& expert) {
+    uint32_t best = wave_max_u32(key[0]);
+    if (best == 0) return 0;
+    bool mine = key[0] == best;
+    if constexpr (BF16) {
+      expert = 0xFFFF - (int)(best & 0xFFFFu);
+      best &= 0xFFFF0000u;
+    } else {
+      const uint32_t l = wave_max_u32(mine ? low[0] : 0u);
+      mine = mine && low[0] == l;
+      expert = (int)~l;
+    }
+#pragma unroll
+    for (int i = 0; i + 1 < PER; ++i) {
+      key[i] = mine ? key[i + 1] : key[i];
+      if constexpr (!BF16) low[i] = mine ? low[i + 1] : low[i];
+    }
+    key[PER - 1] = mine ? 0u : key[PER - 1];
+    return best;
+  }
+};
+
+template <int PER, bool BF16>
+__device__ __forceinline__ void load_logits(const RouteCall& c, int64_t t, int lane, float (&v)[PER]) {
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int e = lane + 64 * i;
+    if constexpr (BF16)
+      v[i] = e < c.experts ? bf16_to_f32(((const uint16_t*)c.logits)[t * c.ld + e]) : -INFINITY;
+    else
+      v[i] = e < c.experts ? ((const float*)c.logits)[t * c.ld + e] : -INFINITY;
+  }
+}
+// A wave a token: ids and weights written, lane j < k has the j-th expert (-1: none).
+template <int PER, bool BF16>
+__device__ __forceinline__ int route_token(const RouteCall& c, int64_t t, int lane, const float (&v)[PER]) {
+  Sorted<PER, BF16> s;
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const uint32_t e = (uint32_t)(lane + 64 * i), key = key_of(v[i]);
+    if constexpr (BF16) {
+      s.key[i] = key ? (key & 0xFFFF0000u) | (0xFFFFu - e) : 0u;      // a bf16 value says nothing in the low half
+    } else {
+      s.key[i] = key;
+      s.low[i] = ~e;
+    }
+  }
+  s.sort();
+  uint32_t kept = 0, first = 0;
+  int id = -1;
+  for (int j = 0; j < c.k; ++j) {
+    int e;
+    const uint32_t key = s.pop(lane, e);
+    if (key == 0) break;
+    if (j == 0) first = key;
+    if (lane == j) kept = key, id = e;
+  }
+  const auto value = [](uint32_t key) { return BF16 && !(key & 0x80000000u) ? as_f32(~key & 0xFFFF0000u) : value_of(key); };
+  const float top = value(first), p = id >= 0 ? expf(value(kept) - top) : 0.0f;
+  float sum = p;
+  if (!c.renormalize) {
+    sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) sum += v[i] > -INFINITY ? expf(v[i] - top) : 0.0f;
+  }
+  sum = wave_sum_f32(sum);
+  if (lane < c.k) {
+    c.ids[t * c.k + lane] = id;
+    c.weights[t * c.k + lane] = id >= 0 ? p / sum : 0.0f;
+  }
+  return id;
 }
 
-// Places of the rows: the experts' offsets, then the rows of earlier workgroups, then the earlier tokens of this one.
-__global__ __launch_bounds__(kRouteWaves* kWave) void route_place_kernel(const RouteCall c, int per_block, const uint16_t* __restrict__ hist) {
-  extern __shared__ uint64_t lds[];
-  uint64_t* mask = lds;                                       // [experts]: tokens of the pass that chose it
-  int32_t* base = (int32_t*)(lds + c.experts);                // [experts]: place of the next row
-  int32_t* total = base + c.experts;                          // [experts]
-  for (int e = threadIdx.x; e < c.experts; e += blockDim.x) {
-    int before = 0, all = 0;
-    for (int b = 0; b < (int)gridDim.x; ++b) {
-      const int n = hist[(int64_t)b * c.experts + e];
-      if (b < (int)blockIdx.x) before += n;
+// exclusive sums of counts[0 .. n), n <= kRouteThreads, by the whole workgroup; returns this thread's and leaves the total
+__device__ __forceinline__ int block_scan(int v, int* wave_sums, int& total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int upto = v;
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const int o = __shfl_up(upto, d, kWave);
+    if (lane >= d) upto += o;
+  }
+  if (lane == 63) wave_sums[wave] = upto;
+  __syncthreads();
+  int before = 0;
+  total = 0;
+#pragma unroll
+  for (int w = 0; w < kRouteWaves; ++w) {
+    const int n = wave_sums[w];
+    if (w < wave) before += n;
+    total += n;
+  }
+  return before + upto - v;
+}
+
+// positions and rows of the tokens of one pass, from a mask of tokens and the next place of every expert; `id` of pair i = first pair + thread
+__device__ __forceinline__ void place_pass(const RouteCall& c, int64_t t0, int n, const uint64_t* mask, const int32_t* base) {
+  for (int i = threadIdx.x; i < n; i += kRouteThreads) {
+    const int id = c.ids[t0 * c.k + i], t = i / c.k;
+    int place = -1;
+    if (id >= 0) {
+      place = base[id] + __popcll(mask[id] & ((1ull << t) - 1));
+      c.rows[place] = (int32_t)(t0 + t);
+    }
+    c.positions[t0 * c.k + i] = place;
+  }
+}
+
+// Few tokens, one launch: a mask of tokens for every expert says all of it.
+template <int PER, bool BF16>
+__global__ __launch_bounds__(kRouteThreads) void route_few_kernel(const RouteCall c) {
+  __shared__ uint64_t mask[64 * PER];
+  __shared__ int32_t base[64 * PER];
+  __shared__ int wave_sums[kRouteWaves];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), e = threadIdx.x;
+  float v[PER];
+  if (wave < c.tokens) load_logits<PER, BF16>(c, wave, lane, v);
+  if (e < c.experts) mask[e] = 0;
+  __syncthreads();
+  for (int64_t t = wave; t < c.tokens; t += kRouteWaves) {
+    const int id = route_token<PER, BF16>(c, t, lane, v);
+    if (lane < c.k && id >= 0) atomicOr((unsigned long long*)&mask[id], 1ull << t);
+    if (t + kRouteWaves < c.tokens) load_logits<PER, BF16>(c, t + kRouteWaves, lane, v);
+  }
+  __syncthreads();
+  int total;
+  const int at = block_scan(e < c.experts ? __popcll(mask[e]) : 0, wave_sums, total);
+  if (e < c.experts) base[e] = c.offsets[e] = at;
+  if (e == 0) c.offsets[c.experts] = total;
+  __threadfence_block();
+  __syncthreads();
+  const int pairs = (int)c.tokens * c.k;
+  for (int i = total + threadIdx.x; i < pairs; i += kRouteThreads) c.rows[i] = -1;
+  place_pass(c, 0, pairs, mask, base);
+}
+
+// Many tokens, first launch: experts and weights, and how many rows of each expert a workgroup's tokens make.
+template <int PER, bool BF16>
+__global__ __launch_bounds__(kRouteThreads) void route_topk_kernel(const RouteCall c, int per_block, uint16_t* __restrict__ hist) {
+  __shared__ uint32_t count[64 * PER];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t first = (int64_t)blockIdx.x * per_block, end = min(first + per_block, c.tokens);
+  float v[PER];
+  if (first + wave < end) load_logits<PER, BF16>(c, first + wave, lane, v);
+  for (int e = threadIdx.x; e < c.experts; e += kRouteThreads) count[e] = 0;
+  __syncthreads();
+  for (int64_t t = first + wave; t < end; t += kRouteWaves) {
+    float next[PER] = {};
+    if (t + kRouteWaves < end) load_logits<PER, BF16>(c, t + kRouteWaves, lane, next);
+    const int id = route_token<PER, BF16>(c, t, lane, v);
+    if (lane < c.k && id >= 0) atomicAdd(&count[id], 1u);
+#pragma unroll
+    for (int i = 0; i < PER; ++i) v[i] = next[i];
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < c.experts; e += kRouteThreads) hist[(int64_t)blockIdx.x * c.experts + e] = (uint16_t)count[e];
+}
+
+// Second launch, places of the rows: the experts' offsets, then the rows of earlier workgroups, then the earlier tokens of this one.
+// Every workgroup sums up all counts itself: at most 512 x 1024 of two bytes, out of the caches.
+__global__ __launch_bounds__(kRouteThreads) void route_place_kernel(const RouteCall c, int per_block, const uint16_t* __restrict__ hist) {
+  __shared__ uint64_t mask[1024];                             // tokens of the pass that chose the expert
+  __shared__ int32_t base[1024];                              // place of its next row
+  __shared__ int32_t part[2 * kRouteThreads];
+  __shared__ int wave_sums[kRouteWaves];
+  const int e = threadIdx.x, blocks = (int)gridDim.x;
+  // thread (expert, share): shares of the workgroups' counts, as many as there are threads for
+  const int width = max(64, (c.experts + 63) / 64 * 64), shares = kRouteThreads / width;
+  const int mine = e % width, share = e / width;
+  int before = 0, all = 0;
+  if (share < shares && mine < c.experts) {
+    const uint16_t* h = hist + mine;
+#pragma unroll 8
+    for (int b = share; b < blocks; b += shares) {
+      const int n = h[(int64_t)b * c.experts];
+      before += b < (int)blockIdx.x ? n : 0;
       all += n;
     }
-    base[e] = before;
-    total[e] = all;
   }
+  part[e] = before;
+  part[kRouteThreads + e] = all;
   __syncthreads();
-  if (threadIdx.x == 0) {
-    int at = 0;
-    for (int e = 0; e < c.experts; ++e) {
-      base[e] += at;
-      if (blockIdx.x == 0) c.offsets[e] = at;
-      at += total[e];
-    }
-    total[0] = at;
-    if (blockIdx.x == 0) c.offsets[c.experts] = at;
+  before = all = 0;
+  if (e < c.experts)
+    for (int s = 0; s < shares; ++s) before += part[s * width + e], all += part[kRouteThreads + s * width + e];
+  int total;
+  const int at = block_scan(all, wave_sums, total);
+  if (e < c.experts) {
+    base[e] = at + before;
+    mask[e] = 0;
+    if (blockIdx.x == 0) c.offsets[e] = at;
   }
-  __syncthreads();
+  if (e == 0 && blockIdx.x == 0) c.offsets[c.experts] = total;
   const int64_t pairs = c.tokens * c.k;
-  for (int64_t i = total[0] + (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < pairs; i += (int64_t)gridDim.x * blockDim.x) c.rows[i] = -1;
+  for (int64_t i = total + (int64_t)blockIdx.x * kRouteThreads + e; i < pairs; i += (int64_t)blocks * kRouteThreads) c.rows[i] = -1;
   const int64_t first = (int64_t)blockIdx.x * per_block, end = min(first + per_block, c.tokens);
   for (int64_t t0 = first; t0 < end; t0 += kTile) {
     const int n = (int)min((int64_t)kTile, end - t0) * c.k;
-    for (int e = threadIdx.x; e < c.experts; e += blockDim.x) mask[e] = 0;
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+    for (int i = e; i < n; i += kRouteThreads) {
       const int id = c.ids[t0 * c.k + i];
       if (id >= 0) atomicOr((unsigned long long*)&mask[id], 1ull << (i / c.k));
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
-      const int id = c.ids[t0 * c.k + i], t = i / c.k;
-      int place = -1;
-      if (id >= 0) {
-        place = base[id] + __popcll(mask[id] & ((1ull << t) - 1));
-        c.rows[place] = (int32_t)(t0 + t);
-      }
-      c.positions[t0 * c.k + i] = place;
-    }
+    place_pass(c, t0, n, mask, base);
     __syncthreads();
-    for (int e = threadIdx.x; e < c.experts; e += blockDim.x) base[e] += __popcll(mask[e]);
-    __syncthreads();
+    if (e < c.experts) base[e] += __popcll(mask[e]), mask[e] = 0;
   }
 }
 
-// out[t] = addend[t] + sum_j weights[t, j] * y[positions[t, j]], j ascending, in binary32, rounded once to bf16.  Eight columns a thread.
-__global__ __launch_bounds__(256) void combine_kernel(const CombineCall c) {
-  const int64_t across = (c.N + 7) / 8, n = c.tokens * across;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-    const int64_t t = i / across, col = (i - t * across) * 8;
-    const int width = (int)min((int64_t)8, c.N - col);
-    float acc[8] = {};
-    const auto add = [&](const uint16_t* from, float w, bool weighted) {
-      uint16_t v[8] = {};
-      if (width == 8)
-        *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(from);
-      else
-        for (int j = 0; j < width; ++j) v[j] = from[j];
+// ---------------------------------------------------------------- the weighted sum
+// out[t] = addend[t] + sum_j weights[t, j] * y[positions[t, j]], j ascending, in binary32, rounded once to bf16.  Eight columns a
+// thread, a token a workgroup: its rows and weights are uniform, and the loads of kAhead rows are under way at a time.  Memory bound.
+constexpr int kAhead = 8, kCombineThreads = 128;
+__global__ __launch_bounds__(kCombineThreads) void combine_kernel(const CombineCall c, int chunks) {
+  const int64_t t = blockIdx.x / (uint32_t)chunks;
+  const int64_t col = ((int64_t)(blockIdx.x % (uint32_t)chunks) * kCombineThreads + threadIdx.x) * 8;
+  if (col >= c.N) return;
+  const int width = (int)min((int64_t)8, c.N - col);
+  const auto load = [&](const uint16_t* from) {
+    uint4 v;
+    if (width == 8) {
+      v = *reinterpret_cast<const uint4*>(from);
+    } else {                                                  // a row may end with its last column
+      uint32_t w[4] = {};
 #pragma unroll
-      for (int j = 0; j < 8; ++j) acc[j] = weighted ? fmaf(w, bf16_to_f32(v[j]), acc[j]) : bf16_to_f32(v[j]);
-    };
-    if (c.addend) add(c.addend + t * c.addend_ld + col, 1.0f, false);
-    for (int j = 0; j < c.k; ++j) {
-      const int64_t p = c.positions[t * c.k + j];
-      if (p >= 0 && p < c.rows) add(c.y + p * c.y_ld + col, c.weights[t * c.k + j], true);
+      for (int j = 0; j < 7; ++j)
+        if (j < width) w[j >> 1] |= (uint32_t)from[j] << (16 * (j & 1));
+      v = make_uint4(w[0], w[1], w[2], w[3]);
     }
-    uint16_t o[8];
+    return v;
+  };
+  float acc[8] = {};
+  if (c.addend) {
+    const uint4 v = load(c.addend + t * c.addend_ld + col);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-    for (int j = 0; j < 8; ++j) o[j] = __builtin_bit_cast(uint16_t, (__bf16)acc[j]);
-    uint16_t* to = c.out + t * c.out_ld + col;
-    if (width == 8)
-      *reinterpret_cast<uint4*>(to) = *reinterpret_cast<uint4*>(o);
-    else
-      for (int j = 0; j < width; ++j) to[j] = o[j];
+    for (int j = 0; j < 8; ++j) acc[j] = j & 1 ? bf16_hi(w[j >> 1]) : bf16_lo(w[j >> 1]);
+  }
+  for (int j0 = 0; j0 < c.k; j0 += kAhead) {
+    uint4 v[kAhead];
+    bool there[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      there[j] = false;
+      if (j0 + j < c.k) {
+        const int p = c.positions[t * c.k + j0 + j];
+        there[j] = p >= 0 && p < c.rows;
+        if (there[j]) v[j] = load(c.y + (int64_t)p * c.y_ld + col);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) {
+      if (!there[j]) continue;
+      const float weight = c.weights[t * c.k + j0 + j];
+      const uint32_t w[4] = {v[j].x, v[j].y, v[j].z, v[j].w};
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[i] = fmaf(weight, i & 1 ? bf16_hi(w[i >> 1]) : bf16_lo(w[i >> 1]), acc[i]);
+    }
+  }
+  uint32_t o[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+    o[j] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)acc[2 * j]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)acc[2 * j + 1]) << 16;
+  uint16_t* to = c.out + t * c.out_ld + col;
+  if (width == 8) {
+    *reinterpret_cast<uint4*>(to) = make_uint4(o[0], o[1], o[2], o[3]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 7; ++j)
+      if (j < width) to[j] = (uint16_t)(o[j >> 1] >> (16 * (j & 1)));
   }
 }
 
@@ -181,25 +354,43 @@ size_t moe_route_workspace_bytes(int64_t tokens, int experts) {
   return align_up((size_t)blocks * experts * 2, 256) + 256;
 }
 
-int run_moe_route(const RouteCall& c, void* ws, hipStream_t st) {
-  // without tokens one workgroup still writes the offsets
-  const int per = c.tokens ? tokens_per_block(c.tokens) : kTile;
-  const int blocks = c.tokens ? (int)((c.tokens + per - 1) / per) : 1;
-  const size_t lds = (size_t)c.experts * 4;
-  uint16_t* hist = (uint16_t*)ws;
-  const int each = (c.experts + 63) / 64;
-  const auto topk = each <= 1 ? route_topk_kernel<1> : each <= 2 ? route_topk_kernel<2> : each <= 4 ? route_topk_kernel<4> : each <= 8 ? route_topk_kernel<8> : route_topk_kernel<16>;
-  topk<<<blocks, kRouteWaves * kWave, lds, st>>>(c, per, hist);
-  int rc = check_hip(hipGetLastError(), "route_topk_kernel");
+template <int PER>
+static int route(const RouteCall& c, uint16_t* hist, hipStream_t st) {
+  if (c.tokens <= kTile) {
+    if (c.bf16)
+      route_few_kernel<PER, true><<<1, kRouteThreads, 0, st>>>(c);
+    else
+      route_few_kernel<PER, false><<<1, kRouteThreads, 0, st>>>(c);
+    return check_hip(hipGetLastError(), "route_few_kernel");
+  }
+  const int per = tokens_per_block(c.tokens), blocks = (int)((c.tokens + per - 1) / per);
+  if (c.bf16)
+    route_topk_kernel<PER, true><<<blocks, kRouteThreads, 0, st>>>(c, per, hist);
+  else
+    route_topk_kernel<PER, false><<<blocks, kRouteThreads, 0, st>>>(c, per, hist);
+  const int rc = check_hip(hipGetLastError(), "route_topk_kernel");
   if (rc) return rc;
-  route_place_kernel<<<blocks, kRouteWaves * kWave, (size_t)c.experts * 16, st>>>(c, per, hist);
+  route_place_kernel<<<blocks, kRouteThreads, 0, st>>>(c, per, hist);
   return check_hip(hipGetLastError(), "route_place_kernel");
+}
+
+int run_moe_route(const RouteCall& c, void* ws, hipStream_t st) {
+  uint16_t* hist = (uint16_t*)ws;
+  const int each = (c.experts + 63) / 64;                     // experts a lane
+  return each <= 1   ? route<1>(c, hist, st)
+         : each <= 2 ? route<2>(c, hist, st)
+         : each <= 4 ? route<4>(c, hist, st)
+         : each <= 8 ? route<8>(c, hist, st)
+                     : route<16>(c, hist, st);
 }
 
 int run_moe_combine(const CombineCall& c, hipStream_t st) {
   if (c.tokens == 0) return PQ_OK;
-  const int64_t blocks = (c.tokens * ((c.N + 7) / 8) + 255) / 256;
-  combine_kernel<<<(unsigned)(blocks < 65536 ? blocks : 65536), 256, 0, st>>>(c);
+  const int64_t chunks = ((c.N + 7) / 8 + kCombineThreads - 1) / kCombineThreads;
+  // a grid has fewer than 2^32 threads
+  if (c.tokens * chunks >= (int64_t)1 << 25)
+    return fail(PQ_ERR_SHAPE, "pq_moe_combine: tokens=%lld N=%lld are too many for one call", (long long)c.tokens, (long long)c.N);
+  combine_kernel<<<(unsigned)(c.tokens * chunks), kCombineThreads, 0, st>>>(c, (int)chunks);
   return check_hip(hipGetLastError(), "combine_kernel");
 }
 
