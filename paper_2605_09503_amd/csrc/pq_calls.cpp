@@ -25,6 +25,8 @@ PyObject* g_operand = nullptr;      // operand(fmt, group, rows, K, like) -> ten
 PyObject* g_workspace = nullptr;    // workspace(op, fmt, group, M, N, K, n_batches, like) -> tensor or None
 PyObject* g_refuse = nullptr;       // refuse(message): raises the error of arguments that do not fit
 PyObject* g_attn_workspace = nullptr;   // attn_workspace(cache, seqs, q_heads, max_len, window) -> tensor
+PyObject* g_route_workspace = nullptr;  // route_workspace(tokens, experts, k, like) -> tensor
+PyObject* g_route = nullptr;            // route(tokens, experts, k, like) -> Route
 
 // thrown when a Python error is set
 struct PyFailed {};
@@ -481,11 +483,160 @@ PQ_CALL(attn_decode) {
   });
 }
 
+// ---- reading back, products by expert, routing: tensors are checked as pq.py's functions check them
+at::Tensor bf16_rows(int64_t rows, int64_t width, c10::Device device) {
+  return at::empty({rows, width}, at::TensorOptions().dtype(at::kBFloat16).device(device));
+}
+void on_current_device(const char* name, const at::Tensor& t, const at::Tensor* like) {
+  if (!t.is_cuda() || (like ? t.device() != like->device() : t.device().index() != c10::hip::current_device()))
+    refuse("%s must lie in the memory of the current GPU, with the call's other tensors", name);
+}
+// contiguous, of these sizes (a second size of -1: one dimension)
+void* array(const char* name, const at::Tensor& t, at::ScalarType type, const char* type_name, int64_t n0, int64_t n1, const at::Tensor& like) {
+  const bool two = n1 >= 0;
+  if (t.scalar_type() != type || t.dim() != (two ? 2 : 1) || t.size(0) != n0 || (two && t.size(1) != n1) || !t.is_contiguous()) {
+    if (two) refuse("%s must be contiguous %s [%lld, %lld]", name, type_name, (long long)n0, (long long)n1);
+    refuse("%s must be contiguous %s [%lld]", name, type_name, (long long)n0);
+  }
+  on_current_device(name, t, &like);
+  return t.data_ptr();
+}
+// bf16 [rows, width] with adjacent columns; the stride of a single row does not matter
+struct Rows2 {
+  void* p;
+  int64_t ld;
+};
+Rows2 rows2(const char* name, const at::Tensor& t, int64_t rows, int64_t width, const at::Tensor* like) {
+  if (t.scalar_type() != at::kBFloat16 || t.dim() != 2 || t.size(0) != rows || t.size(1) != width || (width > 1 && t.stride(1) != 1))
+    refuse("%s must be bfloat16 [%lld, %lld] with adjacent columns", name, (long long)rows, (long long)width);
+  on_current_device(name, t, like);
+  return Rows2{t.data_ptr(), rows > 1 ? t.stride(0) : (width + 7) / 8 * 8};
+}
+
+PQ_CALL(dequantize) {
+  return guarded([&] {
+    PQ_TAKE(pq_dequantize, 4, "fmt", "group", "codes", "scales", "tensor_scale", "y");
+    const int fmt = (int)as_int(a[0]), group = (int)as_int(a[1]);
+    const at::Tensor& codes = as_tensor(a[2], "codes");
+    if (codes.dim() < 2) fail(PyExc_IndexError, "tuple index out of range");
+    const int64_t rows = codes.size(0), K = codes.size(1) * 2;
+    void *scales = pointer(a[3]), *ts = pointer(a[4]);
+    const at::Tensor y = given(a[5]) ? as_tensor(a[5], "y") : bf16_rows(rows, K, codes.device());
+    void *c = codes.data_ptr(), *yp = y.data_ptr(), *st = stream();
+    const int64_t ldy = y.stride(0);
+    call([&] { return pq_dequantize((pq_format)fmt, group, (const uint8_t*)c, scales, (const float*)ts, rows, K, yp, ldy, st); });
+    return THPVariable_Wrap(y);
+  });
+}
+
+PQ_CALL(qgemm_grouped) {
+  return guarded([&] {
+    PQ_TAKE(pq_qgemm_grouped, 9, "fmt", "group", "a_operand", "a_rows", "w_operands", "offsets", "y", "N", "K", "rows", "bias");
+    const int fmt = (int)as_int(a[0]), group = (int)as_int(a[1]);
+    const int64_t a_rows = as_int(a[3]), N = as_int(a[7]), K = as_int(a[8]);
+    const at::Tensor &ao = as_tensor(a[2], "a_operand"), &w = as_tensor(a[4], "w_operands"), &off = as_tensor(a[5], "offsets"), &y = as_tensor(a[6], "y");
+    if (w.dim() != 2 || w.scalar_type() != at::kByte || !w.is_contiguous()) refuse("w_operands must be contiguous uint8 [experts, bytes of an operand]");
+    if (y.dim() != 2) refuse("y must be bfloat16 [M, %lld] with adjacent columns", (long long)N);
+    const int64_t experts = w.size(0), M = y.size(0);
+    const size_t need = pq_operand_bytes((pq_format)fmt, group, N, K);
+    if (need && (size_t)w.size(1) != need) refuse("w_operands must hold %zu bytes an expert", need);
+    const Rows2 yr = rows2("y", y, M, N, nullptr);
+    on_current_device("w_operands", w, &y);
+    on_current_device("a_operand", ao, &y);
+    if (ao.scalar_type() != at::kByte || !ao.is_contiguous() || (size_t)ao.numel() < pq_operand_bytes((pq_format)fmt, group, a_rows, K))
+      refuse("a_operand must be contiguous uint8 and hold an operand of %lld rows", (long long)a_rows);
+    if (experts > INT32_MAX) refuse("w_operands has too many experts");
+    const void* op = array("offsets", off, at::kInt, "torch.int32", experts + 1, -1, y);
+    const void* rp = given(a[9]) ? array("rows", as_tensor(a[9], "rows"), at::kInt, "torch.int32", M, -1, y) : nullptr;
+    const void* bp = given(a[10]) ? array("bias", as_tensor(a[10], "bias"), at::kBFloat16, "torch.bfloat16", experts, N, y) : nullptr;
+    void *ap = ao.data_ptr(), *wp = w.data_ptr(), *st = stream();
+    call([&] {
+      return pq_qgemm_grouped((pq_format)fmt, group, ap, a_rows, wp, (int)experts, (const int32_t*)op, (const int32_t*)rp, M, N, K, bp, yr.p, yr.ld, st);
+    });
+    return none();
+  });
+}
+
+PQ_CALL(moe_route) {
+  return guarded([&] {
+    PQ_TAKE(pq_moe_route, 2, "logits", "k", "renormalize", "out", "workspace");
+    const at::Tensor& x = as_tensor(a[0], "logits");
+    if (x.dim() != 2 || (x.scalar_type() != at::kFloat && x.scalar_type() != at::kBFloat16) || (x.size(1) > 1 && x.stride(1) != 1))
+      refuse("logits must be float32 or bfloat16 [tokens, experts] with adjacent experts");
+    const int64_t tokens = x.size(0), experts = x.size(1), k = as_int(a[1]);
+    const int renormalize = given(a[2]) ? PyObject_IsTrue(a[2]) : 1;
+    if (renormalize < 0) throw PyFailed{};
+    if (k > INT32_MAX || k < INT32_MIN || experts > INT32_MAX) refuse("k=%lld or experts=%lld out of range", (long long)k, (long long)experts);
+    on_current_device("logits", x, nullptr);
+    PyObject* w = nullptr;
+    if (given(a[4])) {
+      w = a[4];
+      Py_INCREF(w);
+    } else {
+      w = PyObject_CallFunction(g_route_workspace, "LLLO", (long long)tokens, (long long)experts, (long long)k, a[0]);
+    }
+    Ref ws(w);
+    const at::Tensor& wt = as_tensor(ws.p, "workspace");
+    if (!wt.is_contiguous()) refuse("workspace must be contiguous");
+    on_current_device("workspace", wt, &x);
+    PyObject* o = nullptr;
+    if (given(a[3])) {
+      o = a[3];
+      Py_INCREF(o);
+    } else {
+      o = PyObject_CallFunction(g_route, "LLLO", (long long)tokens, (long long)experts, (long long)k, a[0]);
+    }
+    Ref out(o);
+    if (!PyTuple_Check(out.p) || PyTuple_GET_SIZE(out.p) != 5) fail(PyExc_TypeError, "out must be a Route");
+    const auto part = [&](int i, const char* name) -> const at::Tensor& { return as_tensor(PyTuple_GET_ITEM(out.p, i), name); };
+    void* ids = array("ids", part(0, "ids"), at::kInt, "torch.int32", tokens, k, x);
+    void* weights = array("weights", part(1, "weights"), at::kFloat, "torch.float32", tokens, k, x);
+    void* offsets = array("offsets", part(2, "offsets"), at::kInt, "torch.int32", experts + 1, -1, x);
+    void* rows = array("rows", part(3, "rows"), at::kInt, "torch.int32", tokens * k, -1, x);
+    void* positions = array("positions", part(4, "positions"), at::kInt, "torch.int32", tokens, k, x);
+    const pq_logits type = x.scalar_type() == at::kBFloat16 ? PQ_LOGITS_BF16 : PQ_LOGITS_F32;
+    void *xp = x.data_ptr(), *wp = wt.data_ptr(), *st = stream();
+    const int64_t ld = tokens > 1 ? x.stride(0) : experts;
+    const size_t bytes = wt.numel() * wt.element_size();
+    call([&] {
+      return pq_moe_route(type, xp, tokens, (int)experts, ld, (int)k, renormalize, (int32_t*)ids, (float*)weights, (int32_t*)offsets, (int32_t*)rows,
+                          (int32_t*)positions, wp, bytes, st);
+    });
+    Py_INCREF(out.p);
+    return out.p;
+  });
+}
+
+PQ_CALL(moe_combine) {
+  return guarded([&] {
+    PQ_TAKE(pq_moe_combine, 3, "y", "positions", "weights", "addend", "out");
+    const at::Tensor &y = as_tensor(a[0], "y"), &pos = as_tensor(a[1], "positions"), &weights = as_tensor(a[2], "weights");
+    if (y.dim() != 2 || pos.dim() != 2) refuse("y must be bfloat16 [rows, N], positions int32 [tokens, k]");
+    const int64_t rows = y.size(0), N = y.size(1), tokens = pos.size(0), k = pos.size(1);
+    const Rows2 yr = rows2("y", y, rows, N, nullptr);
+    const void* pp = array("positions", pos, at::kInt, "torch.int32", tokens, k, y);
+    const void* wp = array("weights", weights, at::kFloat, "torch.float32", tokens, k, y);
+    const Rows2 ar = given(a[3]) ? rows2("addend", as_tensor(a[3], "addend"), tokens, N, &y) : Rows2{nullptr, 0};
+    const at::Tensor out = given(a[4])    ? as_tensor(a[4], "out")
+                           : N % 8 == 0 ? bf16_rows(tokens, N, y.device())
+                                        : bf16_rows(tokens, (N + 7) / 8 * 8, y.device()).narrow(1, 0, N);
+    const Rows2 outr = rows2("out", out, tokens, N, &y);
+    if (k > INT32_MAX) refuse("k=%lld out of range", (long long)k);
+    void* st = stream();
+    call([&] {
+      return pq_moe_combine(yr.p, rows, yr.ld, (const int32_t*)pp, (const float*)wp, tokens, (int)k, N, ar.p, ar.ld, outr.p, outr.ld, st);
+    });
+    return THPVariable_Wrap(out);
+  });
+}
+
 PyObject* bind(PyObject*, PyObject* args) {
-  PyObject* given_by[5];
-  if (!PyArg_ParseTuple(args, "OOOOO", &given_by[0], &given_by[1], &given_by[2], &given_by[3], &given_by[4])) return nullptr;
-  PyObject** const slots[5] = {&g_raise, &g_operand, &g_workspace, &g_refuse, &g_attn_workspace};
-  for (int i = 0; i < 5; ++i) {
+  constexpr int n = 7;
+  PyObject* given_by[n] = {};
+  if (!PyArg_ParseTuple(args, "OOOOO|OO", &given_by[0], &given_by[1], &given_by[2], &given_by[3], &given_by[4], &given_by[5], &given_by[6])) return nullptr;
+  PyObject** const slots[n] = {&g_raise, &g_operand, &g_workspace, &g_refuse, &g_attn_workspace, &g_route_workspace, &g_route};
+  for (int i = 0; i < n; ++i) {
+    if (!given_by[i]) continue;                // what stands stays
     Py_INCREF(given_by[i]);
     Py_XSETREF(*slots[i], given_by[i]);
   }
@@ -523,7 +674,18 @@ PyMethodDef methods[] = {
     PQ_METHOD(attn_decode, "(cache, q, table, lengths, max_len, scale, out=None, lse=None, window=0, workspace=None)",
               "Attention of one new token a sequence, q bf16 [seqs, q_heads, head_dim], over the lengths[b] (int32) tokens whose pages\n"
               "table[b] (int32) names; out like q (allocated unless given), lse float32 [seqs, q_heads].  max_len: no sequence is longer."),
-    {"bind", bind, METH_VARARGS, "bind(raise_, operand, workspace, refuse, attn_workspace): the helpers of pq.py"},
+    PQ_METHOD(dequantize, "(fmt, group, codes, scales, tensor_scale=None, y=None)",
+              "The values that stored codes [rows, K/2] and scales stand for, bf16 [rows, K] (allocated unless given)."),
+    PQ_METHOD(qgemm_grouped, "(fmt, group, a_operand, a_rows, w_operands, offsets, y, N, K, rows=None, bias=None)",
+              "y[i] (bf16 [M, N]) = row rows[i] (int32 [M], or i) of A times the weights of the expert whose rows offsets (int32 [experts + 1])\n"
+              "places i in, plus bias[expert] (bf16 [experts, N]).  w_operands: uint8 [experts, pq_operand_bytes(fmt, group, N, K)]."),
+    PQ_METHOD(moe_route, "(logits, k, renormalize=True, out=None, workspace=None)",
+              "The k largest of every row of logits (float32 or bf16 [tokens, experts]), their softmax weights, and the order of the rows by\n"
+              "expert (allocated unless given)."),
+    PQ_METHOD(moe_combine, "(y, positions, weights, addend=None, out=None)",
+              "out[t] = addend[t] + sum_j weights[t, j] * y[positions[t, j]], bf16 [tokens, N] (allocated unless given); y bf16 [rows, N],\n"
+              "positions int32 and weights float32 [tokens, k]."),
+    {"bind", bind, METH_VARARGS, "bind(raise_, operand, workspace, refuse, attn_workspace, route_workspace, route): the helpers of pq.py"},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pq_calls", "Hot calls of the binding (see pq.py).", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

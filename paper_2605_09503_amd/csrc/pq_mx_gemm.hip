@@ -125,6 +125,13 @@ __device__ __forceinline__ int opaque(int v) {
   return v;
 }
 
+// a pointer that is the same in all lanes, where the compiler does not see that it is
+__device__ __forceinline__ const uint8_t* uniform(const uint8_t* p) {
+  const uint64_t u = (uint64_t)p;
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)u), hi = __builtin_amdgcn_readfirstlane((uint32_t)(u >> 32));
+  return (const uint8_t*)((uint64_t)hi << 32 | lo);
+}
+
 // the row of A that row m of y is made from, -1 where the index is none of A's
 __device__ __forceinline__ int a_row_of(const MxCall& c, int64_t m) {
   if (!c.rows) return (int)m;
@@ -492,7 +499,8 @@ template <int FM, int KW>
 struct Split {
   static constexpr int bm = 32 * FM, bn = 32;
   static constexpr int scales = (bm + bn) * kMxRowBytes;
-  static constexpr int stages = 4, stage = (bm + bn) * kMxRowBytes + FM * 256, own = stages * stage, lds = KW * own;
+  static constexpr int stages = FM == 1 ? 4 : 3;                       // two workgroups of four waves a compute unit
+  static constexpr int stage = (bm + bn) * kMxRowBytes + FM * 256, own = stages * stage, lds = KW * own;
   static constexpr int loads = (bm + bn) / 16 + FM;
   static constexpr int pitch = 36;                                     // floats a row of sums: rows start four banks apart
   static_assert(bm * pitch * 4 <= own, "the sums take a wave's own part");
@@ -616,6 +624,155 @@ __global__ __launch_bounds__(KW * 64) void mx_gemm_split_kernel(const MxCall c) 
   }
 }
 
+// ---------------------------------------------------------------- small tiles, a wave each
+// Where there are enough of them, every wave computes tiles of 32 FM x 32 by itself, one after another, three panels ahead also across
+// tiles: nothing to meet for and nothing to add up.  The waves of a workgroup take neighbouring columns of the same rows.
+template <int FM>
+struct Alone {
+  static constexpr int bm = 32 * FM, bn = 32, waves = 4;
+  static constexpr int scales = (bm + bn) * kMxRowBytes;
+  static constexpr int stages = FM == 1 ? 4 : 2, stage = (bm + bn) * kMxRowBytes + FM * 256, own = stages * stage;
+  static constexpr int table = waves * own, lds = table + Tiles<true>::kTableBytes;
+  static constexpr int least = 2 + 1 + FM;                             // loads of a panel: W's, one of A's at least, scales
+};
+
+template <int FM>
+__global__ __launch_bounds__(256) void mx_gemm_alone_kernel(const MxCall c) {
+  using S = Alone<FM>;
+  extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
+  const Tiles<true> tiles(c, S::bm, S::bn * S::waves, reinterpret_cast<int32_t*>(lds + S::table));
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  unsigned char* own = lds + wave * S::own;
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)own;
+  const int panels = (int)mx_panels(c.K);
+  const size_t as_at = mx_scales_at(c.a_rows, c.K), ws_at = mx_scales_at(c.N, c.K);
+
+  // loader, at tile load_tile; a tile of columns from N on is none of this wave's
+  int load_tile = tiles.next, load_panel = 0, a_last = 0;
+  Tile lt;
+  const uint8_t *a_from, *w_from, *s_from;                             // s_from: a lane's own, of W's rows below lane 32, of A's above
+  const size_t a_step = (size_t)c.a_rows * kMxRowBytes, w_step = (size_t)c.N * kMxRowBytes;
+  const bool of_w = lane < 32;
+  const size_t s_step = (size_t)(of_w ? c.N : c.a_rows) * kMxRowScales;
+  uint32_t a_off[2 * FM], w_off[2], s_off[FM];
+  const auto find = [&](int tile, Tile& t) {
+    t = tiles.at(c, S::bm, S::bn * S::waves, tile);
+    t.n0 += S::bn * wave;
+    return (bool)__builtin_amdgcn_readfirstlane(t.n0 < c.N);
+  };
+  const auto aim = [&] {                                               // load_tile moves past tiles that are none of this wave's
+    while (load_tile < tiles.end && !find(load_tile, lt)) load_tile += tiles.step;
+    if (load_tile >= tiles.end) return;
+    a_last = (int)(lt.end - lt.first) - 1;
+    const int w_last = (int)min((int64_t)S::bn, c.N - lt.n0) - 1;
+    const auto a_row = [&](int row) { return (uint32_t)max(a_row_of(c, lt.first + min(row, a_last)), 0); };
+    a_from = uniform(c.a);
+    const uint8_t* w = c.w + (size_t)lt.expert * c.w_next;
+    w_from = uniform(w + lt.n0 * kMxRowBytes);
+    s_from = of_w ? w + ws_at + lt.n0 * kMxRowScales : c.a + as_at;
+#pragma unroll
+    for (int i = 0; i < 2 * FM; ++i) {
+      const int row = 16 * i + (lane >> 2);
+      a_off[i] = a_row(row) * kMxRowBytes + block_at(row, lane & 3);
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int row = 16 * i + (lane >> 2);
+      w_off[i] = (uint32_t)min(row, w_last) * kMxRowBytes + block_at(row, lane & 3);
+    }
+#pragma unroll
+    for (int i = 0; i < FM; ++i) s_off[i] = (of_w ? (uint32_t)min(lane, w_last) : a_row(32 * i + lane - 32)) * kMxRowScales;
+  };
+  // A's rows come sixteen a load; sixteens that the tile has not are left out (what LDS holds instead makes sums that are not stored)
+  const auto load = [&](int stage) {
+    if (load_tile >= tiles.end) return;
+    const uint32_t to = lds0 + stage * S::stage;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) load16_to_lds(to + S::bm * kMxRowBytes + i * 1024, w_from, w_off[i]);
+#pragma unroll
+    for (int i = 0; i < 2 * FM; ++i)
+      if (i == 0 || 16 * i <= a_last) load16_to_lds(to + i * 1024, a_from, a_off[i]);
+#pragma unroll
+    for (int i = 0; i < FM; ++i) load4_to_lds(to + S::scales + i * 256, s_from + s_off[i]);
+    a_from += a_step;
+    w_from += w_step;
+    s_from += s_step;
+    if (++load_panel == panels) {
+      load_panel = 0;
+      load_tile += tiles.step;
+      aim();
+    }
+  };
+
+  const int row = lane & 31, half = lane >> 5;
+  float16v acc[FM];
+  const auto multiply = [&](int stage) {
+    const unsigned char* at = own + stage * S::stage;
+    int4v wf[2], af[2][FM];
+    const int sw = (int)(*reinterpret_cast<const uint32_t*>(at + S::scales + row * 4) >> (8 * half));
+    int sa[FM];
+#pragma unroll
+    for (int j = 0; j < FM; ++j) sa[j] = (int)(*reinterpret_cast<const uint32_t*>(at + S::scales + j * 256 + 128 + row * 4) >> (8 * half));
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      wf[s] = *reinterpret_cast<const int4v*>(at + (S::bm + row) * kMxRowBytes + block_at(row, 2 * s + half));
+#pragma unroll
+      for (int j = 0; j < FM; ++j) af[s][j] = *reinterpret_cast<const int4v*>(at + (32 * j + row) * kMxRowBytes + block_at(row, 2 * s + half));
+    }
+#pragma unroll
+    for (int j = 0; j < FM; ++j) {
+      acc[j] = mfma<0>(wf[0], af[0][j], acc[j], sw, sa[j]);
+      acc[j] = mfma<2>(wf[1], af[1][j], acc[j], sw, sa[j]);
+    }
+  };
+
+  aim();
+  int tile = load_tile;
+#pragma unroll
+  for (int i = 0; i < S::stages; ++i) load(i);
+  int stage = 0;
+  for (; tile < tiles.end; tile += tiles.step) {
+    Tile t;
+    if (!find(tile, t)) continue;
+#pragma unroll
+    for (int j = 0; j < FM; ++j) acc[j] = float16v{};
+    for (int p = 0; p < panels; ++p) {
+      // behind the panel that is waited for come the loads of stages - 1 others, each of `least` at least, or none at the end
+      if (load_tile < tiles.end)
+        arrived<(S::stages - 1) * S::least>();
+      else
+        arrived<0>();
+      multiply(stage);
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");               // this stage's reads are done
+      load(stage);
+      stage = (stage + 1) & (S::stages - 1);
+    }
+    // a lane has row l % 32 and columns 8 q + 4 (l / 32) .. + 3; the halves of the wave exchange what makes eight columns
+    const int cols = (int)min(c.N - t.n0, (int64_t)S::bn);
+    float bias[16] = {};
+    if (c.bias) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) bias[e] = bf16_to_f32(c.bias[t.expert * c.N + t.n0 + min(8 * (e >> 2) + 4 * half + (e & 3), cols - 1)]);
+    }
+#pragma unroll
+    for (int j = 0; j < FM; ++j) {
+      const int64_t m = t.first + 32 * j + row;
+      const bool ok = m < t.end && a_row_of(c, min(m, t.end - 1)) >= 0;
+      if (c.out_f32) continue;                                         // no grouped call asks for it
+#pragma unroll
+      for (int q = 0; q < 4; q += 2) {
+        const auto pack = [&](int g, int e) { return pack_bf16(acc[j][4 * g + e] + bias[4 * g + e], acc[j][4 * g + e + 1] + bias[4 * g + e + 1]); };
+        const auto x = __builtin_amdgcn_permlane32_swap(pack(q, 0), pack(q + 1, 0), false, false);
+        const auto z = __builtin_amdgcn_permlane32_swap(pack(q, 2), pack(q + 1, 2), false, false);
+        const int64_t n = t.n0 + 8 * (q + half);
+        if (ok && n < c.N) store8(c, m, n, make_uint4(x[0], z[0], x[1], z[1]));
+      }
+    }
+  }
+  arrived<0>();                                                        // loads into this wave's LDS
+}
+
 // `most`: workgroups that run at a time and go through all tiles, or 0: one for every tile that there could be (those beyond the
 // tiles that there are end at once)
 template <class K>
@@ -647,11 +804,24 @@ int launch_split(const MxCall& c, hipStream_t st) {
   return launch(mx_gemm_split_kernel<FM, KW, GROUPED>, "mx_gemm_split_kernel", c, 32 * FM, 32, KW, Split<FM, KW>::lds, 0, allowed, st);
 }
 
+template <int FM>
+int launch_alone(const MxCall& c, hipStream_t st) {
+  using S = Alone<FM>;
+  static std::atomic<uint64_t> allowed{0};
+  return launch(mx_gemm_alone_kernel<FM>, "mx_gemm_alone_kernel", c, S::bm, S::bn * S::waves, S::waves, S::lds, kUnits * (160 * 1024 / S::lds), allowed, st);
+}
+
 template <bool GROUPED>
 int run(const MxCall& c, hipStream_t st) {
   const int64_t groups = GROUPED ? c.experts : 1, each = (c.M + groups - 1) / groups;
-  if (each <= 32) return launch_split<1, 4, GROUPED>(c, st);
-  if (each <= 64) return launch_split<2, 4, GROUPED>(c, st);
+  const int64_t narrow = (c.N + 31) / 32;                              // tiles of 32 columns
+  if (each <= 64) {
+    if constexpr (GROUPED) {
+      if ((c.M < groups ? c.M : groups) * narrow >= 2048) return each <= 32 ? launch_alone<1>(c, st) : launch_alone<2>(c, st);
+    }
+    if (each > 32) return launch_split<2, 4, GROUPED>(c, st);
+    return groups * narrow <= kUnits && c.K >= 2048 ? launch_split<1, 8, GROUPED>(c, st) : launch_split<1, 4, GROUPED>(c, st);
+  }
   if (((each + 255) / 256) * ((c.N + 255) / 256) * groups < 200) return launch_shared<128, 128, 2, 2, GROUPED>(c, st);
   return launch_shared<256, 256, 2, 4, GROUPED>(c, st);
 }

@@ -188,7 +188,7 @@ def _stream():
 # is not built (it needs a host compiler and the interpreter's headers) or was built for another torch.
 _CALLS = ("pq_quantize_act", "pq_quantize_act_packed", "pq_norm_quantize_act_packed", "pq_hadamard_quantize_act_packed",
           "pq_qgemm", "pq_qgemm_packed", "pq_qgemm_packed_f32", "pq_qgemm_packed_bias", "pq_calib_moments", "pq_kv_write",
-          "pq_kv_read", "pq_attn_decode")
+          "pq_kv_read", "pq_attn_decode", "pq_dequantize", "pq_qgemm_grouped", "pq_moe_route", "pq_moe_combine")
 _CALLS_PATH = os.path.join(os.path.dirname(_LIB_PATH), "_pq_calls.so")
 _calls = None           # the module, or False where it cannot be had
 
@@ -209,6 +209,14 @@ def _new_attn_workspace(cache, seqs: int, q_heads: int, max_len: int, window: in
     return pq_attn_decode_workspace(cache, seqs, q_heads, max_len, window)
 
 
+def _new_route_workspace(tokens: int, experts: int, k: int, like: torch.Tensor) -> torch.Tensor:
+    return pq_moe_route_workspace(tokens, experts, k, like.device)
+
+
+def _new_route(tokens: int, experts: int, k: int, like: torch.Tensor):
+    return alloc_route(tokens, experts, k, like.device)
+
+
 def _new_workspace(op: int, fmt: int, group: int, M: int, N: int, K: int, n_batches: int, like: torch.Tensor):
     return _workspace(pq_workspace_bytes(op, fmt, group, M, N, K, n_batches), like.device)
 
@@ -225,7 +233,7 @@ def _bind_calls():
         loader = importlib.machinery.ExtensionFileLoader("_pq_calls", _CALLS_PATH)
         module = importlib.util.module_from_spec(importlib.util.spec_from_loader("_pq_calls", loader))
         loader.exec_module(module)
-        module.bind(_raise, _new_operand, _new_workspace, _refuse, _new_attn_workspace)
+        module.bind(_raise, _new_operand, _new_workspace, _refuse, _new_attn_workspace, _new_route_workspace, _new_route)
         bound = {name: getattr(module, name) for name in _CALLS}
     except (ImportError, AttributeError, OSError) as e:
         warnings.warn("the native binding of the hot calls cannot be used, ctypes takes 2 us more a call (%s); build it with "

@@ -5,6 +5,7 @@ import pytest
 import torch
 
 from paper_2605_09503_amd import pq
+from test_kv_python_binding import python  # noqa: F401
 from test_abi import FAKE, PQ_ERR_FORMAT, PQ_ERR_NULL, PQ_ERR_SHAPE, PQ_ERR_WORKSPACE, lib  # noqa: F401
 
 ODD = C.c_void_p(0x1008)
@@ -105,24 +106,41 @@ def test_combine(lib):  # noqa: F811
     assert f(T=0) == 0 and f(T=0, y=None, out=None) == 0
 
 
-def test_python_arguments(lib):  # noqa: F811
-    # tensors in host memory never reach a kernel
+@pytest.mark.parametrize("native", [True, False])
+def test_python_arguments(lib, python, native):  # noqa: F811
+    # the native calls, and the functions of pq.py that stand in for them; tensors in host memory never reach a kernel
+    m = pq if native else python
     z = lambda *shape, dtype=torch.uint8: torch.zeros(shape, dtype=dtype)
     need = pq.pq_operand_bytes(MX, 32, 8, 64)
     y, off = z(4, 8, dtype=torch.bfloat16), z(3, dtype=torch.int32)
-    for call in (lambda: pq.pq_qgemm_grouped(MX, 32, z(need), 4, z(2, need), off, y, 8, 64),
-                 lambda: pq.pq_moe_route(z(4, 8, dtype=torch.float32), 2),
-                 lambda: pq.pq_moe_combine(y, z(2, 2, dtype=torch.int32), z(2, 2, dtype=torch.float32))):
-        with pytest.raises(pq.PQError, match="GPU"):
+
+    def refused(call, match=None):
+        with pytest.raises(Exception, match=match) as e:
             call()
-    for call in (lambda: pq.pq_qgemm_grouped(MX, 32, z(need), 4, z(2, need + 256), off, y, 8, 64),
-                 lambda: pq.pq_qgemm_grouped(MX, 32, z(need), 4, z(2 * need), off, y, 8, 64),
-                 lambda: pq.pq_qgemm_grouped(MX, 32, z(need), 4, z(2, need), off, y.float(), 8, 64),
-                 lambda: pq.pq_moe_route(z(4, 8, dtype=torch.float64), 2),
-                 lambda: pq.pq_moe_route(z(8, dtype=torch.float32), 2),
-                 lambda: pq.pq_moe_route(z(8, 4, dtype=torch.float32).T, 2),
-                 lambda: pq.pq_moe_combine(y.float(), z(2, 2, dtype=torch.int32), z(2, 2, dtype=torch.float32)),
-                 lambda: pq.pq_moe_combine(y, z(2, dtype=torch.int32), z(2, 2, dtype=torch.float32)),
-                 lambda: pq.pack_experts(z(9, 32), z(9, 2), 4)):
-        with pytest.raises(pq.PQError):
-            call()
+        assert type(e.value).__name__ == "PQError" and e.value.code == PQ_ERR_SHAPE
+
+    for call in (lambda: m.pq_qgemm_grouped(MX, 32, z(need), 4, z(2, need), off, y, 8, 64),
+                 lambda: m.pq_moe_route(z(4, 8, dtype=torch.float32), 2),
+                 lambda: m.pq_moe_combine(y, z(2, 2, dtype=torch.int32), z(2, 2, dtype=torch.float32))):
+        refused(call, "GPU")
+    for call in (lambda: m.pq_qgemm_grouped(MX, 32, z(need), 4, z(2, need + 256), off, y, 8, 64),
+                 lambda: m.pq_qgemm_grouped(MX, 32, z(need), 4, z(2 * need), off, y, 8, 64),
+                 lambda: m.pq_qgemm_grouped(MX, 32, z(need), 4, z(2, need), off, y.float(), 8, 64),
+                 lambda: m.pq_qgemm_grouped(MX, 32, z(need), 4, z(2, need), off, y[:, :4], 8, 64),
+                 lambda: m.pq_moe_route(z(4, 8, dtype=torch.float64), 2),
+                 lambda: m.pq_moe_route(z(8, dtype=torch.float32), 2),
+                 lambda: m.pq_moe_route(z(8, 4, dtype=torch.float32).T, 2),
+                 lambda: m.pq_moe_combine(y.float(), z(2, 2, dtype=torch.int32), z(2, 2, dtype=torch.float32)),
+                 lambda: m.pq_moe_combine(y, z(2, dtype=torch.int32), z(2, 2, dtype=torch.float32)),
+                 lambda: m.pack_experts(z(9, 32), z(9, 2), 4)):
+        refused(call)
+
+
+@pytest.mark.parametrize("name", ["pq_dequantize", "pq_qgemm_grouped", "pq_moe_route", "pq_moe_combine"])
+def test_native_and_python_signatures(lib, python, name):  # noqa: F811
+    import inspect
+    native = getattr(pq, name)
+    assert inspect.isbuiltin(native)
+    want = inspect.signature(getattr(python, name))
+    got = inspect.signature(native)
+    assert [(p.name, p.default) for p in got.parameters.values()] == [(p.name, p.default) for p in want.parameters.values()]
