@@ -201,14 +201,14 @@ struct Shared {
   // behind the stages, for this tile and the next: bias of its columns, a word each, and (grouped) the index of its rows; the table
   static constexpr int bias = stages * stage, index = bias + 2 * BN * 4, table = index + 2 * BM * 4;
   static constexpr int lds(bool grouped) { return grouped ? table + Tiles<true>::kTableBytes : index; }
-  static constexpr int few = 5;            // panels: with fewer the loads reach past the next tile, whose bias and index are read as they are needed
+  static constexpr int few = 5;            // panels: with fewer (FEW) the loads reach past the next tile, bias and index are read as they are needed
   static_assert(fn * 32 <= 64, "a lane a column");
   static_assert((as_loads + ws_loads) % waves == 0 && as_loads % s_loads == 0, "every wave issues as many loads");
 };
 
 // A workgroup goes through its tiles, and through the panels of each, without a stop: three panels are on their way while one is
 // multiplied, also where they are the next tile's.
-template <int BM, int BN, int WM, int WN, bool GROUPED>
+template <int BM, int BN, int WM, int WN, bool GROUPED, bool FEW>
 __global__ __launch_bounds__(WM* WN * 64, 2) void mx_gemm_shared_kernel(const MxCall c) {
   using S = Shared<BM, BN, WM, WN>;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
@@ -216,10 +216,11 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void mx_gemm_shared_kernel(const Mx
   if (tiles.next >= tiles.end) return;
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int wave_m = wave % WM, wave_n = wave / WM;
+  const int wave_m = wave / WN, wave_n = wave % WN;
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char*)lds;
   const int panels = (int)mx_panels(c.K);
-  const bool ahead = panels >= S::few, index_ahead = GROUPED && c.rows && ahead;
+  constexpr bool ahead = !FEW;
+  const bool index_ahead = GROUPED && ahead && c.rows;
   const size_t as_at = mx_scales_at(c.a_rows, c.K), ws_at = mx_scales_at(c.N, c.K);
 
   // Loader: a load takes 16 rows' pieces of a panel, lane l the block that belongs at place l % 4 of row l / 4 (the same for all of a
@@ -253,7 +254,8 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void mx_gemm_shared_kernel(const Mx
     // grouped: the rows as the index gives them, which load() makes offsets of before it first uses them
     const auto a_row = [&](int row) {
       row = min(row, a_last);
-      return !GROUPED ? (uint32_t)row : index_ahead ? 0u : c.rows ? (uint32_t)c.rows[lt.first + row] : (uint32_t)lt.first + row;
+      if (GROUPED && FEW && c.rows) return (uint32_t)c.rows[lt.first + row];
+      return GROUPED ? (uint32_t)lt.first + row : (uint32_t)row;      // with an index ahead load() puts its rows in their place
     };
 #pragma unroll
     for (int i = 0; i < S::a_loads; ++i) {
@@ -321,12 +323,6 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void mx_gemm_shared_kernel(const Mx
   float16v acc[S::fn][S::fm];
   int4v af[2][S::fm], wf[2][S::fn];
   int asc[S::fm], wsc[S::fn];                  // scale bytes of this lane's two blocks of a panel: 0 and 2
-  const auto clear = [&] {
-#pragma unroll
-    for (int i = 0; i < S::fn; ++i)
-#pragma unroll
-      for (int j = 0; j < S::fm; ++j) acc[i][j] = float16v{};
-  };
   const auto read = [&](int set, int stage, int s) {
     const unsigned char *wp = lds + ((stage * S::stage + w_base) ^ (32 * s)), *ap = lds + ((stage * S::stage + a_base) ^ (32 * s));
 #pragma unroll
@@ -360,8 +356,27 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void mx_gemm_shared_kernel(const Mx
       for (int j = 0; j < S::fm; ++j) asm volatile("" : "+v"(acc[i][j]));
   };
 
-  // A lane has row l % 32 of a fragment and columns 8 q + 4 (l / 32) + 0 .. 3; the two halves of the wave exchange what makes eight
-  // columns of a row, lanes below 32 of q = 0 and 2, those above of 1 and 3.  The stores are S::stores of a wave whatever they
+  // the sums begin with the bias of their columns, zeros in LDS where there is none
+  const auto begin = [&](const Tile& t, int slot) {
+    const int l = opaque(lane), h = l >> 5, n0 = wave_n * S::fn * 32;
+    if (FEW && c.bias) {                                       // this wave's columns, as the loader would have left them
+      if (l < S::fn * 32)
+        reinterpret_cast<uint32_t*>(lds + S::bias)[slot * BN + n0 + l] = c.bias[t.expert * c.N + min(t.n0 + n0 + l, c.N - 1)];
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    }
+#pragma unroll
+    for (int i = 0; i < S::fn; ++i)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint4v b = *reinterpret_cast<const uint4v*>(lds + S::bias + (slot * BN + n0 + 32 * i + 8 * q + 4 * h) * 4);
+#pragma unroll
+        for (int j = 0; j < S::fm; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] = as_f32(b[e] << 16);
+      }
+  };
+
+  // A lane has row l % 32 of a fragment and columns 8 q + 4 (l / 32) + 0 .. 3.  The stores are S::stores of a wave whatever they
   // keep (what has no place goes past the buffer's end and is dropped), so that waits can count past them.
   const auto store = [&](const Tile& t, int slot) {
     if (c.out_f32) {                                           // for checks of the sums: no care taken of its speed
@@ -380,30 +395,13 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void mx_gemm_shared_kernel(const Mx
     const int l = opaque(lane), h = l >> 5;
     const int64_t n0 = t.n0 + wave_n * S::fn * 32;
     const int cols = (int)min(c.N - n0, (int64_t)S::fn * 32);  // of this wave; may be none
-    if (c.bias && !ahead) {                                    // this wave's columns, as the loader would have left them
-      if (l < S::fn * 32)
-        reinterpret_cast<uint32_t*>(lds + S::bias)[slot * BN + wave_n * S::fn * 32 + l] = c.bias[t.expert * c.N + min(n0 + l, c.N - 1)];
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-    }
-    // added also where there is none (zeros): sums that a branch changes would be copied
-#pragma unroll
-    for (int i = 0; i < S::fn; ++i)
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const uint4v b = *reinterpret_cast<const uint4v*>(lds + S::bias + (slot * BN + wave_n * S::fn * 32 + 32 * i + 8 * q + 4 * h) * 4);
-#pragma unroll
-        for (int j = 0; j < S::fm; ++j)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[i][j][4 * q + e] += as_f32(b[e] << 16);
-        __builtin_amdgcn_sched_barrier(0);
-      }
     uint64_t kept[(S::fm + 1) / 2];                            // rows of this wave that have one of A's
     if (GROUPED && c.rows) {
 #pragma unroll
       for (int j = 0; j < (S::fm + 1) / 2; ++j) {
         const int r = wave_m * S::fm * 32 + 64 * j + l;
         const int64_t m = min(t.first + r, t.end - 1);
-        const uint32_t from = index_ahead ? reinterpret_cast<const uint32_t*>(lds + S::index)[slot * BM + min(r, BM - 1)] : (uint32_t)c.rows[m];
+        const uint32_t from = ahead ? reinterpret_cast<const uint32_t*>(lds + S::index)[slot * BM + min(r, BM - 1)] : (uint32_t)c.rows[m];
         kept[j] = __ballot(from < (uint32_t)c.a_rows);
       }
     }
@@ -411,29 +409,46 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void mx_gemm_shared_kernel(const Mx
 #pragma unroll
     for (int j = 0; j < S::fm; ++j) {
       const int64_t m0 = t.first + (wave_m * S::fm + j) * 32;
-      const int rows = (int)min(t.end - m0, (int64_t)32), r = l & 31;
-      bool ok = r < rows;
-      if (GROUPED && c.rows) ok = ok && (kept[j / 2] >> (32 * (j & 1) + r) & 1);
+      const int rows = (int)min(t.end - m0, (int64_t)32), r = l & 15, piece = 16 * (l >> 4 & 1) + 8 * h;      // first column in a fragment
       uint16_t* y = (uint16_t*)c.y + m0 * c.ldy + n0;
       const auto buf = __builtin_amdgcn_make_buffer_rsrc(y, 0, 0x7FFFFFF0, 0x00027000);
-      const int at = r * (int)c.ldy * 2 + 16 * h;
+      bool ok[2];
 #pragma unroll
-      for (int i = 0; i < S::fn; ++i)
+      for (int s = 0; s < 2; ++s) {
+        ok[s] = r + 16 * s < rows;
+        if (GROUPED && c.rows) ok[s] = ok[s] && (kept[j / 2] >> (32 * (j & 1) + 16 * s + r) & 1);
+      }
 #pragma unroll
-        for (int q = 0; q < 4; q += 2) {
+      for (int i = 0; i < S::fn; ++i) {
+        // halves of the wave: eight columns of a row a lane, columns 16 q + 8 (l / 32); then rows of sixteen lanes: q = 0 and 1 of a row
+        // side by side, 64 bytes of it in one store (with 32: 8192 x 12288 x 8192 NT1, 65536 x 2816 x 2048 NT2)
+        uint4v half_row[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
           const auto pack = [&](int g, int e) { return pack_bf16(acc[i][j][4 * g + e], acc[i][j][4 * g + e + 1]); };
-          const auto x = __builtin_amdgcn_permlane32_swap(pack(q, 0), pack(q + 1, 0), false, false);
-          const auto z = __builtin_amdgcn_permlane32_swap(pack(q, 2), pack(q + 1, 2), false, false);
-          const int col = 32 * i + 8 * q + 8 * h;
-          const uint4v v = {x[0], z[0], x[1], z[1]};
-          __builtin_amdgcn_raw_buffer_store_b128(v, buf, ok && col + 8 <= cols ? at + 64 * i + 16 * q : kNowhere, 0, 0);
+          const auto x = __builtin_amdgcn_permlane32_swap(pack(2 * q, 0), pack(2 * q + 1, 0), false, false);
+          const auto z = __builtin_amdgcn_permlane32_swap(pack(2 * q, 2), pack(2 * q + 1, 2), false, false);
+          half_row[q] = uint4v{x[0], z[0], x[1], z[1]};
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const auto x = __builtin_amdgcn_permlane16_swap(half_row[0][e], half_row[1][e], false, false);
+          half_row[0][e] = x[0];
+          half_row[1][e] = x[1];
+        }
+        const int col = 32 * i + piece;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const int at = (r + 16 * s) * (int)c.ldy * 2 + 2 * col;
+          __builtin_amdgcn_raw_buffer_store_b128(half_row[s], buf, ok[s] && col + 8 <= cols ? at : kNowhere, 0, 0);
           if (c.N & 7) {                                       // uniform; the last columns of rows that end inside eight
 #pragma unroll
             for (int e = 0; e < 7; ++e)
-              __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(v[e >> 1] >> (16 * (e & 1))), buf,
-                                                    ok && col + 8 > cols && col + e < cols ? at + 64 * i + 16 * q + 2 * e : kNowhere, 0, 0);
+              __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(half_row[s][e >> 1] >> (16 * (e & 1))), buf,
+                                                    ok[s] && col + 8 > cols && col + e < cols ? at + 2 * e : kNowhere, 0, 0);
           }
         }
+      }
     }
   };
 
@@ -460,14 +475,10 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void mx_gemm_shared_kernel(const Mx
   read(0, 0, 0);
   bool stored = false;                                         // the tile before this one issued S::stores stores, and they may be under way
   for (int tile = tiles.next; tile < tiles.end; tile += tiles.step) {
-    clear();
-    for (int p = 0; p < panels; ++p) {
-      load((stage + S::stages - 1) & (S::stages - 1));
-      read(1, stage, 1);
-      PQ_MULTIPLY(0);
-      __builtin_amdgcn_sched_barrier(0);
-      // What is waited for is the next panel.  Behind its loads come those of two more, and in a tile's first two panels the
-      // stores of the tile before.
+    const auto fetch = [&] { load((stage + S::stages - 1) & (S::stages - 1)); };
+    // What is waited for is the next panel.  Behind its loads come those of two more, and in a tile's first two panels the
+    // stores of the tile before.
+    const auto turn = [&](int p) {
       if (!more || drain)
         arrived<0>();
       else if (stored && p < 2)
@@ -476,18 +487,37 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void mx_gemm_shared_kernel(const Mx
         arrived<(S::stages - 2) * S::loads>();
       meet();
       stage = (stage + 1) & (S::stages - 1);
-      read(0, stage, 0);                                       // of no use behind the last panel of all
-      int na[S::fm], nw[S::fn];
+    };
+    int na[S::fm], nw[S::fn];
+    if (t.first + wave_m * S::fm * 32 < t.end) {
+      begin(t, slot);
+      for (int p = 0; p < panels; ++p) {
+        fetch();
+        read(1, stage, 1);
+        PQ_MULTIPLY(0);
+        __builtin_amdgcn_sched_barrier(0);
+        turn(p);
+        read(0, stage, 0);                                     // of no use behind the last panel of all
+        read_scales(stage, na, nw);
+        PQ_MULTIPLY(1);
+        __builtin_amdgcn_sched_barrier(0);
+        take_scales(na, nw);
+      }
+      store(t, slot);
+      stored = panels >= 2 && !c.out_f32 && (c.N & 7) == 0;
+    } else {                                                   // none of this wave's rows are in the tile: the others have the matrix units
+      for (int p = 0; p < panels; ++p) {
+        fetch();
+        turn(p);
+      }
+      stored = false;
+      read(0, stage, 0);
       read_scales(stage, na, nw);
-      PQ_MULTIPLY(1);
-      __builtin_amdgcn_sched_barrier(0);
       take_scales(na, nw);
     }
-    store(t, slot);
-    stored = panels >= 2 && !c.out_f32 && (c.N & 7) == 0;
     slot ^= 1;
-    // the loads are up to three panels ahead, in the next tile where a tile has more than three
-    if (tile + tiles.step < tiles.end) t = panels > 3 ? lt : tiles.at(c, BM, BN, tile + tiles.step);
+    // the loads are three panels ahead, in the next tile where a tile has more than three
+    if (tile + tiles.step < tiles.end) t = !FEW ? lt : tiles.at(c, BM, BN, tile + tiles.step);
   }
 #undef PQ_MULTIPLY
 }
@@ -794,9 +824,11 @@ constexpr int kUnits = 256;                  // compute units
 template <int BM, int BN, int WM, int WN, bool GROUPED>
 int launch_shared(const MxCall& c, hipStream_t st) {
   using S = Shared<BM, BN, WM, WN>;
-  static std::atomic<uint64_t> allowed{0};
-  return launch(mx_gemm_shared_kernel<BM, BN, WM, WN, GROUPED>, "mx_gemm_shared_kernel", c, BM, BN, S::waves, S::lds(GROUPED),
-                kUnits * (160 * 1024 / S::lds(GROUPED)), allowed, st);
+  static std::atomic<uint64_t> allowed{0}, allowed_few{0};
+  constexpr int lds = S::lds(GROUPED), most = kUnits * (160 * 1024 / lds);
+  if (mx_panels(c.K) < S::few)
+    return launch(mx_gemm_shared_kernel<BM, BN, WM, WN, GROUPED, true>, "mx_gemm_shared_kernel", c, BM, BN, S::waves, lds, most, allowed_few, st);
+  return launch(mx_gemm_shared_kernel<BM, BN, WM, WN, GROUPED, false>, "mx_gemm_shared_kernel", c, BM, BN, S::waves, lds, most, allowed, st);
 }
 template <int FM, int KW, bool GROUPED>
 int launch_split(const MxCall& c, hipStream_t st) {
