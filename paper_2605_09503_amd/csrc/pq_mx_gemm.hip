@@ -843,19 +843,53 @@ int launch_alone(const MxCall& c, hipStream_t st) {
   return launch(mx_gemm_alone_kernel<FM>, "mx_gemm_alone_kernel", c, S::bm, S::bn * S::waves, S::waves, S::lds, kUnits * (160 * 1024 / S::lds), allowed, st);
 }
 
+// Which kernel: the one that takes the shortest time by a model of each in us, fitted to all of them timed at M 1 .. 2048, N 1024, 4096
+// and 12288, K 512, 2048 and 8192.  Small tiles read more than they multiply and are bound by what the units take from the caches;
+// large ones take some us a turn and a time a panel, and only pay where there are enough of them.  Of 126 shapes the choice is within
+// 7 % of the best for 120, within 29 % for all.  us, split 32 and 64 rows, shared 128, 256:
+//   M 32, N 4096, K 2048    4.5   4.2   8.1  11.6        M 256, N 4096, K 8192   14.8  11.7  24.8  45.0
+//   M 512, N 12288, K 512  22.3  16.1   7.9  11.3        M 1024, N 12288, K 8192  138   104    62    55
+enum class Kernel { split32, split64, shared128, shared256 };
+Kernel choose(const MxCall& c, bool grouped) {
+  const double panels = (double)mx_panels(c.K), groups = grouped ? (double)(c.experts < c.M ? c.experts : c.M) : 1.0;
+  // tiles of rows: a group's last is half full on average
+  const auto tiles = [&](int bm, int bn) {
+    const double whole = (double)c.M / bm, rows = grouped ? (whole + 0.5 * groups > groups ? whole + 0.5 * groups : groups) : (double)((c.M + bm - 1) / bm);
+    return rows * (double)((c.N + bn - 1) / bn);
+  };
+  const double weights = groups * (double)c.N * panels * (kMxRowBytes + kMxRowScales) / 5.2e6;        // at 5.2 TB/s
+  const auto split = [&](int fm) {
+    const double n = tiles(32 * fm, 32), traffic = n * panels * (fm == 1 ? 4.35e-3 : 6.65e-3) / 24.0;   // MB at 24 TB/s
+    const double wait = panels / 4 * (fm == 1 ? 0.165 : 0.245);
+    return 2.8 + 0.8 * n / 512 + 0.25 * (traffic + wait) + (traffic > wait ? traffic > weights ? traffic : weights : wait > weights ? wait : weights);
+  };
+  const auto shared = [&](int bm) {
+    const double n = tiles(bm, bm), turns = (double)(int64_t)((n + kUnits - 1) / kUnits);
+    const double full = n < kUnits ? n / kUnits : 1.0;                   // how much of the chip works
+    const double panel = bm == 128 ? (turns <= 1 ? 0.33 : 0.29 * turns) : turns * (0.62 + 0.35 * full), t = panels * panel;
+    return (bm == 128 ? 2.8 + turns : 2.6 + turns * (1.5 + 3.0 * full)) + (t > weights ? t : weights);
+  };
+  const double t[4] = {split(1), split(2), shared(128), shared(256)};
+  int best = 0;
+  for (int i = 1; i < 4; ++i)
+    if (t[i] < t[best]) best = i;
+  return (Kernel)best;
+}
+
 template <bool GROUPED>
 int run(const MxCall& c, hipStream_t st) {
-  const int64_t groups = GROUPED ? c.experts : 1, each = (c.M + groups - 1) / groups;
-  const int64_t narrow = (c.N + 31) / 32;                              // tiles of 32 columns
-  if (each <= 64) {
-    if constexpr (GROUPED) {
-      if ((c.M < groups ? c.M : groups) * narrow >= 2048) return each <= 32 ? launch_alone<1>(c, st) : launch_alone<2>(c, st);
-    }
-    if (each > 32) return launch_split<2, 4, GROUPED>(c, st);
-    return groups * narrow <= kUnits && c.K >= 2048 ? launch_split<1, 8, GROUPED>(c, st) : launch_split<1, 4, GROUPED>(c, st);
+  const Kernel k = choose(c, GROUPED);
+  if constexpr (GROUPED) {
+    // enough tiles of 32 columns for every wave of the chip: no need to share K
+    const int64_t rows = (c.M + 31) / 32 > c.experts ? (c.M + 31) / 32 : c.experts < c.M ? c.experts : c.M;
+    if (k <= Kernel::split64 && rows * ((c.N + 31) / 32) >= 2048) return k == Kernel::split32 ? launch_alone<1>(c, st) : launch_alone<2>(c, st);
   }
-  if (((each + 255) / 256) * ((c.N + 255) / 256) * groups < 200) return launch_shared<128, 128, 2, 2, GROUPED>(c, st);
-  return launch_shared<256, 256, 2, 4, GROUPED>(c, st);
+  switch (k) {
+    case Kernel::split32: return launch_split<1, 4, GROUPED>(c, st);
+    case Kernel::split64: return launch_split<2, 4, GROUPED>(c, st);
+    case Kernel::shared128: return launch_shared<128, 128, 2, 2, GROUPED>(c, st);
+    default: return launch_shared<256, 256, 2, 4, GROUPED>(c, st);
+  }
 }
 
 }  // namespace
