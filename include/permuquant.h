@@ -340,7 +340,7 @@ int pq_qgemm_f32(pq_format fmt, int group, const uint8_t* a_codes, const void* a
                  int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
 
 /* The output tile (rows x columns of Y a workgroup computes) that a product of this shape takes: 256 x 256, 224 x 256,
- * 128 x 128, or one of 64 x 96, 64 x 64, 64 x 32 and 32 x 32 whose waves split K.  Host only.  K is added in fp32 in
+ * 128 x 128, or one of 64 x 96, 64 x 64, 64 x 32 and 32 x 32 whose waves split K (MXFP4: 256 x 256, 128 x 128, 64 x 32 or 32 x 32).  Host only.  K is added in fp32 in
  * an order that is fixed for a tile and differs between them, so a row of Y is the same bits from run to run but may
  * differ by the rounding of that sum between calls with other M or N.                                          */
 int pq_qgemm_tile(pq_format fmt, int group, int64_t M, int64_t N, int64_t K, int* tile_m, int* tile_n);
@@ -609,10 +609,11 @@ int pq_attn_decode(const pq_kv_cache* cache, const void* q_bf16, int64_t q_ld, i
  * outputs that it takes part in, are NaN.  Stored as the other formats: codes [rows, K / 2], scales uint8 [rows, K / 32].
  *
  * The format of pq_quantize_act, pq_quantize_weights (tensor_scale_out receives 1), pq_operand_bytes, pq_pack_operand,
- * pq_quantize_act_packed, pq_qgemm_packed, pq_qgemm_packed_bias and pq_qgemm_packed_f32, with group 32, any K that is a multiple of 32,
- * tensor scales ignored, and of the calls below; other calls refuse it with PQ_ERR_FORMAT.  Its operands are panels of 128 channels,
+ * pq_quantize_act_packed, pq_qgemm_packed, pq_qgemm_packed_bias, pq_qgemm_packed_f32 and pq_qgemm_tile, with group 32, any K that is a
+ * multiple of 32, tensor scales ignored, and of the calls below; other calls refuse it with PQ_ERR_FORMAT.  perm is 16-byte aligned, ldy of
+ * the products at most 2^24.  Its operands are panels of 128 channels,
  * zero from K on (pq_operand_bytes counts them).
- * Products are exact, sums fp32 over the whole of K, in an order that depends on M, N and K.
+ * Products are exact, sums fp32 over the whole of K, in an order that depends on M, N and K; they begin with the bias or it is added last.
  */
 
 /*
@@ -633,7 +634,8 @@ int pq_dequantize(pq_format fmt, int group, const uint8_t* codes, const void* sc
  * offsets: int32 [experts + 1] device, non-decreasing; values outside 0 .. M are cut to it.  Experts without rows cost nothing.
  * rows: int32 [M] device or NULL (then a_rows >= M).  A row whose index is outside 0 .. a_rows - 1 is left as it was.
  * M: rows of y, an upper bound of offsets[experts] (host); what lies outside offsets[0] .. offsets[experts] - 1 is left as it was.
- * bias: bf16 [experts, N] or NULL.  y: bf16 [M, ldy].  M and a_rows may be 0; experts at most 65536.  May be captured into a graph.
+ * bias: bf16 [experts, N] or NULL.  y: bf16 [M, ldy], ldy >= N, a multiple of 8 and at most 2^24.  M and a_rows may be 0; experts at most
+ * 65536.  y overlaps none of the inputs.  May be captured into a graph.
  */
 int pq_qgemm_grouped(pq_format fmt, int group, const void* a_operand, int64_t a_rows, const void* w_operands, int experts,
                      const int32_t* offsets, const int32_t* rows, int64_t M, int64_t N, int64_t K, const void* bias_bf16, void* y_bf16,

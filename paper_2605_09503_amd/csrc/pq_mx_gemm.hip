@@ -894,6 +894,17 @@ int run(const MxCall& c, hipStream_t st) {
 
 }  // namespace
 
+void mx_gemm_tile(int64_t M, int64_t N, int64_t K, int* bm, int* bn) {
+  MxCall c{};
+  c.M = M, c.N = N, c.K = K, c.experts = 1;
+  switch (choose(c, false)) {
+    case Kernel::split32: *bm = *bn = 32; break;
+    case Kernel::split64: *bm = 64, *bn = 32; break;
+    case Kernel::shared128: *bm = *bn = 128; break;
+    default: *bm = *bn = 256;
+  }
+}
+
 int run_mx_gemm(const MxCall& c, hipStream_t st) {
   if (c.M == 0) return PQ_OK;
   return c.offsets ? run<true>(c, st) : run<false>(c, st);

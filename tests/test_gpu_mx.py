@@ -2,8 +2,8 @@
 
 Tolerances.  Codes, scales and read-back values are exact.  A product's terms are exact; a 32 x 32 x 64 instruction adds 64 of them to
 an fp32 sum, and each of its additions is taken to lose at most 2^-23 of the terms' absolute sum (2^-24 rounded, twice that cut off): K / 64
-instructions in turn and some 8 additions that join parts give (K / 64 + 8) 2^-23 of sum |terms|.  A bias adds 2^-24 of what it gives; bf16
-outputs are rounded once (2^-8 of themselves).  Weights: e^x of an argument that is off by 2^-24 of itself (|x| < 100) and a few
+instructions in turn and some 8 additions that join parts give (K / 64 + 8) 2^-23 of sum |terms|.  A bias is one of the terms: the sum may
+begin with it.  bf16 outputs are rounded once (2^-8 of themselves).  Weights: e^x of an argument that is off by 2^-24 of itself (|x| < 100) and a few
 roundings in sum and quotient: 1e-5.  The weighted sum: k + 1 fused steps of 2^-24 of the terms' absolute sum, then bf16's 2^-8."""
 import numpy as np
 import pytest
@@ -166,8 +166,7 @@ def test_product(M, N, K):
     assert bool((y[M:] == 5).all()) and bool((y[:, N:] == 5).all())
     bias = rows_of(rng, 1, (N + 31) // 32 * 32, odd=False)[0, :N].clone()
     pq.pq_qgemm_packed_bias(MX, 32, a, None, b, None, bias, y[:M], M, N, K)
-    ref = ref + f64(bias[None])
-    close(y[:M, :N], ref, bound(K, mag) + 2.0 ** -24 * np.abs(ref))
+    close(y[:M, :N], ref + f64(bias[None]), bound(K, mag + np.abs(f64(bias[None]))))
     assert bool((y[M:] == 5).all()) and bool((y[:, N:] == 5).all())
 
 
@@ -196,6 +195,46 @@ def test_product_of_extremes(M, N, K):
     assert (np.abs(got - ref)[fine] <= (bound(K, mag) + 2.0 ** -126)[fine]).all()
 
 
+def big(rows, K, seed, scale=1.0):
+    """bf16 [rows, K] and its quantized values in float64, both on the GPU (the quantizers have tests of their own)."""
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    x = (torch.randn(rows, K, generator=g, device=DEV) * scale * torch.exp(torch.randn(K, generator=g, device=DEV))).to(torch.bfloat16)
+    codes, scales = pq.alloc_quantized(MX, 32, rows, K)
+    pq.pq_quantize_act(MX, 32, x, None, None, codes, scales)
+    return x, codes, scales, pq.pq_dequantize(MX, 32, codes, scales).double()
+
+
+def close_big(got, ref, err):
+    assert bool((torch.isnan(got) == torch.isnan(ref)).all())
+    worst = ((got.double() - ref).abs() / (err + 2.0 ** -8 * (ref.abs() + err) + 2.0 ** -133)).nan_to_num(0.0).max().item()
+    assert worst <= 1.0, worst
+
+
+# several tiles for every workgroup, with one to seven panels of 128 channels each: the loads of a tile begin in the one before it, or
+# three before it; edges in both directions, rows that end inside eight columns
+@pytest.mark.parametrize("M,N,K,tile", [(5757, 2618, 32, 128), (3153, 3068, 160, 128), (3018, 3480, 384, 128), (3179, 3592, 512, 128), (3955, 4469, 640, 128),
+                                        (2650, 5944, 672, 128), (4063, 4060, 256, 256), (7352, 8877, 288, 256), (5692, 5624, 480, 256), (4999, 5733, 512, 256), (4522, 6360, 608, 256),
+                                        (4423, 6544, 1184, 256), (45, 9001, 2080, 64), (150, 3001, 96, 64), (90, 2000, 512, 32), (333, 1000, 4128, 64)])
+@pytest.mark.parametrize("bias", [False, True])
+def test_product_of_many_tiles(M, N, K, tile, bias):
+    assert pq.pq_qgemm_tile(MX, 32, M, N, K)[0] == tile
+    x, _, _, xq = big(M, K, 1)
+    _, codes, scales, wq = big(N, K, 2, 0.02)
+    b = torch.randn(N, generator=torch.Generator(device=DEV).manual_seed(3), device=DEV).to(torch.bfloat16)
+    a, w = operand(x), pq.pq_pack_operand(MX, 32, codes, scales)
+    ldy = (N + 7) // 8 * 8 + 8
+    y = torch.full((M + 1, ldy), 5.0, dtype=torch.bfloat16, device=DEV)
+    if bias:
+        pq.pq_qgemm_packed_bias(MX, 32, a, None, w, None, b, y[:M], M, N, K)
+    else:
+        pq.pq_qgemm_packed(MX, 32, a, None, w, None, y[:M], M, N, K)
+    ref, mag = xq @ wq.T, xq.abs() @ wq.T.abs()
+    if bias:
+        ref, mag = ref + b.double(), mag + b.double().abs()
+    close_big(y[:M, :N], ref, (K / 64 + 8) * 2.0 ** -23 * mag)
+    assert bool((y[M:] == 5).all()) and bool((y[:, N:] == 5).all())
+
+
 def test_product_repeats_its_bits():
     rng = np.random.default_rng(1)
     for M, N, K in ((3, 700, 4096), (70, 900, 2048), (700, 900, 1024)):
@@ -222,7 +261,7 @@ def experts_case(rng, sizes, a_rows, N, K, gather, bias, first=0, behind=0):
             r = rows[i] if gather else i
             part = wq[e * N:(e + 1) * N]
             ref[i] = part @ xq[r] + b[e]
-            err[i] = bound(K, np.abs(part) @ np.abs(xq[r])) + 2.0 ** -24 * np.abs(ref[i])
+            err[i] = bound(K, np.abs(part) @ np.abs(xq[r]) + np.abs(b[e]))
     t = lambda v: None if v is None else torch.from_numpy(np.ascontiguousarray(v)).to(DEV)
     codes, scales = stored(mx.quantize(f64(w)))
     return dict(a=operand(x), w=pq.pack_experts(codes, scales, E), offsets=t(offsets.astype(np.int32)), rows=t(rows),
@@ -245,6 +284,45 @@ def test_grouped(sizes, a_rows, N, K, gather, bias):
     rng = np.random.default_rng(len(sizes) + a_rows + N)
     c = experts_case(rng, sizes, a_rows, N, K, gather, bias, first=0 if gather is False else 2, behind=0 if gather is False else 3)
     close(grouped(c, a_rows, N, K), c["ref"], c["err"])
+
+
+# experts of all lengths by every kernel: few and many panels, an index or none, more experts than the kernels keep a table of
+@pytest.mark.parametrize("E,M,a_rows,N,K,gather,bias,few_experts", [
+    (64, 9000, 1500, 2056, 640, True, True, 0), (64, 9000, 1500, 2056, 544, True, False, 0), (64, 9000, 1500, 2050, 512, True, True, 0), (64, 9000, 1500, 2056, 96, True, True, 0),
+    (8, 30000, 30000, 1288, 704, False, True, 0), (8, 30000, 7000, 1288, 672, True, True, 0), (8, 30000, 7000, 1285, 256, True, False, 0), (8, 40000, 9000, 2056, 1152, True, True, 3),
+    (300, 2400, 300, 520, 1056, True, True, 0), (300, 2400, 300, 515, 160, True, False, 0), (100, 4500, 500, 1032, 576, True, True, 0), (100, 4500, 4500, 1032, 320, False, True, 9),
+    (1500, 3000, 400, 264, 288, True, True, 0), (1100, 60000, 4000, 512, 640, True, False, 0), (1100, 60000, 60000, 512, 128, False, True, 0), (3, 90, 40, 1000, 2080, True, True, 0)])
+def test_grouped_of_all_lengths(E, M, a_rows, N, K, gather, bias, few_experts):
+    rng = np.random.default_rng(E + M + K)
+    share = np.exp(rng.standard_normal(E))
+    share[rng.random(E) < 0.2] = 0.0
+    if few_experts:
+        share[rng.permutation(E)[:E - few_experts]] = 0.0                 # all rows go to a few of them
+    sizes = np.floor(share / share.sum() * (M - 5)).astype(np.int64)      # the last rows are nobody's
+    offsets = np.concatenate([[0], np.cumsum(sizes)])
+    x, _, _, xq = big(a_rows, K, 1)
+    _, codes, scales, wq = big(E * N, K, 2, 0.02)
+    b = torch.randn(E, N, generator=torch.Generator(device=DEV).manual_seed(3), device=DEV).to(torch.bfloat16)
+    rows = torch.from_numpy(rng.integers(0, a_rows, M).astype(np.int32)).to(DEV) if gather else None
+    if gather:
+        rows[7::97] = -1
+        rows[11::101] = a_rows
+    y = torch.full((M, (N + 7) // 8 * 8 + 8), 5.0, dtype=torch.bfloat16, device=DEV)
+    pq.pq_qgemm_grouped(MX, 32, operand(x), a_rows, pq.pack_experts(codes, scales, E), torch.from_numpy(offsets.astype(np.int32)).to(DEV), y[:, :N], N, K,
+                        rows=rows, bias=b if bias else None)
+    assert bool((y[:, N:] == 5).all()) and bool((y[offsets[-1]:] == 5).all())
+    for e in range(E):
+        if sizes[e] == 0:
+            continue
+        at = slice(offsets[e], offsets[e + 1])
+        index = rows[at].long() if gather else torch.arange(offsets[e], offsets[e + 1], device=DEV)
+        known = (index >= 0) & (index < a_rows)
+        part, aq = wq[e * N:(e + 1) * N], xq[index.clamp(0, a_rows - 1)]
+        ref, mag = aq @ part.T, aq.abs() @ part.T.abs()
+        if bias:
+            ref, mag = ref + b[e].double(), mag + b[e].double().abs()
+        ref, mag = torch.where(known[:, None], ref, 5.0), torch.where(known[:, None], mag, 0.0)
+        close_big(y[at, :N], ref, (K / 64 + 8) * 2.0 ** -23 * mag)
 
 
 def test_grouped_leaves_other_rows():

@@ -48,9 +48,19 @@ def test_products(lib):  # noqa: F811
     assert g(a=None) == g(w=None) == g(y=None) == PQ_ERR_NULL
     assert g(gr=16) == PQ_ERR_FORMAT
     assert g(M=0) == g(N=0) == g(K=48) == g(ldy=4) == g(ldy=12) == g(a=ODD) == g(y=ODD) == g(M=(1 << 24) + 1) == PQ_ERR_SHAPE
-    assert g(M=1 << 24, N=1 << 24, ldy=1 << 24) == PQ_ERR_SHAPE                      # more tiles than a launch has
+    assert g(M=1 << 24, N=1 << 24, ldy=1 << 24) == g(ldy=(1 << 24) + 8) == PQ_ERR_SHAPE      # more tiles than a launch has
     assert lib.pq_qgemm_packed_bias(MX, 32, FAKE, None, FAKE, None, 8, 8, 64, None, FAKE, 8, None) == PQ_ERR_NULL
     assert lib.pq_qgemm_packed_f32(MX, 32, FAKE, None, FAKE, None, 8, 8, 64, FAKE, 4, None) == PQ_ERR_SHAPE
+
+
+def test_tile(lib):  # noqa: F811
+    assert pq.pq_qgemm_tile(MX, 32, 1, 4096, 4096) == (32, 32)
+    assert pq.pq_qgemm_tile(MX, 32, 60, 12288, 4096) == (64, 32)
+    assert pq.pq_qgemm_tile(MX, 32, 2000, 4096, 2048) == (128, 128)
+    assert pq.pq_qgemm_tile(MX, 32, 8192, 12288, 8192) == (256, 256)
+    for bad in [(MX, 16, 8, 8, 64), (MX, 32, 0, 8, 64), (MX, 32, 8, 8, 48)]:
+        with pytest.raises(pq.PQError):
+            pq.pq_qgemm_tile(*bad)
 
 
 def test_calls_that_do_not_offer_it(lib):  # noqa: F811
@@ -78,7 +88,7 @@ def test_grouped(lib):  # noqa: F811
     assert g(experts=0) == g(experts=65537) == g(M=-1) == g(a_rows=-1) == g(N=0) == g(K=48) == g(ldy=12) == g(ldy=0) == PQ_ERR_SHAPE
     assert g(a=ODD) == g(w=ODD) == g(y=ODD) == g(bias=ODD) == g(off=ODD2) == g(rows=ODD2) == PQ_ERR_SHAPE
     assert g(rows=None) == PQ_ERR_SHAPE                                              # 8 rows cannot make 16 in order
-    assert g(M=1 << 24, N=1 << 24, ldy=1 << 24) == PQ_ERR_SHAPE
+    assert g(M=1 << 24, N=1 << 24, ldy=1 << 24) == g(ldy=(1 << 24) + 8) == PQ_ERR_SHAPE
     assert g(M=0) == 0 and g(a_rows=0) == 0 and g(M=0, a=None, y=None) == 0          # nothing to do, nothing launched
 
 
