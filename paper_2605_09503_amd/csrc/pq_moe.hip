@@ -40,10 +40,31 @@ __device__ __forceinline__ float wave_sum_f32(float v) {
   return (a + b) + (c + d);
 }
 
-// A lane's PER experts, lane + 64 i, largest first: a wave's largest is then one of the lanes' first, and the lane that has it moves
+// largest and sum over the LANES lanes of a token, in each of them: a row of sixteen, or the wave
+__device__ __forceinline__ uint32_t row_max_u32(uint32_t v) {
+  v = max(v, dpp_u32<0xB1>(v));
+  v = max(v, dpp_u32<0x4E>(v));
+  v = max(v, dpp_u32<0x141>(v));
+  return max(v, dpp_u32<0x140>(v));
+}
+template <int LANES>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
+  if constexpr (LANES == 16) return row_max_u32(v);
+  return wave_max_u32(v);
+}
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
+  if constexpr (LANES == 64) return wave_sum_f32(v);
+  v += dpp_f32<0xB1>(v);
+  v += dpp_f32<0x4E>(v);
+  v += dpp_f32<0x141>(v);
+  return v + dpp_f32<0x140>(v);
+}
+
+// A lane's PER experts, lane + LANES i, largest first: a token's largest is then one of its lanes' first, and the lane that has it moves
 // on to its next.  A bf16 logit and its expert fit one word (the expert's complement below, so that equal logits order by
 // expert); binary32 logits keep the expert beside the key.
-template <int PER, bool BF16>
+template <int PER, bool BF16, int LANES>
 struct Sorted {
   uint32_t key[PER], low[BF16 ? 1 : PER];                     // low: complement of the expert
   __device__ __forceinline__ void order(int i, int j) {       // the larger of two to place i
@@ -69,18 +90,16 @@ struct Sorted {
           for (int i = 0; i < k; ++i)
             if (i + j + k < PER && (i + j) / (2 * p) == (i + j + k) / (2 * p)) order(i + j, i + j + k);
   }
-  // the wave's largest: its key (0: none is left) and expert, uniform; it is taken out
-  __device__ __forceinline__ uint32_t pop(int lane, int& expert) {
-    uint32_t best = wave_max_u32(key[0]);
-    if (best == 0) return 0;
+  // the token's largest: its key and expert (0 and -1: none is left); it is taken out
+  __device__ __forceinline__ uint32_t pop(int& expert) {
+    uint32_t best = lanes_max<LANES>(key[0]);
     bool mine = key[0] == best;
     if constexpr (BF16) {
-      expert = 0xFFFF - (int)(best & 0xFFFFu);
-      best &= 0xFFFF0000u;
+      expert = best ? 0xFFFF - (int)(best & 0xFFFFu) : -1;
     } else {
-      const uint32_t l = wave_max_u32(mine ? low[0] : 0u);
+      const uint32_t l = lanes_max<LANES>(mine ? low[0] : 0u);
       mine = mine && low[0] == l;
-      expert = (int)~l;
+      expert = best ? (int)~l : -1;
     }
 #pragma unroll
     for (int i = 0; i + 1 < PER; ++i) {
@@ -88,28 +107,33 @@ struct Sorted {
       if constexpr (!BF16) low[i] = mine ? low[i + 1] : low[i];
     }
     key[PER - 1] = mine ? 0u : key[PER - 1];
-    return best;
+    return BF16 ? best & 0xFFFF0000u : best;
   }
 };
 
-template <int PER, bool BF16>
-__device__ __forceinline__ void load_logits(const RouteCall& c, int64_t t, int lane, float (&v)[PER]) {
+// e^x for a sum whose largest term is 1: x times log2 e is off by 2^-24 of itself, which changes the term by |x| 2^-24 of itself, at most
+// 0.37 2^-24 of the largest.
+__device__ __forceinline__ float exp_in_sum(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+
+// A token's logits, expert sub + LANES i at place i of lane `sub` of its LANES
+template <int PER, bool BF16, int LANES>
+__device__ __forceinline__ void load_logits(const RouteCall& c, int64_t t, int sub, float (&v)[PER]) {
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int e = lane + 64 * i;
+    const int e = sub + LANES * i;
     if constexpr (BF16)
       v[i] = e < c.experts ? bf16_to_f32(((const uint16_t*)c.logits)[t * c.ld + e]) : -INFINITY;
     else
       v[i] = e < c.experts ? ((const float*)c.logits)[t * c.ld + e] : -INFINITY;
   }
 }
-// A wave a token: ids and weights written, lane j < k has the j-th expert (-1: none).
-template <int PER, bool BF16>
-__device__ __forceinline__ int route_token(const RouteCall& c, int64_t t, int lane, const float (&v)[PER]) {
-  Sorted<PER, BF16> s;
+// LANES lanes a token: ids and weights written (where `there`), lane j < k has the j-th expert (-1: none).
+template <int PER, bool BF16, int LANES>
+__device__ __forceinline__ int route_token(const RouteCall& c, int64_t t, bool there, int sub, const float (&v)[PER]) {
+  Sorted<PER, BF16, LANES> s;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const uint32_t e = (uint32_t)(lane + 64 * i), key = key_of(v[i]);
+    const uint32_t e = (uint32_t)(sub + LANES * i), key = key_of(v[i]);
     if constexpr (BF16) {
       s.key[i] = key ? (key & 0xFFFF0000u) | (0xFFFFu - e) : 0u;      // a bf16 value says nothing in the low half
     } else {
@@ -122,10 +146,9 @@ __device__ __forceinline__ int route_token(const RouteCall& c, int64_t t, int la
   int id = -1;
   for (int j = 0; j < c.k; ++j) {
     int e;
-    const uint32_t key = s.pop(lane, e);
-    if (key == 0) break;
+    const uint32_t key = s.pop(e);
     if (j == 0) first = key;
-    if (lane == j) kept = key, id = e;
+    if (sub == j) kept = key, id = e;
   }
   const auto value = [](uint32_t key) { return BF16 && !(key & 0x80000000u) ? as_f32(~key & 0xFFFF0000u) : value_of(key); };
   const float top = value(first), p = id >= 0 ? expf(value(kept) - top) : 0.0f;
@@ -133,14 +156,14 @@ __device__ __forceinline__ int route_token(const RouteCall& c, int64_t t, int la
   if (!c.renormalize) {
     sum = 0.0f;
 #pragma unroll
-    for (int i = 0; i < PER; ++i) sum += v[i] > -INFINITY ? expf(v[i] - top) : 0.0f;
+    for (int i = 0; i < PER; ++i) sum += v[i] > -INFINITY ? exp_in_sum(v[i] - top) : 0.0f;
   }
-  sum = wave_sum_f32(sum);
-  if (lane < c.k) {
-    c.ids[t * c.k + lane] = id;
-    c.weights[t * c.k + lane] = id >= 0 ? p / sum : 0.0f;
+  sum = lanes_sum<LANES>(sum);
+  if (there && sub < c.k) {
+    c.ids[t * c.k + sub] = id;
+    c.weights[t * c.k + sub] = id >= 0 ? p / sum : 0.0f;
   }
-  return id;
+  return there ? id : -1;
 }
 
 // exclusive sums of counts[0 .. n), n <= kRouteThreads, by the whole workgroup; returns this thread's and leaves the total
@@ -179,20 +202,22 @@ __device__ __forceinline__ void place_pass(const RouteCall& c, int64_t t0, int n
 }
 
 // Few tokens, one launch: a mask of tokens for every expert says all of it.
-template <int PER, bool BF16>
+template <int PER, bool BF16, int LANES>
 __global__ __launch_bounds__(kRouteThreads) void route_few_kernel(const RouteCall c) {
-  __shared__ uint64_t mask[64 * PER];
-  __shared__ int32_t base[64 * PER];
+  __shared__ uint64_t mask[LANES * PER];
+  __shared__ int32_t base[LANES * PER];
   __shared__ int wave_sums[kRouteWaves];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), e = threadIdx.x;
+  const int sub = threadIdx.x % LANES, group = threadIdx.x / LANES, e = threadIdx.x, tokens = (int)c.tokens;
+  constexpr int groups = kRouteThreads / LANES;
   float v[PER];
-  if (wave < c.tokens) load_logits<PER, BF16>(c, wave, lane, v);
+  if (tokens > 0) load_logits<PER, BF16, LANES>(c, min(group, tokens - 1), sub, v);      // without tokens there are no logits
   if (e < c.experts) mask[e] = 0;
   __syncthreads();
-  for (int64_t t = wave; t < c.tokens; t += kRouteWaves) {
-    const int id = route_token<PER, BF16>(c, t, lane, v);
-    if (lane < c.k && id >= 0) atomicOr((unsigned long long*)&mask[id], 1ull << t);
-    if (t + kRouteWaves < c.tokens) load_logits<PER, BF16>(c, t + kRouteWaves, lane, v);
+  for (int t0 = 0; t0 < tokens; t0 += groups) {
+    const int t = t0 + group;
+    const int id = route_token<PER, BF16, LANES>(c, t, t < tokens, sub, v);
+    if (sub < c.k && id >= 0) atomicOr((unsigned long long*)&mask[id], 1ull << t);
+    if (t0 + groups < tokens) load_logits<PER, BF16, LANES>(c, min(t + groups, tokens - 1), sub, v);
   }
   __syncthreads();
   int total;
@@ -201,26 +226,28 @@ __global__ __launch_bounds__(kRouteThreads) void route_few_kernel(const RouteCal
   if (e == 0) c.offsets[c.experts] = total;
   __threadfence_block();
   __syncthreads();
-  const int pairs = (int)c.tokens * c.k;
+  const int pairs = tokens * c.k;
   for (int i = total + threadIdx.x; i < pairs; i += kRouteThreads) c.rows[i] = -1;
   place_pass(c, 0, pairs, mask, base);
 }
 
 // Many tokens, first launch: experts and weights, and how many rows of each expert a workgroup's tokens make.
-template <int PER, bool BF16>
+template <int PER, bool BF16, int LANES>
 __global__ __launch_bounds__(kRouteThreads) void route_topk_kernel(const RouteCall c, int per_block, uint16_t* __restrict__ hist) {
-  __shared__ uint32_t count[64 * PER];
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  __shared__ uint32_t count[LANES * PER];
+  const int sub = threadIdx.x % LANES, group = threadIdx.x / LANES;
+  constexpr int groups = kRouteThreads / LANES;
   const int64_t first = (int64_t)blockIdx.x * per_block, end = min(first + per_block, c.tokens);
   float v[PER];
-  if (first + wave < end) load_logits<PER, BF16>(c, first + wave, lane, v);
+  load_logits<PER, BF16, LANES>(c, min(first + group, end - 1), sub, v);
   for (int e = threadIdx.x; e < c.experts; e += kRouteThreads) count[e] = 0;
   __syncthreads();
-  for (int64_t t = first + wave; t < end; t += kRouteWaves) {
+  for (int64_t t0 = first; t0 < end; t0 += groups) {
+    const int64_t t = t0 + group;
     float next[PER] = {};
-    if (t + kRouteWaves < end) load_logits<PER, BF16>(c, t + kRouteWaves, lane, next);
-    const int id = route_token<PER, BF16>(c, t, lane, v);
-    if (lane < c.k && id >= 0) atomicAdd(&count[id], 1u);
+    if (t0 + groups < end) load_logits<PER, BF16, LANES>(c, min(t + groups, end - 1), sub, next);
+    const int id = route_token<PER, BF16, LANES>(c, t, t < end, sub, v);
+    if (sub < c.k && id >= 0) atomicAdd(&count[id], 1u);
 #pragma unroll
     for (int i = 0; i < PER; ++i) v[i] = next[i];
   }
@@ -354,20 +381,20 @@ size_t moe_route_workspace_bytes(int64_t tokens, int experts) {
   return align_up((size_t)blocks * experts * 2, 256) + 256;
 }
 
-template <int PER>
+template <int PER, int LANES>
 static int route(const RouteCall& c, uint16_t* hist, hipStream_t st) {
   if (c.tokens <= kTile) {
     if (c.bf16)
-      route_few_kernel<PER, true><<<1, kRouteThreads, 0, st>>>(c);
+      route_few_kernel<PER, true, LANES><<<1, kRouteThreads, 0, st>>>(c);
     else
-      route_few_kernel<PER, false><<<1, kRouteThreads, 0, st>>>(c);
+      route_few_kernel<PER, false, LANES><<<1, kRouteThreads, 0, st>>>(c);
     return check_hip(hipGetLastError(), "route_few_kernel");
   }
   const int per = tokens_per_block(c.tokens), blocks = (int)((c.tokens + per - 1) / per);
   if (c.bf16)
-    route_topk_kernel<PER, true><<<blocks, kRouteThreads, 0, st>>>(c, per, hist);
+    route_topk_kernel<PER, true, LANES><<<blocks, kRouteThreads, 0, st>>>(c, per, hist);
   else
-    route_topk_kernel<PER, false><<<blocks, kRouteThreads, 0, st>>>(c, per, hist);
+    route_topk_kernel<PER, false, LANES><<<blocks, kRouteThreads, 0, st>>>(c, per, hist);
   const int rc = check_hip(hipGetLastError(), "route_topk_kernel");
   if (rc) return rc;
   route_place_kernel<<<blocks, kRouteThreads, 0, st>>>(c, per, hist);
@@ -376,12 +403,13 @@ static int route(const RouteCall& c, uint16_t* hist, hipStream_t st) {
 
 int run_moe_route(const RouteCall& c, void* ws, hipStream_t st) {
   uint16_t* hist = (uint16_t*)ws;
+  // Sixteen lanes a token where its experts fit their registers and its k experts the lanes: what a step of the selection costs is shared
+  // by four tokens (16381 tokens, 256 experts, k 8: the first launch 11.2 us, with a wave a token 15.8).
+  if (c.experts <= 256 && c.k <= 16) {
+    return c.experts <= 64 ? route<4, 16>(c, hist, st) : c.experts <= 128 ? route<8, 16>(c, hist, st) : route<16, 16>(c, hist, st);
+  }
   const int each = (c.experts + 63) / 64;                     // experts a lane
-  return each <= 1   ? route<1>(c, hist, st)
-         : each <= 2 ? route<2>(c, hist, st)
-         : each <= 4 ? route<4>(c, hist, st)
-         : each <= 8 ? route<8>(c, hist, st)
-                     : route<16>(c, hist, st);
+  return each <= 4 ? route<4, 64>(c, hist, st) : each <= 8 ? route<8, 64>(c, hist, st) : route<16, 64>(c, hist, st);
 }
 
 int run_moe_combine(const CombineCall& c, hipStream_t st) {

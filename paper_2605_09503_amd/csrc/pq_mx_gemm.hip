@@ -531,7 +531,7 @@ struct Split {
   static constexpr int scales = (bm + bn) * kMxRowBytes;
   static constexpr int stages = FM == 1 ? 4 : 3;                       // two workgroups of four waves a compute unit
   static constexpr int stage = (bm + bn) * kMxRowBytes + FM * 256, own = stages * stage, lds = KW * own;
-  static constexpr int loads = (bm + bn) / 16 + FM;
+  static constexpr int least = 2 + 1 + FM;                             // loads of a panel: W's, one of A's at least, scales
   static constexpr int pitch = 36;                                     // floats a row of sums: rows start four banks apart
   static_assert(bm * pitch * 4 <= own, "the sums take a wave's own part");
 };
@@ -575,8 +575,10 @@ __global__ __launch_bounds__(KW * 64) void mx_gemm_split_kernel(const MxCall c) 
     const uint32_t to = lds0 + stage * S::stage;
 #pragma unroll
     for (int i = 0; i < 2; ++i) load16_to_lds(to + S::bm * kMxRowBytes + i * 1024, w + p * w_next * kMxRowBytes, w_at[i]);
+    // rows that the tile has not are left out: what LDS holds instead makes sums that are not stored
 #pragma unroll
-    for (int i = 0; i < 2 * FM; ++i) load16_to_lds(to + i * 1024, a + p * a_next * kMxRowBytes, a_at[i]);
+    for (int i = 0; i < 2 * FM; ++i)
+      if (16 * i + (lane >> 2) <= a_last) load16_to_lds(to + i * 1024, a + p * a_next * kMxRowBytes, a_at[i]);
 #pragma unroll
     for (int i = 0; i < FM; ++i) load4_to_lds(to + S::scales + i * 256, s_base + p * s_next + s_at[i]);
   };
@@ -609,8 +611,9 @@ __global__ __launch_bounds__(KW * 64) void mx_gemm_split_kernel(const MxCall c) 
     if (wave + i * KW < panels) load(wave + i * KW, i);
   int stage = 0;
   for (int p = wave; p < panels; p += KW) {
+    // behind the panel that is waited for come the loads of stages - 1 others, each of `least` at least, or fewer at the end
     if (p + (S::stages - 1) * KW < panels)
-      arrived<(S::stages - 1) * S::loads>();
+      arrived<(S::stages - 1) * S::least>();
     else
       arrived<0>();
     multiply(stage);
@@ -714,7 +717,7 @@ __global__ __launch_bounds__(256) void mx_gemm_alone_kernel(const MxCall c) {
 #pragma unroll
     for (int i = 0; i < FM; ++i) s_off[i] = (of_w ? (uint32_t)min(lane, w_last) : a_row(32 * i + lane - 32)) * kMxRowScales;
   };
-  // A's rows come sixteen a load; sixteens that the tile has not are left out (what LDS holds instead makes sums that are not stored)
+  // rows that the tile has not are left out: what LDS holds instead makes sums that are not stored
   const auto load = [&](int stage) {
     if (load_tile >= tiles.end) return;
     const uint32_t to = lds0 + stage * S::stage;
@@ -722,7 +725,7 @@ __global__ __launch_bounds__(256) void mx_gemm_alone_kernel(const MxCall c) {
     for (int i = 0; i < 2; ++i) load16_to_lds(to + S::bm * kMxRowBytes + i * 1024, w_from, w_off[i]);
 #pragma unroll
     for (int i = 0; i < 2 * FM; ++i)
-      if (i == 0 || 16 * i <= a_last) load16_to_lds(to + i * 1024, a_from, a_off[i]);
+      if (16 * i + (lane >> 2) <= a_last) load16_to_lds(to + i * 1024, a_from, a_off[i]);
 #pragma unroll
     for (int i = 0; i < FM; ++i) load4_to_lds(to + S::scales + i * 256, s_from + s_off[i]);
     a_from += a_step;
@@ -849,6 +852,11 @@ int launch_alone(const MxCall& c, hipStream_t st) {
 // 7 % of the best for 120, within 29 % for all.  us, split 32 and 64 rows, shared 128, 256:
 //   M 32, N 4096, K 2048    4.5   4.2   8.1  11.6        M 256, N 4096, K 8192   14.8  11.7  24.8  45.0
 //   M 512, N 12288, K 512  22.3  16.1   7.9  11.3        M 1024, N 12288, K 8192  138   104    62    55
+// enough tiles of 32 columns for every wave of the chip: no need to share K
+bool enough_alone(const MxCall& c) {
+  const int64_t whole = (c.M + 31) / 32, rows = whole > c.experts ? whole : c.experts < c.M ? c.experts : c.M;
+  return rows * ((c.N + 31) / 32) >= 2048;
+}
 enum class Kernel { split32, split64, shared128, shared256 };
 Kernel choose(const MxCall& c, bool grouped) {
   const double panels = (double)mx_panels(c.K), groups = grouped ? (double)(c.experts < c.M ? c.experts : c.M) : 1.0;
@@ -858,8 +866,10 @@ Kernel choose(const MxCall& c, bool grouped) {
     return rows * (double)((c.N + bn - 1) / bn);
   };
   const double weights = groups * (double)c.N * panels * (kMxRowBytes + kMxRowScales) / 5.2e6;        // at 5.2 TB/s
+  const bool alone = grouped && enough_alone(c);
   const auto split = [&](int fm) {
     const double n = tiles(32 * fm, 32), traffic = n * panels * (fm == 1 ? 4.35e-3 : 6.65e-3) / 24.0;   // MB at 24 TB/s
+    if (alone) return 2.8 + (traffic > weights ? traffic : weights);
     const double wait = panels / 4 * (fm == 1 ? 0.165 : 0.245);
     return 2.8 + 0.8 * n / 512 + 0.25 * (traffic + wait) + (traffic > wait ? traffic > weights ? traffic : weights : wait > weights ? wait : weights);
   };
@@ -880,9 +890,7 @@ template <bool GROUPED>
 int run(const MxCall& c, hipStream_t st) {
   const Kernel k = choose(c, GROUPED);
   if constexpr (GROUPED) {
-    // enough tiles of 32 columns for every wave of the chip: no need to share K
-    const int64_t rows = (c.M + 31) / 32 > c.experts ? (c.M + 31) / 32 : c.experts < c.M ? c.experts : c.M;
-    if (k <= Kernel::split64 && rows * ((c.N + 31) / 32) >= 2048) return k == Kernel::split32 ? launch_alone<1>(c, st) : launch_alone<2>(c, st);
+    if (k <= Kernel::split64 && enough_alone(c)) return k == Kernel::split32 ? launch_alone<1>(c, st) : launch_alone<2>(c, st);
   }
   switch (k) {
     case Kernel::split32: return launch_split<1, 4, GROUPED>(c, st);

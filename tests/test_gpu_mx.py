@@ -371,7 +371,7 @@ def check_route(r, want, exact_weights=False):
     assert np.abs(r.weights.cpu().double().numpy() - want.weights).max(initial=0.0) <= 1e-5
 
 
-@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 64, 6), (5, 3, 3), (7, 65, 8), (64, 16, 2), (65, 128, 4), (200, 300, 10), (130, 1024, 32), (1000, 256, 8)])
+@pytest.mark.parametrize("T,E,k", [(1, 1, 1), (1, 64, 6), (5, 3, 3), (7, 65, 8), (64, 16, 2), (65, 128, 4), (200, 300, 10), (130, 1024, 32), (90, 100, 20), (64, 256, 16), (1000, 256, 8)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("renormalize", [True, False])
 def test_route(T, E, k, dtype, renormalize):
