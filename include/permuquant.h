@@ -631,7 +631,8 @@ int pq_dequantize(pq_format fmt, int group, const uint8_t* codes, const void* sc
  *
  * a_operand: a_rows rows, as pq_quantize_act_packed leaves them (tokens once, however many experts they go to).
  * w_operands: one operand an expert, as pq_pack_operand makes it of N rows, pq_operand_bytes(fmt, group, N, K) bytes apart.
- * offsets: int32 [experts + 1] device, non-decreasing; values outside 0 .. M are cut to it.  Experts without rows cost nothing.
+ * offsets: int32 [experts + 1] device, non-decreasing; values outside 0 .. M are cut to it (others may leave rows as they were, but touch
+ * nothing else).  Experts without rows cost nothing.
  * rows: int32 [M] device or NULL (then a_rows >= M).  A row whose index is outside 0 .. a_rows - 1 is left as it was.
  * M: rows of y, an upper bound of offsets[experts] (host); what lies outside offsets[0] .. offsets[experts] - 1 is left as it was.
  * bias: bf16 [experts, N] or NULL.  y: bf16 [M, ldy], ldy >= N, a multiple of 8 and at most 2^24.  M and a_rows may be 0; experts at most
@@ -653,7 +654,8 @@ int pq_qgemm_grouped(pq_format fmt, int group, const void* a_operand, int64_t a_
  *
  * logits: float or bf16 [tokens, ld], ld >= experts.  ids, positions: int32 [tokens, k]; weights: float [tokens, k]; offsets: int32
  * [experts + 1]; rows: int32 [tokens * k].  tokens 0 .. 2^24, experts 1 .. 1024, k 1 .. min(32, experts).  Softmax in binary32.
- * workspace: pq_moe_route_workspace_bytes(...) bytes, need not be initialised; calls that may overlap need workspaces of their own.
+ * workspace: pq_moe_route_workspace_bytes(...) bytes, need not be initialised; one for more tokens serves fewer; calls that may overlap need
+ * workspaces of their own.
  * May be captured into a graph; the same bits from run to run.
  */
 typedef enum { PQ_LOGITS_F32 = 0, PQ_LOGITS_BF16 = 1 } pq_logits;

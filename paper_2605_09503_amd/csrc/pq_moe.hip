@@ -405,8 +405,9 @@ int tokens_per_block(int64_t tokens) { return (int)((tokens + (int64_t)kTile * k
 }  // namespace
 
 size_t moe_route_workspace_bytes(int64_t tokens, int experts) {
-  const int64_t per = tokens ? tokens_per_block(tokens) : 1, blocks = (tokens + per - 1) / per;
-  return align_up((size_t)blocks * counts_of(experts) * 2, 256) + 256;
+  // no less for more tokens: a workspace serves every smaller call
+  const int64_t blocks = (tokens + kTile - 1) / kTile;
+  return align_up((size_t)(blocks < kMaxBlocks ? blocks : kMaxBlocks) * counts_of(experts) * 2, 256) + 256;
 }
 
 template <int PER, int LANES>

@@ -62,8 +62,10 @@ struct Tiles {
           lds[kTable + e + lane] = from;
           if (e + lane == c.experts - 1) lds[kTable + e + lane + 1] = to;
         }
-        total = __builtin_amdgcn_readlane(upto, 63);
+        total = min(__builtin_amdgcn_readlane(upto, 63), 1 << 26);
       }
+      // offsets that do not decrease make no more tiles than this; with others there may be more than can be counted: none is computed
+      if (total > (int)((c.M + bm - 1) / bm + min((int64_t)c.experts, c.M))) total = 0;
       if (table) __syncthreads();
     } else {
       total = (int)((c.M + bm - 1) / bm);

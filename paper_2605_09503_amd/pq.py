@@ -832,6 +832,10 @@ def pack_experts(codes: torch.Tensor, scales: torch.Tensor, experts: int) -> tor
     uint8 [experts, pq_operand_bytes(FMT_MXFP4, 32, N, K)]."""
     if codes.dim() != 2 or scales.dim() != 2 or experts <= 0 or codes.shape[0] % experts or scales.shape[0] != codes.shape[0]:
         _refuse("codes and scales must have the same rows, a multiple of %d" % experts)
+    if codes.dtype != torch.uint8 or scales.dtype != torch.uint8 or scales.shape[1] * 16 != codes.shape[1]:
+        _refuse("codes must be uint8 [rows, K/2] and scales uint8 [rows, K/32]")
+    _on_current_device("codes", codes)
+    _on_current_device("scales", scales, codes)
     N, K = codes.shape[0] // experts, codes.shape[1] * 2
     need = pq_operand_bytes(FMT_MXFP4, 32, N, K)
     if need == 0:

@@ -349,6 +349,17 @@ def test_grouped_leaves_other_rows():
     assert grouped(c, a_rows, N, K).numel() == 0
 
 
+@pytest.mark.parametrize("E,M,N,K", [(4, 48, 48, 288), (70, 700, 264, 640), (70, 20, 40, 96), (1100, 5000, 264, 288)])
+def test_grouped_of_offsets_that_go_up_and_down(E, M, N, K):
+    # rows in them may be computed or not, others are not touched
+    x, _, _, _ = big(M, K, 1)
+    _, codes, scales, _ = big(E * N, K, 2)
+    offsets = torch.tensor(([0, M - 1] * E)[:E + 1], dtype=torch.int32, device=DEV)
+    y = torch.full((M + 1, (N + 7) // 8 * 8 + 8), 5.0, dtype=torch.bfloat16, device=DEV)
+    pq.pq_qgemm_grouped(MX, 32, operand(x), M, pq.pack_experts(codes, scales, E), offsets, y[:M, :N], N, K)
+    assert bool((y[M - 1:] == 5).all()) and bool((y[:, N:] == 5).all())
+
+
 def test_grouped_of_one_expert_is_the_product():
     rng = np.random.default_rng(4)
     for M, N, K in ((3, 100, 512), (90, 300, 800), (520, 520, 256)):

@@ -94,6 +94,8 @@ def test_grouped(lib):  # noqa: F811
 
 def test_route(lib):  # noqa: F811
     assert pq.pq_moe_route_workspace_bytes(0, 4, 2) > 0
+    need = [pq.pq_moe_route_workspace_bytes(t, 257, 8) for t in (0, 1, 64, 65, 4000, 32768, 32769, 70000, 1 << 24)]
+    assert need == sorted(need) and need[-1] >= 512 * 257 * 2           # one for more tokens serves fewer
     for bad in [(-1, 4, 2), (4, 0, 1), (4, 1025, 2), (4, 4, 0), (4, 4, 5), (4, 64, 33), ((1 << 24) + 1, 4, 2)]:
         assert pq.pq_moe_route_workspace_bytes(*bad) == 0
         with pytest.raises(pq.PQError):
@@ -142,7 +144,9 @@ def test_python_arguments(lib, python, native):  # noqa: F811
                  lambda: m.pq_moe_route(z(8, 4, dtype=torch.float32).T, 2),
                  lambda: m.pq_moe_combine(y.float(), z(2, 2, dtype=torch.int32), z(2, 2, dtype=torch.float32)),
                  lambda: m.pq_moe_combine(y, z(2, dtype=torch.int32), z(2, 2, dtype=torch.float32)),
-                 lambda: m.pack_experts(z(9, 32), z(9, 2), 4)):
+                 lambda: m.pack_experts(z(9, 32), z(9, 2), 4),
+                 lambda: m.pack_experts(z(8, 32), z(8, 4), 4),
+                 lambda: m.pack_experts(z(8, 32), z(8, 2), 4)):
         refused(call)
 
 
