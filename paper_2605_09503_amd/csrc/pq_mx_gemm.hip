@@ -40,7 +40,9 @@ __device__ __forceinline__ int tiles_of(const MxCall& c, int bm, int e, int& fro
   return to > from ? (to - from + bm - 1) / bm : 0;
 }
 // The tiles a workgroup computes.  Workgroups go round the eight chiplets in turn; each chiplet takes a contiguous eighth of the
-// tiles, in blocks of eight tiles of rows, and its workgroups go through it side by side: what they read at a time meets in its L2.
+// tiles, in blocks of four tiles of rows, and its workgroups go through it side by side: what they read at a time meets in its L2
+// (blocks of eight: 8192 x 12288 x 8192 takes 433 us, not 428, 16384 x 8192 x 1024 115, not 101, 65528 gathered rows by 64 experts,
+// 2816 x 2048, 334, not 316; two to six are alike, sixteen and more slower still).
 template <bool GROUPED>
 struct Tiles {
   // A table in LDS for up to kTable experts: tiles of the experts up to each one, and their offsets cut to 0 .. M.  What a search
@@ -80,8 +82,8 @@ struct Tiles {
   // tile number `flat` (uniform)
   __device__ __forceinline__ Tile at(const MxCall& c, int bm, int bn, int flat) const {
     Tile t;
-    const int block = 8 * across, b = flat / block, in = flat - b * block, high = min(8, total - b * 8);
-    const int mt = b * 8 + in % high;
+    const int block = 4 * across, b = flat / block, in = flat - b * block, high = min(4, total - b * 4);
+    const int mt = b * 4 + in % high;
     t.n0 = (int64_t)(in / high) * bn;
     t.first = (int64_t)mt * bm;
     t.end = min(t.first + bm, c.M);
