@@ -517,14 +517,25 @@ PQ_CALL(dequantize) {
   return guarded([&] {
     PQ_TAKE(pq_dequantize, 4, "fmt", "group", "codes", "scales", "tensor_scale", "y");
     const int fmt = (int)as_int(a[0]), group = (int)as_int(a[1]);
-    const at::Tensor& codes = as_tensor(a[2], "codes");
-    if (codes.dim() < 2) fail(PyExc_IndexError, "tuple index out of range");
+    const at::Tensor &codes = as_tensor(a[2], "codes"), &scales = as_tensor(a[3], "scales");
+    if (codes.dim() != 2 || codes.scalar_type() != at::kByte || !codes.is_contiguous()) refuse("codes must be contiguous uint8 [rows, K/2]");
     const int64_t rows = codes.size(0), K = codes.size(1) * 2;
-    void *scales = pointer(a[3]), *ts = pointer(a[4]);
+    on_current_device("codes", codes, nullptr);
+    const auto type = fmt == PQ_FMT_NVFP4 || fmt == PQ_FMT_MXFP4 ? at::kByte : at::kFloat;
+    if (scales.scalar_type() != type || !scales.is_contiguous() || scales.numel() * group != rows * K)
+      refuse("scales must be contiguous, one for every %d channels", group);
+    on_current_device("scales", scales, &codes);
+    const void* ts = nullptr;
+    if (given(a[4])) {
+      const at::Tensor& t = as_tensor(a[4], "tensor_scale");
+      if (t.scalar_type() != at::kFloat || t.numel() < 1) refuse("tensor_scale must be float32");
+      on_current_device("tensor_scale", t, &codes);
+      ts = t.data_ptr();
+    }
     const at::Tensor y = given(a[5]) ? as_tensor(a[5], "y") : bf16_rows(rows, K, codes.device());
-    void *c = codes.data_ptr(), *yp = y.data_ptr(), *st = stream();
-    const int64_t ldy = y.stride(0);
-    call([&] { return pq_dequantize((pq_format)fmt, group, (const uint8_t*)c, scales, (const float*)ts, rows, K, yp, ldy, st); });
+    const Rows2 yr = rows2("y", y, rows, K, &codes);
+    void *c = codes.data_ptr(), *sp = scales.data_ptr(), *st = stream();
+    call([&] { return pq_dequantize((pq_format)fmt, group, (const uint8_t*)c, sp, (const float*)ts, rows, K, yr.p, yr.ld, st); });
     return THPVariable_Wrap(y);
   });
 }

@@ -337,7 +337,8 @@ __global__ __launch_bounds__(kRouteThreads) void route_place_kernel(const RouteC
 
 // ---------------------------------------------------------------- the weighted sum
 // out[t] = addend[t] + sum_j weights[t, j] * y[positions[t, j]], j ascending, in binary32, rounded once to bf16.  Eight columns a
-// thread, a token a workgroup: its rows and weights are uniform, and the loads of kAhead rows are under way at a time.  Memory bound.
+// thread, a token a workgroup: its rows and weights are uniform, and the loads of kAhead rows are under way at a time.  Memory bound:
+// 8191 tokens, k 8, 5120 columns, an addend: 839 MB in 157 to 160 us, 5.3 TB/s (a large copy: 5.1); with a row after the other 179.
 constexpr int kAhead = 8, kCombineThreads = 128;
 __global__ __launch_bounds__(kCombineThreads) void combine_kernel(const CombineCall c, int chunks) {
   const int64_t t = blockIdx.x / (uint32_t)chunks;

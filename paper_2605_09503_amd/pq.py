@@ -820,10 +820,21 @@ def pq_attn_decode(cache: KVCache, q: torch.Tensor, table: torch.Tensor, lengths
 def pq_dequantize(fmt: int, group: int, codes: torch.Tensor, scales: torch.Tensor, tensor_scale: Optional[torch.Tensor] = None,
                   y: Optional[torch.Tensor] = None) -> torch.Tensor:
     """The values that stored codes [rows, K/2] and scales stand for, bf16 [rows, K] (allocated unless given)."""
+    if codes.dim() != 2 or codes.dtype != torch.uint8 or not codes.is_contiguous():
+        _refuse("codes must be contiguous uint8 [rows, K/2]")
     rows, K = codes.shape[0], codes.shape[1] * 2
+    _on_current_device("codes", codes)
+    if scales.dtype != scale_dtype(fmt) or not scales.is_contiguous() or scales.numel() * group != rows * K:
+        _refuse("scales must be contiguous, one for every %d channels" % group)
+    _on_current_device("scales", scales, codes)
+    if tensor_scale is not None:
+        if tensor_scale.dtype != torch.float32 or tensor_scale.numel() < 1:
+            _refuse("tensor_scale must be float32")
+        _on_current_device("tensor_scale", tensor_scale, codes)
     if y is None:
         y = torch.empty((rows, K), dtype=torch.bfloat16, device=codes.device)
-    _check(load().pq_dequantize(fmt, group, _ptr(codes), _ptr(scales), _ptr(tensor_scale), rows, K, _ptr(y), y.stride(0), _stream()))
+    yp, ldy = _rows2("y", y, rows, K, codes)
+    _check(load().pq_dequantize(fmt, group, _ptr(codes), _ptr(scales), _ptr(tensor_scale), rows, K, yp, ldy, _stream()))
     return y
 
 

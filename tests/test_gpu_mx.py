@@ -142,6 +142,21 @@ def test_dequantize_other_formats(fmt, group):
     assert np.array_equal(np.where(got == 0x8000, 0, got), np.where(want == 0x8000, 0, want))
 
 
+def test_dequantize_refuses_tensors_that_do_not_fit():
+    codes, scales = pq.alloc_quantized(MX, 32, 4, 64)
+    out = lambda *shape, **kw: torch.empty(shape, device=DEV, **{"dtype": torch.bfloat16, **kw})
+    for args, kw in [((codes, scales[:3]), {}), ((codes, scales.float()), {}), ((codes, scales.cpu()), {}), ((codes, scales), dict(y=out(3, 64))),
+                     ((codes, scales), dict(y=out(4, 64, dtype=torch.float32))), ((codes, scales), dict(y=out(64, 4).T)),
+                     ((codes, scales), dict(y=out(1, 64).expand(4, 64))), ((codes, scales), dict(y=out(4, 60)))]:
+        with pytest.raises(pq.PQError):
+            pq.pq_dequantize(MX, 32, *args, **kw)
+    with pytest.raises(pq.PQError):
+        pq.pq_dequantize(pq.FMT_NVFP4, 16, codes, torch.zeros(4, 4, dtype=torch.uint8, device=DEV), torch.ones(1, dtype=torch.float64, device=DEV))
+    y = out(1, 64)
+    pq.pq_dequantize(MX, 32, codes[:1].zero_(), scales[:1].zero_(), y=y)
+    assert not y.any()
+
+
 # ------------------------------------------------------------------------ products
 
 SHAPES = [(1, 1, 32), (1, 8, 96), (1, 300, 4096), (2, 517, 1056), (16, 64, 256), (17, 40, 288), (31, 136, 512), (33, 1000, 544), (64, 257, 2016), (65, 128, 1024),

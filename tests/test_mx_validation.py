@@ -133,6 +133,7 @@ def test_python_arguments(lib, python, native):  # noqa: F811
 
     for call in (lambda: m.pq_qgemm_grouped(MX, 32, z(need), 4, z(2, need), off, y, 8, 64),
                  lambda: m.pq_moe_route(z(4, 8, dtype=torch.float32), 2),
+                 lambda: m.pq_dequantize(MX, 32, z(4, 32), z(4, 2)),
                  lambda: m.pq_moe_combine(y, z(2, 2, dtype=torch.int32), z(2, 2, dtype=torch.float32))):
         refused(call, "GPU")
     for call in (lambda: m.pq_qgemm_grouped(MX, 32, z(need), 4, z(2, need + 256), off, y, 8, 64),
@@ -144,6 +145,9 @@ def test_python_arguments(lib, python, native):  # noqa: F811
                  lambda: m.pq_moe_route(z(8, 4, dtype=torch.float32).T, 2),
                  lambda: m.pq_moe_combine(y.float(), z(2, 2, dtype=torch.int32), z(2, 2, dtype=torch.float32)),
                  lambda: m.pq_moe_combine(y, z(2, dtype=torch.int32), z(2, 2, dtype=torch.float32)),
+                 lambda: m.pq_dequantize(MX, 32, z(4, 32, dtype=torch.int8), z(4, 2)),
+                 lambda: m.pq_dequantize(MX, 32, z(4 * 32), z(4, 2)),
+                 lambda: m.pq_dequantize(MX, 32, z(4, 64)[:, :32], z(4, 2)),
                  lambda: m.pack_experts(z(9, 32), z(9, 2), 4),
                  lambda: m.pack_experts(z(8, 32), z(8, 4), 4),
                  lambda: m.pack_experts(z(8, 32), z(8, 2), 4)):
