@@ -340,7 +340,8 @@ int pq_qgemm_f32(pq_format fmt, int group, const uint8_t* a_codes, const void* a
                  int64_t ldy, void* workspace, size_t workspace_bytes, void* stream);
 
 /* The output tile (rows x columns of Y a workgroup computes) that a product of this shape takes: 256 x 256, 224 x 256,
- * 128 x 128, or one of 64 x 96, 64 x 64, 64 x 32 and 32 x 32 whose waves split K (MXFP4: 256 x 256, 128 x 128, 64 x 32 or 32 x 32).  Host only.  K is added in fp32 in
+ * 128 x 128, or one of 64 x 96, 64 x 64, 64 x 32 and 32 x 32 whose waves split K (MXFP4: 256 x 256,
+ * 128 x 128, 64 x 64, 32 x 64 or 32 x 32).  Host only.  K is added in fp32 in
  * an order that is fixed for a tile and differs between them, so a row of Y is the same bits from run to run but may
  * differ by the rounding of that sum between calls with other M or N.                                          */
 int pq_qgemm_tile(pq_format fmt, int group, int64_t M, int64_t N, int64_t K, int* tile_m, int* tile_n);

@@ -533,26 +533,28 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void mx_gemm_shared_kernel(const Mx
 }
 
 // ---------------------------------------------------------------- small tiles whose waves share K
-// Each of KW waves multiplies the whole tile of 32 FM x 32 over every KW-th panel, its panels in a part of LDS of its own (no
+// Each of KW waves multiplies the whole tile of 32 FM x 32 FN over every KW-th panel, its panels in a part of LDS of its own (no
 // barrier while it runs), then the waves' sums are added up in their order.
 // Few rows: bound by the weights' bytes, 1 x 6144 x 4096 4.6 us (13 MB: 2.9 TB/s with the start and the end of the launch, 2.7 us at the
 // rate of a large copy), and from some 32 rows on by what the units take from the caches, since every tile of rows reads the weights and
-// every tile of columns the rows: 56 x 12288 x 4096 9.3 us as tiles of 64 x 32.  Four waves and four stages (three for 64 rows), two
-// workgroups a unit, have 64 KB (48) of weights a unit under way; eight waves, and tiles of 128 x 32, were no faster.
-template <int FM, int KW>
+// every tile of columns the rows.  32 x 32 where there are few of them, 32 x 64 and 64 x 64 for more, us at N 12288:
+//   K 8192, M 16   12.6  11.1  11.7     M 56  17.8  17.5  14.5     K 512, M 56   4.9  3.9  4.3     M 128  7.3  5.7  7.2
+// (64 x 32 tiles take 13.1, 17.5, 4.0, 6.0: never less than both of the others by 4 %.)  Four waves and four stages (three for 32 x 64), two
+// workgroups a unit, one of 64 x 64, have 48 to 64 KB of weights a unit under way; eight waves, and tiles of 128 x 32, were no faster.
+template <int FM, int FN, int KW>
 struct Split {
-  static constexpr int bm = 32 * FM, bn = 32;
-  static constexpr int scales = (bm + bn) * kMxRowBytes;
-  static constexpr int stages = FM == 1 ? 4 : 3;                       // two workgroups of four waves a compute unit
-  static constexpr int stage = (bm + bn) * kMxRowBytes + FM * 256, own = stages * stage, lds = KW * own;
-  static constexpr int least = 2 + 1 + FM;                             // loads of a panel: W's, one of A's at least, scales
-  static constexpr int pitch = 36;                                     // floats a row of sums: rows start four banks apart
+  static constexpr int bm = 32 * FM, bn = 32 * FN;
+  static constexpr int scales = (bm + bn) * kMxRowBytes, s_loads = FN == 1 ? FM : 2;
+  static constexpr int stages = FM * FN == 2 ? 3 : 4;                  // two workgroups of four waves a compute unit, or one of the largest tiles
+  static constexpr int stage = (bm + bn) * kMxRowBytes + s_loads * 256, own = stages * stage, lds = KW * own;
+  static constexpr int least = 2 * FN + 1 + s_loads;                   // loads of a panel: W's, one of A's at least, scales
+  static constexpr int pitch = bn + 4;                                     // floats a row of sums: rows start four banks apart
   static_assert(bm * pitch * 4 <= own, "the sums take a wave's own part");
 };
 
-template <int FM, int KW, bool GROUPED>
+template <int FM, int FN, int KW, bool GROUPED>
 __global__ __launch_bounds__(KW * 64) void mx_gemm_split_kernel(const MxCall c) {
-  using S = Split<FM, KW>;
+  using S = Split<FM, FN, KW>;
   extern __shared__ __attribute__((aligned(16))) unsigned char lds[];
   const Tiles<GROUPED> tiles(c, S::bm, S::bn, nullptr);
   if (tiles.next >= tiles.end) return;
@@ -567,58 +569,72 @@ __global__ __launch_bounds__(KW * 64) void mx_gemm_split_kernel(const MxCall c) 
   const uint8_t *as = c.a + mx_scales_at(c.a_rows, c.K), *ws = c.w + (size_t)t.expert * c.w_next + mx_scales_at(c.N, c.K) + t.n0 * kMxRowScales;
   const size_t a_next = (size_t)c.a_rows, w_next = (size_t)c.N;
   const auto a_row = [&](int row) { return (uint32_t)max(a_row_of(c, t.first + min(row, a_last)), 0); };
-  uint32_t a_at[2 * FM], w_at[2], s_at[FM];
+  uint32_t a_at[2 * FM], w_at[2 * FN], s_at[S::s_loads];
 #pragma unroll
   for (int i = 0; i < 2 * FM; ++i) {
     const int row = 16 * i + (lane >> 2);
     a_at[i] = a_row(row) * kMxRowBytes + block_at(row, lane & 3);
   }
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
+  for (int i = 0; i < 2 * FN; ++i) {
     const int row = 16 * i + (lane >> 2);
     w_at[i] = (uint32_t)min(row, w_last) * kMxRowBytes + block_at(row, lane & 3);
   }
-  // scales: W's 32 rows and A's first 32 in one load, A's other 32 (and W's again) in the next
+  // scales: W's 32 rows and A's first 32 in one load, A's other 32 (and W's again) in the next; of 64 rows of W in a load of their own
   const bool of_w = lane < 32;
 #pragma unroll
-  for (int i = 0; i < FM; ++i) s_at[i] = (of_w ? (uint32_t)min(lane, w_last) : a_row(32 * i + lane - 32)) * kMxRowScales;
-  const uint8_t* s_base = of_w ? ws : as;
-  const size_t s_next = (of_w ? w_next : a_next) * kMxRowScales;
+  for (int i = 0; i < S::s_loads; ++i) {
+    if constexpr (FN == 1)
+      s_at[i] = (of_w ? (uint32_t)min(lane, w_last) : a_row(32 * i + lane - 32)) * kMxRowScales;
+    else
+      s_at[i] = (i == 0 ? (uint32_t)min(lane, w_last) : a_row(min(lane, S::bm - 1))) * kMxRowScales;
+  }
+  const auto s_base = [&](int i, int p) {
+    const bool w_rows = FN == 1 ? of_w : i == 0;
+    return (w_rows ? ws : as) + p * ((w_rows ? w_next : a_next) * kMxRowScales);
+  };
+  constexpr int sw_at = S::scales, sa_at = S::scales + (FN == 1 ? 128 : 256), sa_step = FN == 1 ? 256 : 128;
   const int panels = (int)mx_panels(c.K);
   const auto load = [&](int p, int stage) {
     const uint32_t to = lds0 + stage * S::stage;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) load16_to_lds(to + S::bm * kMxRowBytes + i * 1024, w + p * w_next * kMxRowBytes, w_at[i]);
+    for (int i = 0; i < 2 * FN; ++i) load16_to_lds(to + S::bm * kMxRowBytes + i * 1024, w + p * w_next * kMxRowBytes, w_at[i]);
     // rows that the tile has not are left out: what LDS holds instead makes sums that are not stored
 #pragma unroll
     for (int i = 0; i < 2 * FM; ++i)
       if (16 * i + (lane >> 2) <= a_last) load16_to_lds(to + i * 1024, a + p * a_next * kMxRowBytes, a_at[i]);
 #pragma unroll
-    for (int i = 0; i < FM; ++i) load4_to_lds(to + S::scales + i * 256, s_base + p * s_next + s_at[i]);
+    for (int i = 0; i < S::s_loads; ++i) load4_to_lds(to + S::scales + i * 256, s_base(i, p) + s_at[i]);
   };
 
   const int row = lane & 31, half = lane >> 5;
-  float16v acc[FM];
+  float16v acc[FN][FM];
 #pragma unroll
-  for (int j = 0; j < FM; ++j) acc[j] = float16v{};
+  for (int i = 0; i < FN; ++i)
+#pragma unroll
+    for (int j = 0; j < FM; ++j) acc[i][j] = float16v{};
   const auto multiply = [&](int stage) {
     const unsigned char* at = own + stage * S::stage;
-    int4v wf[2], af[2][FM];
-    const int sw = (int)(*reinterpret_cast<const uint32_t*>(at + S::scales + row * 4) >> (8 * half));
-    int sa[FM];
+    int4v wf[2][FN], af[2][FM];
+    int sw[FN], sa[FM];
 #pragma unroll
-    for (int j = 0; j < FM; ++j) sa[j] = (int)(*reinterpret_cast<const uint32_t*>(at + S::scales + j * 256 + 128 + row * 4) >> (8 * half));
+    for (int i = 0; i < FN; ++i) sw[i] = (int)(*reinterpret_cast<const uint32_t*>(at + sw_at + i * 128 + row * 4) >> (8 * half));
+#pragma unroll
+    for (int j = 0; j < FM; ++j) sa[j] = (int)(*reinterpret_cast<const uint32_t*>(at + sa_at + j * sa_step + row * 4) >> (8 * half));
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
-      wf[s] = *reinterpret_cast<const int4v*>(at + (S::bm + row) * kMxRowBytes + block_at(row, 2 * s + half));
+#pragma unroll
+      for (int i = 0; i < FN; ++i) wf[s][i] = *reinterpret_cast<const int4v*>(at + (S::bm + 32 * i + row) * kMxRowBytes + block_at(row, 2 * s + half));
 #pragma unroll
       for (int j = 0; j < FM; ++j) af[s][j] = *reinterpret_cast<const int4v*>(at + (32 * j + row) * kMxRowBytes + block_at(row, 2 * s + half));
     }
 #pragma unroll
-    for (int j = 0; j < FM; ++j) {
-      acc[j] = mfma<0>(wf[0], af[0][j], acc[j], sw, sa[j]);
-      acc[j] = mfma<2>(wf[1], af[1][j], acc[j], sw, sa[j]);
-    }
+    for (int i = 0; i < FN; ++i)
+#pragma unroll
+      for (int j = 0; j < FM; ++j) {
+        acc[i][j] = mfma<0>(wf[0][i], af[0][j], acc[i][j], sw[i], sa[j]);
+        acc[i][j] = mfma<2>(wf[1][i], af[1][j], acc[i][j], sw[i], sa[j]);
+      }
   };
 #pragma unroll
   for (int i = 0; i < S::stages; ++i)
@@ -641,14 +657,17 @@ __global__ __launch_bounds__(KW * 64) void mx_gemm_split_kernel(const MxCall c) 
   arrived<0>();
   float* part = reinterpret_cast<float*>(own);
 #pragma unroll
-  for (int j = 0; j < FM; ++j)
+  for (int i = 0; i < FN; ++i)
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      *reinterpret_cast<float4*>(part + (32 * j + row) * S::pitch + 8 * q + 4 * half) = make_float4(acc[j][4 * q], acc[j][4 * q + 1], acc[j][4 * q + 2], acc[j][4 * q + 3]);
+    for (int j = 0; j < FM; ++j)
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<float4*>(part + (32 * j + row) * S::pitch + 32 * i + 8 * q + 4 * half) =
+            make_float4(acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]);
   __syncthreads();
   const float* parts = reinterpret_cast<const float*>(lds);
-  for (int i = tid; i < S::bm * 4; i += KW * 64) {
-    const int r = i >> 2, col = (i & 3) * 8;
+  for (int i = tid; i < S::bm * 4 * FN; i += KW * 64) {
+    const int r = i / (4 * FN), col = i % (4 * FN) * 8;
     const int64_t m = t.first + r, n = t.n0 + col;
     if (m >= t.end || n >= c.N || a_row_of(c, m) < 0) continue;
     float v[8] = {};
@@ -849,10 +868,10 @@ int launch_shared(const MxCall& c, hipStream_t st) {
     return launch(mx_gemm_shared_kernel<BM, BN, WM, WN, GROUPED, true>, "mx_gemm_shared_kernel", c, BM, BN, S::waves, lds, most, allowed_few, st);
   return launch(mx_gemm_shared_kernel<BM, BN, WM, WN, GROUPED, false>, "mx_gemm_shared_kernel", c, BM, BN, S::waves, lds, most, allowed, st);
 }
-template <int FM, int KW, bool GROUPED>
+template <int FM, int FN, int KW, bool GROUPED>
 int launch_split(const MxCall& c, hipStream_t st) {
   static std::atomic<uint64_t> allowed{0};
-  return launch(mx_gemm_split_kernel<FM, KW, GROUPED>, "mx_gemm_split_kernel", c, 32 * FM, 32, KW, Split<FM, KW>::lds, 0, allowed, st);
+  return launch(mx_gemm_split_kernel<FM, FN, KW, GROUPED>, "mx_gemm_split_kernel", c, 32 * FM, 32 * FN, KW, Split<FM, FN, KW>::lds, 0, allowed, st);
 }
 
 template <int FM>
@@ -862,18 +881,20 @@ int launch_alone(const MxCall& c, hipStream_t st) {
   return launch(mx_gemm_alone_kernel<FM>, "mx_gemm_alone_kernel", c, S::bm, S::bn * S::waves, S::waves, S::lds, kUnits * (160 * 1024 / S::lds), allowed, st);
 }
 
-// Which kernel: the one that takes the shortest time by a model of each in us, fitted to all of them timed at M 1 .. 2048, N 1024, 4096
-// and 12288, K 512, 2048 and 8192.  Small tiles read more than they multiply and are bound by what the units take from the caches;
-// large ones take some us a turn and a time a panel, and only pay where there are enough of them.  Of 126 shapes the choice is within
-// 7 % of the best for 120, within 29 % for all.  us, split 32 and 64 rows, shared 128, 256:
-//   M 32, N 4096, K 2048    4.5   4.2   8.1  11.6        M 256, N 4096, K 8192   14.8  11.7  24.8  45.0
-//   M 512, N 12288, K 512  22.3  16.1   7.9  11.3        M 1024, N 12288, K 8192  138   104    62    55
+// Which kernel: the one that takes the shortest time by a model of each in us.  Small tiles read more than they multiply and are bound by what
+// the units take from the caches: a start, some us and a time a panel for every round of 256 tiles, and the weights' bytes.  Large ones
+// take some us a turn and a time a panel, and only pay where there are enough of them.  Fitted to all kernels timed at M 16 .. 768, N 1024 ..
+// 16384 and K 512 .. 8192 (200 shapes: the choice is within 7 % of the best for 191, within 13 % for all), the two largest tiles at M up to
+// 8192 as well.  us, 32 x 32, 32 x 64, 64 x 64, 128 x 128:
+//   M 32, N 4096, K 2048    3.9   4.4   5.1   8.1        M 256, N 4096, K 8192   15.4  12.4  10.3  25.1
+//   M 512, N 12288, K 512  23.5  15.6  19.0   7.9        M 256, N 12288, K 8192  48.5  38.2  35.5  25.8
+// and 128 x 128 and 256 x 256 at M 1024, N 12288, K 8192  62  55.
 // enough tiles of 32 columns for every wave of the chip: no need to share K
 bool enough_alone(const MxCall& c) {
   const int64_t whole = (c.M + 31) / 32, rows = whole > c.experts ? whole : c.experts < c.M ? c.experts : c.M;
   return rows * ((c.N + 31) / 32) >= 2048;
 }
-enum class Kernel { split32, split64, shared128, shared256 };
+enum class Kernel { split32x32, split32x64, split64x64, alone32, alone64, shared128, shared256 };
 Kernel choose(const MxCall& c, bool grouped) {
   const double panels = (double)mx_panels(c.K), groups = grouped ? (double)(c.experts < c.M ? c.experts : c.M) : 1.0;
   // tiles of rows: a group's last is half full on average
@@ -881,13 +902,16 @@ Kernel choose(const MxCall& c, bool grouped) {
     const double whole = (double)c.M / bm, rows = grouped ? (whole + 0.5 * groups > groups ? whole + 0.5 * groups : groups) : (double)((c.M + bm - 1) / bm);
     return rows * (double)((c.N + bn - 1) / bn);
   };
-  const double weights = groups * (double)c.N * panels * (kMxRowBytes + kMxRowScales) / 5.2e6;        // at 5.2 TB/s
-  const bool alone = grouped && enough_alone(c);
-  const auto split = [&](int fm) {
-    const double n = tiles(32 * fm, 32), traffic = n * panels * (fm == 1 ? 4.35e-3 : 6.65e-3) / 24.0;   // MB at 24 TB/s
-    if (alone) return 2.8 + (traffic > weights ? traffic : weights);
-    const double wait = panels / 4 * (fm == 1 ? 0.165 : 0.245);
-    return 2.8 + 0.8 * n / 512 + 0.25 * (traffic + wait) + (traffic > wait ? traffic > weights ? traffic : weights : wait > weights ? wait : weights);
+  const double mb = groups * (double)c.N * panels * (kMxRowBytes + kMxRowScales) / 1e6, weights = mb / 5.2;      // at 5.2 TB/s
+  const auto split = [&](int fm, int fn) {
+    const double rounds = (double)(int64_t)((tiles(32 * fm, 32 * fn) + kUnits - 1) / kUnits);
+    return fm == 2   ? 0.56 + rounds * (3.07 + 0.0913 * panels) + 0.063 * mb
+           : fn == 2 ? 2.26 + rounds * (0.73 + 0.0619 * panels) + 0.075 * mb
+                     : 2.20 + rounds * (0.59 + 0.0418 * panels) + 0.063 * mb;
+  };
+  const auto alone = [&](int fm) {
+    const double traffic = tiles(32 * fm, 32) * panels * (fm == 1 ? 4.35e-3 : 6.65e-3) / 24.0;           // MB at 24 TB/s
+    return 2.8 + (traffic > weights ? traffic : weights);
   };
   const auto shared = [&](int bm) {
     const double n = tiles(bm, bm), turns = (double)(int64_t)((n + kUnits - 1) / kUnits);
@@ -895,22 +919,34 @@ Kernel choose(const MxCall& c, bool grouped) {
     const double panel = bm == 128 ? (turns <= 1 ? 0.33 : 0.29 * turns) : turns * (0.62 + 0.35 * full), t = panels * panel;
     return (bm == 128 ? 2.8 + turns : 2.6 + turns * (1.5 + 3.0 * full)) + (t > weights ? t : weights);
   };
-  const double t[4] = {split(1), split(2), shared(128), shared(256)};
-  int best = 0;
-  for (int i = 1; i < 4; ++i)
-    if (t[i] < t[best]) best = i;
-  return (Kernel)best;
+  const bool many = grouped && enough_alone(c);
+  Kernel best = many ? Kernel::alone32 : Kernel::split32x32;
+  double least = many ? alone(1) : split(1, 1);
+  const auto consider = [&](Kernel k, double t) {
+    if (t < least) best = k, least = t;
+  };
+  if (many) {
+    consider(Kernel::alone64, alone(2));
+  } else {
+    consider(Kernel::split32x64, split(1, 2));
+    consider(Kernel::split64x64, split(2, 2));
+  }
+  consider(Kernel::shared128, shared(128));
+  consider(Kernel::shared256, shared(256));
+  return best;
 }
 
 template <bool GROUPED>
 int run(const MxCall& c, hipStream_t st) {
   const Kernel k = choose(c, GROUPED);
   if constexpr (GROUPED) {
-    if (k <= Kernel::split64 && enough_alone(c)) return k == Kernel::split32 ? launch_alone<1>(c, st) : launch_alone<2>(c, st);
+    if (k == Kernel::alone32) return launch_alone<1>(c, st);
+    if (k == Kernel::alone64) return launch_alone<2>(c, st);
   }
   switch (k) {
-    case Kernel::split32: return launch_split<1, 4, GROUPED>(c, st);
-    case Kernel::split64: return launch_split<2, 4, GROUPED>(c, st);
+    case Kernel::split32x32: return launch_split<1, 1, 4, GROUPED>(c, st);
+    case Kernel::split32x64: return launch_split<1, 2, 4, GROUPED>(c, st);
+    case Kernel::split64x64: return launch_split<2, 2, 4, GROUPED>(c, st);
     case Kernel::shared128: return launch_shared<128, 128, 2, 2, GROUPED>(c, st);
     default: return launch_shared<256, 256, 2, 4, GROUPED>(c, st);
   }
@@ -922,8 +958,9 @@ void mx_gemm_tile(int64_t M, int64_t N, int64_t K, int* bm, int* bn) {
   MxCall c{};
   c.M = M, c.N = N, c.K = K, c.experts = 1;
   switch (choose(c, false)) {
-    case Kernel::split32: *bm = *bn = 32; break;
-    case Kernel::split64: *bm = 64, *bn = 32; break;
+    case Kernel::split32x32: *bm = *bn = 32; break;
+    case Kernel::split32x64: *bm = 32, *bn = 64; break;
+    case Kernel::split64x64: *bm = *bn = 64; break;
     case Kernel::shared128: *bm = *bn = 128; break;
     default: *bm = *bn = 256;
   }

@@ -229,7 +229,8 @@ def close_big(got, ref, err):
 # three before it; edges in both directions, rows that end inside eight columns
 @pytest.mark.parametrize("M,N,K,tile", [(5757, 2618, 32, 128), (3153, 3068, 160, 128), (3018, 3480, 384, 128), (3179, 3592, 512, 128), (3955, 4469, 640, 128),
                                         (2650, 5944, 672, 128), (4063, 4060, 256, 256), (7352, 8877, 288, 256), (5692, 5624, 480, 256), (4999, 5733, 512, 256), (4522, 6360, 608, 256),
-                                        (4423, 6544, 1184, 256), (45, 9001, 2080, 64), (150, 3001, 96, 64), (90, 2000, 512, 32), (333, 1000, 4128, 64)])
+                                        (4423, 6544, 1184, 256), (45, 9001, 2080, 64), (150, 3001, 96, 32), (90, 2000, 512, 32), (333, 1000, 4128, 32),
+                                        (1, 12345, 8192, 32), (200, 4099, 8192, 32), (200, 4090, 8192, 64), (700, 905, 1056, 64), (64, 12288, 96, 64), (61, 9002, 32, 64)])
 @pytest.mark.parametrize("bias", [False, True])
 def test_product_of_many_tiles(M, N, K, tile, bias):
     assert pq.pq_qgemm_tile(MX, 32, M, N, K)[0] == tile
@@ -306,7 +307,9 @@ def test_grouped(sizes, a_rows, N, K, gather, bias):
     (64, 9000, 1500, 2056, 640, True, True, 0), (64, 9000, 1500, 2056, 544, True, False, 0), (64, 9000, 1500, 2050, 512, True, True, 0), (64, 9000, 1500, 2056, 96, True, True, 0),
     (8, 30000, 30000, 1288, 704, False, True, 0), (8, 30000, 7000, 1288, 672, True, True, 0), (8, 30000, 7000, 1285, 256, True, False, 0), (8, 40000, 9000, 2056, 1152, True, True, 3),
     (300, 2400, 300, 520, 1056, True, True, 0), (300, 2400, 300, 515, 160, True, False, 0), (100, 4500, 500, 1032, 576, True, True, 0), (100, 4500, 4500, 1032, 320, False, True, 9),
-    (1500, 3000, 400, 264, 288, True, True, 0), (1100, 60000, 4000, 512, 640, True, False, 0), (1100, 60000, 60000, 512, 128, False, True, 0), (3, 90, 40, 1000, 2080, True, True, 0)])
+    (1500, 3000, 400, 264, 288, True, True, 0), (1100, 60000, 4000, 512, 640, True, False, 0), (1100, 60000, 60000, 512, 128, False, True, 0), (3, 90, 40, 1000, 2080, True, True, 0),
+    (4, 300, 90, 1000, 2080, True, True, 0), (8, 200, 200, 1502, 2080, False, True, 0), (4, 200, 50, 2500, 672, True, True, 0), (4, 200, 200, 2501, 672, False, False, 2),
+    (8, 100, 30, 2001, 96, True, False, 0)])
 def test_grouped_of_all_lengths(E, M, a_rows, N, K, gather, bias, few_experts):
     rng = np.random.default_rng(E + M + K)
     share = np.exp(rng.standard_normal(E))

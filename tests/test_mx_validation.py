@@ -55,7 +55,8 @@ def test_products(lib):  # noqa: F811
 
 def test_tile(lib):  # noqa: F811
     assert pq.pq_qgemm_tile(MX, 32, 1, 4096, 4096) == (32, 32)
-    assert pq.pq_qgemm_tile(MX, 32, 60, 12288, 4096) == (64, 32)
+    assert pq.pq_qgemm_tile(MX, 32, 16, 12288, 8192) == (32, 64)
+    assert pq.pq_qgemm_tile(MX, 32, 60, 12288, 4096) == (64, 64)
     assert pq.pq_qgemm_tile(MX, 32, 2000, 4096, 2048) == (128, 128)
     assert pq.pq_qgemm_tile(MX, 32, 8192, 12288, 8192) == (256, 256)
     for bad in [(MX, 16, 8, 8, 64), (MX, 32, 0, 8, 64), (MX, 32, 8, 8, 48)]:
