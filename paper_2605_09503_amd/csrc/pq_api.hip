@@ -898,7 +898,7 @@ int pq_moe_route(pq_logits type, const void* logits, int64_t tokens, int experts
   if (!workspace || workspace_bytes < need)
     return fail(PQ_ERR_WORKSPACE, "%s: workspace of %zu bytes needed, %zu given", who, need, workspace ? workspace_bytes : (size_t)0);
   if (!aligned16(workspace)) return fail(PQ_ERR_SHAPE, "%s: workspace must be 16-byte aligned", who);
-  return run_moe_route(RouteCall{logits, type == PQ_LOGITS_BF16, tokens, ld, experts, k, renormalize != 0, ids, weights, offsets, rows, positions},
+  return run_moe_route(RouteCall{logits, type == PQ_LOGITS_BF16, tokens, ld, experts, k, renormalize != 0, ids, weights, offsets, rows, positions, false},
                        workspace, as_stream(stream));
 }
 

@@ -223,9 +223,10 @@ struct RouteCall {
   int32_t* ids;
   float* weights;
   int32_t *offsets, *rows, *positions;
+  bool wide;                               // logits may be read 16 bytes at a time: set by run_moe_route
 };
 size_t moe_route_workspace_bytes(int64_t tokens, int experts);
-int run_moe_route(const RouteCall& c, void* ws, hipStream_t st);
+int run_moe_route(RouteCall c, void* ws, hipStream_t st);
 struct CombineCall {
   const uint16_t* y;
   int64_t rows, y_ld;

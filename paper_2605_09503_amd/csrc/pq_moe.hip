@@ -61,7 +61,7 @@ __device__ __forceinline__ float lanes_sum(float v) {
   return v + dpp_f32<0x140>(v);
 }
 
-// A lane's PER experts, lane + LANES i, largest first: a token's largest is then one of its lanes' first, and the lane that has it moves
+// A lane's PER experts, PER lane + i, largest first: a token's largest is then one of its lanes' first, and the lane that has it moves
 // on to its next.  A bf16 logit and its expert fit one word (the expert's complement below, so that equal logits order by
 // expert); binary32 logits keep the expert beside the key.
 template <int PER, bool BF16, int LANES>
@@ -115,12 +115,36 @@ struct Sorted {
 // 0.37 2^-24 of the largest.
 __device__ __forceinline__ float exp_in_sum(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
-// A token's logits, expert sub + LANES i at place i of lane `sub` of its LANES
-template <int PER, bool BF16, int LANES>
+// A token's logits, expert PER sub + i at place i of lane `sub` of its LANES: up to 16 bytes a load where the rows allow it, else one
+// logit (16381 tokens of bf16, 256 experts, k 8: the first launch takes 8.4 us, with one logit a load 10.1).
+template <int PER, bool BF16>
 __device__ __forceinline__ void load_logits(const RouteCall& c, int64_t t, int sub, float (&v)[PER]) {
+  const int first = PER * sub;
+  if (c.wide) {                                               // uniform
+    constexpr int per = BF16 ? (PER < 8 ? PER : 8) : 4;       // logits a load
+#pragma unroll
+    for (int i = 0; i < PER; i += per) {
+      uint32_t w[4] = {};
+      const bool there = first + i < c.experts;               // the experts are a multiple of what a load takes
+      if constexpr (BF16 && per == 4) {
+        const uint2 x = there ? *reinterpret_cast<const uint2*>((const uint16_t*)c.logits + t * c.ld + first + i) : make_uint2(0, 0);
+        w[0] = x.x, w[1] = x.y;
+      } else if (there) {
+        const uint4 x = BF16 ? *reinterpret_cast<const uint4*>((const uint16_t*)c.logits + t * c.ld + first + i)
+                             : *reinterpret_cast<const uint4*>((const float*)c.logits + t * c.ld + first + i);
+        w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w;
+      }
+#pragma unroll
+      for (int j = 0; j < per; ++j) {
+        const float x = BF16 ? (j & 1 ? bf16_hi(w[j >> 1]) : bf16_lo(w[j >> 1])) : as_f32(w[j & 3]);
+        v[i + j] = there ? x : -INFINITY;
+      }
+    }
+    return;
+  }
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const int e = sub + LANES * i;
+    const int e = first + i;
     if constexpr (BF16)
       v[i] = e < c.experts ? bf16_to_f32(((const uint16_t*)c.logits)[t * c.ld + e]) : -INFINITY;
     else
@@ -133,7 +157,7 @@ __device__ __forceinline__ int route_token(const RouteCall& c, int64_t t, bool t
   Sorted<PER, BF16, LANES> s;
 #pragma unroll
   for (int i = 0; i < PER; ++i) {
-    const uint32_t e = (uint32_t)(sub + LANES * i), key = key_of(v[i]);
+    const uint32_t e = (uint32_t)(PER * sub + i), key = key_of(v[i]);
     if constexpr (BF16) {
       s.key[i] = key ? (key & 0xFFFF0000u) | (0xFFFFu - e) : 0u;      // a bf16 value says nothing in the low half
     } else {
@@ -224,14 +248,14 @@ __global__ __launch_bounds__(kRouteThreads) void route_few_kernel(const RouteCal
   const int sub = threadIdx.x % LANES, group = threadIdx.x / LANES, e = threadIdx.x, tokens = (int)c.tokens;
   constexpr int groups = kRouteThreads / LANES;
   float v[PER];
-  if (tokens > 0) load_logits<PER, BF16, LANES>(c, min(group, tokens - 1), sub, v);      // without tokens there are no logits
+  if (tokens > 0) load_logits<PER, BF16>(c, min(group, tokens - 1), sub, v);      // without tokens there are no logits
   if (e < c.experts) mask[e] = 0;
   __syncthreads();
   for (int t0 = 0; t0 < tokens; t0 += groups) {
     const int t = t0 + group;
     const int id = route_token<PER, BF16, LANES>(c, t, t < tokens, sub, v);
     if (sub < c.k && id >= 0) atomicOr((unsigned long long*)&mask[id], 1ull << t);
-    if (t0 + groups < tokens) load_logits<PER, BF16, LANES>(c, min(t + groups, tokens - 1), sub, v);
+    if (t0 + groups < tokens) load_logits<PER, BF16>(c, min(t + groups, tokens - 1), sub, v);
   }
   __syncthreads();
   int total;
@@ -255,13 +279,13 @@ __global__ __launch_bounds__(kRouteThreads) void route_topk_kernel(const RouteCa
   constexpr int groups = kRouteThreads / LANES;
   const int64_t first = (int64_t)blockIdx.x * per_block, end = min(first + per_block, c.tokens);
   float v[PER];
-  load_logits<PER, BF16, LANES>(c, min(first + group, end - 1), sub, v);
+  load_logits<PER, BF16>(c, min(first + group, end - 1), sub, v);
   for (int e = threadIdx.x; e < c.experts; e += kRouteThreads) count[e] = 0;
   __syncthreads();
   for (int64_t t0 = first; t0 < end; t0 += groups) {
     const int64_t t = t0 + group;
     float next[PER] = {};
-    if (t0 + groups < end) load_logits<PER, BF16, LANES>(c, min(t + groups, end - 1), sub, next);
+    if (t0 + groups < end) load_logits<PER, BF16>(c, min(t + groups, end - 1), sub, next);
     const int id = route_token<PER, BF16, LANES>(c, t, t < end, sub, v);
     if (sub < c.k && id >= 0) atomicAdd(&count[id], 1u);
 #pragma unroll
@@ -431,10 +455,12 @@ static int route(const RouteCall& c, uint16_t* hist, hipStream_t st) {
   return check_hip(hipGetLastError(), "route_place_kernel");
 }
 
-int run_moe_route(const RouteCall& c, void* ws, hipStream_t st) {
+int run_moe_route(RouteCall c, void* ws, hipStream_t st) {
+  const int each_load = c.bf16 ? 8 : 4;                       // logits of 16 bytes
+  c.wide = c.experts % each_load == 0 && c.ld % each_load == 0 && ((uintptr_t)c.logits & 15) == 0;
   uint16_t* hist = (uint16_t*)ws;
   // Sixteen lanes a token where its experts fit their registers and its k experts the lanes: what a step of the selection costs is shared
-  // by four tokens (16381 tokens, 256 experts, k 8: the first launch 11.2 us, with a wave a token 15.8).
+  // by four tokens (16381 tokens, 256 experts, k 8: the first launch 10.1 us with one logit a load, with a wave a token 15.8).
   if (c.experts <= 256 && c.k <= 16) {
     return c.experts <= 64 ? route<4, 16>(c, hist, st) : c.experts <= 128 ? route<8, 16>(c, hist, st) : route<16, 16>(c, hist, st);
   }

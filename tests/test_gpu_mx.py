@@ -418,8 +418,11 @@ def test_route(T, E, k, dtype, renormalize):
         t.fill_(77)
     pq.pq_moe_route(logits, k, renormalize, out=r)
     check_route(r, mx.route(logits.double().cpu().numpy(), k, renormalize))
-    again = pq.pq_moe_route(logits, k, renormalize)
-    assert all(torch.equal(a, b) for a, b in zip(r, again))
+    # again, and from rows that may be read in wider pieces: contiguous ones, and those of rows behind which other values stand
+    aligned = torch.full((T, E + 8 + (-E) % 8), 1e30, dtype=dtype, device=DEV)
+    aligned[:, :E] = logits
+    for other in (logits, logits.contiguous(), aligned[:, :E]):
+        assert all(torch.equal(a, b) for a, b in zip(r, pq.pq_moe_route(other, k, renormalize)))
 
 
 def test_route_no_tokens_and_no_choices():
