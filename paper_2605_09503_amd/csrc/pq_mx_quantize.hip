@@ -39,7 +39,10 @@ int64_t blocks_of(int64_t rows, int64_t K) {
   return (rows + kRows * (kThreads / 64) - 1) / (kRows * (kThreads / 64)) * ((K + kChunk - 1) / kChunk);
 }
 // a grid has fewer than 2^32 threads (2^24 workgroups: 2^37 elements)
-bool too_many(int64_t rows, int64_t K) { return blocks_of(rows, K) >= (int64_t)1 << 24; }
+bool too_many(int64_t rows, int64_t K) {
+  constexpr int64_t most = (int64_t)1 << 37;                   // the product below does not overflow
+  return rows > most || K > most || blocks_of(rows, K) >= (int64_t)1 << 24;
+}
 
 // Stored layout: four lanes a group.
 template <bool GATHER>

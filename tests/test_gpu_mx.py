@@ -482,6 +482,77 @@ def test_combine(T, k, N, addend):
         assert torch.equal(add[:, :N], out[:T, :N]) and bool((add[:, N:] == 4).all())
 
 
+# ------------------------------------------------------------------------ what lies more than 2^32 bytes from where it begins
+
+def test_far_rows_of_quantizers_and_products():
+    M, N, K = 1 << 20, 2304, 2304                              # x and y 4.8 GB
+    g = torch.Generator(device=DEV).manual_seed(1)
+    x = torch.zeros(M, K, dtype=torch.bfloat16, device=DEV)
+    at = torch.tensor([0, 5, M // 2 + 77, M - 130, M - 1], device=DEV)
+    x[at] = torch.randn(len(at), K, generator=g, device=DEV).to(torch.bfloat16)
+    codes, scales = pq.alloc_quantized(MX, 32, M, K)
+    pq.pq_quantize_act(MX, 32, x, None, None, codes, scales)
+    few, few_scales = pq.alloc_quantized(MX, 32, len(at), K)
+    pq.pq_quantize_act(MX, 32, x[at], None, None, few, few_scales)
+    assert torch.equal(codes[at], few) and torch.equal(scales[at], few_scales) and int((scales != 0).sum()) == few_scales.count_nonzero()
+    xq = pq.pq_dequantize(MX, 32, few, few_scales).double()
+    y = pq.pq_dequantize(MX, 32, codes, scales)
+    assert torch.equal(y[at].double(), xq) and int(y.count_nonzero()) == xq.count_nonzero()
+    _, wc, ws, wq = big(N, K, 2, 0.02)
+    a = operand(x)
+    del x
+    pq.pq_qgemm_packed(MX, 32, a, None, pq.pq_pack_operand(MX, 32, wc, ws), None, y, M, N, K)
+    close_big(y[at], xq @ wq.T, (K / 64 + 8) * 2.0 ** -23 * (xq.abs() @ wq.T.abs()))
+    other = torch.ones(M, dtype=torch.bool, device=DEV)
+    other[at] = False
+    assert not y[other].any()
+
+
+def test_far_experts_rows_and_tokens():
+    # weights of 150 experts 4.9 GB, tokens' operand 4.6 GB; then rows 5 GB
+    E, N, K, a_rows = 150, 15360, 4096, 2200000
+    g = torch.Generator(device=DEV).manual_seed(2)
+    w = torch.zeros(E, pq.pq_operand_bytes(MX, 32, N, K), dtype=torch.uint8, device=DEV)
+    _, wc, ws, wq = big(N, K, 3, 0.02)
+    w[E - 1] = pq.pq_pack_operand(MX, 32, wc, ws)
+    x = torch.zeros(a_rows, K, dtype=torch.bfloat16, device=DEV)
+    at = torch.tensor([a_rows - 1, 3, a_rows - 200, a_rows // 2 + 1], dtype=torch.int32, device=DEV)
+    x[at.long()] = torch.randn(len(at), K, generator=g, device=DEV).to(torch.bfloat16)
+    a = operand(x)
+    few, few_scales = pq.alloc_quantized(MX, 32, len(at), K)
+    pq.pq_quantize_act(MX, 32, x[at.long()], None, None, few, few_scales)
+    xq = pq.pq_dequantize(MX, 32, few, few_scales).double()
+    del x
+    offsets = torch.full((E + 1,), 0, dtype=torch.int32, device=DEV)
+    for M in (len(at), 300):                                   # small tiles, large ones
+        offsets[E] = M
+        index = at.repeat((M + len(at) - 1) // len(at))[:M].contiguous()
+        y = torch.empty(M, N, dtype=torch.bfloat16, device=DEV)
+        pq.pq_qgemm_grouped(MX, 32, a, a_rows, w, offsets, y, N, K, rows=index)
+        ref, mag = xq @ wq.T, xq.abs() @ wq.T.abs()
+        for i in range(0, M, len(at)):
+            n = min(len(at), M - i)
+            close_big(y[i:i + n], ref[:n], ((K / 64 + 8) * 2.0 ** -23 * mag)[:n])
+    del a, w
+    rows, tokens, width = 2500000, 2400000, 1024
+    z = torch.zeros(rows, width, dtype=torch.bfloat16, device=DEV)
+    z[-2:] = torch.randn(2, width, generator=g, device=DEV).to(torch.bfloat16)
+    positions = torch.full((tokens, 2), -1, dtype=torch.int32, device=DEV)
+    positions[-1] = torch.tensor([rows - 1, rows - 2], dtype=torch.int32)
+    weights = torch.full((tokens, 2), 0.5, device=DEV)
+    out = pq.pq_moe_combine(z, positions, weights)
+    assert torch.equal(out[-1], (0.5 * z[-1].float() + 0.5 * z[-2].float()).to(torch.bfloat16)) and not out[:-1].any()
+
+
+def test_far_logits():
+    T, E = 1200000, 1024                                       # 4.9 GB
+    x = torch.zeros(T, E, device=DEV)
+    x[torch.arange(T, device=DEV), torch.arange(T, device=DEV) % E] = 1.0
+    r = pq.pq_moe_route(x, 1)
+    assert torch.equal(r.ids[:, 0], (torch.arange(T, device=DEV) % E).int())
+    assert torch.equal(r.rows.long(), torch.arange(T, device=DEV).reshape(-1)[torch.argsort(r.ids[:, 0], stable=True)])
+
+
 # ------------------------------------------------------------------------ together
 
 class Layer:

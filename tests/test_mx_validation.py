@@ -29,6 +29,7 @@ def test_quantizers(lib):  # noqa: F811
     assert qa(x=None) == qa(codes=None) == qa(s=None) == PQ_ERR_NULL
     assert qa(g=16) == qa(g=64) == qa(fmt=5) == PQ_ERR_FORMAT
     assert qa(K=48, ld=48) == qa(K=0) == qa(M=0) == qa(ld=56) == qa(ld=68) == qa(x=ODD) == qa(codes=ODD) == qa(s=ODD) == qa(perm=ODD) == PQ_ERR_SHAPE
+    assert qa(M=1 << 40, K=1 << 12, ld=1 << 12) == qa(M=1 << 62) == qa(M=1 << 60, K=1 << 58, ld=1 << 58) == PQ_ERR_SHAPE
     qp = lambda g=32, x=FAKE, M=4, K=64, ld=64, op=FAKE, size=1 << 20, codes=None, s=None: lib.pq_quantize_act_packed(MX, g, x, M, K, ld, None, op, size, codes, s, None)
     assert qp(x=None) == qp(op=None) == qp(codes=FAKE) == qp(s=FAKE) == PQ_ERR_NULL
     assert qp(g=16) == PQ_ERR_FORMAT
