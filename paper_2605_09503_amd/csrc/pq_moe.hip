@@ -247,11 +247,12 @@ __global__ __launch_bounds__(kRouteThreads) void route_few_kernel(const RouteCal
   __shared__ int wave_sums[kRouteWaves];
   const int sub = threadIdx.x % LANES, group = threadIdx.x / LANES, e = threadIdx.x, tokens = (int)c.tokens;
   constexpr int groups = kRouteThreads / LANES;
+  const int wave_first = threadIdx.x / kWave * (kWave / LANES);
   float v[PER];
-  if (tokens > 0) load_logits<PER, BF16>(c, min(group, tokens - 1), sub, v);      // without tokens there are no logits
+  if (wave_first < tokens) load_logits<PER, BF16>(c, min(group, tokens - 1), sub, v);      // without tokens there are no logits
   if (e < c.experts) mask[e] = 0;
   __syncthreads();
-  for (int t0 = 0; t0 < tokens; t0 += groups) {
+  for (int t0 = 0; t0 + wave_first < tokens; t0 += groups) {      // waves without a token leave the unit to the others
     const int t = t0 + group;
     const int id = route_token<PER, BF16, LANES>(c, t, t < tokens, sub, v);
     if (sub < c.k && id >= 0) atomicOr((unsigned long long*)&mask[id], 1ull << t);
@@ -277,12 +278,13 @@ __global__ __launch_bounds__(kRouteThreads) void route_topk_kernel(const RouteCa
   __shared__ uint32_t count[LANES * PER];
   const int sub = threadIdx.x % LANES, group = threadIdx.x / LANES;
   constexpr int groups = kRouteThreads / LANES;
+  const int wave_first = threadIdx.x / kWave * (kWave / LANES);
   const int64_t first = (int64_t)blockIdx.x * per_block, end = min(first + per_block, c.tokens);
   float v[PER];
-  load_logits<PER, BF16>(c, min(first + group, end - 1), sub, v);
+  if (first + wave_first < end) load_logits<PER, BF16>(c, min(first + group, end - 1), sub, v);
   for (int e = threadIdx.x; e < c.experts; e += kRouteThreads) count[e] = 0;
   __syncthreads();
-  for (int64_t t0 = first; t0 < end; t0 += groups) {
+  for (int64_t t0 = first; t0 + wave_first < end; t0 += groups) {
     const int64_t t = t0 + group;
     float next[PER] = {};
     if (t0 + groups < end) load_logits<PER, BF16>(c, min(t + groups, end - 1), sub, next);
@@ -424,27 +426,40 @@ __global__ __launch_bounds__(kCombineThreads) void combine_kernel(const CombineC
   }
 }
 
-// tokens a workgroup takes: whole passes, so few workgroups that each can sum up what the others counted
-int tokens_per_block(int64_t tokens) { return (int)((tokens + (int64_t)kTile * kMaxBlocks - 1) / ((int64_t)kTile * kMaxBlocks)) * kTile; }
+// Workgroups of the two launches: every one of the second sums up what all of the first counted, so few where few tokens make the first
+// short.  256 experts, k 8, binary32, us with at most 64, 128 and 256: 1024 tokens 12.5 12.6 12.5, 4096 18.6 13.6 14.1, 8192 19.1 19.2 15.4;
+// 1024 experts 21.3 17.9 20.1, 45.4 32.1 28.6, 50.0 50.2 38.0.
+int64_t most_blocks(int64_t tokens) {
+  const int64_t some = (tokens + 15) / 16, passes = (tokens + kTile - 1) / kTile, few = some < 64 ? 64 : some < 256 ? some : 256;
+  return passes <= few ? few : passes < kMaxBlocks ? passes : kMaxBlocks;
+}
+// Tokens a workgroup takes: a wave of them on every SIMD (`unit`) at least, so that their steps do not wait for each other's, or whole passes
+// (256 tokens, 1024 experts, k 8, binary32: 14 us, 42 with 64 tokens a workgroup).
+int tokens_per_block(int64_t tokens, int unit) {
+  const int64_t most = most_blocks(tokens), least = (tokens + most - 1) / most;
+  const int by = least < kTile ? unit : kTile;
+  return (int)((least + by - 1) / by) * by;
+}
 
 }  // namespace
 
 size_t moe_route_workspace_bytes(int64_t tokens, int experts) {
   // no less for more tokens: a workspace serves every smaller call
-  const int64_t blocks = (tokens + kTile - 1) / kTile;
-  return align_up((size_t)(blocks < kMaxBlocks ? blocks : kMaxBlocks) * counts_of(experts) * 2, 256) + 256;
+  return align_up((size_t)most_blocks(tokens) * counts_of(experts) * 2, 256) + 256;
 }
 
 template <int PER, int LANES>
 static int route(const RouteCall& c, uint16_t* hist, hipStream_t st) {
-  if (c.tokens <= kTile) {
+  // One launch for one pass of a workgroup, half of it where a step is long: us with one and two launches, 64 experts, k 8, 64 tokens 5.2 7.1;
+  // 256 experts, 32 tokens 8.4 10.1, 64 tokens 12.0 10.2 (bf16 8.0 8.4); 1024 experts, 4 tokens 7.1 10.1, 16 tokens 12.8 11.4
+  if (c.tokens <= kRouteThreads / LANES / (PER == 16 && !c.bf16 ? 2 : 1)) {
     if (c.bf16)
       route_few_kernel<PER, true, LANES><<<1, kRouteThreads, 0, st>>>(c);
     else
       route_few_kernel<PER, false, LANES><<<1, kRouteThreads, 0, st>>>(c);
     return check_hip(hipGetLastError(), "route_few_kernel");
   }
-  const int per = tokens_per_block(c.tokens), blocks = (int)((c.tokens + per - 1) / per);
+  const int per = tokens_per_block(c.tokens, 4 * kWave / LANES), blocks = (int)((c.tokens + per - 1) / per);
   if (c.bf16)
     route_topk_kernel<PER, true, LANES><<<blocks, kRouteThreads, 0, st>>>(c, per, hist);
   else

@@ -437,7 +437,7 @@ def test_route_no_tokens_and_no_choices():
     assert r.ids.tolist() == [[1, 0, 3, 2]] * 3 and r.weights.tolist() == [[1.0, 0.0, 0.0, 0.0]] * 3
 
 
-@pytest.mark.parametrize("T,E,k", [(33000, 8, 2), (70001, 33, 3)])
+@pytest.mark.parametrize("T,E,k", [(33000, 8, 2), (70001, 33, 3), (1025, 1000, 7), (4099, 200, 12), (9000, 600, 20), (16385, 64, 4), (33, 256, 8), (9, 1024, 4), (17, 500, 32)])
 def test_route_of_many_tokens(T, E, k):
     # more tokens than one pass of all workgroups
     x = torch.randn(T, E, generator=torch.Generator(device=DEV).manual_seed(T), device=DEV)
