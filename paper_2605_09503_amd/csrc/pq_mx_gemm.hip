@@ -536,7 +536,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void mx_gemm_shared_kernel(const Mx
 // Each of KW waves multiplies the whole tile of 32 FM x 32 FN over every KW-th panel, its panels in a part of LDS of its own (no
 // barrier while it runs), then the waves' sums are added up in their order.
 // Few rows: bound by the weights' bytes, 1 x 6144 x 4096 4.6 us (13 MB: 2.9 TB/s with the start and the end of the launch, 2.7 us at the
-// rate of a large copy), and from some 32 rows on by what the units take from the caches, since every tile of rows reads the weights and
+// rate of a large copy; 56 x 12288 x 4096 9.1 us), and from some 32 rows on by what the units take from the caches, since every tile of rows reads the weights and
 // every tile of columns the rows.  32 x 32 where there are few of them, 32 x 64 and 64 x 64 for more, us at N 12288:
 //   K 8192, M 16   12.6  11.1  11.7     M 56  17.8  17.5  14.5     K 512, M 56   4.9  3.9  4.3     M 128  7.3  5.7  7.2
 // (64 x 32 tiles take 13.1, 17.5, 4.0, 6.0: never less than both of the others by 4 %.)  Four waves and four stages (three for 32 x 64), two
