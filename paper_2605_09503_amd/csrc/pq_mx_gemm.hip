@@ -59,7 +59,7 @@ struct Tiles {
       for (int e = 0; e < c.experts; e += 64) {
         int from, to;
         const int upto = total + wave_scan(tiles_of(c, bm, e + lane, from, to));
-        if (table) {                                             // every wave writes the same
+        if (table && e + lane < c.experts) {                     // every wave writes the same, each word once
           lds[e + lane] = upto;
           lds[kTable + e + lane] = from;
           if (e + lane == c.experts - 1) lds[kTable + e + lane + 1] = to;

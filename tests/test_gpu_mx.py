@@ -641,3 +641,48 @@ def test_layer_in_graphs_and_streams():
     torch.cuda.synchronize()
     for layer, w in zip(layers, want):
         assert torch.equal(layer.out, w)
+
+
+# ------------------------------------------------------------------------ every kernel of the products by expert
+
+def by_expert(sizes, a_rows, N, K, gather, bias, first=0, behind=3):
+    """One call and its check against float64: experts of these sizes, rows in front of and behind theirs that are nobody's."""
+    E, M = len(sizes), first + int(sum(sizes)) + behind
+    offsets = first + np.concatenate([[0], np.cumsum(sizes)]).astype(np.int64)
+    x, _, _, xq = big(a_rows, K, 1)
+    _, codes, scales, wq = big(E * N, K, 2, 0.02)
+    g = torch.Generator(device=DEV).manual_seed(3)
+    b = torch.randn(E, N, generator=g, device=DEV).to(torch.bfloat16) if bias else None
+    rows = torch.randint(0, a_rows, (M,), generator=g, device=DEV, dtype=torch.int32) if gather else None
+    if gather:
+        rows[7::97] = -1
+        rows[11::101] = a_rows
+    y = torch.full((M, (N + 7) // 8 * 8 + 8), 5.0, dtype=torch.bfloat16, device=DEV)
+    pq.pq_qgemm_grouped(MX, 32, operand(x), a_rows, pq.pack_experts(codes, scales, E), torch.from_numpy(offsets.astype(np.int32)).to(DEV), y[:, :N], N, K,
+                        rows=rows, bias=b)
+    assert bool((y[:, N:] == 5).all()) and bool((y[:first] == 5).all()) and bool((y[offsets[-1]:] == 5).all())
+    for e in range(E):
+        if sizes[e] == 0:
+            continue
+        at = slice(offsets[e], offsets[e + 1])
+        index = rows[at].long() if gather else torch.arange(offsets[e], offsets[e + 1], device=DEV)
+        known = ((index >= 0) & (index < a_rows))[:, None]
+        part, aq = wq[e * N:(e + 1) * N], xq[index.clamp(0, a_rows - 1)]
+        ref, mag = aq @ part.T, aq.abs() @ part.T.abs()
+        if bias:
+            ref, mag = ref + b[e].double(), mag + b[e].double().abs()
+        close_big(y[at, :N], torch.where(known, ref, 5.0), (K / 64 + 8) * 2.0 ** -23 * torch.where(known, mag, 0.0))
+
+
+# the table of experts in LDS: its last word stands behind lanes that are all taken, behind idle ones, and at the table's end; tiles of 128 rows, of
+# 256, and waves with tiles of 32 and 64 rows
+@pytest.mark.parametrize("E,each,N,K", [(1, 5500, 264, 2048), (63, 100, 1032, 2048), (64, 100, 1032, 2048), (65, 100, 1032, 2048), (127, 100, 1032, 2048), (129, 100, 1032, 2048),
+                                        (3, 2000, 2048, 2048), (65, 1000, 2048, 2048),
+                                        (63, 20, 1032, 64), (65, 20, 1032, 64), (1000, 5, 264, 512), (1023, 5, 264, 512), (1024, 5, 264, 512),
+                                        (63, 64, 1032, 512), (129, 70, 1032, 512), (1000, 64, 520, 256)])
+@pytest.mark.parametrize("last", ["full", "empty"])
+def test_grouped_last_expert(E, each, N, K, last):
+    sizes = [each] * E
+    if last == "empty":
+        sizes[-1] = 0
+    by_expert(sizes, 3000, N, K, True, True, first=1)
