@@ -247,13 +247,16 @@ int pq_quantize_weights(pq_format fmt, int group, const void* w, int64_t N, int6
   if (!aligned16(w) || !aligned16(codes) || !aligned16(scales) || (fmt == PQ_FMT_MXFP4 && !aligned16(perm)))
     return fail(PQ_ERR_SHAPE, "pq_quantize_weights: tensors must be 16-byte aligned");
   hipStream_t st = as_stream(stream);
+  if (fmt == PQ_FMT_MXFP4) {                                   // first: it refuses what is too large
+    rc = launch_mx_quantize_rows(w, N, K, K, perm, codes, scales, st);
+    return rc ? rc : launch_fill_float(tensor_scale_out, 1.0f, st);
+  }
   if (fmt == PQ_FMT_NVFP4) {
     rc = launch_absmax_to_tensor_scale(w, N * K, tensor_scale_out, st);
   } else {
     rc = launch_fill_float(tensor_scale_out, 1.0f, st);
   }
   if (rc) return rc;
-  if (fmt == PQ_FMT_MXFP4) return launch_mx_quantize_rows(w, N, K, K, perm, codes, scales, st);
   return launch_quantize_rows(fmt, group, w, N, K, K, perm, tensor_scale_out, codes, scales, st);
 }
 

@@ -164,3 +164,8 @@ def test_native_and_python_signatures(lib, python, name):  # noqa: F811
     want = inspect.signature(getattr(python, name))
     got = inspect.signature(native)
     assert [(p.name, p.default) for p in got.parameters.values()] == [(p.name, p.default) for p in want.parameters.values()]
+
+
+def test_weights_too_large_are_refused_before_a_launch(lib):  # noqa: F811
+    qw = lambda N, K: lib.pq_quantize_weights(MX, 32, FAKE, N, K, None, FAKE, FAKE, FAKE, None)
+    assert qw(1 << 40, 1 << 12) == qw(1 << 62, 64) == qw(1 << 60, 1 << 58) == PQ_ERR_SHAPE
