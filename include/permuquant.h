@@ -643,6 +643,10 @@ int pq_qgemm_grouped(pq_format fmt, int group, const void* a_operand, int64_t a_
                      const int32_t* offsets, const int32_t* rows, int64_t M, int64_t N, int64_t K, const void* bias_bf16, void* y_bf16,
                      int64_t ldy, void* stream);
 
+/* The output tile that pq_qgemm_grouped takes for these sizes, as pq_qgemm_tile: 256 x 256, 128 x 128; 64 x 64, 32 x 64 or 32 x 32, whose
+ * waves split K; 64 x 128 or 32 x 128, four waves side by side with 32 columns each.  M 1 .. 2^24.  Host only.                  */
+int pq_qgemm_grouped_tile(pq_format fmt, int group, int experts, int64_t M, int64_t N, int64_t K, int* tile_m, int* tile_n);
+
 /*
  * Routing of tokens to experts.  Of every token's logits the k largest, largest first (equal logits: the lower index first), and the
  * order in which the experts' rows stand:

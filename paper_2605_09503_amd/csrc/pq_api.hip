@@ -351,7 +351,7 @@ int pq_qgemm_tile(pq_format fmt, int group, int64_t M, int64_t N, int64_t K, int
   if (M <= 0 || N <= 0 || K % 32 || M > (1 << 24) || N > (1 << 24) || K > (1 << 24))
     return fail(PQ_ERR_SHAPE, "pq_qgemm_tile: no product of M=%lld N=%lld K=%lld", (long long)M, (long long)N, (long long)K);
   if (fmt == PQ_FMT_MXFP4)
-    mx_gemm_tile(M, N, K, tile_m, tile_n);
+    mx_gemm_tile(0, M, N, K, tile_m, tile_n);
   else
     tile_size(choose_tile(fmt, group, M, N, K), tile_m, tile_n);
   return PQ_OK;
@@ -872,6 +872,18 @@ int pq_qgemm_grouped(pq_format fmt, int group, const void* a_operand, int64_t a_
   return run_mx_gemm(MxCall{(const uint8_t*)a_operand, a_rows, (const uint8_t*)w_operands, mx_operand_bytes(N, K), experts, offsets, rows, M, N,
                             K, (const uint16_t*)bias, y, ldy, false},
                      as_stream(stream));
+}
+
+int pq_qgemm_grouped_tile(pq_format fmt, int group, int experts, int64_t M, int64_t N, int64_t K, int* tile_m, int* tile_n) {
+  const char* who = "pq_qgemm_grouped_tile";
+  if (!tile_m || !tile_n) return fail(PQ_ERR_NULL, "%s: a required pointer is NULL", who);
+  if (fmt != PQ_FMT_MXFP4) return fail(PQ_ERR_FORMAT, "%s: MXFP4 only, got format %d", who, (int)fmt);
+  int rc = check_linear_format(fmt, group, K);
+  if (rc) return rc;
+  if (experts <= 0 || experts > 65536 || M <= 0 || N <= 0 || M > (1 << 24) || N > (1 << 24) || K > (1 << 24))
+    return fail(PQ_ERR_SHAPE, "%s: no product of experts=%d M=%lld N=%lld K=%lld", who, experts, (long long)M, (long long)N, (long long)K);
+  mx_gemm_tile(experts, M, N, K, tile_m, tile_n);
+  return PQ_OK;
 }
 
 static int check_route(const char* who, int64_t tokens, int experts, int k) {

@@ -211,7 +211,7 @@ struct MxCall {
   bool out_f32;
 };
 int run_mx_gemm(const MxCall& c, hipStream_t st);
-void mx_gemm_tile(int64_t M, int64_t N, int64_t K, int* bm, int* bn);      // of one product
+void mx_gemm_tile(int experts, int64_t M, int64_t N, int64_t K, int* bm, int* bn);      // experts 0: of one product
 
 // routing to experts and the weighted sum of what they made (pq_moe.hip)
 struct RouteCall {

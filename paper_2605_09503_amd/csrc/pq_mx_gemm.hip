@@ -954,15 +954,17 @@ int run(const MxCall& c, hipStream_t st) {
 
 }  // namespace
 
-void mx_gemm_tile(int64_t M, int64_t N, int64_t K, int* bm, int* bn) {
+void mx_gemm_tile(int experts, int64_t M, int64_t N, int64_t K, int* bm, int* bn) {
   MxCall c{};
-  c.M = M, c.N = N, c.K = K, c.experts = 1;
-  switch (choose(c, false)) {
+  c.M = M, c.N = N, c.K = K, c.experts = experts ? experts : 1;
+  switch (choose(c, experts > 0)) {
     case Kernel::split32x32: *bm = *bn = 32; break;
     case Kernel::split32x64: *bm = 32, *bn = 64; break;
     case Kernel::split64x64: *bm = *bn = 64; break;
+    case Kernel::alone32: *bm = Alone<1>::bm, *bn = Alone<1>::bn * Alone<1>::waves; break;
+    case Kernel::alone64: *bm = Alone<2>::bm, *bn = Alone<2>::bn * Alone<2>::waves; break;
     case Kernel::shared128: *bm = *bn = 128; break;
-    default: *bm = *bn = 256;
+    case Kernel::shared256: *bm = *bn = 256; break;
   }
 }
 

@@ -147,6 +147,7 @@ def _declare(lib):
     lib.pq_attn_decode.argtypes = [vp, vp, i64, i64, vp, i64, vp, i64, i32, i64, i64, C.c_float, vp, i64, i64, vp, vp, sz, vp]
     lib.pq_dequantize.argtypes = [i32, i32, vp, vp, vp, i64, i64, vp, i64, vp]
     lib.pq_qgemm_grouped.argtypes = [i32, i32, vp, i64, vp, i32, vp, vp, i64, i64, i64, vp, vp, i64, vp]
+    lib.pq_qgemm_grouped_tile.argtypes = [i32, i32, i32, i64, i64, i64, C.POINTER(i32), C.POINTER(i32)]
     lib.pq_moe_route_workspace_bytes.restype = sz
     lib.pq_moe_route_workspace_bytes.argtypes = [i64, i32, i32]
     lib.pq_moe_route.argtypes = [i32, vp, i64, i32, i64, i32, i32, vp, vp, vp, vp, vp, vp, sz, vp]
@@ -902,6 +903,13 @@ def pq_qgemm_grouped(fmt: int, group: int, a_operand: torch.Tensor, a_rows: int,
     rp = None if rows is None else _array("rows", rows, torch.int32, (M,), y)
     bp = None if bias is None else _array("bias", bias, torch.bfloat16, (experts, N), y)
     _check(load().pq_qgemm_grouped(fmt, group, _ptr(a_operand), a_rows, _ptr(w_operands), experts, op, rp, M, N, K, bp, yp, ldy, _stream()))
+
+
+def pq_qgemm_grouped_tile(fmt: int, group: int, experts: int, M: int, N: int, K: int):
+    """(rows, columns) of the output tile that pq_qgemm_grouped takes for these sizes."""
+    m, n = C.c_int(), C.c_int()
+    _check(load().pq_qgemm_grouped_tile(fmt, group, experts, M, N, K, C.byref(m), C.byref(n)))
+    return m.value, n.value
 
 
 class Route(NamedTuple):

@@ -686,3 +686,155 @@ def test_grouped_last_expert(E, each, N, K, last):
     if last == "empty":
         sizes[-1] = 0
     by_expert(sizes, 3000, N, K, True, True, first=1)
+
+
+def skewed(E, total, seed):
+    """Sizes of E experts, uneven, some of them empty; all of total."""
+    rng = np.random.default_rng(seed)
+    share = np.exp(rng.standard_normal(E))
+    if E > 2:
+        share[rng.random(E) < 0.2] = 0.0
+        share[rng.integers(E)] = 1.0
+    sizes = np.floor(share / share.sum() * total).astype(np.int64)
+    sizes[np.argmax(sizes)] += total - sizes.sum()
+    return sizes
+
+
+# each kernel by expert, the large tiles with one to four panels (their index and bias are read as they are needed) and more (loaded ahead), with whole
+# pieces of eight columns and without, and with more experts than the kernels keep a table of
+BY_EXPERT = [(66, 2330, 261, 32, 128, 128), (66, 2330, 264, 64, 128, 128), (8, 3300, 261, 160, 128, 128), (8, 3300, 264, 160, 128, 128), (3, 3300, 261, 384, 128, 128),
+             (3, 3300, 264, 384, 128, 128), (11, 3150, 261, 512, 128, 128), (8, 16384, 4096, 512, 128, 128), (66, 2300, 261, 640, 128, 128), (66, 2300, 264, 640, 128, 128),
+             (1030, 185000, 264, 2048, 128, 128), (1030, 176000, 261, 2048, 128, 128),
+             (2, 5300, 2816, 512, 256, 256), (8, 40000, 2816, 512, 256, 256), (2, 5200, 6003, 512, 256, 256), (2, 3000, 4096, 640, 256, 256), (3, 6000, 2048, 1152, 256, 256),
+             (20, 30000, 2045, 1152, 256, 256), (1030, 3200000, 256, 512, 256, 256), (1030, 840000, 256, 1024, 256, 256),
+             (63, 1300, 1029, 96, 32, 128), (1100, 5000, 261, 640, 32, 128), (63, 5000, 1029, 512, 64, 128), (1030, 200000, 520, 256, 64, 128),
+             (8, 400, 1032, 64, 64, 64), (8, 300, 1032, 64, 32, 64), (8, 300, 261, 2048, 32, 32)]
+
+
+@pytest.mark.parametrize("E,M,N,K,tile_m,tile_n,gather,bias", [c + f for c in BY_EXPERT for f in ((True, True), (True, False), (False, True), (False, False))
+                                                               if c[1] < 100000 or f[0] == f[1]])
+def test_grouped_by_every_kernel(E, M, N, K, tile_m, tile_n, gather, bias):
+    assert pq.pq_qgemm_grouped_tile(MX, 32, E, M, N, K) == (tile_m, tile_n)
+    first = 5
+    by_expert(skewed(E, M - first - 3, E + K), 1500 if gather else M, N, K, gather, bias, first=first)
+
+
+# ------------------------------------------------------------------------ the large tiles: sums, values that are not finite, repeated and captured calls
+
+LARGE = [(2100, 1029, 32, 128), (2100, 1029, 384, 128), (1700, 1030, 640, 128), (1777, 4008, 2016, 128), (4063, 4060, 256, 256), (4423, 6541, 1184, 256)]
+
+
+@pytest.mark.parametrize("M,N,K,tile", LARGE)
+def test_sums_of_large_tiles(M, N, K, tile):
+    assert pq.pq_qgemm_tile(MX, 32, M, N, K) == (tile, tile)
+    x, _, _, xq = big(M, K, 1)
+    _, codes, scales, wq = big(N, K, 2, 0.02)
+    ldy = (N + 7) // 8 * 8 + 8
+    y = torch.full((M + 1, ldy), 5.0, device=DEV)
+    pq.pq_qgemm_packed_f32(MX, 32, operand(x), None, pq.pq_pack_operand(MX, 32, codes, scales), None, y[:M], M, N, K)
+    off = (y[:M, :N].double() - xq @ wq.T).abs()
+    assert bool((off <= (K / 64 + 8) * 2.0 ** -23 * (xq.abs() @ wq.T.abs()) + 2.0 ** -133).all())
+    assert bool((y[M:] == 5).all()) and bool((y[:, N:] == 5).all())
+
+
+def odd_values(x, w):
+    """Puts values that are not finite, the largest and the smallest scales into some rows of x and of w."""
+    M, K = x.shape
+    x[0] *= 2.0 ** -100
+    x[M // 2] *= 2.0 ** 60
+    x[3, 5] = float("inf")
+    x[M - 1, K - 1] = float("nan")
+    x[M // 3, :32] = -float("inf")
+    x[7] = 0.0
+    w[1] *= 2.0 ** -100
+    w[w.shape[0] - 1, K - 2] = float("nan")
+    w[2] *= 2.0 ** 50
+
+
+def quantized(t):
+    codes, scales = pq.alloc_quantized(MX, 32, *t.shape)
+    pq.pq_quantize_act(MX, 32, t, None, None, codes, scales)
+    return codes, scales, pq.pq_dequantize(MX, 32, codes, scales).double()
+
+
+@pytest.mark.parametrize("M,N,K,tile", LARGE)
+@pytest.mark.parametrize("f32", [False, True])
+def test_values_not_finite_in_large_tiles(M, N, K, tile, f32):
+    # a group with one of them makes its row or its column NaN and nothing else; scales from far below to far above 1 beside it
+    x, w = big(M, K, 1)[0], big(N, K, 2, 0.02)[0]
+    odd_values(x, w)
+    (_, _, xq), (codes, scales, wq) = quantized(x), quantized(w)
+    ref, mag = xq @ wq.T, xq.abs() @ wq.T.abs()
+    assert int(torch.isnan(ref).all(dim=1).sum()) == 3 and int(torch.isnan(ref).all(dim=0).sum()) == 1
+    y = torch.empty(M, (N + 7) // 8 * 8, dtype=torch.float32 if f32 else torch.bfloat16, device=DEV)
+    assert pq.pq_qgemm_tile(MX, 32, M, N, K) == (tile, tile)
+    (pq.pq_qgemm_packed_f32 if f32 else pq.pq_qgemm_packed)(MX, 32, operand(x), None, pq.pq_pack_operand(MX, 32, codes, scales), None, y, M, N, K)
+    got = y[:, :N].double()
+    assert torch.equal(torch.isnan(got), torch.isnan(ref))
+    # a sum below what binary32 holds whole may be cut to zero at every step
+    allowed = (K / 64 + 8) * 2.0 ** -23 * mag * (1 + 2.0 ** -8) + (0 if f32 else 2.0 ** -8) * ref.abs() + (K / 64 + 8) * 2.0 ** -126
+    assert bool(((got - ref).abs() <= allowed)[~torch.isnan(ref)].all())
+
+
+@pytest.mark.parametrize("E,M,N,K,tile_m,tile_n", [c for c in BY_EXPERT if c[1] < 10000])
+def test_grouped_values_not_finite(E, M, N, K, tile_m, tile_n):
+    assert pq.pq_qgemm_grouped_tile(MX, 32, E, M, N, K) == (tile_m, tile_n)
+    a_rows = 700
+    x, w = big(a_rows, K, 1)[0], big(E * N, K, 2, 0.02)[0]
+    odd_values(x, w)
+    (_, _, xq), (codes, scales, wq) = quantized(x), quantized(w)
+    sizes = skewed(E, M, E + K)
+    offsets = np.concatenate([[0], np.cumsum(sizes)])
+    rows = torch.randint(0, a_rows, (M,), generator=torch.Generator(device=DEV).manual_seed(3), device=DEV, dtype=torch.int32)
+    y = torch.full((M, (N + 7) // 8 * 8), 5.0, dtype=torch.bfloat16, device=DEV)
+    pq.pq_qgemm_grouped(MX, 32, operand(x), a_rows, pq.pack_experts(codes, scales, E), torch.from_numpy(offsets.astype(np.int32)).to(DEV), y[:, :N], N, K, rows=rows)
+    for e in np.nonzero(sizes)[0]:
+        at = slice(offsets[e], offsets[e + 1])
+        part, aq = wq[e * N:(e + 1) * N], xq[rows[at].long()]
+        ref, mag, got = aq @ part.T, aq.abs() @ part.T.abs(), y[at, :N].double()
+        assert torch.equal(torch.isnan(got), torch.isnan(ref))
+        allowed = (K / 64 + 8) * 2.0 ** -23 * mag * (1 + 2.0 ** -8) + 2.0 ** -8 * ref.abs() + (K / 64 + 8) * 2.0 ** -126
+        assert bool(((got - ref).abs() <= allowed)[~torch.isnan(ref)].all())
+
+
+def test_large_products_repeat_their_bits_and_replay():
+    # every kernel, dense and by expert: call after call, captured into graphs that are replayed with other inputs, eager calls between them
+    calls = []
+    for M, N, K, tile in LARGE:
+        w = pq.pq_pack_operand(MX, 32, *big(N, K, 2, 0.02)[1:3])
+        x = torch.zeros(M, K, dtype=torch.bfloat16, device=DEV)
+        a, y = operand(x), torch.zeros(M, (N + 7) // 8 * 8, dtype=torch.bfloat16, device=DEV)
+
+        def dense(x=x, a=a, w=w, y=y, M=M, N=N, K=K):
+            pq.pq_quantize_act_packed(MX, 32, x, None, a)
+            pq.pq_qgemm_packed(MX, 32, a, None, w, None, y, M, N, K)
+        calls.append((dense, x, y[:, :N]))
+    for E, M, N, K, tile_m, tile_n in [c for c in BY_EXPERT if c[1] < 7000]:
+        w = pq.pack_experts(*big(E * N, K, 2, 0.02)[1:3], E)
+        x = torch.zeros(900, K, dtype=torch.bfloat16, device=DEV)
+        a, y = operand(x), torch.zeros(M, (N + 7) // 8 * 8, dtype=torch.bfloat16, device=DEV)
+        offsets = torch.from_numpy(np.concatenate([[0], np.cumsum(skewed(E, M, E + K))]).astype(np.int32)).to(DEV)
+        rows = torch.randint(0, 900, (M,), generator=torch.Generator(device=DEV).manual_seed(3), device=DEV, dtype=torch.int32)
+
+        def by(x=x, a=a, w=w, y=y, N=N, K=K, offsets=offsets, rows=rows):
+            pq.pq_quantize_act_packed(MX, 32, x, None, a)
+            pq.pq_qgemm_grouped(MX, 32, a, 900, w, offsets, y[:, :N], N, K, rows=rows)
+        calls.append((by, x, y[:, :N]))
+    for call, x, y in calls:
+        call()                                                 # before a capture: what a kernel's first launch sets
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            call()
+        for seed in range(3):
+            x.copy_(big(*x.shape, 10 + seed)[0])
+            call()
+            want = y.clone()
+            for _ in range(2):
+                y.fill_(4.0)
+                call()
+                assert torch.equal(y, want)
+                y.fill_(6.0)
+                g.replay()
+                torch.cuda.synchronize()
+                assert torch.equal(y, want)

@@ -169,3 +169,19 @@ def test_native_and_python_signatures(lib, python, name):  # noqa: F811
 def test_weights_too_large_are_refused_before_a_launch(lib):  # noqa: F811
     qw = lambda N, K: lib.pq_quantize_weights(MX, 32, FAKE, N, K, None, FAKE, FAKE, FAKE, None)
     assert qw(1 << 40, 1 << 12) == qw(1 << 62, 64) == qw(1 << 60, 1 << 58) == PQ_ERR_SHAPE
+
+
+def test_grouped_tile(lib):  # noqa: F811
+    f = lambda *a: pq.pq_qgemm_grouped_tile(MX, 32, *a)
+    assert f(8, 16, 512, 2048) == (32, 32)
+    assert f(8, 300, 1032, 64) == (32, 64)
+    assert f(8, 400, 1032, 64) == (64, 64)
+    assert f(128, 1536, 1536, 2560) == (32, 128)
+    assert f(63, 5000, 1032, 512) == (64, 128)
+    assert f(8, 4000, 264, 64) == (128, 128)
+    assert f(64, 65528, 2816, 2048) == (256, 256)
+    f = lambda fmt=MX, g=32, E=4, M=8, N=8, K=64: lib.pq_qgemm_grouped_tile(fmt, g, E, M, N, K, C.byref(C.c_int()), C.byref(C.c_int()))
+    assert f() == 0
+    assert lib.pq_qgemm_grouped_tile(MX, 32, 4, 8, 8, 64, None, C.byref(C.c_int())) == PQ_ERR_NULL
+    assert f(fmt=pq.FMT_INT4) == f(g=16) == PQ_ERR_FORMAT
+    assert f(E=0) == f(E=65537) == f(M=0) == f(M=(1 << 24) + 1) == f(N=0) == f(K=48) == f(K=0) == PQ_ERR_SHAPE
