@@ -111,8 +111,10 @@ struct Sorted {
   }
 };
 
-// e^x for a sum whose largest term is 1: x times log2 e is off by 2^-24 of itself, which changes the term by |x| 2^-24 of itself, at most
-// 0.37 2^-24 of the largest.
+// e^x, x <= 0, for a sum whose largest term is 1, by the unit's power of two.  The product with log2 e is rounded (2^-24 of it) and so is the constant
+// (0.22 2^-24), which together change the term by 1.23 |x| 2^-24 of itself, at most 0.45 2^-24 of the largest; the unit adds a last place,
+// 2^-23 of the term.  Weights over all of 256 normal logits of deviation 2, 8192 tokens: off by 6.6 10^-8 of themselves in the root mean square,
+// those of a plain binary32 softmax by 5.7 10^-8.
 __device__ __forceinline__ float exp_in_sum(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 
 // A token's logits, expert PER sub + i at place i of lane `sub` of its LANES: up to 16 bytes a load where the rows allow it, else one

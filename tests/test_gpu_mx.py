@@ -838,3 +838,49 @@ def test_large_products_repeat_their_bits_and_replay():
                 g.replay()
                 torch.cuda.synchronize()
                 assert torch.equal(y, want)
+
+
+# ------------------------------------------------------------------------ routing's weights, relative to themselves
+
+def routed(x, k, renormalize):
+    """What pq_moe_route leaves for logits x, by sorting and float64; with each choice's logit less the largest."""
+    T, E = x.shape
+    v = x.double()
+    v = torch.where(torch.isnan(v), -float("inf"), v)
+    value, ids = torch.sort(v, dim=1, descending=True, stable=True)
+    value, ids = value[:, :k], torch.where(value[:, :k] == -float("inf"), -1, ids[:, :k])
+    top = torch.where(value[:, :1] == -float("inf"), 0.0, value[:, :1])
+    total = torch.exp((value if renormalize else v) - top).sum(dim=1, keepdim=True)
+    weights = torch.where(ids >= 0, torch.exp(value - top) / total, 0.0)
+    chosen = (ids.reshape(-1) >= 0).nonzero()[:, 0]
+    order = chosen[torch.argsort(ids.reshape(-1)[chosen], stable=True)]
+    rows, positions = torch.full((T * k,), -1, device=DEV), torch.full((T * k,), -1, device=DEV)
+    rows[:len(order)] = order // k
+    positions[order] = torch.arange(len(order), device=DEV)
+    offsets = torch.zeros(E + 1, dtype=torch.int64, device=DEV)
+    offsets[1:] = torch.bincount(ids.reshape(-1)[chosen], minlength=E).cumsum(0)
+    return ids, weights, offsets, rows, positions.reshape(T, k), torch.where(ids >= 0, value - top, 0.0)
+
+
+# One launch and two, one step of a workgroup's tokens and several, sixteen lanes a token and a wave; few and many experts a lane.
+# Units of 2^-24 of a weight: the difference of two logits is rounded (|x|), e^x is off by at most two; of the sum's terms every one by the difference and
+# the product with log2 e (2.3 |x| of it with the constant's own rounding; over all terms 2.3 ln E at most, the entropy's bound) and by two, its at most
+# 15 + 6 additions by one each; the quotient by one.
+@pytest.mark.parametrize("T,E,k", [(1, 8, 2), (7, 64, 6), (64, 64, 8), (33, 256, 8), (16, 1024, 4), (17, 1024, 8), (300, 60, 4), (1000, 256, 8), (2500, 300, 20), (16385, 64, 4),
+                                   (20000, 130, 12), (33000, 256, 8), (9000, 600, 20), (9001, 1000, 7), (70001, 33, 3)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("renormalize", [True, False])
+@pytest.mark.parametrize("spread", [0.3, 6.0])
+def test_route_weights(T, E, k, dtype, renormalize, spread):
+    g = torch.Generator(device=DEV).manual_seed(T + E)
+    x = (torch.randn(T, E, generator=g, device=DEV) * spread).to(dtype)
+    odd = torch.rand(T, E, generator=g, device=DEV)
+    x[odd < 0.05] = -float("inf")
+    x[odd > 0.98] = float("nan")
+    x[torch.rand(T, generator=g, device=DEV) < 0.02] = -float("inf")
+    r = pq.pq_moe_route(x, k, renormalize)
+    ids, weights, offsets, rows, positions, below = routed(x, k, renormalize)
+    for got, want in ((r.ids, ids), (r.offsets, offsets), (r.rows, rows), (r.positions, positions)):
+        assert torch.equal(got.long(), want.long())
+    allowed = (below.abs() + 2.3 * float(np.log(E)) + 27) * 2.0 ** -24 * weights + 2.0 ** -126
+    assert bool(((r.weights.double() - weights).abs() <= allowed).all())
