@@ -241,24 +241,21 @@ __device__ __forceinline__ void place_pass(const RouteCall& c, int64_t t0, int n
   }
 }
 
-// Few tokens, one launch: a mask of tokens for every expert says all of it.
+// Few tokens, one for every LANES threads at most, one launch: a mask of tokens for every expert says all of it.
 template <int PER, bool BF16, int LANES>
 __global__ __launch_bounds__(kRouteThreads) void route_few_kernel(const RouteCall c) {
   __shared__ uint64_t mask[LANES * PER];
   __shared__ int32_t base[LANES * PER];
   __shared__ int wave_sums[kRouteWaves];
-  const int sub = threadIdx.x % LANES, group = threadIdx.x / LANES, e = threadIdx.x, tokens = (int)c.tokens;
-  constexpr int groups = kRouteThreads / LANES;
-  const int wave_first = threadIdx.x / kWave * (kWave / LANES);
+  const int sub = threadIdx.x % LANES, t = threadIdx.x / LANES, e = threadIdx.x, tokens = (int)c.tokens;
+  const bool any = (int)(threadIdx.x / kWave) * (kWave / LANES) < tokens;      // waves without a token read nothing and leave the unit to the others
   float v[PER];
-  if (wave_first < tokens) load_logits<PER, BF16>(c, min(group, tokens - 1), sub, v);      // without tokens there are no logits
+  if (any) load_logits<PER, BF16>(c, min(t, tokens - 1), sub, v);
   if (e < c.experts) mask[e] = 0;
   __syncthreads();
-  for (int t0 = 0; t0 + wave_first < tokens; t0 += groups) {      // waves without a token leave the unit to the others
-    const int t = t0 + group;
+  if (any) {
     const int id = route_token<PER, BF16, LANES>(c, t, t < tokens, sub, v);
     if (sub < c.k && id >= 0) atomicOr((unsigned long long*)&mask[id], 1ull << t);
-    if (t0 + groups < tokens) load_logits<PER, BF16>(c, min(t + groups, tokens - 1), sub, v);
   }
   __syncthreads();
   int total;
