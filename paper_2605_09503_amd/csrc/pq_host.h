@@ -208,7 +208,7 @@ struct MxCall {
   const uint16_t* bias;                    // [experts, N] or null
   void* y;
   int64_t ldy;
-  bool out_f32;
+  bool out_f32;                            // of one product only
 };
 int run_mx_gemm(const MxCall& c, hipStream_t st);
 void mx_gemm_tile(int experts, int64_t M, int64_t N, int64_t K, int* bm, int* bn);      // experts 0: of one product

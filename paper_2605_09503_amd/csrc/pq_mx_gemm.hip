@@ -388,7 +388,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void mx_gemm_shared_kernel(const Mx
   // A lane has row l % 32 of a fragment and columns 8 q + 4 (l / 32) + 0 .. 3.  The stores are S::stores of a wave whatever they
   // keep (what has no place goes past the buffer's end and is dropped), so that waits can count past them.
   const auto store = [&](const Tile& t, int slot) {
-    if (c.out_f32) {                                           // for checks of the sums: no care taken of its speed
+    if (!GROUPED && c.out_f32) {                               // for checks of the sums: no care taken of its speed
       const int l = opaque(lane);
 #pragma unroll
       for (int i = 0; i < S::fn; ++i)
@@ -514,7 +514,7 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void mx_gemm_shared_kernel(const Mx
         take_scales(na, nw);
       }
       store(t, slot);
-      stored = panels >= 2 && !c.out_f32 && (c.N & 7) == 0;
+      stored = panels >= 2 && (GROUPED || !c.out_f32) && (c.N & 7) == 0;
     } else {                                                   // none of this wave's rows are in the tile: the others have the matrix units
       for (int p = 0; p < panels; ++p) {
         fetch();
@@ -681,7 +681,7 @@ __global__ __launch_bounds__(KW * 64) void mx_gemm_split_kernel(const MxCall c) 
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] += bf16_to_f32(c.bias[t.expert * c.N + min(n + e, c.N - 1)]);
     }
-    if (c.out_f32) {
+    if (!GROUPED && c.out_f32) {
       for (int e = 0; e < 8; ++e)
         if (n + e < c.N) ((float*)c.y)[m * c.ldy + n + e] = v[e];
     } else {
@@ -827,7 +827,6 @@ __global__ __launch_bounds__(256) void mx_gemm_alone_kernel(const MxCall c) {
     for (int j = 0; j < FM; ++j) {
       const int64_t m = t.first + 32 * j + row;
       const bool ok = m < t.end && a_row_of(c, min(m, t.end - 1)) >= 0;
-      if (c.out_f32) continue;                                         // no grouped call asks for it
 #pragma unroll
       for (int q = 0; q < 4; q += 2) {
         const auto pack = [&](int g, int e) { return pack_bf16(acc[j][4 * g + e] + bias[4 * g + e], acc[j][4 * g + e + 1] + bias[4 * g + e + 1]); };
