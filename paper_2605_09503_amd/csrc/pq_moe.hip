@@ -19,46 +19,29 @@ __device__ __forceinline__ uint32_t key_of(float v) {
 }
 __device__ __forceinline__ float value_of(uint32_t key) { return as_f32(key & 0x80000000u ? key & 0x7FFFFFFFu : ~key); }
 
-// largest over the wave, uniform: inside rows of 16 lanes by DPP exchanges, then the four rows on the scalar unit
-__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+// largest and sum, in a fixed order, over the LANES lanes of a token, in each of them: inside a row of sixteen lanes by DPP exchanges, then (a wave
+// a token) the four rows on the scalar unit
+template <int LANES>
+__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
   v = max(v, dpp_u32<0xB1>(v));                               // quad_perm [1,0,3,2]
   v = max(v, dpp_u32<0x4E>(v));                               // quad_perm [2,3,0,1]
   v = max(v, dpp_u32<0x141>(v));                              // row_half_mirror
   v = max(v, dpp_u32<0x140>(v));                              // row_mirror
+  if constexpr (LANES == 16) return v;
   const uint32_t a = __builtin_amdgcn_readlane(v, 0), b = __builtin_amdgcn_readlane(v, 16), c = __builtin_amdgcn_readlane(v, 32),
                  d = __builtin_amdgcn_readlane(v, 48);
   return max(max(a, b), max(c, d));
 }
-// the sum over the wave in a fixed order, in every lane
-__device__ __forceinline__ float wave_sum_f32(float v) {
+template <int LANES>
+__device__ __forceinline__ float lanes_sum(float v) {
   v += dpp_f32<0xB1>(v);
   v += dpp_f32<0x4E>(v);
   v += dpp_f32<0x141>(v);
   v += dpp_f32<0x140>(v);
+  if constexpr (LANES == 16) return v;
   const float a = as_f32(__builtin_amdgcn_readlane(as_u32(v), 0)), b = as_f32(__builtin_amdgcn_readlane(as_u32(v), 16)),
               c = as_f32(__builtin_amdgcn_readlane(as_u32(v), 32)), d = as_f32(__builtin_amdgcn_readlane(as_u32(v), 48));
   return (a + b) + (c + d);
-}
-
-// largest and sum over the LANES lanes of a token, in each of them: a row of sixteen, or the wave
-__device__ __forceinline__ uint32_t row_max_u32(uint32_t v) {
-  v = max(v, dpp_u32<0xB1>(v));
-  v = max(v, dpp_u32<0x4E>(v));
-  v = max(v, dpp_u32<0x141>(v));
-  return max(v, dpp_u32<0x140>(v));
-}
-template <int LANES>
-__device__ __forceinline__ uint32_t lanes_max(uint32_t v) {
-  if constexpr (LANES == 16) return row_max_u32(v);
-  return wave_max_u32(v);
-}
-template <int LANES>
-__device__ __forceinline__ float lanes_sum(float v) {
-  if constexpr (LANES == 64) return wave_sum_f32(v);
-  v += dpp_f32<0xB1>(v);
-  v += dpp_f32<0x4E>(v);
-  v += dpp_f32<0x141>(v);
-  return v + dpp_f32<0x140>(v);
 }
 
 // A lane's PER experts, PER lane + i, largest first: a token's largest is then one of its lanes' first, and the lane that has it moves
@@ -413,8 +396,7 @@ __global__ __launch_bounds__(kCombineThreads) void combine_kernel(const CombineC
   }
   uint32_t o[4];
 #pragma unroll
-  for (int j = 0; j < 4; ++j)
-    o[j] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)acc[2 * j]) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)acc[2 * j + 1]) << 16;
+  for (int j = 0; j < 4; ++j) o[j] = pack_bf16(acc[2 * j], acc[2 * j + 1]);
   uint16_t* to = c.out + t * c.out_ld + col;
   if (width == 8) {
     *reinterpret_cast<uint4*>(to) = make_uint4(o[0], o[1], o[2], o[3]);

@@ -45,6 +45,11 @@ __device__ __forceinline__ uint32_t mx_quantize8(const uint4& x, uint32_t& byte)
   return mx_codes8(x, byte == 255u ? 1.0f : mx_scale_value(byte));
 }
 
+// two values rounded to bf16, nearest even, a in the low half
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+  return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)a) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)b) << 16;
+}
+
 // ---------------------------------------------------------------- operand of the product
 // Panels of 128 channels: codes[panel][row][64 bytes], scales[panel][row][4 bytes], channels from K on zero (codes and scales).
 // The rows of a tile lie next to each other whatever K is: whole lines are read (rows K / 2 bytes apart would meet in few channels of

@@ -176,9 +176,6 @@ __device__ __forceinline__ float16v mfma(const int4v& w, const int4v& a, const f
 }
 
 // ---------------------------------------------------------------- outputs
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-  return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)a) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)b) << 16;
-}
 // outputs n .. n + 7 of row m, n a multiple of 8
 __device__ __forceinline__ void store8(const MxCall& c, int64_t m, int64_t n, const uint4& v) {
   uint16_t* y = (uint16_t*)c.y + m * c.ldy + n;

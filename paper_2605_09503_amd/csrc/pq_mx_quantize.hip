@@ -115,9 +115,6 @@ __device__ __forceinline__ float e2m1_value(uint32_t code) {
   const float v = 0.5f * (float)((0xC8643210u >> (4 * (code & 7u))) & 15u);
   return code & 8u ? -v : v;
 }
-__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
-  return (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)a) | (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)b) << 16;
-}
 template <int FMT>
 __device__ __forceinline__ uint4 dequantize8(uint32_t q, float scale, float T) {
   if constexpr (FMT == PQ_FMT_MXFP4) {
