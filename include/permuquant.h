@@ -615,12 +615,14 @@ int pq_attn_decode(const pq_kv_cache* cache, const void* q_bf16, int64_t q_ld, i
  * the products at most 2^24.  Its operands are panels of 128 channels,
  * zero from K on (pq_operand_bytes counts them).
  * Products are exact, sums fp32 over the whole of K, in an order that depends on M, N and K; they begin with the bias or it is added last.
+ * A product, dense or by expert, whose output would make 2^24 tiles (2^23 of 256 x 256) is refused with PQ_ERR_SHAPE; with fewer than 2^30
+ * outputs none is.
  */
 
 /*
  * The values that stored codes and scales stand for, as bf16 [rows, ldy]: code * scale (* tensor scale, NVFP4) in binary32, rounded to
- * nearest even (MXFP4: exact below 2^128).  All formats; arguments as for pq_quantize_act.  rows and K at most 2^24; ldy >= K, a multiple
- * of 8.
+ * nearest even (MXFP4: exact below 2^128).  All formats; arguments as for pq_quantize_act.  rows and K at most 2^24, and ceil(rows / 16) *
+ * ceil(K / 512) below 2^24 (as for the quantizers of MXFP4: some 2^37 values); ldy >= K, a multiple of 8.
  */
 int pq_dequantize(pq_format fmt, int group, const uint8_t* codes, const void* scales, const float* tensor_scale, int64_t rows, int64_t K,
                   void* y_bf16, int64_t ldy, void* stream);
@@ -673,7 +675,8 @@ int pq_moe_route(pq_logits type, const void* logits, int64_t tokens, int experts
  *   out[t, n] = addend[t, n] + sum_j weights[t, j] * y[positions[t, j], n]          (addend NULL: 0)
  * y: bf16 [rows, y_ld]; positions: int32 [tokens, k], outside 0 .. rows - 1: left out (NaN in other rows does not matter); weights: float
  * [tokens, k]; addend, out: bf16 [tokens, ld]; strides >= N and multiples of 8.  out may be addend itself (the same strides), but
- * overlaps neither it otherwise nor y.  tokens 0 .. 2^24, k 1 .. 32.
+ * overlaps neither it otherwise nor y.  tokens 0 .. 2^24, N 1 .. 2^24, tokens * ceil(N / 1024) below 2^25 (a call over some of the tokens
+ * at a time makes the same outputs); k 1 .. 32.
  */
 int pq_moe_combine(const void* y_bf16, int64_t rows, int64_t y_ld, const int32_t* positions, const float* weights, int64_t tokens, int k,
                    int64_t N, const void* addend_bf16, int64_t addend_ld, void* out_bf16, int64_t out_ld, void* stream);

@@ -185,3 +185,15 @@ def test_grouped_tile(lib):  # noqa: F811
     assert lib.pq_qgemm_grouped_tile(MX, 32, 4, 8, 8, 64, None, C.byref(C.c_int())) == PQ_ERR_NULL
     assert f(fmt=pq.FMT_INT4) == f(g=16) == PQ_ERR_FORMAT
     assert f(E=0) == f(E=65537) == f(M=0) == f(M=(1 << 24) + 1) == f(N=0) == f(K=48) == f(K=0) == PQ_ERR_SHAPE
+
+
+def test_calls_past_the_largest_grid(lib):  # noqa: F811
+    c = lambda T, N: lib.pq_moe_combine(FAKE, 8, 1 << 24, FAKE, FAKE, T, 2, N, None, 0, FAKE, 1 << 24, None)
+    assert c(1 << 24, 1025) == c((1 << 23) + 1, 4096) == c(1 << 11, 1 << 24) == PQ_ERR_SHAPE
+    d = lambda rows, K: lib.pq_dequantize(MX, 32, FAKE, FAKE, None, rows, K, FAKE, 1 << 24, None)
+    assert d(1 << 24, 1 << 13) == d(1 << 13, 1 << 24) == d(1 << 24, 1 << 24) == PQ_ERR_SHAPE
+    qp = lambda M, K: lib.pq_quantize_act_packed(MX, 32, FAKE, M, K, K, None, FAKE, 1 << 60, None, None, None)
+    assert qp(1 << 24, 1 << 13) == qp(1 << 13, 1 << 24) == PQ_ERR_SHAPE
+    g = lambda E, M, N: lib.pq_qgemm_grouped(MX, 32, FAKE, 1 << 24, FAKE, E, FAKE, FAKE, M, N, 32, None, FAKE, 1 << 24, None)
+    assert g(128, 512, 1 << 24) == g(1, 1 << 24, 1 << 24) == PQ_ERR_SHAPE
+    assert lib.pq_qgemm_packed(MX, 32, FAKE, None, FAKE, None, 46340, 5931641, 32, FAKE, 1 << 24, None) == PQ_ERR_SHAPE
