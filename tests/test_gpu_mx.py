@@ -884,3 +884,47 @@ def test_route_weights(T, E, k, dtype, renormalize, spread):
         assert torch.equal(got.long(), want.long())
     allowed = (below.abs() + 2.3 * float(np.log(E)) + 27) * 2.0 ** -24 * weights + 2.0 ** -126
     assert bool(((r.weights.double() - weights).abs() <= allowed).all())
+
+
+# ------------------------------------------------------------------------ every value under every scale; reading back the other formats
+
+def test_every_bf16_value_under_every_scale():
+    # every finite value beside a largest one that sets the scale, for each scale under which it is not itself larger
+    for byte in range(253):
+        largest = (byte + 2) << 7                                          # 2^(byte - 125)
+        magnitudes = np.arange(largest + 128, dtype=np.uint16)             # those up to the next power of two set the same scale
+        values = np.concatenate([magnitudes, magnitudes | 0x8000])
+        b = np.full((-(-len(values) // 31), 32), largest, dtype=np.uint16)
+        b[:, :31] = np.resize(values, (len(b), 31))
+        t = pq.bf16_from_bits(b, DEV)
+        codes, scales = pq.alloc_quantized(MX, 32, *t.shape)
+        pq.pq_quantize_act(MX, 32, t, None, None, codes, scales)
+        want = mx.quantize(OF.bf16_bits_to_f64(b))
+        assert bool((want.scale == byte).all()) and bool((scales == byte).all()), byte
+        assert np.array_equal(codes.cpu().numpy(), mx.packed_codes(want)), byte
+
+
+def test_every_code_under_every_scale():
+    code = np.tile(np.arange(16, dtype=np.uint8), (256, 2))
+    q = mx.MxQuant(code, np.arange(256, dtype=np.uint8)[:, None])
+    want = mx.dequantize(q)
+    held = ~(np.abs(want) >= 2.0 ** 128)                                   # bf16 has no larger ones; NaN among them
+    got = f64(pq.pq_dequantize(MX, 32, *stored(q)))
+    assert np.array_equal(got[held], want[held], equal_nan=True)
+
+
+@pytest.mark.parametrize("rows,K,gap", [(1, 256, 0), (19, 768, 8), (65, 5376, 0), (300, 512, 16)])
+@pytest.mark.parametrize("fmt,group", [(pq.FMT_NVFP4, 16)] + [(f, g) for f in (pq.FMT_INT4, pq.FMT_INT3) for g in (32, 64, 128, 256)])
+def test_dequantize_all_formats(fmt, group, rows, K, gap):
+    rng = np.random.default_rng(rows + K)
+    x = rows_of(rng, rows, K)
+    ts = torch.full((1,), float(np.float32(np.abs(f64(x)).max() / 2688)), device=DEV)
+    codes, scales = pq.alloc_quantized(fmt, group, rows, K)
+    pq.pq_quantize_act(fmt, group, x, None, ts, codes, scales)
+    q = OQ.quantize(fmt, group, f64(x), np.float32(ts.item()))
+    want = OF.f64_to_bf16_bits_rne(OF.fl32(OQ.dequantize(fmt, group, q)))
+    wide = torch.full((rows + 1, K + 2 * gap), 3.0, dtype=torch.bfloat16, device=DEV)
+    pq.pq_dequantize(fmt, group, codes, scales, ts, y=wide[:rows, gap:gap + K])
+    got = bits(wide[:rows, gap:gap + K])
+    assert np.array_equal(np.where(got == 0x8000, 0, got), np.where(want == 0x8000, 0, want))       # a zero has no sign in the oracle
+    assert bool((wide[rows:] == 3).all()) and bool((wide[:, :gap] == 3).all()) and bool((wide[:, gap + K:] == 3).all())
