@@ -41,8 +41,8 @@ __device__ __forceinline__ int tiles_of(const MxCall& c, int bm, int e, int& fro
 }
 // The tiles a workgroup computes.  Workgroups go round the eight chiplets in turn; each chiplet takes a contiguous eighth of the
 // tiles, in blocks of four tiles of rows, and its workgroups go through it side by side: what they read at a time meets in its L2
-// (blocks of eight: 8192 x 12288 x 8192 takes 433 us, not 428, 16384 x 8192 x 1024 115, not 101, 65528 gathered rows by 64 experts,
-// 2816 x 2048, 334, not 316; two to six are alike, sixteen and more slower still).
+// (blocks of eight: 8192 x 12288 x 8192 takes 407 us, not 388, 16384 x 8192 x 1024 112, not 102, 65536 gathered rows by 64 experts,
+// 2816 x 2048, 333, not 320; two to six are alike, sixteen and more slower still).
 template <bool GROUPED>
 struct Tiles {
   // A table in LDS for up to kTable experts: tiles of the experts up to each one, and their offsets cut to 0 .. M.  What a search
@@ -209,11 +209,11 @@ struct Shared {
 
 // A workgroup goes through its tiles, and through the panels of each, without a stop: three panels are on their way while one is
 // multiplied, also where they are the next tile's.
-// Bound by the matrix unit under the chip's power limit: 8192 x 12288 x 8192 takes 390 to 410 us = 4.0 to 4.2 PFLOP/s; the products
-// alone, on the same operands without a load, 294, and with operands of zeros the kernel takes 290.  A wave of a 256 x 256 tile has 4 x 2
+// Bound by the matrix unit under the chip's power limit: 8192 x 12288 x 8192 takes 384 to 413 us = 4.0 to 4.3 PFLOP/s, on operands of zeros, by the
+// same instructions, 281 to 305; without the loads behind the first four panels 359 to 368, without the stores 367 to 372.  A wave of a 256 x 256 tile has 4 x 2
 // fragments and reads 3/4 KB of LDS a matrix instruction, one of a 128 x 128 tile 2 x 2 and 1 KB; from memory the larger tile takes half
 // as much.  Four waves of 128 x 128 each, 256 x 128 tiles, and eight stages of 128 x 128 were slower.  128 x 128 tiles, two workgroups a
-// unit, for outputs that make too few large ones: 1777 x 4008 x 2016 15.3 us.
+// unit, for outputs that make too few large ones: 1777 x 4008 x 2016 15.0 us.
 template <int BM, int BN, int WM, int WN, bool GROUPED, bool FEW>
 __global__ __launch_bounds__(WM* WN * 64, 2) void mx_gemm_shared_kernel(const MxCall c) {
   using S = Shared<BM, BN, WM, WN>;
@@ -427,8 +427,8 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void mx_gemm_shared_kernel(const Mx
 #pragma unroll
       for (int i = 0; i < S::fn; ++i) {
         // halves of the wave: eight columns of a row a lane, columns 16 q + 8 (l / 32); then rows of sixteen lanes: q = 0 and 1 of a row
-        // side by side, 64 bytes of it in one store (with 32 bytes 8192 x 12288 x 8192 takes 390 us, not 377, 65536 rows x 2816 x
-        // 2048 of 64 experts 264, not 241)
+        // side by side, 64 bytes of it in one store (with 32 bytes 16384 x 8192 x 1024 takes 107 us, not 102, 65536 rows x 2816 x
+        // 2048 of 64 experts 254, not 250)
         uint4v half_row[2];
 #pragma unroll
         for (int q = 0; q < 2; ++q) {
@@ -537,7 +537,8 @@ __global__ __launch_bounds__(WM* WN * 64, 2) void mx_gemm_shared_kernel(const Mx
 // every tile of columns the rows.  32 x 32 where there are few of them, 32 x 64 and 64 x 64 for more, us at N 12288:
 //   K 8192, M 16   12.6  11.1  11.7     M 56  17.8  17.5  14.5     K 512, M 56   4.9  3.9  4.3     M 128  7.3  5.7  7.2
 // (64 x 32 tiles take 13.1, 17.5, 4.0, 6.0: never less than both of the others by 4 %.)  Four waves and four stages (three for 32 x 64), two
-// workgroups a unit, one of 64 x 64, have 48 to 64 KB of weights a unit under way; eight waves, and tiles of 128 x 32, were no faster.
+// workgroups a unit, one of 64 x 64, have 48 to 64 KB of weights a unit under way beside the panel that each wave multiplies; eight waves, and tiles
+// of 128 x 32, were no faster.
 template <int FM, int FN, int KW>
 struct Split {
   static constexpr int bm = 32 * FM, bn = 32 * FN;
@@ -879,12 +880,16 @@ int launch_alone(const MxCall& c, hipStream_t st) {
 
 // Which kernel: the one that takes the shortest time by a model of each in us.  Small tiles read more than they multiply and are bound by what
 // the units take from the caches: a start, some us and a time a panel for every round of 256 tiles, and the weights' bytes.  Large ones
-// take some us a turn and a time a panel, and only pay where there are enough of them.  Fitted to all kernels timed at M 16 .. 768, N 1024 ..
+// take some us a turn and a time a panel, and only pay where there are enough of them.  Fitted to the dense kernels timed at M 16 .. 768, N 1024 ..
 // 16384 and K 512 .. 8192 (200 shapes: the choice is within 7 % of the best for 191, within 13 % for all), the two largest tiles at M up to
 // 8192 as well.  us, 32 x 32, 32 x 64, 64 x 64, 128 x 128:
 //   M 32, N 4096, K 2048    3.9   4.4   5.1   8.1        M 256, N 4096, K 8192   15.4  12.4  10.3  25.1
 //   M 512, N 12288, K 512  23.5  15.6  19.0   7.9        M 256, N 12288, K 8192  48.5  38.2  35.5  25.8
 // and 128 x 128 and 256 x 256 at M 1024, N 12288, K 8192  62  55.
+// By expert the same constants stand, and the kernels of a wave a tile take the weights' bytes or what the units take from the caches: not fitted.  Against
+// all kernels at 8, 64 and 256 experts, 16 to 1000 rows of each, N 1024 and 4096, K 128 to 4096, rows spread evenly and not (288 shapes) the choice is
+// within 7 % of the best for 146 and within 30 % for 239.  The worst are those of few panels and many rows, where a wave a tile is taken and what its
+// outputs, its start and its end cost is left out: 200000 rows and more, K 128, take 1.9 to 2.1 times as long as with 256 x 256 tiles.
 // enough tiles of 32 columns for every wave of the chip: no need to share K
 bool enough_alone(const MxCall& c) {
   const int64_t whole = (c.M + 31) / 32, rows = whole > c.experts ? whole : c.experts < c.M ? c.experts : c.M;
